@@ -645,6 +645,62 @@ int dh_attn_ctx_bwd(int dtype, int batch, int seq, int q_off, int nq, int nkv, i
 size_t dh_attn_ctx_bwd_workspace_bytes(int dtype, int batch, int seq, int q_off, int nq, int nkv, int d);
 
 /* ------------------------------------------------------------------------------------------
+ * Packed micro-batches: one row of T tokens holds n_docs documents back to back and rows of padding around them.
+ * Document n is rows doc_start[n] .. doc_start[n+1]-1; rows before doc_start[0] and from doc_start[n_docs] on belong to none.  A row
+ * sees the rows of its document up to itself; with a prefix, the first prefix[n] rows of document n see one another whole.
+ * doc_start and prefix are DEVICE arrays (they come with the micro-batch, no host round trip).  Documents may be empty.  Starts that do not ascend,
+ * or lie outside 0..T, leave the rows they would give to two documents or none in an unspecified one of them or in none; nothing outside the buffers is touched.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+  int T;                    /* rows of the buffers */
+  int n_docs;               /* documents, >= 0 */
+  int nq, nkv;              /* query and key/value heads of the attention that reads the table; nkv divides nq */
+  const int32_t* doc_start; /* device [n_docs+1], ascending */
+  const int32_t* prefix;    /* device [n_docs] rows of each document's prefix (cut to its length), or NULL: none */
+  int32_t* pos;             /* device [T] written by dh_docs_plan: position in the row's document (0 for rows of none), or NULL */
+  void* table;              /* device, dh_docs_table_bytes(T, nq, nkv) bytes, 16-byte aligned, written by dh_docs_plan */
+} dh_docs;
+size_t dh_docs_table_bytes(int T, int nq, int nkv);
+/* Fills table (and pos) from doc_start and prefix: once for a micro-batch, whose layers all read it. */
+int dh_docs_plan(const dh_docs* docs, void* stream);
+
+/* Grouped-query attention inside documents.  Layouts as dh_attn_fwd / dh_attn_bwd: qkv[T,(nq+2nkv)d] (already rotated), o[T,nq*d], lse[nq,T],
+ * delta[nq,T]; docs as dh_docs_plan has filled it.  cap > 0: every scaled score x counts as cap * tanh(x / cap); 0: as it is.  Rows of no document are
+ * neither read nor written, in o, lse and dqkv alike.  What a row does not see does not reach its results, infinities and NaNs among it.
+ * d: multiple of 8 up to 256 for DH_F32, 64 or 128 for DH_BF16.  qkv, o, dout, dqkv: 16-byte aligned.  ws: device workspace of the _workspace_bytes
+ * queries (fewer bytes: DH_ERR_WORKSPACE_TOO_SMALL).  Backward writes dqkv (dk, dv summed over the query heads of a group in a fixed order) and delta. */
+int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes,
+                     void* stream);
+size_t dh_attn_docs_fwd_workspace_bytes(int dtype, int T, int nq, int nkv, int d);
+int dh_attn_docs_bwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, const void* o, const void* dout, const float* lse,
+                     void* dqkv, float* delta, void* ws, size_t ws_bytes, void* stream);
+size_t dh_attn_docs_bwd_workspace_bytes(int dtype, int T, int nq, int nkv, int d);
+
+/* Rotary embedding whose positions are a table with one column for each of n_axes axes (1..4): a position in a document, or time, height and width
+ * of an image's or a video's patch.  axis_pairs: HOST [n_axes], each >= 1, head_dim/2 in all: the first axis_pairs[0] RoPE pairs of a head turn by the
+ * first column, the next by the second, and so on.  Pair i of a head turns by pos * base^(-2i/d) with DH_ROPE_AXES_SHARED, and pair j of an axis of n pairs by
+ * pos * base^(-j/n) with DH_ROPE_AXES_OWN.  pos: device [T, n_axes], any int32.  t: rows of t_stride elements that begin with n_heads heads
+ * side by side; out: rows of out_stride elements, likewise; out == t with the same stride turns in place, otherwise the two must not overlap.  pairing:
+ * dh_rope_pairing; inverse != 0 turns back (the backward of the rotation).  head_dim: multiple of 16 up to 512; strides: multiples of 8; t, out 16-byte aligned. */
+typedef enum { DH_ROPE_AXES_SHARED = 0, DH_ROPE_AXES_OWN = 1 } dh_rope_axes_form;
+int dh_rope_axes(int dtype, int pairing, int form, int T, int n_axes, const int* axis_pairs, const int32_t* pos, int n_heads, int head_dim,
+                 float base, int inverse, const void* t, int t_stride, void* out, int out_stride, void* stream);
+
+/* Tensors of one call over many: HOST array; data and out are device pointers, aligned to their elements. */
+typedef struct {
+  const void* data;
+  void* out;  /* dh_grad_clip: where the result goes; NULL = data itself.  May not overlap another tensor, or data other than as a whole. */
+  size_t n;   /* elements */
+  int dtype;  /* dh_dtype */
+} dh_tensor;
+/* norm[0] = sqrt(sum of squares over all elements of all tensors), squared and added in float64 in a fixed order, rounded once to float32.
+ * ws: dh_grad_norm_ws_bytes.  dh_grad_clip: out = data * c where c = max_norm / (norm + 1e-6) in float32 is below 1 and norm is finite, otherwise out = data
+ * (nothing is written where out is data); norm: device float32, as dh_grad_norm has left it.  n_tensors >= 0; max_norm > 0. */
+int dh_grad_norm(int n_tensors, const dh_tensor* tensors, float* norm, void* ws, size_t ws_bytes, void* stream);
+size_t dh_grad_norm_ws_bytes(int n_tensors, const dh_tensor* tensors);
+int dh_grad_clip(int n_tensors, const dh_tensor* tensors, const float* norm, float max_norm, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Mixture-of-experts operators (Sec. 6.1, top-2 gating; operator bases Router, Permute, AlltoAll and
  * Group-GEMM of Table 2).  Expert parallelism on one GPU: the E logical experts are
  * e = source_rank * n_local + local_expert; this GPU holds the n_local local experts and receives
@@ -657,6 +713,20 @@ int dh_moe_route(int T, int E, const float* logits, int32_t* idx, float* prob, v
 /* dlogits[T,E] = gradient of the router given dprob[T,2]; zero outside the two kept experts. */
 int dh_moe_route_bwd(int T, int E, const float* dprob, const int32_t* idx, const float* prob,
                      float* dlogits, void* stream);
+
+/* Balance loss of the router, its z loss and the rows of each expert.  The first N = min(max(*n_live, 0), T) tokens count (n_live: DEVICE int32, e.g. the
+ * row behind the last document of a packed micro-batch; NULL: all T).  With p = softmax(logits[t,:]) over all E experts and idx as dh_moe_route gives it:
+ *   counts[e] = number of (t,k) with idx[t,k] = e;  prob_mean[e] = 1/N sum_t p[t,e];  lse[t] = log sum_e exp(logits[t,e])
+ *   loss[0] = E sum_e counts[e]/(2N) prob_mean[e] (1 when balanced);  loss[1] = 1/N sum_t lse[t]^2
+ * A token whose logits are all minus infinity adds nothing to prob_mean and to loss[1]; N = 0 gives zeros.  lse of tokens that do not count is left as it was.
+ * Backward: dlogits[t,e] = dloss[0] E/N p (counts[e]/(2N) - sum_e' counts[e']/(2N) p[t,e']) + dloss[1] 2/N lse[t] p (counts are constants), zero
+ * for tokens that do not count; accumulate != 0 adds it to dlogits, e.g. to what dh_moe_route_bwd left there.  dloss: DEVICE [2].
+ * logits, prob_mean, lse, loss, dloss, dlogits float32; 2 <= E <= 256; sums in a fixed order.  ws: dh_moe_balance_ws_bytes. */
+int dh_moe_balance_fwd(int T, int E, const float* logits, const int32_t* idx, const int32_t* n_live, int32_t* counts, float* prob_mean, float* lse,
+                       float* loss, void* ws, size_t ws_bytes, void* stream);
+size_t dh_moe_balance_ws_bytes(int T, int E);
+int dh_moe_balance_bwd(int T, int E, const float* logits, const float* lse, const int32_t* counts, const int32_t* n_live, const float* dloss,
+                       int accumulate, float* dlogits, void* stream);
 
 /* Index tables of one routing decision, all int32 device arrays owned by the caller.  "Assignment"
  * a = 2t+k is token t's k-th expert.  Send order: assignments grouped by expert ascending, inside an

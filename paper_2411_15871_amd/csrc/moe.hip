@@ -48,6 +48,154 @@ __global__ void moe_route_bwd_kernel(int T, int E, const float* __restrict__ dpr
   }
 }
 
+// ------------------------------------------------------------------------------------ balance loss, z loss, rows per expert
+// A group of L lanes works on a token, NE logits a lane (expert = lane of the group + L * i), so that a wave reads 64/L consecutive rows at once.  A lane's
+// experts are the same for all its tokens: it adds their probabilities in registers, and the block's lanes meet in LDS once at the end, in order.  The counts are
+// integers added in LDS, in any order.  Each block leaves its sums in the workspace: [blocks][E] probabilities, [blocks][E] counts, [blocks] z.
+#define BAL_THREADS 1024
+#define BAL_BLOCKS 256
+__device__ __forceinline__ int live_tokens(const int32_t* n_live, int T) { return n_live ? min(max(*n_live, 0), T) : T; }
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+template <int L> __device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+template <int L, int NE>
+__global__ __launch_bounds__(BAL_THREADS) void moe_balance_kernel(int T, int E, const float* __restrict__ logits, const int32_t* __restrict__ idx, const int32_t* __restrict__ n_live,
+                                                                  float* __restrict__ lse, float* __restrict__ part_p, int32_t* __restrict__ part_n, float* __restrict__ part_z) {
+  constexpr int GROUPS = BAL_THREADS / L;
+  __shared__ float sums[GROUPS > 1 ? BAL_THREADS * NE : 1], zs[GROUPS];
+  __shared__ int hist[256];
+  const int N = live_tokens(n_live, T), el = threadIdx.x % L, group = threadIdx.x / L;
+  if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+  __syncthreads();
+  for (size_t i = (size_t)blockIdx.x * BAL_THREADS + threadIdx.x; i < 2 * (size_t)N; i += (size_t)gridDim.x * BAL_THREADS) {
+    const int e = idx[i];
+    if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
+  }
+  float p[NE], z = 0.f;
+#pragma unroll
+  for (int i = 0; i < NE; i++) p[i] = 0.f;
+  // whole waves go round together: a group without a token repeats the last one and does not count it
+  const size_t stride = (size_t)gridDim.x * GROUPS;
+  for (size_t t0 = (size_t)blockIdx.x * GROUPS + (threadIdx.x & ~63) / L; t0 < (size_t)N; t0 += stride) {
+    const size_t want = t0 + (threadIdx.x & 63) / L, t = want < (size_t)N ? want : N - 1;
+    float v[NE], x[NE], m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NE; i++) v[i] = el + L * i < E ? logits[t * E + el + L * i] : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NE; i++) m = fmaxf(m, v[i]);
+    m = lanes_max<L>(m);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < NE; i++) { x[i] = expf(v[i] - ref); s += x[i]; }
+    s = lanes_sum<L>(s);
+    const float l = ref + logf(s), inv = s == 0.f ? 0.f : 1.f / s;
+    if (want < (size_t)N) {
+#pragma unroll
+      for (int i = 0; i < NE; i++) p[i] = fmaf(x[i], inv, p[i]);
+      if (el == 0) {
+        lse[t] = l;
+        z = s == 0.f ? z : fmaf(l, l, z);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NE; i++) sums[group * (L * NE) + el + L * i] = p[i];
+  if (el == 0) zs[group] = z;
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += BAL_THREADS) {
+    float a = 0.f;
+    for (int g = 0; g < GROUPS; g++) a += sums[g * (L * NE) + e];
+    part_p[(size_t)blockIdx.x * E + e] = a;
+    part_n[(size_t)blockIdx.x * E + e] = hist[e];
+  }
+  if (threadIdx.x == 0) {
+    float a = 0.f;
+    for (int g = 0; g < GROUPS; g++) a += zs[g];
+    part_z[blockIdx.x] = a;
+  }
+}
+// One block adds the blocks' sums: thread (expert, slice of the blocks), slices in order.
+__global__ __launch_bounds__(1024) void moe_balance_finish_kernel(int T, int E, int blocks, const int32_t* __restrict__ n_live, const float* __restrict__ part_p,
+                                                                  const int32_t* __restrict__ part_n, const float* __restrict__ part_z, int32_t* __restrict__ counts,
+                                                                  float* __restrict__ prob_mean, float* __restrict__ loss) {
+  __shared__ float ps[1024], fp[256], zz[4];
+  __shared__ int ns[1024];
+  const int N = live_tokens(n_live, T), slices = 1024 / E, e = threadIdx.x % E, slice = threadIdx.x / E;
+  const int per = (blocks + slices - 1) / slices, b0 = slice * per, b1 = min(blocks, b0 + per);
+  const float inv = N > 0 ? 1.f / (float)N : 0.f;
+  float p = 0.f;
+  int n = 0;
+  if (slice < slices) {
+#pragma unroll 8
+    for (int b = b0; b < b1; b++) {
+      p += part_p[(size_t)b * E + e];
+      n += part_n[(size_t)b * E + e];
+    }
+    ps[threadIdx.x] = p;
+    ns[threadIdx.x] = n;
+  }
+  float z = 0.f;
+  for (int b = threadIdx.x; b < blocks && threadIdx.x < 256; b += 256) z += part_z[b];
+  z = wave_sum(z);
+  if (threadIdx.x < 256 && (threadIdx.x & 63) == 0) zz[threadIdx.x >> 6] = z;
+  __syncthreads();
+  if (slice == 0) {
+    for (int k = 1; k < slices; k++) { p += ps[k * E + e]; n += ns[k * E + e]; }
+    counts[e] = n;
+    prob_mean[e] = p * inv;
+    fp[e] = (float)n * (0.5f * inv) * (p * inv);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    float b = 0.f;
+    for (int k = threadIdx.x; k < E; k += 64) b += fp[k];
+    b = wave_sum(b);
+    if (threadIdx.x == 0) {
+      loss[0] = (float)E * b;
+      loss[1] = (zz[0] + zz[1] + zz[2] + zz[3]) * inv;
+    }
+  }
+}
+// dlogits, in the groups of the forward pass: one read and one write of the logits' size.
+template <int L, int NE>
+__global__ __launch_bounds__(256) void moe_balance_bwd_kernel(int T, int E, const float* __restrict__ logits, const float* __restrict__ lse, const int32_t* __restrict__ counts,
+                                                              const int32_t* __restrict__ n_live, const float* __restrict__ dloss, int accumulate, float* __restrict__ dlogits) {
+  constexpr int GROUPS = 256 / L;
+  const int N = live_tokens(n_live, T), el = threadIdx.x % L;
+  const float inv = N > 0 ? 1.f / (float)N : 0.f, gb = dloss[0] * (float)E * inv, gz = dloss[1] * 2.f * inv;
+  float f[NE];
+#pragma unroll
+  for (int i = 0; i < NE; i++) f[i] = el + L * i < E ? (float)counts[el + L * i] * (0.5f * inv) : 0.f;
+  for (size_t t0 = (size_t)blockIdx.x * GROUPS + (threadIdx.x & ~63) / L; t0 < (size_t)T; t0 += (size_t)gridDim.x * GROUPS) {
+    const size_t t = t0 + (threadIdx.x & 63) / L;
+    const bool live = t < (size_t)N;
+    const float l = live ? lse[t] : 0.f;
+    float p[NE], s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NE; i++) {
+      p[i] = live && l != -INFINITY && el + L * i < E ? expf(logits[t * E + el + L * i] - l) : 0.f;
+      s = fmaf(p[i], f[i], s);
+    }
+    s = lanes_sum<L>(s);
+    if (t < (size_t)T && (live || !accumulate)) {
+#pragma unroll
+      for (int i = 0; i < NE; i++)
+        if (el + L * i < E) {
+          const float g = live && l != -INFINITY ? p[i] * fmaf(gb, f[i] - s, gz * l) : 0.f;
+          float* to = dlogits + t * E + el + L * i;
+          *to = accumulate ? *to + g : g;
+        }
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------ permutation plan (M2, M3)
 // Block e ranks the assignments (a = 2t+k, ascending) that chose expert e: a wave owns a contiguous sixteenth of them, 64 at a time, counts its
 // matches from the lanes' votes, and hands out ranks behind those of the waves before it.  Bound by two rounds of loads (8192 assignments: a
@@ -224,6 +372,59 @@ extern "C" int dh_moe_route_bwd(int T, int E, const float* dprob, const int32_t*
   if (T == 0) return DH_OK;
   if (!dprob || !idx || !prob || !dlogits) DH_FAIL(DH_ERR_INVALID_ARG, "moe_route_bwd: null pointer");
   moe_route_bwd_kernel<<<(unsigned)std::min<size_t>(((size_t)T * E + 255) / 256, ROUTE_BWD_BLOCKS), 256, 0, (hipStream_t)stream>>>(T, E, dprob, idx, prob, dlogits);
+  DH_LAUNCH_CHECK();
+  return DH_OK;
+}
+
+// GO(L, NE) for E experts: as many lanes as experts (a power of two), 64 with several logits a lane.
+#define BALANCE_FOR(E, GO)                    \
+  do {                                        \
+    if ((E) <= 2) GO(2, 1);                   \
+    else if ((E) <= 4) GO(4, 1);              \
+    else if ((E) <= 8) GO(8, 1);              \
+    else if ((E) <= 16) GO(16, 1);            \
+    else if ((E) <= 32) GO(32, 1);            \
+    else if ((E) <= 64) GO(64, 1);            \
+    else if ((E) <= 128) GO(64, 2);           \
+    else GO(64, 4);                           \
+  } while (0)
+static int balance_lanes(int E) { int l = 2; while (l < E && l < 64) l *= 2; return l; }
+static int balance_blocks(int T, int E) { return (int)std::min<size_t>(BAL_BLOCKS, std::max<size_t>(1, ((size_t)T * balance_lanes(E) + BAL_THREADS - 1) / BAL_THREADS)); }
+
+extern "C" size_t dh_moe_balance_ws_bytes(int T, int E) {
+  if (T < 0 || E < 2 || E > 256) return 0;
+  return (size_t)balance_blocks(T, E) * (2 * (size_t)E + 1) * 4;
+}
+
+extern "C" int dh_moe_balance_fwd(int T, int E, const float* logits, const int32_t* idx, const int32_t* n_live, int32_t* counts, float* prob_mean, float* lse, float* loss, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  if (T < 0 || E < 2 || E > 256) DH_FAIL(DH_ERR_SHAPE, "moe_balance_fwd: T=%d E=%d (E must be 2..256)", T, E);
+  if (!counts || !prob_mean || !loss || (T > 0 && (!logits || !idx || !lse))) DH_FAIL(DH_ERR_INVALID_ARG, "moe_balance_fwd: null pointer");
+  const size_t need = dh_moe_balance_ws_bytes(T, E);
+  if (!ws || ws_bytes < need) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "moe_balance_fwd: workspace %zu < %zu bytes", ws_bytes, need);
+  const int blocks = balance_blocks(T, E);
+  float* part_p = (float*)ws;
+  int32_t* part_n = (int32_t*)(part_p + (size_t)blocks * E);
+  float* part_z = (float*)(part_n + (size_t)blocks * E);
+  hipStream_t s = (hipStream_t)stream;
+#define GO(L, NE) moe_balance_kernel<L, NE><<<blocks, BAL_THREADS, 0, s>>>(T, E, logits, idx, n_live, lse, part_p, part_n, part_z)
+  BALANCE_FOR(E, GO);
+#undef GO
+  DH_LAUNCH_CHECK();
+  moe_balance_finish_kernel<<<1, 1024, 0, s>>>(T, E, blocks, n_live, part_p, part_n, part_z, counts, prob_mean, loss);
+  DH_LAUNCH_CHECK();
+  return DH_OK;
+}
+
+extern "C" int dh_moe_balance_bwd(int T, int E, const float* logits, const float* lse, const int32_t* counts, const int32_t* n_live, const float* dloss, int accumulate, float* dlogits,
+                                  void* stream) {
+  if (T < 0 || E < 2 || E > 256) DH_FAIL(DH_ERR_SHAPE, "moe_balance_bwd: T=%d E=%d (E must be 2..256)", T, E);
+  if (T == 0) return DH_OK;
+  if (!logits || !lse || !counts || !dloss || !dlogits) DH_FAIL(DH_ERR_INVALID_ARG, "moe_balance_bwd: null pointer");
+  const unsigned blocks = (unsigned)std::min<size_t>(2048, ((size_t)T * balance_lanes(E) + 255) / 256);
+#define GO(L, NE) moe_balance_bwd_kernel<L, NE><<<blocks, 256, 0, (hipStream_t)stream>>>(T, E, logits, lse, counts, n_live, dloss, accumulate, dlogits)
+  BALANCE_FOR(E, GO);
+#undef GO
   DH_LAUNCH_CHECK();
   return DH_OK;
 }

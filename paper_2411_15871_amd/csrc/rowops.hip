@@ -342,6 +342,70 @@ __global__ __launch_bounds__(256) void rope_kernel(T* __restrict__ t, size_t row
   }
 }
 
+// The same with positions from a table of n_axes columns; the first pairs[0] pairs turn by the first column, the next by the second ...  Each block forms the
+// frequencies of a head's pairs in LDS once, in double; a thread rotates 8 pairs of HEADS heads.
+#define ROPE_MAX_AXES 4
+#define ROPE_MAX_D 512
+struct RopeAxes { int n, first[ROPE_MAX_AXES + 1]; };  // first[a]: first pair of axis a
+template <typename T, bool ADJACENT, int HEADS>
+__global__ __launch_bounds__(256) void rope_axes_kernel(const T* t, int t_stride, T* out, int out_stride, size_t row0, unsigned threads, int n_heads, int d, RopeAxes ax, int own,
+                                                        double log2_base, const int32_t* __restrict__ pos, int inverse) {
+  __shared__ double theta[ROPE_MAX_D / 2];
+  const int half = d / 2;
+  for (int i = threadIdx.x; i < half; i += 256) {
+    int a = 0;
+    while (a + 1 < ax.n && i >= ax.first[a + 1]) a++;
+    theta[i] = exp2(-(own ? (double)(i - ax.first[a]) / (double)(ax.first[a + 1] - ax.first[a]) : (double)i / (double)half) * log2_base);
+  }
+  __syncthreads();
+  const unsigned idx = blockIdx.x * 256 + threadIdx.x, chunks = half / 8, groups = (n_heads + HEADS - 1) / HEADS;
+  if (idx >= threads) return;
+  const int c = idx % chunks, head0 = idx / chunks % groups * HEADS;
+  const size_t row = row0 + idx / (chunks * groups);
+  const size_t at = (size_t)head0 * d + (ADJACENT ? c * 16 : c * 8);
+  const T* pa = t + row * t_stride + at;
+  T* qa = out + row * out_stride + at;
+  Raw8<T> ra[HEADS], rb[HEADS];
+#pragma unroll
+  for (int h = 0; h < HEADS; h++)
+    if (head0 + h < n_heads) {
+      ra[h].load(pa + h * d);
+      rb[h].load(pa + h * d + (ADJACENT ? 8 : half));
+    }
+  float sn[8], co[8];
+  int p[ROPE_MAX_AXES];
+#pragma unroll
+  for (int a = 0; a < ROPE_MAX_AXES; a++) p[a] = a < ax.n ? pos[row * ax.n + a] : 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const int pair = c * 8 + i;
+    int q = p[0];
+#pragma unroll
+    for (int a = 1; a < ROPE_MAX_AXES; a++) q = a < ax.n && pair >= ax.first[a] ? p[a] : q;
+    double ang = (double)q * theta[pair];
+    ang -= 6.283185307179586476925 * rint(ang * 0.15915494309189533577);
+    sincosf((float)ang, &sn[i], &co[i]);
+    if (inverse) sn[i] = -sn[i];
+  }
+#pragma unroll
+  for (int h = 0; h < HEADS; h++) {
+    if (head0 + h >= n_heads) break;
+    Vec8<T> lo, hi;
+    lo.from(ra[h]);
+    hi.from(rb[h]);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {  // pair i: (lo[i], hi[i]), or the two elements side by side
+      float& x = ADJACENT ? (i < 4 ? lo.v[2 * i] : hi.v[2 * i - 8]) : lo.v[i];
+      float& y = ADJACENT ? (i < 4 ? lo.v[2 * i + 1] : hi.v[2 * i - 7]) : hi.v[i];
+      const float a = x, b = y;
+      x = fmaf(a, co[i], -__fmul_rn(b, sn[i]));  // the same roundings whatever HEADS is
+      y = fmaf(b, co[i], __fmul_rn(a, sn[i]));
+    }
+    lo.store(qa + h * d);
+    hi.store(qa + h * d + (ADJACENT ? 8 : half));
+  }
+}
+
 // ------------------------------------------------------------------------------------ SwiGLU
 template <typename T>
 __global__ void swiglu_fwd_kernel(const T* __restrict__ gu, T* __restrict__ a, int rows, int F) {
@@ -535,6 +599,41 @@ extern "C" int dh_rope_pairs(int dtype, int pairing, int T, int seq, int pos0, i
     if (dtype == DH_BF16) { if (pairing == DH_ROPE_ADJACENT) GO2(bf16_t, true); else GO2(bf16_t, false); }
     else { if (pairing == DH_ROPE_ADJACENT) GO(float, true, 1); else GO2(float, false); }
 #undef GO2
+#undef GO
+    DH_LAUNCH_CHECK();
+  }
+  return DH_OK;
+}
+
+extern "C" int dh_rope_axes(int dtype, int pairing, int form, int T, int n_axes, const int* axis_pairs, const int32_t* pos, int n_heads, int head_dim, float base, int inverse,
+                            const void* t, int t_stride, void* out, int out_stride, void* stream) {
+  if (dtype != DH_F32 && dtype != DH_BF16) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: unknown dtype %d", dtype);
+  if (pairing != DH_ROPE_HALVES && pairing != DH_ROPE_ADJACENT) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: unknown pairing %d", pairing);
+  if (form != DH_ROPE_AXES_SHARED && form != DH_ROPE_AXES_OWN) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: unknown form %d", form);
+  if (!(base > 0.f) || base > 1e30f) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: base %g must be positive and finite", (double)base);
+  if (T < 0 || n_heads <= 0 || head_dim <= 0 || head_dim % 16 || head_dim > ROPE_MAX_D || t_stride % 8 || out_stride % 8 || t_stride / head_dim < n_heads || out_stride / head_dim < n_heads)
+    DH_FAIL(DH_ERR_SHAPE, "rope_axes: T=%d heads=%d d=%d strides=%d,%d (d must be a multiple of 16 up to %d)", T, n_heads, head_dim, t_stride, out_stride, ROPE_MAX_D);
+  if (n_axes < 1 || n_axes > ROPE_MAX_AXES) DH_FAIL(DH_ERR_SHAPE, "rope_axes: %d axes (1..%d)", n_axes, ROPE_MAX_AXES);
+  if (!axis_pairs) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: null pointer");
+  RopeAxes ax = {n_axes, {0}};
+  for (int a = 0; a < n_axes; a++) {
+    if (axis_pairs[a] < 1 || axis_pairs[a] > head_dim / 2 - ax.first[a]) DH_FAIL(DH_ERR_SHAPE, "rope_axes: axis %d has %d pairs", a, axis_pairs[a]);
+    ax.first[a + 1] = ax.first[a] + axis_pairs[a];
+  }
+  if (ax.first[n_axes] != head_dim / 2) DH_FAIL(DH_ERR_SHAPE, "rope_axes: %d pairs for heads of %d", ax.first[n_axes], head_dim / 2);
+  if (T == 0) return DH_OK;
+  if (!t || !out || !pos) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: null pointer");
+  if (((uintptr_t)t | (uintptr_t)out) & 15) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: t and out must be 16-byte aligned");
+  if (t == out && t_stride != out_stride) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: in place both strides are the same");
+  const double l2b = log2((double)base);
+  const size_t per_row = (size_t)n_heads * (head_dim / 16), most = std::max<size_t>(1, ((size_t)1 << 31) / per_row);
+  for (size_t row0 = 0; row0 < (size_t)T; row0 += most) {  // (a launch's threads are counted in 32 bits)
+    const unsigned threads = (unsigned)(std::min(most, (size_t)T - row0) * per_row);
+#define GO(TT, ADJ)                                                                                                                                  \
+  rope_axes_kernel<TT, ADJ, 1><<<(threads + 255) / 256, 256, 0, (hipStream_t)stream>>>((const TT*)t, t_stride, (TT*)out, out_stride, row0, threads, n_heads, \
+                                                                                       head_dim, ax, form == DH_ROPE_AXES_OWN, l2b, pos, inverse)
+    if (dtype == DH_BF16) { if (pairing == DH_ROPE_ADJACENT) GO(bf16_t, true); else GO(bf16_t, false); }
+    else { if (pairing == DH_ROPE_ADJACENT) GO(float, true); else GO(float, false); }
 #undef GO
     DH_LAUNCH_CHECK();
   }

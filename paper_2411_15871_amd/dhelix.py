@@ -22,6 +22,7 @@ DH_F32, DH_BF16 = 0, 1
 DH_ARCH_LLAMA, DH_ARCH_GPT, DH_ARCH_MOE, DH_ARCH_LLAMA_CP = 0, 1, 2, 3
 DH_ROPE_HALVES, DH_ROPE_ADJACENT = 0, 1
 DH_GELU_TANH, DH_GELU_ERF = 0, 1
+DH_ROPE_AXES_SHARED, DH_ROPE_AXES_OWN = 0, 1
 DH_WS_FWD, DH_WS_BWD, DH_WS_SI = 0, 1, 2
 DH_COMM_ALLREDUCE, DH_COMM_ALLGATHER, DH_COMM_REDUCESCATTER = 0, 1, 2
 DH_COMM_A2A_DISPATCH, DH_COMM_A2A_COMBINE = 3, 4
@@ -126,6 +127,15 @@ class dh_plan(C.Structure):
 
 # Every symbol include/dhelix.h declares, with its C signature.
 _P, _I, _Z, _D, _F = C.c_void_p, C.c_int, C.c_size_t, C.c_double, C.c_float
+class dh_docs(C.Structure):
+    _fields_ = [("T", C.c_int), ("n_docs", C.c_int), ("nq", C.c_int), ("nkv", C.c_int), ("doc_start", C.c_void_p), ("prefix", C.c_void_p),
+                ("pos", C.c_void_p), ("table", C.c_void_p)]
+
+
+class dh_tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_size_t), ("dtype", C.c_int)]
+
+
 SIGNATURES = {
     "dh_last_error": (C.c_char_p, []),
     "dh_layer_create": (_I, [C.POINTER(dh_layer_config), C.POINTER(_P)]),
@@ -223,6 +233,19 @@ SIGNATURES = {
     "dh_bias_residual_add": (_I, [_I, _I, _I, _P, _P, _P, _P, _P]),
     "dh_colsum": (_I, [_I, _I, _I, _P, _P, _P, _Z, _P]),
     "dh_colsum_ws_bytes": (_Z, [_I, _I]),
+    "dh_docs_table_bytes": (_Z, [_I, _I, _I]),
+    "dh_docs_plan": (_I, [C.POINTER(dh_docs), _P]),
+    "dh_attn_docs_fwd": (_I, [_I, C.POINTER(dh_docs), _I, _F, _P, _P, _P, _P, _Z, _P]),
+    "dh_attn_docs_fwd_workspace_bytes": (_Z, [_I, _I, _I, _I, _I]),
+    "dh_attn_docs_bwd": (_I, [_I, C.POINTER(dh_docs), _I, _F, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dh_attn_docs_bwd_workspace_bytes": (_Z, [_I, _I, _I, _I, _I]),
+    "dh_rope_axes": (_I, [_I, _I, _I, _I, _I, C.POINTER(C.c_int), _P, _I, _I, _F, _I, _P, _I, _P, _I, _P]),
+    "dh_grad_norm": (_I, [_I, C.POINTER(dh_tensor), _P, _P, _Z, _P]),
+    "dh_grad_norm_ws_bytes": (_Z, [_I, C.POINTER(dh_tensor)]),
+    "dh_grad_clip": (_I, [_I, C.POINTER(dh_tensor), _P, _F, _P]),
+    "dh_moe_balance_fwd": (_I, [_I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dh_moe_balance_ws_bytes": (_Z, [_I, _I]),
+    "dh_moe_balance_bwd": (_I, [_I, _I, _P, _P, _P, _P, _P, _I, _P, _P]),
 }
 for _name, (_res, _args) in SIGNATURES.items():
     _fn = getattr(lib, _name)
@@ -797,3 +820,78 @@ def dh_colsum(dtype, T, N, x, out, ws, ws_bytes, stream=None):
 
 FWD_OPS = op_names(DH_ARCH_LLAMA, 0)
 BWD_OPS = op_names(DH_ARCH_LLAMA, 1)
+
+
+def docs(T, n_docs, nq, nkv, doc_start, prefix, pos, table):
+    """dh_docs of a packed micro-batch; the tensors have to outlive it."""
+    return dh_docs(T, n_docs, nq, nkv, _ptr(doc_start), _ptr(prefix), _ptr(pos), _ptr(table))
+
+
+def dh_docs_table_bytes(T, nq, nkv):
+    return lib.dh_docs_table_bytes(T, nq, nkv)
+
+
+def dh_docs_plan(docs, stream=None):
+    _check(lib.dh_docs_plan(C.byref(docs), _stream(stream)))
+
+
+def dh_attn_docs_fwd(dtype, docs, d, cap, qkv, o, lse, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_attn_docs_fwd(dtype, C.byref(docs), d, cap, _ptr(qkv), _ptr(o), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dh_attn_docs_fwd_workspace_bytes(dtype, T, nq, nkv, d):
+    return lib.dh_attn_docs_fwd_workspace_bytes(dtype, T, nq, nkv, d)
+
+
+def dh_attn_docs_bwd(dtype, docs, d, cap, qkv, o, dout, lse, dqkv, delta, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_attn_docs_bwd(dtype, C.byref(docs), d, cap, _ptr(qkv), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dqkv), _ptr(delta), _ptr(ws), ws_bytes,
+                                _stream(stream)))
+
+
+def dh_attn_docs_bwd_workspace_bytes(dtype, T, nq, nkv, d):
+    return lib.dh_attn_docs_bwd_workspace_bytes(dtype, T, nq, nkv, d)
+
+
+def dh_rope_axes(dtype, pairing, form, T, axis_pairs, pos, n_heads, head_dim, base, inverse, t, t_stride, out, out_stride, stream=None):
+    pairs = (C.c_int * len(axis_pairs))(*axis_pairs)
+    _check(lib.dh_rope_axes(dtype, pairing, form, T, len(axis_pairs), pairs, _ptr(pos), n_heads, head_dim, base, int(inverse), _ptr(t), t_stride, _ptr(out),
+                            out_stride, _stream(stream)))
+
+
+def tensor_list(tensors, out=None):
+    """dh_tensor array of torch tensors (float32 or bfloat16, contiguous), which have to outlive it; out: where dh_grad_clip writes, None = in place."""
+    array = (dh_tensor * len(tensors))()
+    for i, t in enumerate(tensors):
+        if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_contiguous():
+            raise ValueError("tensor %d: contiguous float32 or bfloat16 is wanted" % i)
+        if out is not None and (out[i].dtype != t.dtype or out[i].numel() != t.numel() or not out[i].is_contiguous()):
+            raise ValueError("tensor %d: its out has to be contiguous, of its type and size" % i)
+        array[i] = dh_tensor(t.data_ptr(), None if out is None else out[i].data_ptr(), t.numel(), DH_BF16 if t.dtype == torch.bfloat16 else DH_F32)
+    return array
+
+
+def dh_grad_norm(tensors, norm, ws, ws_bytes, stream=None):
+    """tensors: of tensor_list."""
+    _check(lib.dh_grad_norm(len(tensors), tensors, _ptr(norm), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dh_grad_norm_ws_bytes(tensors):
+    return lib.dh_grad_norm_ws_bytes(len(tensors), tensors)
+
+
+def dh_grad_clip(tensors, norm, max_norm, stream=None):
+    _check(lib.dh_grad_clip(len(tensors), tensors, _ptr(norm), max_norm, _stream(stream)))
+
+
+def dh_moe_balance_fwd(T, E, logits, idx, n_live, counts, prob_mean, lse, loss, ws, ws_bytes, stream=None):
+    _check(lib.dh_moe_balance_fwd(T, E, _ptr(logits), _ptr(idx), _ptr(n_live), _ptr(counts), _ptr(prob_mean), _ptr(lse), _ptr(loss), _ptr(ws), ws_bytes,
+                                  _stream(stream)))
+
+
+def dh_moe_balance_ws_bytes(T, E):
+    return lib.dh_moe_balance_ws_bytes(T, E)
+
+
+def dh_moe_balance_bwd(T, E, logits, lse, counts, n_live, dloss, accumulate, dlogits, stream=None):
+    _check(lib.dh_moe_balance_bwd(T, E, _ptr(logits), _ptr(lse), _ptr(counts), _ptr(n_live), _ptr(dloss), 1 if accumulate else 0, _ptr(dlogits),
+                                  _stream(stream)))
