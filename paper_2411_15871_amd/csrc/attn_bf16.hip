@@ -2007,3 +2007,5 @@ int dh_launch_attn_bwd_bf16(int batch, int seq_q, int nq, int nkv, int d, const 
 #undef DH_ATTN_BWD
   return DH_OK;
 }
+
+#include "attn_docs_bf16.h"

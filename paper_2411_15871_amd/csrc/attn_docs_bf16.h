@@ -1,0 +1,678 @@
+// bf16 attention over packed documents on the matrix cores, forward and backward (part of attn_bf16.hip, whose tiles, fragments and layouts it uses).
+//
+// A block of 128 rows lies anywhere in the packed row of documents and walks the one run of 64-row tiles that any of its rows meets (borders ascend with the row): the
+// documents need no padding, and a block of short documents walks few tiles.  What a lane's row sees inside a tile is an interval, one comparison an element, and only
+// tiles that some row of the wave does not see whole are masked.  The runs come from the lists that dh_docs_plan has made (docs.h): longest first, long ones cut, partial
+// results merged in order by a launch behind.
+//
+// Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN: a wave whose result is not finite makes the rows
+// concerned again, one at a time, over exactly what they see (docs_row_*).  Rows outside all documents are never read: transfers take the nearest row of a document.
+//
+// CAP: x = cap tanh(x / cap) as cap - 2 cap r with r = 1 / (1 + e^(2x/cap)), one exponential and one reciprocal more an element; its slope is 4 r (1 - r) = 4 e r r.
+#pragma once
+#include "docs.h"
+
+struct DocsTiled {
+  DocsAttn a;
+  float exp_scale;  // score -> exponent of 2 without a cap; with one: score -> log2 of e^(2x/cap)
+  float cap_log2;   // cap * log2(e)
+};
+// Visible interval of a lane's row, [at, at + n): empty for rows of no document; and the wave's: some row sees [any0, any1), every row of a document [all0, all1).
+struct DocsSeen { int at, n, any0, any1, all0, all1; };
+__device__ __forceinline__ DocsSeen docs_seen(bool live, int from, int end) {
+  const uint32_t rows = (uint32_t)__ballot(live);  // both halves of a wave hold the same 32 rows
+  DocsSeen s = {from, live ? end - from : 0, INT32_MAX, INT32_MIN, INT32_MAX, INT32_MIN};
+  if (rows != 0) {
+    const int first = __builtin_ctz(rows), last = 31 - __builtin_clz(rows);
+    s.any0 = __builtin_amdgcn_readlane(from, first);
+    s.any1 = __builtin_amdgcn_readlane(end, last);
+    s.all0 = __builtin_amdgcn_readlane(from, last);
+    s.all1 = __builtin_amdgcn_readlane(end, first);
+  }
+  return s;
+}
+// Per-lane byte offsets as tile_voff, rows clamped to [first, last].
+template <int D>
+__device__ __forceinline__ void docs_voff(uint32_t (&v)[ATile<D>::IPW], int ld, int wave, int lane, int first, int last) {
+  using TL = ATile<D>;
+#pragma unroll
+  for (int j = 0; j < TL::IPW; j++) {
+    const int p = (wave * TL::IPW + j) * 64 + lane;
+    const int row = p / TL::CPR, c = (p % TL::CPR) ^ TL::swz(row);
+    v[j] = (uint32_t)(((size_t)max(first, min(row, last)) * ld + c * 8) * sizeof(bf16_t));
+  }
+}
+// Whether any of N accumulator tiles holds an infinity or a NaN.
+template <int N>
+__device__ __forceinline__ bool docs_not_finite(const f32x16 (&t)[N]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < N; i++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) m = max(m, __builtin_bit_cast(uint32_t, t[i][r]) & 0x7fffffffu);
+  return m >= 0x7f800000u;
+}
+// A score as an exponent of 2 under the cap; e and r as above.
+__device__ __forceinline__ float docs_cap_exponent(float s, float k, float cap_log2, float& e, float& r) {
+  e = fast_exp2(fminf(s * k, 64.f));  // beyond 2^64 the tanh is 1 in float32, its slope 2^-62
+  r = __builtin_amdgcn_rcpf(1.f + e);
+  return fmaf(-2.f * cap_log2, r, cap_log2);
+}
+// ================================================================================ forward
+// grid (units * nq)
+template <int D, bool CAP>
+__global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o, float* __restrict__ lse,
+                                                                       float* __restrict__ part_o, float* __restrict__ part_ml) {
+  using TL = ATile<D>;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];  // K ring, then V ring
+  const lds_char* sm = (const lds_char*)smem;
+  const DocsView& v = p.a.v;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
+  const int nq = p.a.nq, nkv = p.a.nkv, h = blockIdx.x % nq, id = blockIdx.x / nq, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
+  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
+  const DocsUnit u = v.units_q[id];
+  const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
+  const int iw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, iq = iw + l32, row = min(iq, T - 1);
+  const int lo = v.lo[row];
+  const bool live = iq < T && v.hi[row] > lo;
+  const int end = max(iq + 1, v.pre[row]);
+  bf16x8 qf[D / 16];
+  load_row_frags<D>(qf, qkv + (size_t)row * ld + (size_t)h * D, live, kg);
+  const DocsSeen see = docs_seen(live, lo, end);
+  const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
+  const char* kbase = reinterpret_cast<const char*>(kcol);
+  const char* vbase = reinterpret_cast<const char*>(kcol + (size_t)nkv * D);
+  const size_t tstride = (size_t)AB_KT * ld * sizeof(bf16_t);
+  f32x16 ot[D / 32];
+  float m = -3.0e38f, l = 0.f;  // finite: a tile that a row does not see leaves it alone
+  pin_frags(qf);
+  FragAddr<D> fa;
+  fa.init(lane);
+  uint32_t voff[TL::IPW];
+  tile_voff<D>(voff, ld, wave, lane, AB_KT);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) ot[dt][r] = 0.f;
+  const uint32_t ldsK = lds_address(smem), ldsV = ldsK + AF_RING * TL::BYTES;
+  auto issue = [&](int t, int slot) {
+    const int first = live0 - t * AB_KT, last = live1 - 1 - t * AB_KT;
+    if (first <= 0 && last >= AB_KT - 1) {
+      tile_dma<D>(kbase + t * tstride, voff, ldsK + slot * TL::BYTES, wave);
+      tile_dma<D>(vbase + t * tstride, voff, ldsV + slot * TL::BYTES, wave);
+    } else {
+      uint32_t vc[TL::IPW];
+      docs_voff<D>(vc, ld, wave, lane, max(first, 0), min(last, AB_KT - 1));
+      tile_dma<D>(kbase + t * tstride, vc, ldsK + slot * TL::BYTES, wave);
+      tile_dma<D>(vbase + t * tstride, vc, ldsV + slot * TL::BYTES, wave);
+    }
+  };
+  issue(u.f0, 0);
+  int slot = 0;
+  for (int t = u.f0; t < u.f1; t++, slot ^= 1) {
+    dma_wait<0>();
+    __syncthreads();  // tile t is visible; every wave is done with tile t-1, whose slot tile t+1 reuses
+    if (t + 1 < u.f1) issue(t + 1, slot ^ 1);
+    const int kb = t * AB_KT;
+    if (kb >= see.any1 || kb + AB_KT <= see.any0) continue;  // no key of the tile is visible to any row of this wave
+    TilePtrs<D> Kp, Vp;
+    Kp.set(sm + slot * TL::BYTES, fa);
+    Vp.set(sm + (AF_RING + slot) * TL::BYTES, fa);
+    f32x16 st[2];
+    score_tiles<D>(st, Kp, qf);
+    if constexpr (CAP) {
+#pragma unroll
+      for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          float e, q;
+          st[mt][r] = docs_cap_exponent(st[mt][r], p.exp_scale, p.cap_log2, e, q);
+        }
+    }
+    if (kb < see.all0 || kb + AB_KT > see.all1) {
+#pragma unroll
+      for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : -INFINITY;
+    }
+    float mx = fmaxf(st[0][0], st[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; r++) mx = fmaxf(mx, fmaxf(st[0][r], st[1][r]));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float scale = CAP ? 1.f : p.exp_scale, mnew = mx * scale;
+    float rs = 0.f;
+    if (__any(mnew > m + AF_TAU)) {  // the reference maximum moves where a row's probabilities would grow beyond 2^AF_TAU
+      const float mn = fmaxf(m, mnew);
+      const float alpha = fast_exp2(m - mn);
+      l *= alpha;
+      m = mn;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) ot[dt][r] *= alpha;
+    }
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        const float x = CAP ? fast_exp2(st[mt][r] - m) : fast_exp2(fmaf(st[mt][r], scale, -m));
+        st[mt][r] = x;
+        rs += x;
+      }
+    rs += __shfl_xor(rs, 32, 64);
+    l += rs;
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+      for (int c = 0; c < 2; c++) {
+        const bf16x8 pf = pack_rows(st[mt], c);
+        const int ro = (mt * 32 + 16 * c) * TL::LD * 2;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; dt++) ot[dt] = MFMA(lds_frag_tr(Vp.t0[dt], Vp.t1[dt], ro), pf, ot[dt]);
+      }
+  }
+  __syncthreads();  // every wave is done with the K/V rings: their LDS serves the output turn
+  const bool bad = live && (docs_not_finite<D / 32>(ot) || !(__builtin_bit_cast(uint32_t, l) < 0x7f800000u));
+  const uint64_t both = __ballot(bad), alive = __ballot(live);
+  const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
+  float* prow = part_o + ((size_t)u.slot * nq + h) * DOCS_BLOCK * D + (size_t)wave * 32 * D;
+  float* pml = part_ml + (((size_t)u.slot * nq + h) * DOCS_BLOCK + wave * 32) * 2;
+  bf16_t* orow = o + (size_t)iw * nq * D + (size_t)h * D;
+  float* lrow = lse + (size_t)h * T + iw;
+  if (u.slot >= 0) {  // partial result of this unit
+    wave_rows_out_f32<D>(
+        reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
+        [&](int dt, int q4) { return f32x4{ot[dt][4 * q4], ot[dt][4 * q4 + 1], ot[dt][4 * q4 + 2], ot[dt][4 * q4 + 3]}; },
+        [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * D : nullptr; });
+    if (lane < 32 && (store >> lane) & 1) {
+      pml[l32 * 2] = m;
+      pml[l32 * 2 + 1] = l;
+    }
+  } else {
+    const float inv = 1.0f / l;
+    wave_rows_out_bf16<D>(
+        reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+        [&](int dt, int q4) { return f32x4{ot[dt][4 * q4] * inv, ot[dt][4 * q4 + 1] * inv, ot[dt][4 * q4 + 2] * inv, ot[dt][4 * q4 + 3] * inv}; },
+        [&](int r) { return (store >> r) & 1 ? orow + (size_t)r * nq * D : nullptr; });
+    if (lane < 32 && (store >> lane) & 1) lrow[l32] = (m + log2f(l)) * 0.6931471805599453f;
+  }
+  for (uint32_t rest = again; rest != 0; rest &= rest - 1) {
+    const int r = __builtin_ctz(rest), i = iw + r, j0 = max(__builtin_amdgcn_readlane(lo, r), u.f0 * AB_KT), j1 = min(__builtin_amdgcn_readlane(end, r), u.f1 * AB_KT);
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, mr = -INFINITY, lr = 0.f;
+    docs_row_fwd(qkv + (size_t)i * ld + (size_t)h * D, kcol, kcol + (size_t)nkv * D, (size_t)ld, j0, j1, D, p.a.scale, p.a.cap, acc, mr, lr);
+#pragma unroll
+    for (int c = 0; c < D / 64; c++) {
+      if (u.slot >= 0) prow[(size_t)r * D + lane + 64 * c] = acc[c];
+      else orow[(size_t)r * nq * D + lane + 64 * c] = (bf16_t)(acc[c] / lr);
+    }
+    if (lane == 0) {
+      if (u.slot >= 0) {
+        pml[r * 2] = j0 < j1 ? mr * LOG2E : -3.0e38f;
+        pml[r * 2 + 1] = lr;
+      } else {
+        lrow[r] = mr + logf(lr);
+      }
+    }
+  }
+}
+
+// Merges the units of the query blocks that were cut, as attn_fwd_combine_kernel.  grid (8 * blocks that may be cut, nq): 16 rows a block, D/16 columns of a row a thread.
+template <int D>
+__global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled p, const float* __restrict__ part_o, const float* __restrict__ part_ml, bf16_t* __restrict__ o,
+                                                                float* __restrict__ lse) {
+  const DocsView& v = p.a.v;
+  const int nq = p.a.nq, k = blockIdx.x >> 3, h = blockIdx.y;
+  if (!docs_fits(v, nq, p.a.nkv) || k >= v.head[DOCS_SPLIT_Q]) return;
+  const DocsSplit s = v.split_q[k];
+  const int r = (blockIdx.x & 7) * 16 + (threadIdx.x >> 4), i = s.block * DOCS_BLOCK + r;
+  if (i >= v.T || v.hi[i] <= v.lo[i]) return;
+  constexpr int CPT = D / 16;
+  const int c0 = (threadIdx.x & 15) * CPT;
+  const size_t unit = ((size_t)s.slot * nq + h) * DOCS_BLOCK + r, step = (size_t)nq * DOCS_BLOCK;  // rows of the first unit's partial result, and to the next unit's
+  float M = -3.0e38f;
+  for (int c = 0; c < s.n; c++) M = fmaxf(M, part_ml[(unit + c * step) * 2]);
+  float L = 0.f, acc[CPT];
+#pragma unroll
+  for (int e = 0; e < CPT; e++) acc[e] = 0.f;
+  for (int c = 0; c < s.n; c++) {
+    const float lc = part_ml[(unit + c * step) * 2 + 1];
+    if (lc == 0.f) continue;  // this unit's tiles hold no key of the row
+    const float w = exp2f(part_ml[(unit + c * step) * 2] - M);
+    L += w * lc;
+    const float* po = part_o + (unit + c * step) * D + c0;
+#pragma unroll
+    for (int e = 0; e < CPT; e += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(po + e);
+      acc[e] += w * x[0]; acc[e + 1] += w * x[1]; acc[e + 2] += w * x[2]; acc[e + 3] += w * x[3];
+    }
+  }
+  const float inv = 1.0f / L;
+  bf16_t* orow = o + ((size_t)i * nq + h) * D + c0;
+#pragma unroll
+  for (int e = 0; e < CPT; e += 4) {
+    bf16x4 x = {(bf16_t)(acc[e] * inv), (bf16_t)(acc[e + 1] * inv), (bf16_t)(acc[e + 2] * inv), (bf16_t)(acc[e + 3] * inv)};
+    *reinterpret_cast<bf16x4*>(orow + e) = x;
+  }
+  if (c0 == 0) lse[(size_t)h * v.T + i] = (M + log2f(L)) * 0.6931471805599453f;
+}
+
+// ================================================================================ backward: dQ
+// As attn_bwd_dq_block; the first unit of a block also stores its rows' delta and lse2 for the dK/dV launch behind it.  grid (units * nq)
+#define DOCS_DQ_RING 2
+template <int D, bool CAP>
+__global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                                                      const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
+                                                                      float* __restrict__ part) {
+  using TL = ATile<D>;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];  // K ring, then V ring
+  const lds_char* sm = (const lds_char*)smem;
+  const DocsView& v = p.a.v;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
+  const int nq = p.a.nq, nkv = p.a.nkv, h = blockIdx.x % nq, id = blockIdx.x / nq, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
+  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
+  const DocsUnit u = v.units_q[id];
+  const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
+  const int iw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, iq = iw + l32, row = min(iq, T - 1);
+  const int lo = v.lo[row];
+  const bool live = iq < T && v.hi[row] > lo;
+  const int end = max(iq + 1, v.pre[row]);
+  bf16x8 qf[D / 16], dof[D / 16];
+  load_row_frags<D>(qf, qkv + (size_t)row * ld + (size_t)h * D, live, kg);
+  load_row_frags<D>(dof, dout + ((size_t)row * nq + h) * D, live, kg);
+  const float l2 = live ? lse[(size_t)h * T + row] * LOG2E : 0.f;
+  float dl = 0.f;
+  {
+    bf16x8 of[D / 16];
+    load_row_frags<D>(of, o + ((size_t)row * nq + h) * D, live, kg);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) dl = fmaf((float)dof[ks][e], (float)of[ks][e], dl);
+    dl += __shfl_xor(dl, 32, 64);
+    if ((u.block2 & 1) && kg == 0 && live) {
+      delta[(size_t)h * T + row] = dl;
+      lse2[(size_t)h * T + row] = l2;
+    }
+  }
+  const DocsSeen see = docs_seen(live, lo, end);
+  const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
+  const char* kbase = reinterpret_cast<const char*>(kcol);
+  const char* vbase = reinterpret_cast<const char*>(kcol + (size_t)nkv * D);
+  const size_t tstride = (size_t)AB_KT * ld * sizeof(bf16_t);
+  f32x16 dqt[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(dqt[dt]);
+  FragAddr<D> fa;
+  fa.init(lane);
+  uint32_t voff[TL::IPW];
+  tile_voff<D>(voff, ld, wave, lane, AB_KT);
+  const uint32_t ldsK = lds_address(smem), ldsV = ldsK + DOCS_DQ_RING * TL::BYTES;
+  auto issue = [&](int t, int slot) {
+    const int first = live0 - t * AB_KT, last = live1 - 1 - t * AB_KT;
+    if (first <= 0 && last >= AB_KT - 1) {
+      tile_dma<D>(kbase + t * tstride, voff, ldsK + slot * TL::BYTES, wave);
+      tile_dma<D>(vbase + t * tstride, voff, ldsV + slot * TL::BYTES, wave);
+    } else {
+      uint32_t vc[TL::IPW];
+      docs_voff<D>(vc, ld, wave, lane, max(first, 0), min(last, AB_KT - 1));
+      tile_dma<D>(kbase + t * tstride, vc, ldsK + slot * TL::BYTES, wave);
+      tile_dma<D>(vbase + t * tstride, vc, ldsV + slot * TL::BYTES, wave);
+    }
+  };
+  pin_frags(qf);
+  pin_frags(dof);
+  pin_scalar(l2);
+  pin_scalar(dl);
+  issue(u.f0, 0);
+  int slot = 0;
+  for (int t = u.f0; t < u.f1; t++, slot ^= 1) {
+    dma_wait<0>();
+    __syncthreads();
+    if (t + 1 < u.f1) issue(t + 1, slot ^ 1);
+    const int kb = t * AB_KT;
+    if (kb >= see.any1 || kb + AB_KT <= see.any0) continue;
+    TilePtrs<D> Kp;
+    Kp.set(sm + slot * TL::BYTES, fa);
+    f32x16 st[2], dp[2];
+    // P^T from S^T beside the dP^T products
+    score_tiles2<D, DOCS_DQ_RING * TL::BYTES, 1>(st, Kp, qf, dp, dof, [&](int j) {
+      constexpr int N = 32 / (D / 16);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int x = j * N + i;
+        const float s = st[x >> 4][x & 15];
+        if constexpr (CAP) {
+          float e, r;
+          const float pr = fast_exp2(docs_cap_exponent(s, p.exp_scale, p.cap_log2, e, r) - l2);
+          st[x >> 4][x & 15] = pr * (4.f * e * r * r);  // times the slope at once: dQ needs no probability by itself
+        } else {
+          st[x >> 4][x & 15] = fast_exp2(fmaf(s, p.exp_scale, -l2));
+        }
+      }
+    });
+    TrFrags<D> fr;
+    tr_fetch<D>(fr, Kp, 0);
+    if (kb < see.all0 || kb + AB_KT > see.all1) {
+#pragma unroll
+      for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : 0.f;
+    }
+    // dS^T = P^T (dP^T - delta) (P^T with its slope), one quarter (8 registers of a tile) ahead of the products that consume it
+    auto ds_quarter = [&](int g) {
+#pragma unroll
+      for (int r = 8 * (g & 1); r < 8 * (g & 1) + 8; r++) st[g >> 1][r] *= dp[g >> 1][r] - dl;
+    };
+    ds_quarter(0);
+    acc_tile_tr<D, false, false>(dqt, fr, Kp, st, Kp, [&](int g) { if (g + 1 < 4) ds_quarter(g + 1); });
+  }
+  __syncthreads();
+  const uint64_t both = __ballot(live && docs_not_finite<D / 32>(dqt)), alive = __ballot(live);
+  const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
+  float* prow = part + (((size_t)u.slot * nq + h) * DOCS_BLOCK + wave * 32) * D;
+  bf16_t* out = dqkv + (size_t)iw * ld + (size_t)h * D;
+  const float scale = p.a.scale;
+  if (u.slot >= 0) {
+    wave_rows_out_f32<D>(
+        reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
+        [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4], dqt[dt][4 * q4 + 1], dqt[dt][4 * q4 + 2], dqt[dt][4 * q4 + 3]}; },
+        [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * D : nullptr; });
+  } else {
+    wave_rows_out_bf16<D>(
+        reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+        [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4] * scale, dqt[dt][4 * q4 + 1] * scale, dqt[dt][4 * q4 + 2] * scale, dqt[dt][4 * q4 + 3] * scale}; },
+        [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld : nullptr; });
+  }
+  for (uint32_t rest = again; rest != 0; rest &= rest - 1) {
+    const int r = __builtin_ctz(rest), i = iw + r, j0 = max(__builtin_amdgcn_readlane(lo, r), u.f0 * AB_KT), j1 = min(__builtin_amdgcn_readlane(end, r), u.f1 * AB_KT);
+    const float dr = __shfl(dl, r, 64), lr = lse[(size_t)h * T + i];
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    docs_row_dq(qkv + (size_t)i * ld + (size_t)h * D, dout + ((size_t)i * nq + h) * D, kcol, kcol + (size_t)nkv * D, (size_t)ld, j0, j1, D, scale, p.a.cap, lr, dr, acc);
+#pragma unroll
+    for (int c = 0; c < D / 64; c++) {
+      if (u.slot >= 0) prow[(size_t)r * D + lane + 64 * c] = acc[c];
+      else out[(size_t)r * ld + lane + 64 * c] = (bf16_t)(acc[c] * scale);
+    }
+  }
+}
+
+// ================================================================================ backward: dK, dV
+// As attn_bwd_dkv_block in phases: a block owns 128 keys of a key/value head and walks the query tiles of the group's heads, one head after the other.  grid (units * nkv)
+template <int D, bool CAP>
+__global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+                                                                        const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv,
+                                                                        float* __restrict__ part) {
+  using TL = ATile<D>;
+  constexpr bool AGPR = D == 128;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];  // Q ring, dO ring, lse2 ring, delta ring
+  const lds_char* sm = (const lds_char*)smem;
+  const DocsView& v = p.a.v;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
+  const int nq = p.a.nq, nkv = p.a.nkv, grp = nq / nkv, hk = blockIdx.x % nkv, id = blockIdx.x / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, T = v.T;
+  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_K]) return;
+  const DocsUnit u = v.units_k[id];
+  const DocsSpan span = v.span_k[id];
+  const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
+  const int jw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, jk = jw + l32, row = min(jk, T - 1);
+  const int lo = v.lo[row], end = v.hi[row];
+  const bool live = jk < T && end > lo;
+  const int from = jk < v.pre[row] ? lo : jk;
+  const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
+  bf16x8 kf[D / 16], vf[D / 16];
+  load_row_frags<D>(kf, kcol + (size_t)row * ld, live, kg);
+  load_row_frags<D>(vf, kcol + (size_t)row * ld + (size_t)nkv * D, live, kg);
+  const DocsSeen see = docs_seen(live, from, end);
+  const char* qbase = reinterpret_cast<const char*>(qkv + (size_t)hq * D);
+  const char* obase = reinterpret_cast<const char*>(dout + (size_t)hq * D);
+  float* lse_s = reinterpret_cast<float*>(smem + 2 * AB_RING * TL::BYTES);
+  float* del_s = lse_s + AB_RING * AB_KT;
+  f32x16 dkt[D / 32], dvt[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) { acc_zero<AGPR>(dkt[dt]); acc_zero<AGPR>(dvt[dt]); }
+  FragAddr<D> fa;
+  fa.init(lane);
+  uint32_t vq[TL::IPW], vo[TL::IPW];
+  tile_voff<D>(vq, ld, wave, lane, AB_KT);
+  tile_voff<D>(vo, ldo, wave, lane, AB_KT);
+  const uint32_t ldsQ = lds_address(smem), ldsO = ldsQ + AB_RING * TL::BYTES;
+  const int nt = span.n, f0 = u.f0, f1 = u.f1;
+  const size_t qstride = (size_t)AB_KT * ld * sizeof(bf16_t), ostride = (size_t)AB_KT * ldo * sizeof(bf16_t);
+  int gi = f0 / nt, ti = span.first + f0 - gi * nt;  // head of the group and tile to transfer next
+  int tc = ti;                                       // tile to work off next
+  const uint32_t ldsS = ldsQ + 2 * AB_RING * TL::BYTES + (wave & 1) * AB_RING * AB_KT * sizeof(float);  // even waves transfer lse2, odd ones delta
+  const float* srow = ((wave & 1) ? delta : lse2) + (size_t)hq * T;
+  pin_frags(kf);
+  pin_frags(vf);
+  auto issue = [&](int slot) {
+    const int first = max(0, live0 - ti * AB_KT), last = min(AB_KT - 1, live1 - 1 - ti * AB_KT);
+    const char* qp = qbase + ti * qstride + gi * (D * sizeof(bf16_t));
+    const char* op = obase + ti * ostride + gi * (D * sizeof(bf16_t));
+    if (first == 0 && last == AB_KT - 1) {
+      tile_dma<D>(qp, vq, ldsQ + slot * TL::BYTES, wave);
+      tile_dma<D>(op, vo, ldsO + slot * TL::BYTES, wave);
+    } else {
+      uint32_t vc[TL::IPW];
+      docs_voff<D>(vc, ld, wave, lane, first, last);
+      tile_dma<D>(qp, vc, ldsQ + slot * TL::BYTES, wave);
+      docs_voff<D>(vc, ldo, wave, lane, first, last);
+      tile_dma<D>(op, vc, ldsO + slot * TL::BYTES, wave);
+    }
+    dma4_base(srow + (size_t)gi * T + (size_t)ti * AB_KT, (uint32_t)(max(first, min(lane, last)) * sizeof(float)), ldsS + slot * AB_KT * sizeof(float));
+    if (++ti == span.first + nt) { ti = span.first; gi++; }
+  };
+  issue(0);
+  if (f0 + 1 < f1) issue(1);
+  int slot = 0;
+  for (int f = f0; f < f1; f++, slot = slot == AB_RING - 1 ? 0 : slot + 1) {
+    if (f + 1 < f1) dma_wait<2 * TL::IPW + 1>(); else dma_wait<0>();
+    __syncthreads();
+    if (f + 2 < f1) issue(slot == 0 ? AB_RING - 1 : slot - 1);
+    const int qb = tc * AB_KT;
+    if (++tc == span.first + nt) tc = span.first;
+    if (qb >= see.any1 || qb + AB_KT <= see.any0) continue;  // no query of the tile sees any key of this wave
+    TilePtrs<D> Qp, Op;
+    Qp.set(sm + slot * TL::BYTES, fa);
+    Op.set(sm + (AB_RING + slot) * TL::BYTES, fa);
+    const float* ls = lse_s + slot * AB_KT;
+    const float* ds = del_s + slot * AB_KT;
+    f32x4 lv[8];  // rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
+#pragma unroll
+    for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ls + 8 * x + 4 * kg);
+    f32x16 st[2], dp[2], slope[CAP ? 2 : 1];
+    // P from S beside the dP products
+    score_tiles2<D, AB_RING * TL::BYTES, 3>(st, Qp, kf, dp, vf, [&](int j) {
+      constexpr int N = 8 / (D / 16) > 0 ? 8 / (D / 16) : 1;
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int x = j * N + i, mt = x >> 2, q4 = x & 3;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float s = st[mt][4 * q4 + e];
+          if constexpr (CAP) {
+            float ex, r;
+            st[mt][4 * q4 + e] = fast_exp2(docs_cap_exponent(s, p.exp_scale, p.cap_log2, ex, r) - lv[x][e]);
+            slope[mt][4 * q4 + e] = 4.f * ex * r * r;
+          } else {
+            st[mt][4 * q4 + e] = fast_exp2(fmaf(s, p.exp_scale, -lv[x][e]));
+          }
+        }
+      }
+    });
+    TrFrags<D> fr;
+    tr_fetch<D>(fr, Op, 0);
+#pragma unroll
+    for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ds + 8 * x + 4 * kg);
+    if (qb < see.all0 || qb + AB_KT > see.all1) {
+      const int first = qb + 4 * kg - see.at;
+#pragma unroll
+      for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          st[mt][r] = (uint32_t)(first + mt * 32 + 8 * (r >> 2) + (r & 3)) < (uint32_t)see.n ? st[mt][r] : 0.f;
+          if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    acc_tile_tr<D, true, AGPR>(dvt, fr, Op, st, Qp, [&](int g) {
+#pragma unroll
+      for (int r = 8 * (g & 1); r < 8 * (g & 1) + 8; r++) {
+        st[g >> 1][r] *= dp[g >> 1][r] - lv[4 * (g >> 1) + (r >> 2)][r & 3];
+        if constexpr (CAP) st[g >> 1][r] *= slope[g >> 1][r];
+      }
+    });
+    acc_tile_tr<D, false, AGPR>(dkt, fr, Qp, st, Qp, [](int) {});
+  }
+  acc_settle<AGPR>(dkt);
+  acc_settle<AGPR>(dvt);
+  __syncthreads();  // every wave is done with the Q/dO rings: their LDS serves the output turn (dK, then dV)
+  const uint64_t both = __ballot(live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt))), alive = __ballot(live);
+  const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
+  const float scale = p.a.scale;
+  auto dk_quad = [&](int dt, int q4) {
+    return f32x4{dkt[dt][4 * q4] * scale, dkt[dt][4 * q4 + 1] * scale, dkt[dt][4 * q4 + 2] * scale, dkt[dt][4 * q4 + 3] * scale};
+  };
+  auto dv_quad = [&](int dt, int q4) { return f32x4{dvt[dt][4 * q4], dvt[dt][4 * q4 + 1], dvt[dt][4 * q4 + 2], dvt[dt][4 * q4 + 3]}; };
+  float* prow = part + (((size_t)u.slot * nkv + hk) * DOCS_BLOCK + wave * 32) * (2 * D);
+  bf16_t* out = dqkv + (size_t)jw * ld + (size_t)(nq + hk) * D;
+  if (u.slot >= 0) {
+    float* reg = reinterpret_cast<float*>(smem) + wave * (32 * D);
+    wave_rows_out_f32<D>(reg, lane, dk_quad, [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * (2 * D) : nullptr; });
+    __builtin_amdgcn_wave_barrier();
+    wave_rows_out_f32<D>(reg, lane, dv_quad, [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * (2 * D) + D : nullptr; });
+  } else {
+    bf16_t* reg = reinterpret_cast<bf16_t*>(smem) + wave * (32 * D);
+    wave_rows_out_bf16<D>(reg, lane, dk_quad, [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld : nullptr; });
+    __builtin_amdgcn_wave_barrier();
+    wave_rows_out_bf16<D>(reg, lane, dv_quad, [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld + (size_t)nkv * D : nullptr; });
+  }
+  for (uint32_t rest = again; rest != 0; rest &= rest - 1) {
+    const int r = __builtin_ctz(rest), a0 = __builtin_amdgcn_readlane(from, r), a1 = __builtin_amdgcn_readlane(end, r);
+    const bf16_t* k = kcol + (size_t)(jw + r) * ld;
+    float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g = f0 / nt; g * nt < f1; g++) {  // the unit's run of tiles of each head
+      const int t0 = span.first + max(f0 - g * nt, 0), t1 = span.first + min(f1 - g * nt, nt);
+      docs_row_dkv(k, k + (size_t)nkv * D, qkv + (size_t)(hq + g) * D, (size_t)ld, dout + (size_t)(hq + g) * D, (size_t)ldo, lse + (size_t)(hq + g) * T, delta + (size_t)(hq + g) * T,
+                   max(a0, t0 * AB_KT), min(a1, t1 * AB_KT), D, scale, p.a.cap, dk, dv);
+    }
+#pragma unroll
+    for (int c = 0; c < D / 64; c++) {
+      const int e = lane + 64 * c;
+      if (u.slot >= 0) {
+        prow[(size_t)r * (2 * D) + e] = dk[c] * scale;
+        prow[(size_t)r * (2 * D) + D + e] = dv[c];
+      } else {
+        out[(size_t)r * ld + e] = (bf16_t)(dk[c] * scale);
+        out[(size_t)r * ld + (size_t)nkv * D + e] = (bf16_t)dv[c];
+      }
+    }
+  }
+}
+
+// Adds the units of the blocks that were cut, in order: rows of dQ (scaled here) and of [dK | dV].  The first nb_q blocks are (16 * blocks that may be cut, nq) of dQ, 8 rows
+// each; the rest (32 * blocks, nkv) of dK/dV, 4 rows each.
+template <int D>
+__global__ __launch_bounds__(256) void attn_docs_reduce_kernel(const DocsTiled p, const float* __restrict__ part_q, const float* __restrict__ part_kv, bf16_t* __restrict__ dqkv, unsigned nb_q,
+                                                               unsigned gqx, unsigned gkx) {
+  const DocsView& v = p.a.v;
+  const int nq = p.a.nq, nkv = p.a.nkv, ld = (nq + 2 * nkv) * D;
+  if (!docs_fits(v, nq, nkv)) return;
+  unsigned id = blockIdx.x;
+  const bool q = id < nb_q;
+  if (!q) id -= nb_q;
+  const unsigned gx = q ? gqx : gkx, x = id % gx;
+  const int h = id / gx, k = q ? x >> 4 : x >> 5, r0 = q ? (x & 15) * 8 : (x & 31) * 4, width = q ? D : 2 * D, heads = q ? nq : nkv;
+  if (k >= v.head[q ? DOCS_SPLIT_Q : DOCS_SPLIT_K]) return;
+  const DocsSplit s = q ? v.split_q[k] : v.split_k[k];
+  const float* part = q ? part_q : part_kv;
+  const size_t unit = ((size_t)s.slot * heads + h) * DOCS_BLOCK, step = (size_t)heads * DOCS_BLOCK * width;
+  const int e = threadIdx.x, row = r0 + e / (width / 4), c4 = (e % (width / 4)) * 4, i = s.block * DOCS_BLOCK + row;
+  if (row >= r0 + (q ? 8 : 4) || i >= v.T || v.hi[i] <= v.lo[i]) return;
+  f32x4 t = {0.f, 0.f, 0.f, 0.f};
+  const float* from = part + (unit + row) * width + c4;
+  for (int c = 0; c < s.n; c++) t += __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + c * step));
+  const float f = q ? p.a.scale : 1.f;
+  bf16x4 out = {(bf16_t)(t[0] * f), (bf16_t)(t[1] * f), (bf16_t)(t[2] * f), (bf16_t)(t[3] * f)};
+  bf16_t* dst = dqkv + (size_t)i * ld + (q ? (size_t)h * D + c4 : c4 < D ? (size_t)(nq + h) * D + c4 : (size_t)(nq + nkv + h) * D + (c4 - D));
+  *reinterpret_cast<bf16x4*>(dst) = out;
+}
+
+// ------------------------------------------------------------------------------------ host side
+static DocsTiled docs_tiled(const DocsAttn& a) {
+  const double log2e = 1.4426950408889634;
+  return {a, (float)(a.cap > 0.f ? 2.0 * log2e / sqrt((double)a.d) / a.cap : log2e / sqrt((double)a.d)), (float)(a.cap * log2e)};
+}
+
+size_t dh_attn_docs_fwd_bf16_ws_bytes(int T, int nq, int nkv, int d) {
+  return (size_t)docs_view_at(nullptr, T, nq, nkv).q.slots * nq * DOCS_BLOCK * ((size_t)d + 2) * sizeof(float);
+}
+
+template <int D, bool CAP>
+static int docs_fwd(const DocsTiled& p, const bf16_t* qkv, bf16_t* o, float* lse, float* ws, hipStream_t stream) {
+  static bool ready[DH_MAX_DEVICES] = {};
+  const size_t lds = 2 * AF_RING * (size_t)ATile<D>::BYTES;
+  bool& set = ready[dh_device_index()];
+  if (!set) {
+    if (int rc = set_lds(attn_docs_fwd_bf16_kernel<D, CAP>, lds)) return rc;
+    set = true;
+  }
+  const DocsCaps& q = p.a.v.q;
+  float* part_ml = ws + (size_t)q.slots * p.a.nq * DOCS_BLOCK * D;
+  attn_docs_fwd_bf16_kernel<D, CAP><<<(unsigned)q.units * p.a.nq, AB_THREADS, lds, stream>>>(p, qkv, o, lse, ws, part_ml);
+  DH_LAUNCH_CHECK();
+  if (q.splits > 0) {
+    attn_docs_combine_kernel<D><<<dim3(8 * q.splits, p.a.nq), 256, 0, stream>>>(p, ws, part_ml, o, lse);
+    DH_LAUNCH_CHECK();
+  }
+  return DH_OK;
+}
+int dh_launch_attn_docs_fwd_bf16(const DocsAttn& a, const bf16_t* qkv, bf16_t* o, float* lse, void* ws, size_t, hipStream_t stream) {
+  const DocsTiled p = docs_tiled(a);
+  if (a.d == 128) return a.cap > 0.f ? docs_fwd<128, true>(p, qkv, o, lse, (float*)ws, stream) : docs_fwd<128, false>(p, qkv, o, lse, (float*)ws, stream);
+  return a.cap > 0.f ? docs_fwd<64, true>(p, qkv, o, lse, (float*)ws, stream) : docs_fwd<64, false>(p, qkv, o, lse, (float*)ws, stream);
+}
+
+struct DocsBwdLayout { size_t lse2, dkv, dq, total; };
+static DocsBwdLayout docs_bwd_layout(const DocsView& v, int nq, int nkv, int d) {
+  DocsBwdLayout l;
+  size_t at = 0;
+  l.lse2 = at; at += dh_align_up((size_t)nq * v.T * sizeof(float), 256);
+  l.dkv = at; at += (size_t)v.k.slots * nkv * DOCS_BLOCK * 2 * d * sizeof(float);
+  l.dq = at; at += (size_t)v.q.slots * nq * DOCS_BLOCK * d * sizeof(float);
+  l.total = at;
+  return l;
+}
+size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view_at(nullptr, T, nq, nkv), nq, nkv, d).total; }
+
+template <int D, bool CAP>
+static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, char* ws, hipStream_t stream) {
+  static bool ready[DH_MAX_DEVICES] = {};
+  const size_t lds_dq = 2 * DOCS_DQ_RING * (size_t)ATile<D>::BYTES, lds_dkv = 2 * AB_RING * ((size_t)ATile<D>::BYTES + AB_KT * sizeof(float));
+  bool& set = ready[dh_device_index()];
+  if (!set) {
+    if (int rc = set_lds(attn_docs_dq_bf16_kernel<D, CAP>, lds_dq)) return rc;
+    if (int rc = set_lds(attn_docs_dkv_bf16_kernel<D, CAP>, lds_dkv)) return rc;
+    set = true;
+  }
+  const int nq = p.a.nq, nkv = p.a.nkv;
+  const DocsCaps &q = p.a.v.q, &k = p.a.v.k;
+  const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
+  float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
+  attn_docs_dq_bf16_kernel<D, CAP><<<(unsigned)q.units * nq, AB_THREADS, lds_dq, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
+  DH_LAUNCH_CHECK();
+  attn_docs_dkv_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv, AB_THREADS, lds_dkv, stream>>>(p, qkv, dout, lse, lse2, delta, dqkv, part_kv);
+  DH_LAUNCH_CHECK();
+  const unsigned gqx = 16 * q.splits, gkx = 32 * k.splits, nb_q = gqx * nq, nb_k = gkx * nkv;
+  if (nb_q + nb_k > 0) {
+    attn_docs_reduce_kernel<D><<<nb_q + nb_k, 256, 0, stream>>>(p, part_q, part_kv, dqkv, nb_q, gqx, gkx);
+    DH_LAUNCH_CHECK();
+  }
+  return DH_OK;
+}
+int dh_launch_attn_docs_bwd_bf16(const DocsAttn& a, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, void* ws, size_t,
+                                 hipStream_t stream) {
+  const DocsTiled p = docs_tiled(a);
+  if (a.d == 128)
+    return a.cap > 0.f ? docs_bwd<128, true>(p, qkv, o, dout, lse, dqkv, delta, (char*)ws, stream) : docs_bwd<128, false>(p, qkv, o, dout, lse, dqkv, delta, (char*)ws, stream);
+  return a.cap > 0.f ? docs_bwd<64, true>(p, qkv, o, dout, lse, dqkv, delta, (char*)ws, stream) : docs_bwd<64, false>(p, qkv, o, dout, lse, dqkv, delta, (char*)ws, stream);
+}

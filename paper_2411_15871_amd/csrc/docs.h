@@ -5,16 +5,80 @@
 // The table: a head of DOCS_HEAD ints, then three ints a row (arrays lo, hi, pre of T): the row's document is rows lo .. hi-1 and its prefix ends before row
 // `pre`.  Rows of no document have lo = hi = pre = their own index.  So row r sees keys lo[r] .. max(r + 1, pre[r]) - 1, and key j is seen by
 // rows (j < pre[j] ? lo[j] : j) .. hi[j] - 1.  All four borders ascend with the row.
+// Behind them the work of the tiled kernels, one list for blocks of 128 queries and one for blocks of 128 keys: units of a block and a run of the 64-row tiles it
+// meets, longest first.  A block with more tiles than the list's chunk length is cut into units of even length, whose partial results get a slot of workspace each;
+// a second list names these blocks.  Lengths follow from the documents, on the device; room for them follows from T and the heads alone.
+#define DOCS_MAX_T (1 << 28)  // tiles of a block, times the heads of a group, are counted in 32 bits
+#define DOCS_MAX_HEADS 1024
 #define DOCS_HEAD 16
-enum { DOCS_LIVE0 = 0, DOCS_LIVE1 = 1 };  // head: the rows of documents are [live0, live1)
+enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_UNITS_Q, DOCS_SPLIT_Q, DOCS_UNITS_K, DOCS_SPLIT_K };  // head: the rows of documents are [live0, live1)
+#define DOCS_BLOCK 128
+#define DOCS_TILE 64
+// A chunk holds at least DOCS_CHUNK tiles, and so many that all heads' tiles together make DOCS_TARGET chunks.
+#define DOCS_CHUNK_Q 8
+#define DOCS_CHUNK_K 8
+#define DOCS_TARGET_Q 1024
+#define DOCS_TARGET_K 768
+struct DocsCaps { int blocks, units, slots, splits; };
+// With chunks of c >= tiles of all blocks / (target / heads): sum of ceil(t / c) <= blocks + target / heads; blocks that are cut have t > c, and their units are
+// fewer than 2 t / c.  A block has at most tiles(T) + 1 tiles of each head of its group.
+static inline DocsCaps docs_caps(int T, int heads, int grp, int target, int chunk) {
+  const long long blocks = ((long long)T + DOCS_BLOCK - 1) / DOCS_BLOCK, most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp, extra = target / heads + 1;
+  const long long slots = most <= chunk ? 0 : blocks * ((most + chunk - 1) / chunk);
+  DocsCaps c;
+  c.blocks = (int)blocks;
+  c.units = (int)(blocks + extra);
+  c.slots = (int)(slots < 2 * extra ? slots : 2 * extra);
+  c.splits = (int)(blocks < extra ? blocks : extra);
+  if (c.slots == 0) c.splits = 0;
+  return c;
+}
+struct DocsUnit { int block2, f0, f1, slot; };       // block * 2 + (1: its first unit); its run of tiles [f0, f1); slot of its partial result or -1
+struct DocsSpan { int first, n, pad0, pad1; };       // of a key block: its query tiles (first, count); f0 and f1 count through the heads of the group
+struct DocsSplit { int block, slot, n, pad; };       // a block that is cut: slots of its n units
 struct DocsView {
   int T;
   const int32_t *head, *lo, *hi, *pre;
+  const DocsUnit *units_q, *units_k;
+  const DocsSpan* span_k;
+  const DocsSplit *split_q, *split_k;
+  DocsCaps q, k;
+  size_t bytes;
 };
-static inline DocsView docs_view(const dh_docs* docs) {
-  const int32_t* t = (const int32_t*)docs->table;
-  return {docs->T, t, t + DOCS_HEAD, t + DOCS_HEAD + (size_t)docs->T, t + DOCS_HEAD + 2 * (size_t)docs->T};
+static inline DocsView docs_view_at(const void* table, int T, int nq, int nkv) {
+  DocsView v;
+  v.T = T;
+  v.q = docs_caps(T, nq, 1, DOCS_TARGET_Q, DOCS_CHUNK_Q);
+  v.k = docs_caps(T, nkv, nq / nkv, DOCS_TARGET_K, DOCS_CHUNK_K);
+  const char* p = (const char*)table;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const char* r = p + at; at = dh_align_up(at + bytes, 16); return r; };
+  v.head = (const int32_t*)take(DOCS_HEAD * sizeof(int32_t));
+  v.lo = (const int32_t*)take((size_t)T * sizeof(int32_t));
+  v.hi = (const int32_t*)take((size_t)T * sizeof(int32_t));
+  v.pre = (const int32_t*)take((size_t)T * sizeof(int32_t));
+  v.units_q = (const DocsUnit*)take((size_t)v.q.units * sizeof(DocsUnit));
+  v.units_k = (const DocsUnit*)take((size_t)v.k.units * sizeof(DocsUnit));
+  v.span_k = (const DocsSpan*)take((size_t)v.k.units * sizeof(DocsSpan));
+  v.split_q = (const DocsSplit*)take((size_t)v.q.splits * sizeof(DocsSplit));
+  v.split_k = (const DocsSplit*)take((size_t)v.k.splits * sizeof(DocsSplit));
+  v.bytes = at;
+  return v;
 }
+static inline DocsView docs_view(const dh_docs* docs) { return docs_view_at(docs->table, docs->T, docs->nq, docs->nkv); }
+// Whether the table was made for these sizes: a kernel that finds others does nothing.
+__device__ __forceinline__ bool docs_fits(const DocsView& v, int nq, int nkv) { return v.head[DOCS_T] == v.T && v.head[DOCS_NQ] == nq && v.head[DOCS_NKV] == nkv; }
+
+struct DocsAttn {
+  DocsView v;
+  int nq, nkv, d;
+  float scale, cap;
+};
+int dh_launch_attn_docs_fwd_bf16(const DocsAttn& a, const bf16_t* qkv, bf16_t* o, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+size_t dh_attn_docs_fwd_bf16_ws_bytes(int T, int nq, int nkv, int d);
+int dh_launch_attn_docs_bwd_bf16(const DocsAttn& a, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, void* ws, size_t ws_bytes,
+                                 hipStream_t stream);
+size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d);
 
 // A scaled score under the cap, and the cap's slope there.
 __device__ __forceinline__ float docs_capped(float x, float cap, float& slope) {

@@ -18,15 +18,133 @@ __device__ __forceinline__ int starts_upto(const int32_t* start, int n, int r) {
   return lo + __popcll(__ballot(lo + lane < hi && start[min(lo + lane, n - 1)] <= r));
 }
 
-// A wave per 64 rows: the document of its first row, then, 64 starts at a time, how many more begin at or before each lane's row.
-__global__ __launch_bounds__(256) void docs_rows_kernel(int T, int n_docs, const int32_t* __restrict__ start, const int32_t* __restrict__ prefix, int32_t* __restrict__ head,
-                                                        int32_t* __restrict__ lo, int32_t* __restrict__ hi, int32_t* __restrict__ pre, int32_t* __restrict__ pos) {
-  const int lane = threadIdx.x & 63, r0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 64, r = r0 + lane;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    const int a = min(max(n_docs > 0 ? start[0] : 0, 0), T);
-    head[DOCS_LIVE0] = a;
-    head[DOCS_LIVE1] = min(max(n_docs > 0 ? start[n_docs] : 0, a), T);
+// The work lists, by one block: thread b looks at block b (b + 256 ...) of 128 rows.  keys: the list of key blocks.
+struct DocsPlanArgs {
+  int T, n_docs, nq, nkv;
+  const int32_t *start, *prefix;
+  int32_t *head, *lo, *hi, *pre, *pos;
+  DocsUnit *units_q, *units_k;
+  DocsSpan* span_k;
+  DocsSplit *split_q, *split_k;
+  DocsCaps q, k;
+};
+// The document of row r: its rows [s, e) and the end of its prefix; false: none.
+__device__ __forceinline__ bool docs_find(const DocsPlanArgs& a, int r, int& s, int& e, int& c) {
+  int lo = 0, hi = a.n_docs + 1;  // how many starts lie at or before r
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.start[mid] <= r) lo = mid + 1;
+    else hi = mid;
   }
+  if (lo < 1 || lo > a.n_docs) return false;
+  s = max(a.start[lo - 1], 0);
+  e = min(a.start[lo], a.T);
+  if (s > r || r >= e) return false;
+  c = a.prefix ? s + min(max(a.prefix[lo - 1], 0), e - s) : s;
+  return true;
+}
+// The tiles that block b meets: first and count (0: none of its rows is of a document).
+__device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, int live0, int live1, bool keys, int b, int& first) {
+  const int r0 = max(b * DOCS_BLOCK, live0), r1 = min(b * DOCS_BLOCK + DOCS_BLOCK, live1) - 1;
+  int s0, e0, c0, s1, e1, c1;
+  if (r0 > r1 || !docs_find(a, r0, s0, e0, c0) || !docs_find(a, r1, s1, e1, c1)) return 0;
+  const int from = keys ? (r0 < c0 ? s0 : r0) : s0, to = keys ? e1 : max(r1 + 1, c1);
+  first = from / DOCS_TILE;
+  return max(0, (to + DOCS_TILE - 1) / DOCS_TILE - first);
+}
+__device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, bool keys) {
+  __shared__ unsigned long long all;
+  __shared__ int longest, next_slot, next_split, hist[64], from[64];
+  const int tid = threadIdx.x, grp = keys ? a.nq / a.nkv : 1, heads = keys ? a.nkv : a.nq;
+  const DocsCaps cap = keys ? a.k : a.q;
+  DocsUnit* units = keys ? a.units_k : a.units_q;
+  DocsSplit* splits = keys ? a.split_k : a.split_q;
+  int live0 = 0, live1 = 0;
+  if (a.n_docs > 0) {
+    live0 = min(max(a.start[0], 0), a.T);
+    live1 = min(max(a.start[a.n_docs], live0), a.T);
+  }
+  if (tid == 0) { all = 0; longest = 1; next_slot = 0; next_split = 0; }
+  if (tid < 64) hist[tid] = 0;
+  __syncthreads();
+  unsigned long long mine = 0;
+  int top = 1, first0 = 0, tiles0 = 0, first;
+  for (int b = tid; b < cap.blocks; b += 256) {
+    const int t = docs_tiles(a, live0, live1, keys, b, first) * grp;
+    if (b == tid) { tiles0 = t; first0 = first; }
+    mine += t;
+    top = max(top, t);
+  }
+  atomicAdd(&all, mine);
+  atomicMax(&longest, top);
+  __syncthreads();
+  const int target = keys ? DOCS_TARGET_K : DOCS_TARGET_Q, least = keys ? DOCS_CHUNK_K : DOCS_CHUNK_Q;
+  const unsigned long long want = (all * heads + target - 1) / target;
+  const int ch = (int)min(max(want, (unsigned long long)least), (unsigned long long)longest), size = min(ch, longest);
+  // units longest first: counted by length in 64 steps, then placed
+  auto bucket = [&](int len) { return 63 - (int)((long long)len * 63 / size); };
+  for (int pass = 0; pass < 2; pass++) {
+    for (int b = tid; b < cap.blocks; b += 256) {
+      int t = tiles0;
+      first = first0;
+      if (b != tid) t = docs_tiles(a, live0, live1, keys, b, first) * grp;
+      if (t == 0) continue;
+      const int n = (t + ch - 1) / ch;
+      int slot = -1;
+      if (pass == 1 && n > 1) {
+        slot = atomicAdd(&next_slot, n);
+        const int k = atomicAdd(&next_split, 1);
+        if (k < cap.splits) splits[k] = {b, slot, n, 0};
+      }
+      for (int u = 0; u < n; u++) {
+        const int f0 = (int)((long long)t * u / n), f1 = (int)((long long)t * (u + 1) / n), k = bucket(f1 - f0);
+        if (pass == 0) atomicAdd(&hist[k], 1);
+        else {
+          const int at = atomicAdd(&from[k], 1);
+          if (at < cap.units) {
+            units[at] = {b * 2 + (u == 0 ? 1 : 0), keys ? f0 : first + f0, keys ? f1 : first + f1, slot < 0 ? -1 : slot + u};
+            if (keys) a.span_k[at] = {first, t / grp, 0, 0};
+          }
+        }
+      }
+    }
+    __syncthreads();
+    if (pass == 0) {
+      if (tid < 64) {
+        int upto = hist[tid];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const int o = __shfl_up(upto, d, 64);
+          if (tid >= d) upto += o;
+        }
+        from[tid] = upto - hist[tid];
+        if (tid == 63) a.head[keys ? DOCS_UNITS_K : DOCS_UNITS_Q] = min(upto, cap.units);
+      }
+      __syncthreads();
+    }
+  }
+  if (tid == 0) {
+    a.head[keys ? DOCS_SPLIT_K : DOCS_SPLIT_Q] = min(next_split, cap.splits);
+    if (!keys) {
+      a.head[DOCS_LIVE0] = live0;
+      a.head[DOCS_LIVE1] = live1;
+      a.head[DOCS_T] = a.T;
+      a.head[DOCS_NQ] = a.nq;
+      a.head[DOCS_NKV] = a.nkv;
+    }
+  }
+}
+
+// Blocks 0 and 1 make the two work lists; in the others a wave takes 64 rows: the document of its first row, then, 64 starts at a time, how many more begin at or
+// before each lane's row.
+__global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
+  if (blockIdx.x < 2) {
+    docs_lists(a, blockIdx.x == 1);
+    return;
+  }
+  const int T = a.T, n_docs = a.n_docs;
+  const int32_t* start = a.start;
+  const int lane = threadIdx.x & 63, r0 = ((blockIdx.x - 2) * 4 + (threadIdx.x >> 6)) * 64, r = r0 + lane;
   if (r0 >= T) return;
   int n = 0;  // starts at or before the lane's row
   if (n_docs > 0) {
@@ -41,25 +159,26 @@ __global__ __launch_bounds__(256) void docs_rows_kernel(int T, int n_docs, const
     }
   }
   if (r >= T) return;
-  int a = r, z = r, c = r;
+  int lo = r, hi = r, pre = r;
   if (n >= 1 && n <= n_docs) {
     const int s = max(start[n - 1], 0), e = min(start[n], T);
     if (s <= r && r < e) {
-      a = s;
-      z = e;
-      c = prefix ? s + min(max(prefix[n - 1], 0), e - s) : s;
+      lo = s;
+      hi = e;
+      pre = a.prefix ? s + min(max(a.prefix[n - 1], 0), e - s) : s;
     }
   }
-  lo[r] = a;
-  hi[r] = z;
-  pre[r] = c;
-  if (pos) pos[r] = r - a;
+  a.lo[r] = lo;
+  a.hi[r] = hi;
+  a.pre[r] = pre;
+  if (a.pos) a.pos[r] = r - lo;
 }
 
 static int check_docs(const char* who, const dh_docs* docs) {
   if (!docs) DH_FAIL(DH_ERR_INVALID_ARG, "%s: null pointer", who);
   if (docs->T < 0 || docs->n_docs < 0 || docs->nq <= 0 || docs->nkv <= 0 || docs->nq % docs->nkv)
     DH_FAIL(DH_ERR_SHAPE, "%s: T=%d n_docs=%d nq=%d nkv=%d", who, docs->T, docs->n_docs, docs->nq, docs->nkv);
+  if (docs->T > DOCS_MAX_T || docs->nq > DOCS_MAX_HEADS) DH_FAIL(DH_ERR_SHAPE, "%s: T=%d nq=%d (at most %d and %d)", who, docs->T, docs->nq, DOCS_MAX_T, DOCS_MAX_HEADS);
   if (docs->T > 0 && (!docs->table || (docs->n_docs > 0 && !docs->doc_start))) DH_FAIL(DH_ERR_INVALID_ARG, "%s: null pointer", who);
   if ((uintptr_t)docs->table & 15) DH_FAIL(DH_ERR_INVALID_ARG, "%s: table must be 16-byte aligned", who);
   return DH_OK;
@@ -67,25 +186,21 @@ static int check_docs(const char* who, const dh_docs* docs) {
 
 extern "C" size_t dh_docs_table_bytes(int T, int nq, int nkv) {
   if (T <= 0 || nq <= 0 || nkv <= 0) return 0;
-  return (DOCS_HEAD + 3 * (size_t)T) * sizeof(int32_t);
+  return docs_view_at(nullptr, T, nq, nkv).bytes;
 }
 
 extern "C" int dh_docs_plan(const dh_docs* docs, void* stream) {
   if (int rc = check_docs("docs_plan", docs)) return rc;
   if (docs->T == 0) return DH_OK;
   const DocsView v = docs_view(docs);
-  docs_rows_kernel<<<(unsigned)(((size_t)docs->T + 255) / 256), 256, 0, (hipStream_t)stream>>>(docs->T, docs->n_docs, docs->doc_start, docs->prefix, (int32_t*)v.head,
-                                                                                           (int32_t*)v.lo, (int32_t*)v.hi, (int32_t*)v.pre, docs->pos);
+  const DocsPlanArgs a = {docs->T, docs->n_docs, docs->nq, docs->nkv, docs->doc_start, docs->prefix, (int32_t*)v.head, (int32_t*)v.lo, (int32_t*)v.hi, (int32_t*)v.pre, docs->pos,
+                          (DocsUnit*)v.units_q, (DocsUnit*)v.units_k, (DocsSpan*)v.span_k, (DocsSplit*)v.split_q, (DocsSplit*)v.split_k, v.q, v.k};
+  docs_plan_kernel<<<2 + (unsigned)(((size_t)docs->T + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
 
 // ------------------------------------------------------------------------------------ attention, a wave a row
-struct DocsAttn {
-  DocsView v;
-  int nq, nkv, d;
-  float scale, cap;
-};
 // grid (rows / 4, nq)
 template <typename T>
 __global__ __launch_bounds__(256) void attn_docs_fwd_rows_kernel(const DocsAttn a, const T* __restrict__ qkv, T* __restrict__ o, float* __restrict__ lse) {
@@ -158,19 +273,24 @@ static int check_attn_docs(const char* who, int dtype, const dh_docs* docs, int 
 static bool unaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 static DocsAttn attn_of(const dh_docs* docs, int d, float cap) { return {docs_view(docs), docs->nq, docs->nkv, d, (float)(1.0 / sqrt((double)d)), cap}; }
 
-extern "C" size_t dh_attn_docs_fwd_workspace_bytes(int, int, int, int, int) { return 0; }
-extern "C" size_t dh_attn_docs_bwd_workspace_bytes(int, int, int, int, int) { return 0; }
+static bool sized(int dtype, int T, int nq, int nkv, int d) {
+  return dtype == DH_BF16 && T > 0 && T <= DOCS_MAX_T && nkv > 0 && nq > 0 && nq <= DOCS_MAX_HEADS && nq % nkv == 0 && (d == 64 || d == 128);
+}
+extern "C" size_t dh_attn_docs_fwd_workspace_bytes(int dtype, int T, int nq, int nkv, int d) { return sized(dtype, T, nq, nkv, d) ? dh_attn_docs_fwd_bf16_ws_bytes(T, nq, nkv, d) : 0; }
+extern "C" size_t dh_attn_docs_bwd_workspace_bytes(int dtype, int T, int nq, int nkv, int d) { return sized(dtype, T, nq, nkv, d) ? dh_attn_docs_bwd_bf16_ws_bytes(T, nq, nkv, d) : 0; }
 
 extern "C" int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
   if (int rc = check_attn_docs("attn_docs_fwd", dtype, docs, d, cap)) return rc;
   if (docs->T == 0 || docs->n_docs == 0) return DH_OK;
   if (!qkv || !o || !lse) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: null pointer");
   if (unaligned16(qkv) || unaligned16(o)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: qkv and o must be 16-byte aligned");
-  (void)ws; (void)ws_bytes;
+  const size_t need = dh_attn_docs_fwd_workspace_bytes(dtype, docs->T, docs->nq, docs->nkv, d);
+  if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_docs_fwd: workspace %zu < %zu bytes", ws_bytes, need);
+  if (unaligned16(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: ws must be 16-byte aligned");
   const DocsAttn a = attn_of(docs, d, cap);
+  if (dtype == DH_BF16) return dh_launch_attn_docs_fwd_bf16(a, (const bf16_t*)qkv, (bf16_t*)o, lse, ws, ws_bytes, (hipStream_t)stream);
   const dim3 grid((unsigned)((docs->T + 3LL) / 4), docs->nq);
-  if (dtype == DH_F32) attn_docs_fwd_rows_kernel<float><<<grid, 256, 0, (hipStream_t)stream>>>(a, (const float*)qkv, (float*)o, lse);
-  else attn_docs_fwd_rows_kernel<bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a, (const bf16_t*)qkv, (bf16_t*)o, lse);
+  attn_docs_fwd_rows_kernel<float><<<grid, 256, 0, (hipStream_t)stream>>>(a, (const float*)qkv, (float*)o, lse);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
@@ -191,8 +311,10 @@ extern "C" int dh_attn_docs_bwd(int dtype, const dh_docs* docs, int d, float cap
   if (docs->T == 0 || docs->n_docs == 0) return DH_OK;
   if (!qkv || !o || !dout || !lse || !dqkv || !delta) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: null pointer");
   if (unaligned16(qkv) || unaligned16(o) || unaligned16(dout) || unaligned16(dqkv)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: qkv, o, dout and dqkv must be 16-byte aligned");
-  (void)ws; (void)ws_bytes;
+  const size_t need = dh_attn_docs_bwd_workspace_bytes(dtype, docs->T, docs->nq, docs->nkv, d);
+  if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_docs_bwd: workspace %zu < %zu bytes", ws_bytes, need);
+  if (unaligned16(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: ws must be 16-byte aligned");
   const DocsAttn a = attn_of(docs, d, cap);
   if (dtype == DH_F32) return bwd_rows<float>(a, (const float*)qkv, (const float*)o, (const float*)dout, lse, (float*)dqkv, delta, (hipStream_t)stream);
-  return bwd_rows<bf16_t>(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)dout, lse, (bf16_t*)dqkv, delta, (hipStream_t)stream);
+  return dh_launch_attn_docs_bwd_bf16(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)dout, lse, (bf16_t*)dqkv, delta, ws, ws_bytes, (hipStream_t)stream);
 }
