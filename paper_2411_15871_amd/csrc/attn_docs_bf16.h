@@ -69,31 +69,16 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = p.a.nq, nkv = p.a.nkv, h = blockIdx.x % nq, id = blockIdx.x / nq, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
+  const DocsUnit u = v.units_q[id];  // fetched beside the head
   if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
-  const DocsUnit u = v.units_q[id];
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int iw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, iq = iw + l32, row = min(iq, T - 1);
-  const int lo = v.lo[row];
-  const bool live = iq < T && v.hi[row] > lo;
-  const int end = max(iq + 1, v.pre[row]);
-  bf16x8 qf[D / 16];
-  load_row_frags<D>(qf, qkv + (size_t)row * ld + (size_t)h * D, live, kg);
-  const DocsSeen see = docs_seen(live, lo, end);
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
   const char* kbase = reinterpret_cast<const char*>(kcol);
   const char* vbase = reinterpret_cast<const char*>(kcol + (size_t)nkv * D);
   const size_t tstride = (size_t)AB_KT * ld * sizeof(bf16_t);
-  f32x16 ot[D / 32];
-  float m = -3.0e38f, l = 0.f;  // finite: a tile that a row does not see leaves it alone
-  pin_frags(qf);
-  FragAddr<D> fa;
-  fa.init(lane);
   uint32_t voff[TL::IPW];
   tile_voff<D>(voff, ld, wave, lane, AB_KT);
-#pragma unroll
-  for (int dt = 0; dt < D / 32; dt++)
-#pragma unroll
-    for (int r = 0; r < 16; r++) ot[dt][r] = 0.f;
   const uint32_t ldsK = lds_address(smem), ldsV = ldsK + AF_RING * TL::BYTES;
   auto issue = [&](int t, int slot) {
     const int first = live0 - t * AB_KT, last = live1 - 1 - t * AB_KT;
@@ -107,7 +92,21 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
       tile_dma<D>(vbase + t * tstride, vc, ldsV + slot * TL::BYTES, wave);
     }
   };
-  issue(u.f0, 0);
+  issue(u.f0, 0);  // the first tile, the row's table entries and its fragments are on their way together
+  const int lo = v.lo[row], hi = v.hi[row], end = max(iq + 1, v.pre[row]);
+  bf16x8 qf[D / 16];
+  load_row_frags<D>(qf, qkv + (size_t)row * ld + (size_t)h * D, iq < T, kg);
+  FragAddr<D> fa;
+  fa.init(lane);
+  f32x16 ot[D / 32];
+  float m = -3.0e38f, l = 0.f;  // finite: a tile that a row does not see leaves it alone
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) ot[dt][r] = 0.f;
+  pin_frags(qf);
+  const bool live = iq < T && hi > lo;
+  const DocsSeen see = docs_seen(live, lo, end);
   int slot = 0;
   for (int t = u.f0; t < u.f1; t++, slot ^= 1) {
     dma_wait<0>();
@@ -237,7 +236,7 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
   for (int e = 0; e < CPT; e++) acc[e] = 0.f;
   for (int c = 0; c < s.n; c++) {
     const float lc = part_ml[(unit + c * step) * 2 + 1];
-    if (lc == 0.f) continue;  // this unit's tiles hold no key of the row
+    if (__builtin_bit_cast(uint32_t, lc) == 0) continue;  // this unit's tiles hold no key of the row (by its bits: this file is built without comparisons of NaNs)
     const float w = exp2f(part_ml[(unit + c * step) * 2] - M);
     L += w * lc;
     const float* po = part_o + (unit + c * step) * D + c0;
@@ -270,41 +269,14 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const 
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = p.a.nq, nkv = p.a.nkv, h = blockIdx.x % nq, id = blockIdx.x / nq, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
+  const DocsUnit u = v.units_q[id];  // fetched beside the head
   if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
-  const DocsUnit u = v.units_q[id];
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int iw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, iq = iw + l32, row = min(iq, T - 1);
-  const int lo = v.lo[row];
-  const bool live = iq < T && v.hi[row] > lo;
-  const int end = max(iq + 1, v.pre[row]);
-  bf16x8 qf[D / 16], dof[D / 16];
-  load_row_frags<D>(qf, qkv + (size_t)row * ld + (size_t)h * D, live, kg);
-  load_row_frags<D>(dof, dout + ((size_t)row * nq + h) * D, live, kg);
-  const float l2 = live ? lse[(size_t)h * T + row] * LOG2E : 0.f;
-  float dl = 0.f;
-  {
-    bf16x8 of[D / 16];
-    load_row_frags<D>(of, o + ((size_t)row * nq + h) * D, live, kg);
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ks++)
-#pragma unroll
-      for (int e = 0; e < 8; e++) dl = fmaf((float)dof[ks][e], (float)of[ks][e], dl);
-    dl += __shfl_xor(dl, 32, 64);
-    if ((u.block2 & 1) && kg == 0 && live) {
-      delta[(size_t)h * T + row] = dl;
-      lse2[(size_t)h * T + row] = l2;
-    }
-  }
-  const DocsSeen see = docs_seen(live, lo, end);
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
   const char* kbase = reinterpret_cast<const char*>(kcol);
   const char* vbase = reinterpret_cast<const char*>(kcol + (size_t)nkv * D);
   const size_t tstride = (size_t)AB_KT * ld * sizeof(bf16_t);
-  f32x16 dqt[D / 32];
-#pragma unroll
-  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(dqt[dt]);
-  FragAddr<D> fa;
-  fa.init(lane);
   uint32_t voff[TL::IPW];
   tile_voff<D>(voff, ld, wave, lane, AB_KT);
   const uint32_t ldsK = lds_address(smem), ldsV = ldsK + DOCS_DQ_RING * TL::BYTES;
@@ -320,11 +292,38 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const 
       tile_dma<D>(vbase + t * tstride, vc, ldsV + slot * TL::BYTES, wave);
     }
   };
+  issue(u.f0, 0);  // the first tile, the row's table entries and its fragments are on their way together
+  const int lo = v.lo[row], hi = v.hi[row], end = max(iq + 1, v.pre[row]);
+  bf16x8 qf[D / 16], dof[D / 16];
+  load_row_frags<D>(qf, qkv + (size_t)row * ld + (size_t)h * D, iq < T, kg);
+  load_row_frags<D>(dof, dout + ((size_t)row * nq + h) * D, iq < T, kg);
+  float l2 = lse[(size_t)h * T + row];
+  float dl = 0.f;
+  {
+    bf16x8 of[D / 16];
+    load_row_frags<D>(of, o + ((size_t)row * nq + h) * D, iq < T, kg);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) dl = fmaf((float)dof[ks][e], (float)of[ks][e], dl);
+    dl += __shfl_xor(dl, 32, 64);
+  }
+  const bool live = iq < T && hi > lo;
+  l2 *= LOG2E;
+  if ((u.block2 & 1) && kg == 0 && live) {
+    delta[(size_t)h * T + row] = dl;
+    lse2[(size_t)h * T + row] = l2;
+  }
+  const DocsSeen see = docs_seen(live, lo, end);
+  f32x16 dqt[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(dqt[dt]);
+  FragAddr<D> fa;
+  fa.init(lane);
   pin_frags(qf);
   pin_frags(dof);
   pin_scalar(l2);
   pin_scalar(dl);
-  issue(u.f0, 0);
   int slot = 0;
   for (int t = u.f0; t < u.f1; t++, slot ^= 1) {
     dma_wait<0>();
@@ -411,28 +410,16 @@ __global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const Do
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = p.a.nq, nkv = p.a.nkv, grp = nq / nkv, hk = blockIdx.x % nkv, id = blockIdx.x / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, T = v.T;
-  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_K]) return;
-  const DocsUnit u = v.units_k[id];
+  const DocsUnit u = v.units_k[id];  // fetched beside the head
   const DocsSpan span = v.span_k[id];
+  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_K]) return;
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int jw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, jk = jw + l32, row = min(jk, T - 1);
-  const int lo = v.lo[row], end = v.hi[row];
-  const bool live = jk < T && end > lo;
-  const int from = jk < v.pre[row] ? lo : jk;
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
-  bf16x8 kf[D / 16], vf[D / 16];
-  load_row_frags<D>(kf, kcol + (size_t)row * ld, live, kg);
-  load_row_frags<D>(vf, kcol + (size_t)row * ld + (size_t)nkv * D, live, kg);
-  const DocsSeen see = docs_seen(live, from, end);
   const char* qbase = reinterpret_cast<const char*>(qkv + (size_t)hq * D);
   const char* obase = reinterpret_cast<const char*>(dout + (size_t)hq * D);
   float* lse_s = reinterpret_cast<float*>(smem + 2 * AB_RING * TL::BYTES);
   float* del_s = lse_s + AB_RING * AB_KT;
-  f32x16 dkt[D / 32], dvt[D / 32];
-#pragma unroll
-  for (int dt = 0; dt < D / 32; dt++) { acc_zero<AGPR>(dkt[dt]); acc_zero<AGPR>(dvt[dt]); }
-  FragAddr<D> fa;
-  fa.init(lane);
   uint32_t vq[TL::IPW], vo[TL::IPW];
   tile_voff<D>(vq, ld, wave, lane, AB_KT);
   tile_voff<D>(vo, ldo, wave, lane, AB_KT);
@@ -443,8 +430,6 @@ __global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const Do
   int tc = ti;                                       // tile to work off next
   const uint32_t ldsS = ldsQ + 2 * AB_RING * TL::BYTES + (wave & 1) * AB_RING * AB_KT * sizeof(float);  // even waves transfer lse2, odd ones delta
   const float* srow = ((wave & 1) ? delta : lse2) + (size_t)hq * T;
-  pin_frags(kf);
-  pin_frags(vf);
   auto issue = [&](int slot) {
     const int first = max(0, live0 - ti * AB_KT), last = min(AB_KT - 1, live1 - 1 - ti * AB_KT);
     const char* qp = qbase + ti * qstride + gi * (D * sizeof(bf16_t));
@@ -462,7 +447,21 @@ __global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const Do
     dma4_base(srow + (size_t)gi * T + (size_t)ti * AB_KT, (uint32_t)(max(first, min(lane, last)) * sizeof(float)), ldsS + slot * AB_KT * sizeof(float));
     if (++ti == span.first + nt) { ti = span.first; gi++; }
   };
-  issue(0);
+  issue(0);  // the first tile, the key's table entries and its fragments are on their way together
+  const int lo = v.lo[row], end = v.hi[row], pre = v.pre[row];
+  bf16x8 kf[D / 16], vf[D / 16];
+  load_row_frags<D>(kf, kcol + (size_t)row * ld, jk < T, kg);
+  load_row_frags<D>(vf, kcol + (size_t)row * ld + (size_t)nkv * D, jk < T, kg);
+  f32x16 dkt[D / 32], dvt[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) { acc_zero<AGPR>(dkt[dt]); acc_zero<AGPR>(dvt[dt]); }
+  FragAddr<D> fa;
+  fa.init(lane);
+  pin_frags(kf);
+  pin_frags(vf);
+  const bool live = jk < T && end > lo;
+  const int from = jk < pre ? lo : jk;
+  const DocsSeen see = docs_seen(live, from, end);
   if (f0 + 1 < f1) issue(1);
   int slot = 0;
   for (int f = f0; f < f1; f++, slot = slot == AB_RING - 1 ? 0 : slot + 1) {

@@ -15,12 +15,12 @@ enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_UNITS_Q, DOCS_SPL
 #define DOCS_BLOCK 128
 #define DOCS_TILE 64
 // A chunk holds at least DOCS_CHUNK tiles, and so many that all heads' tiles together make DOCS_TARGET chunks.
-#define DOCS_CHUNK_Q 8
-#define DOCS_CHUNK_K 8
-#define DOCS_TARGET_Q 1024
-#define DOCS_TARGET_K 768
+#define DOCS_CHUNK_Q 4
+#define DOCS_CHUNK_K 6
+#define DOCS_TARGET_Q 512
+#define DOCS_TARGET_K 384
 struct DocsCaps { int blocks, units, slots, splits; };
-// With chunks of c >= tiles of all blocks / (target / heads): sum of ceil(t / c) <= blocks + target / heads; blocks that are cut have t > c, and their units are
+// With chunks of c > tiles of all blocks / (target / heads): sum of ceil(t / c) <= blocks + target / heads; blocks that are cut have t > c, and their units are
 // fewer than 2 t / c.  A block has at most tiles(T) + 1 tiles of each head of its group.
 static inline DocsCaps docs_caps(int T, int heads, int grp, int target, int chunk) {
   const long long blocks = ((long long)T + DOCS_BLOCK - 1) / DOCS_BLOCK, most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp, extra = target / heads + 1;

@@ -19,6 +19,7 @@ __device__ __forceinline__ int starts_upto(const int32_t* start, int n, int r) {
 }
 
 // The work lists, by one block: thread b looks at block b (b + 256 ...) of 128 rows.  keys: the list of key blocks.
+#define DOCS_STARTS 4096
 struct DocsPlanArgs {
   int T, n_docs, nq, nkv;
   const int32_t *start, *prefix;
@@ -28,31 +29,34 @@ struct DocsPlanArgs {
   DocsSplit *split_q, *split_k;
   DocsCaps q, k;
 };
-// The document of row r: its rows [s, e) and the end of its prefix; false: none.
-__device__ __forceinline__ bool docs_find(const DocsPlanArgs& a, int r, int& s, int& e, int& c) {
+// The document of row r: its rows [s, e) and the end of its prefix; false: none.  start: a.start, or its copy in LDS.
+template <class Start>
+__device__ __forceinline__ bool docs_find(const DocsPlanArgs& a, const Start* start, int r, int& s, int& e, int& c) {
   int lo = 0, hi = a.n_docs + 1;  // how many starts lie at or before r
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if (a.start[mid] <= r) lo = mid + 1;
+    if (start[mid] <= r) lo = mid + 1;
     else hi = mid;
   }
   if (lo < 1 || lo > a.n_docs) return false;
-  s = max(a.start[lo - 1], 0);
-  e = min(a.start[lo], a.T);
+  s = max(start[lo - 1], 0);
+  e = min(start[lo], a.T);
   if (s > r || r >= e) return false;
   c = a.prefix ? s + min(max(a.prefix[lo - 1], 0), e - s) : s;
   return true;
 }
 // The tiles that block b meets: first and count (0: none of its rows is of a document).
-__device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, int live0, int live1, bool keys, int b, int& first) {
+template <class Start>
+__device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* start, int live0, int live1, bool keys, int b, int& first) {
   const int r0 = max(b * DOCS_BLOCK, live0), r1 = min(b * DOCS_BLOCK + DOCS_BLOCK, live1) - 1;
   int s0, e0, c0, s1, e1, c1;
-  if (r0 > r1 || !docs_find(a, r0, s0, e0, c0) || !docs_find(a, r1, s1, e1, c1)) return 0;
+  if (r0 > r1 || !docs_find(a, start, r0, s0, e0, c0) || !docs_find(a, start, r1, s1, e1, c1)) return 0;
   const int from = keys ? (r0 < c0 ? s0 : r0) : s0, to = keys ? e1 : max(r1 + 1, c1);
   first = from / DOCS_TILE;
   return max(0, (to + DOCS_TILE - 1) / DOCS_TILE - first);
 }
-__device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, bool keys) {
+template <class Start>
+__device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* start, bool keys) {
   __shared__ unsigned long long all;
   __shared__ int longest, next_slot, next_split, hist[64], from[64];
   const int tid = threadIdx.x, grp = keys ? a.nq / a.nkv : 1, heads = keys ? a.nkv : a.nq;
@@ -61,8 +65,8 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, bool keys) {
   DocsSplit* splits = keys ? a.split_k : a.split_q;
   int live0 = 0, live1 = 0;
   if (a.n_docs > 0) {
-    live0 = min(max(a.start[0], 0), a.T);
-    live1 = min(max(a.start[a.n_docs], live0), a.T);
+    live0 = min(max(start[0], 0), a.T);
+    live1 = min(max(start[a.n_docs], live0), a.T);
   }
   if (tid == 0) { all = 0; longest = 1; next_slot = 0; next_split = 0; }
   if (tid < 64) hist[tid] = 0;
@@ -70,42 +74,49 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, bool keys) {
   unsigned long long mine = 0;
   int top = 1, first0 = 0, tiles0 = 0, first;
   for (int b = tid; b < cap.blocks; b += 256) {
-    const int t = docs_tiles(a, live0, live1, keys, b, first) * grp;
+    const int t = docs_tiles(a, start, live0, live1, keys, b, first) * grp;
     if (b == tid) { tiles0 = t; first0 = first; }
     mine += t;
     top = max(top, t);
   }
-  atomicAdd(&all, mine);
-  atomicMax(&longest, top);
+  if (mine > 0) {
+    atomicAdd(&all, mine);
+    atomicMax(&longest, top);
+  }
   __syncthreads();
+  // all heads' tiles over the target, rounded up (float64 holds them exactly; a quotient off by a rounding still leaves the bounds of docs_caps: the next whole number is taken)
   const int target = keys ? DOCS_TARGET_K : DOCS_TARGET_Q, least = keys ? DOCS_CHUNK_K : DOCS_CHUNK_Q;
-  const unsigned long long want = (all * heads + target - 1) / target;
-  const int ch = (int)min(max(want, (unsigned long long)least), (unsigned long long)longest), size = min(ch, longest);
-  // units longest first: counted by length in 64 steps, then placed
-  auto bucket = [&](int len) { return 63 - (int)((long long)len * 63 / size); };
+  const double want = floor((double)all * heads / target) + 1.0;
+  const int ch = (int)fmin(fmax(want, (double)least), (double)longest);
+  const float steps = 63.f / (float)ch;
+  // Units longest first, counted by length in 64 steps, then placed.  A block of t tiles makes n = ceil(t / ch) units, t % n of them a tile longer than the others.
+  auto bucket = [&](int len) { return min(max(63 - (int)((float)len * steps), 0), 63); };
   for (int pass = 0; pass < 2; pass++) {
     for (int b = tid; b < cap.blocks; b += 256) {
       int t = tiles0;
       first = first0;
-      if (b != tid) t = docs_tiles(a, live0, live1, keys, b, first) * grp;
+      if (b != tid) t = docs_tiles(a, start, live0, live1, keys, b, first) * grp;
       if (t == 0) continue;
-      const int n = (t + ch - 1) / ch;
+      const int n = (t + ch - 1) / ch, len = t / n, more = t - len * n, k0 = bucket(len + 1), k1 = bucket(len);
+      if (pass == 0) {
+        if (more > 0) atomicAdd(&hist[k0], more);
+        atomicAdd(&hist[k1], n - more);
+        continue;
+      }
       int slot = -1;
-      if (pass == 1 && n > 1) {
+      if (n > 1) {
         slot = atomicAdd(&next_slot, n);
         const int k = atomicAdd(&next_split, 1);
         if (k < cap.splits) splits[k] = {b, slot, n, 0};
       }
-      for (int u = 0; u < n; u++) {
-        const int f0 = (int)((long long)t * u / n), f1 = (int)((long long)t * (u + 1) / n), k = bucket(f1 - f0);
-        if (pass == 0) atomicAdd(&hist[k], 1);
-        else {
-          const int at = atomicAdd(&from[k], 1);
-          if (at < cap.units) {
-            units[at] = {b * 2 + (u == 0 ? 1 : 0), keys ? f0 : first + f0, keys ? f1 : first + f1, slot < 0 ? -1 : slot + u};
-            if (keys) a.span_k[at] = {first, t / grp, 0, 0};
-          }
+      const int at0 = more > 0 ? atomicAdd(&from[k0], more) : 0, at1 = atomicAdd(&from[k1], n - more) - more;
+      for (int u = 0, f = keys ? 0 : first; u < n; u++) {
+        const int at = (u < more ? at0 : at1) + u, end = f + len + (u < more ? 1 : 0);
+        if (at < cap.units) {
+          units[at] = {b * 2 + (u == 0 ? 1 : 0), f, end, slot < 0 ? -1 : slot + u};
+          if (keys) a.span_k[at] = {first, t / grp, 0, 0};
         }
+        f = end;
       }
     }
     __syncthreads();
@@ -138,8 +149,16 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, bool keys) {
 // Blocks 0 and 1 make the two work lists; in the others a wave takes 64 rows: the document of its first row, then, 64 starts at a time, how many more begin at or
 // before each lane's row.
 __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
-  if (blockIdx.x < 2) {
-    docs_lists(a, blockIdx.x == 1);
+  if (blockIdx.x < 2) {  // a chain of searches, in LDS where the starts fit (17 documents, 4096 rows: 13 us from memory)
+    __shared__ int copy[DOCS_STARTS];
+    const bool keys = blockIdx.x == 1;
+    if (a.n_docs >= DOCS_STARTS) {
+      docs_lists(a, a.start, keys);
+    } else {
+      for (int i = threadIdx.x; i < (a.n_docs > 0 ? a.n_docs + 1 : 0); i += 256) copy[i] = a.start[i];
+      __syncthreads();
+      docs_lists(a, (const __attribute__((address_space(3))) int*)copy, keys);
+    }
     return;
   }
   const int T = a.T, n_docs = a.n_docs;
