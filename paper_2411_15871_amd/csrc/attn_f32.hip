@@ -486,3 +486,5 @@ int dh_launch_attn_bwd_f32(int batch, int seq, int nq, int nkv, int d, const flo
   if (d <= 128) return bwd_f32<8>(batch, seq, nq, nkv, d, qkv, kv, ldkv, q_off, o, dout, lse, dqkv, dkv, lddkv, delta, stream);
   return bwd_f32<16>(batch, seq, nq, nkv, d, qkv, kv, ldkv, q_off, o, dout, lse, dqkv, dkv, lddkv, delta, stream);
 }
+
+#include "attn_docs_f32.h"

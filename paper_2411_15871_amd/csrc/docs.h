@@ -74,6 +74,8 @@ struct DocsAttn {
   int nq, nkv, d;
   float scale, cap;
 };
+int dh_launch_attn_docs_fwd_f32(const DocsAttn& a, const float* qkv, float* o, float* lse, hipStream_t stream);
+int dh_launch_attn_docs_bwd_f32(const DocsAttn& a, const float* qkv, const float* o, const float* dout, const float* lse, float* dqkv, float* delta, hipStream_t stream);
 int dh_launch_attn_docs_fwd_bf16(const DocsAttn& a, const bf16_t* qkv, bf16_t* o, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 size_t dh_attn_docs_fwd_bf16_ws_bytes(int T, int nq, int nkv, int d);
 int dh_launch_attn_docs_bwd_bf16(const DocsAttn& a, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, void* ws, size_t ws_bytes,

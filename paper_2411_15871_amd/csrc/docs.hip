@@ -219,67 +219,6 @@ extern "C" int dh_docs_plan(const dh_docs* docs, void* stream) {
   return DH_OK;
 }
 
-// ------------------------------------------------------------------------------------ attention, a wave a row
-// grid (rows / 4, nq)
-template <typename T>
-__global__ __launch_bounds__(256) void attn_docs_fwd_rows_kernel(const DocsAttn a, const T* __restrict__ qkv, T* __restrict__ o, float* __restrict__ lse) {
-  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, hk = h / (a.nq / a.nkv), d = a.d;
-  if (r >= a.v.T) return;
-  const int lo = a.v.lo[r], hi = max(r + 1, a.v.pre[r]);
-  if (a.v.hi[r] <= lo) return;
-  const size_t ld = (size_t)(a.nq + 2 * a.nkv) * d;
-  const T* k = qkv + (size_t)(a.nq + hk) * d;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  docs_row_fwd(qkv + (size_t)r * ld + (size_t)h * d, k, k + (size_t)a.nkv * d, ld, lo, hi, d, a.scale, a.cap, acc, m, l);
-  T* out = o + ((size_t)r * a.nq + h) * d;
-#pragma unroll
-  for (int c = 0; c < 4; c++)
-    if (lane + 64 * c < d) out[lane + 64 * c] = from_f32<T>(acc[c] / l);
-  if (lane == 0) lse[(size_t)h * a.v.T + r] = m + logf(l);
-}
-// dQ and delta; grid (rows / 4, nq)
-template <typename T>
-__global__ __launch_bounds__(256) void attn_docs_dq_rows_kernel(const DocsAttn a, const T* __restrict__ qkv, const T* __restrict__ o, const T* __restrict__ dout,
-                                                                const float* __restrict__ lse, T* __restrict__ dqkv, float* __restrict__ delta) {
-  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, hk = h / (a.nq / a.nkv), d = a.d;
-  if (r >= a.v.T) return;
-  const int lo = a.v.lo[r], hi = max(r + 1, a.v.pre[r]);
-  if (a.v.hi[r] <= lo) return;
-  const size_t ld = (size_t)(a.nq + 2 * a.nkv) * d, row = ((size_t)r * a.nq + h) * d, st = (size_t)h * a.v.T + r;
-  const T* k = qkv + (size_t)(a.nq + hk) * d;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f}, dl = 0.f;
-  for (int c = lane; c < d; c += 64) dl = fmaf(to_f32(dout[row + c]), to_f32(o[row + c]), dl);
-  dl = wave_sum(dl);
-  if (lane == 0) delta[st] = dl;
-  docs_row_dq(qkv + (size_t)r * ld + (size_t)h * d, dout + row, k, k + (size_t)a.nkv * d, ld, lo, hi, d, a.scale, a.cap, lse[st], dl, acc);
-  T* out = dqkv + (size_t)r * ld + (size_t)h * d;
-#pragma unroll
-  for (int c = 0; c < 4; c++)
-    if (lane + 64 * c < d) out[lane + 64 * c] = from_f32<T>(acc[c] * a.scale);
-}
-// dK, dV; grid (rows / 4, nkv)
-template <typename T>
-__global__ __launch_bounds__(256) void attn_docs_dkv_rows_kernel(const DocsAttn a, const T* __restrict__ qkv, const T* __restrict__ dout, const float* __restrict__ lse,
-                                                                 const float* __restrict__ delta, T* __restrict__ dqkv) {
-  const int lane = threadIdx.x & 63, j = blockIdx.x * 4 + (threadIdx.x >> 6), hk = blockIdx.y, grp = a.nq / a.nkv, d = a.d;
-  if (j >= a.v.T) return;
-  const int first = j < a.v.pre[j] ? a.v.lo[j] : j, end = a.v.hi[j];
-  if (end <= a.v.lo[j]) return;
-  const size_t ld = (size_t)(a.nq + 2 * a.nkv) * d;
-  const T* k = qkv + (size_t)j * ld + (size_t)(a.nq + hk) * d;
-  float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int h = hk * grp; h < (hk + 1) * grp; h++)
-    docs_row_dkv(k, k + (size_t)a.nkv * d, qkv + (size_t)h * d, ld, dout + (size_t)h * d, (size_t)a.nq * d, lse + (size_t)h * a.v.T, delta + (size_t)h * a.v.T, first, end, d, a.scale,
-                 a.cap, dk, dv);
-  T* out = dqkv + (size_t)j * ld + (size_t)(a.nq + hk) * d;
-#pragma unroll
-  for (int c = 0; c < 4; c++)
-    if (lane + 64 * c < d) {
-      out[lane + 64 * c] = from_f32<T>(dk[c] * a.scale);
-      out[(size_t)a.nkv * d + lane + 64 * c] = from_f32<T>(dv[c]);
-    }
-}
-
 // ------------------------------------------------------------------------------------ entry points
 static int check_attn_docs(const char* who, int dtype, const dh_docs* docs, int d, float cap) {
   if (int rc = check_docs(who, docs)) return rc;
@@ -308,20 +247,7 @@ extern "C" int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap
   if (unaligned16(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: ws must be 16-byte aligned");
   const DocsAttn a = attn_of(docs, d, cap);
   if (dtype == DH_BF16) return dh_launch_attn_docs_fwd_bf16(a, (const bf16_t*)qkv, (bf16_t*)o, lse, ws, ws_bytes, (hipStream_t)stream);
-  const dim3 grid((unsigned)((docs->T + 3LL) / 4), docs->nq);
-  attn_docs_fwd_rows_kernel<float><<<grid, 256, 0, (hipStream_t)stream>>>(a, (const float*)qkv, (float*)o, lse);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
-}
-
-template <typename T>
-static int bwd_rows(const DocsAttn& a, const T* qkv, const T* o, const T* dout, const float* lse, T* dqkv, float* delta, hipStream_t stream) {
-  const unsigned rows = (unsigned)((a.v.T + 3LL) / 4);
-  attn_docs_dq_rows_kernel<T><<<dim3(rows, a.nq), 256, 0, stream>>>(a, qkv, o, dout, lse, dqkv, delta);
-  DH_LAUNCH_CHECK();
-  attn_docs_dkv_rows_kernel<T><<<dim3(rows, a.nkv), 256, 0, stream>>>(a, qkv, dout, lse, delta, dqkv);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
+  return dh_launch_attn_docs_fwd_f32(a, (const float*)qkv, (float*)o, lse, (hipStream_t)stream);
 }
 
 extern "C" int dh_attn_docs_bwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, const void* o, const void* dout, const float* lse, void* dqkv, float* delta,
@@ -334,6 +260,6 @@ extern "C" int dh_attn_docs_bwd(int dtype, const dh_docs* docs, int d, float cap
   if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_docs_bwd: workspace %zu < %zu bytes", ws_bytes, need);
   if (unaligned16(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: ws must be 16-byte aligned");
   const DocsAttn a = attn_of(docs, d, cap);
-  if (dtype == DH_F32) return bwd_rows<float>(a, (const float*)qkv, (const float*)o, (const float*)dout, lse, (float*)dqkv, delta, (hipStream_t)stream);
+  if (dtype == DH_F32) return dh_launch_attn_docs_bwd_f32(a, (const float*)qkv, (const float*)o, (const float*)dout, lse, (float*)dqkv, delta, (hipStream_t)stream);
   return dh_launch_attn_docs_bwd_bf16(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)dout, lse, (bf16_t*)dqkv, delta, ws, ws_bytes, (hipStream_t)stream);
 }
