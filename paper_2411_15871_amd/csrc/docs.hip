@@ -57,8 +57,8 @@ __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* st
 }
 template <class Start>
 __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* start, bool keys) {
-  __shared__ unsigned long long all;
-  __shared__ int longest, next_slot, next_split, hist[64], from[64];
+  __shared__ unsigned long long wave_all[4], wave_cut[4];
+  __shared__ int wave_top[4], hist[64], from[64];
   const int tid = threadIdx.x, grp = keys ? a.nq / a.nkv : 1, heads = keys ? a.nkv : a.nq;
   const DocsCaps cap = keys ? a.k : a.q;
   DocsUnit* units = keys ? a.units_k : a.units_q;
@@ -68,9 +68,7 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
     live0 = min(max(start[0], 0), a.T);
     live1 = min(max(start[a.n_docs], live0), a.T);
   }
-  if (tid == 0) { all = 0; longest = 1; next_slot = 0; next_split = 0; }
   if (tid < 64) hist[tid] = 0;
-  __syncthreads();
   unsigned long long mine = 0;
   int top = 1, first0 = 0, tiles0 = 0, first;
   for (int b = tid; b < cap.blocks; b += 256) {
@@ -79,11 +77,15 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
     mine += t;
     top = max(top, t);
   }
-  if (mine > 0) {
-    atomicAdd(&all, mine);
-    atomicMax(&longest, top);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {  // (a lane's addition to one place of LDS after the other took 3 us)
+    mine += __shfl_xor(mine, d, 64);
+    top = max(top, __shfl_xor(top, d, 64));
   }
+  if ((tid & 63) == 0) { wave_all[tid >> 6] = mine; wave_top[tid >> 6] = top; }
   __syncthreads();
+  const unsigned long long all = wave_all[0] + wave_all[1] + wave_all[2] + wave_all[3];
+  const int longest = max(max(wave_top[0], wave_top[1]), max(wave_top[2], wave_top[3]));
   // all heads' tiles over the target, rounded up (float64 holds them exactly; a quotient off by a rounding still leaves the bounds of docs_caps: the next whole number is taken)
   const int target = keys ? DOCS_TARGET_K : DOCS_TARGET_Q, least = keys ? DOCS_CHUNK_K : DOCS_CHUNK_Q;
   const double want = floor((double)all * heads / target) + 1.0;
@@ -91,51 +93,60 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
   const float steps = 63.f / (float)ch;
   // Units longest first, counted by length in 64 steps, then placed.  A block of t tiles makes n = ceil(t / ch) units, t % n of them a tile longer than the others.
   auto bucket = [&](int len) { return min(max(63 - (int)((float)len * steps), 0), 63); };
-  for (int pass = 0; pass < 2; pass++) {
-    for (int b = tid; b < cap.blocks; b += 256) {
-      int t = tiles0;
-      first = first0;
-      if (b != tid) t = docs_tiles(a, start, live0, live1, keys, b, first) * grp;
-      if (t == 0) continue;
-      const int n = (t + ch - 1) / ch, len = t / n, more = t - len * n, k0 = bucket(len + 1), k1 = bucket(len);
-      if (pass == 0) {
-        if (more > 0) atomicAdd(&hist[k0], more);
-        atomicAdd(&hist[k1], n - more);
-        continue;
-      }
-      int slot = -1;
-      if (n > 1) {
-        slot = atomicAdd(&next_slot, n);
-        const int k = atomicAdd(&next_split, 1);
-        if (k < cap.splits) splits[k] = {b, slot, n, 0};
-      }
-      const int at0 = more > 0 ? atomicAdd(&from[k0], more) : 0, at1 = atomicAdd(&from[k1], n - more) - more;
-      for (int u = 0, f = keys ? 0 : first; u < n; u++) {
-        const int at = (u < more ? at0 : at1) + u, end = f + len + (u < more ? 1 : 0);
-        if (at < cap.units) {
-          units[at] = {b * 2 + (u == 0 ? 1 : 0), f, end, slot < 0 ? -1 : slot + u};
-          if (keys) a.span_k[at] = {first, t / grp, 0, 0};
-        }
-        f = end;
-      }
-    }
-    __syncthreads();
-    if (pass == 0) {
-      if (tid < 64) {
-        int upto = hist[tid];
+  for (int b = tid; b < cap.blocks; b += 256) {
+    const int t = b == tid ? tiles0 : docs_tiles(a, start, live0, live1, keys, b, first) * grp;
+    if (t == 0) continue;
+    const int n = (t + ch - 1) / ch, len = t / n, more = t - len * n;
+    if (more > 0) atomicAdd(&hist[bucket(len + 1)], more);
+    atomicAdd(&hist[bucket(len)], n - more);
+  }
+  __syncthreads();
+  if (tid < 64) {
+    int upto = hist[tid];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int o = __shfl_up(upto, d, 64);
-          if (tid >= d) upto += o;
-        }
-        from[tid] = upto - hist[tid];
-        if (tid == 63) a.head[keys ? DOCS_UNITS_K : DOCS_UNITS_Q] = min(upto, cap.units);
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d, 64);
+      if (tid >= d) upto += o;
+    }
+    from[tid] = upto - hist[tid];
+    if (tid == 63) a.head[keys ? DOCS_UNITS_K : DOCS_UNITS_Q] = min(upto, cap.units);
+  }
+  unsigned long long cut = 0;  // slots and, in the upper half, blocks that are cut, before this round's
+  for (int b0 = 0; b0 < cap.blocks; b0 += 256) {
+    const int b = b0 + tid;
+    first = first0;
+    const int t = b >= cap.blocks ? 0 : b0 == 0 ? tiles0 : docs_tiles(a, start, live0, live1, keys, b, first) * grp;
+    const int n = (t + ch - 1) / ch;
+    const unsigned long long own = n > 1 ? (1ull << 32) + n : 0;
+    unsigned long long upto = own;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned long long o = __shfl_up(upto, d, 64);
+      if ((tid & 63) >= d) upto += o;
+    }
+    __syncthreads();  // `from` is there; the round before is through with wave_cut
+    if ((tid & 63) == 63) wave_cut[tid >> 6] = upto;
+    __syncthreads();
+    for (int w = 0; w < (tid >> 6); w++) upto += wave_cut[w];
+    const unsigned long long before = cut + upto - own;
+    cut += wave_cut[0] + wave_cut[1] + wave_cut[2] + wave_cut[3];
+    if (t == 0) continue;
+    const int slot = n > 1 ? (int)(uint32_t)before : -1, k = (int)(before >> 32);
+    if (n > 1 && k < cap.splits) splits[k] = {b, slot, n, 0};
+    const int len = t / n, more = t - len * n;
+    const int at0 = more > 0 ? atomicAdd(&from[bucket(len + 1)], more) : 0, at1 = atomicAdd(&from[bucket(len)], n - more) - more;
+    const DocsSpan span = {first, t / grp, 0, 0};
+    for (int u = 0, f = keys ? 0 : first; u < n; u++) {
+      const int at = (u < more ? at0 : at1) + u, end = f + len + (u < more ? 1 : 0);
+      if (at < cap.units) {
+        units[at] = {b * 2 + (u == 0 ? 1 : 0), f, end, slot < 0 ? -1 : slot + u};
+        if (keys) a.span_k[at] = span;
       }
-      __syncthreads();
+      f = end;
     }
   }
   if (tid == 0) {
-    a.head[keys ? DOCS_SPLIT_K : DOCS_SPLIT_Q] = min(next_split, cap.splits);
+    a.head[keys ? DOCS_SPLIT_K : DOCS_SPLIT_Q] = min((int)(cut >> 32), cap.splits);
     if (!keys) {
       a.head[DOCS_LIVE0] = live0;
       a.head[DOCS_LIVE1] = live1;
@@ -171,7 +182,7 @@ __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
     n = base;
     for (bool more = true; more;) {
       const int s = base + lane <= n_docs ? start[base + lane] : INT32_MAX;
-#pragma unroll
+#pragma unroll 8
       for (int i = 0; i < 64; i++) n += __builtin_amdgcn_readlane(s, i) <= r ? 1 : 0;
       base += 64;
       more = base <= n_docs && __builtin_amdgcn_readlane(s, 63) < r0 + 64;
