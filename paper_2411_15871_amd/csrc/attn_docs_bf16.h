@@ -222,14 +222,15 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
                                                                 float* __restrict__ lse) {
   const DocsView& v = p.a.v;
   const int nq = p.a.nq, k = blockIdx.x >> 3, h = blockIdx.y;
-  if (!docs_fits(v, nq, p.a.nkv) || k >= v.head[DOCS_SPLIT_Q]) return;
   const DocsSplit s = v.split_q[k];
+  if (!docs_fits(v, nq, p.a.nkv) || k >= v.head[DOCS_SPLIT_Q]) return;
   const int r = (blockIdx.x & 7) * 16 + (threadIdx.x >> 4), i = s.block * DOCS_BLOCK + r;
   if (i >= v.T || v.hi[i] <= v.lo[i]) return;
   constexpr int CPT = D / 16;
   const int c0 = (threadIdx.x & 15) * CPT;
   const size_t unit = ((size_t)s.slot * nq + h) * DOCS_BLOCK + r, step = (size_t)nq * DOCS_BLOCK;  // rows of the first unit's partial result, and to the next unit's
   float M = -3.0e38f;
+#pragma unroll 8
   for (int c = 0; c < s.n; c++) M = fmaxf(M, part_ml[(unit + c * step) * 2]);
   float L = 0.f, acc[CPT];
 #pragma unroll
@@ -257,18 +258,18 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
 }
 
 // ================================================================================ backward: dQ
-// As attn_bwd_dq_block; the first unit of a block also stores its rows' delta and lse2 for the dK/dV launch behind it.  grid (units * nq)
+// As attn_bwd_dq_block, unit id of head h.  STORE: the first unit of a block also stores its rows' delta and lse2 for the dK/dV launch behind it; otherwise
+// attn_bwd_prep_kernel has.
 #define DOCS_DQ_RING 2
-template <int D, bool CAP>
-__global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
-                                                                      const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
-                                                                      float* __restrict__ part) {
+template <int D, bool CAP, bool STORE>
+__device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                              const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   using TL = ATile<D>;
   extern __shared__ __attribute__((aligned(1024))) char smem[];  // K ring, then V ring
   const lds_char* sm = (const lds_char*)smem;
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
-  const int nq = p.a.nq, nkv = p.a.nkv, h = blockIdx.x % nq, id = blockIdx.x / nq, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
+  const int nq = p.a.nq, nkv = p.a.nkv, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
   const DocsUnit u = v.units_q[id];  // fetched beside the head
   if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const 
   }
   const bool live = iq < T && hi > lo;
   l2 *= LOG2E;
-  if ((u.block2 & 1) && kg == 0 && live) {
+  if (STORE && (u.block2 & 1) && kg == 0 && live) {
     delta[(size_t)h * T + row] = dl;
     lse2[(size_t)h * T + row] = l2;
   }
@@ -398,18 +399,17 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const 
 }
 
 // ================================================================================ backward: dK, dV
-// As attn_bwd_dkv_block in phases: a block owns 128 keys of a key/value head and walks the query tiles of the group's heads, one head after the other.  grid (units * nkv)
+// As attn_bwd_dkv_block in phases: a block owns 128 keys of a key/value head and walks the query tiles of the group's heads, one head after the other.  Unit id of key/value head hk.
 template <int D, bool CAP>
-__global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
-                                                                        const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv,
-                                                                        float* __restrict__ part) {
+__device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int hk, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+                                               const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   using TL = ATile<D>;
   constexpr bool AGPR = D == 128;
   extern __shared__ __attribute__((aligned(1024))) char smem[];  // Q ring, dO ring, lse2 ring, delta ring
   const lds_char* sm = (const lds_char*)smem;
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
-  const int nq = p.a.nq, nkv = p.a.nkv, grp = nq / nkv, hk = blockIdx.x % nkv, id = blockIdx.x / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, T = v.T;
+  const int nq = p.a.nq, nkv = p.a.nkv, grp = nq / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, T = v.T;
   const DocsUnit u = v.units_k[id];  // fetched beside the head
   const DocsSpan span = v.span_k[id];
   if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_K]) return;
@@ -568,6 +568,29 @@ __global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const Do
   }
 }
 
+// The two as launches of their own (dQ first: it stores the rows' statistics that the dK/dV blocks read), grids (units * nq) and (units * nkv) ...
+template <int D, bool CAP>
+__global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                                                      const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
+                                                                      float* __restrict__ part) {
+  docs_dq_block<D, CAP, true>(p, blockIdx.x / p.a.nq, blockIdx.x % p.a.nq, qkv, o, dout, lse, lse2, delta, dqkv, part);
+}
+template <int D, bool CAP>
+__global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+                                                                        const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv,
+                                                                        float* __restrict__ part) {
+  docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse, lse2, delta, dqkv, part);
+}
+// ... and as one, behind attn_bwd_prep_kernel, for grids that leave units of the chip idle: dK/dV units (the longer ones) first.  grid (units_k * nkv + units_q * nq)
+template <int D, bool CAP>
+__global__ __launch_bounds__(AB_THREADS) void attn_docs_bwd_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                                                        const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
+                                                                        float* __restrict__ part_q, float* __restrict__ part_kv) {
+  const unsigned n_k = (unsigned)p.a.v.k.units * p.a.nkv;
+  if (blockIdx.x < n_k) docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse, lse2, delta, dqkv, part_kv);
+  else docs_dq_block<D, CAP, false>(p, (blockIdx.x - n_k) / p.a.nq, (blockIdx.x - n_k) % p.a.nq, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
+}
+
 // Adds the units of the blocks that were cut, in order: rows of dQ (scaled here) and of [dK | dV].  The first nb_q blocks are (16 * blocks that may be cut, nq) of dQ, 8 rows
 // each; the rest (32 * blocks, nkv) of dK/dV, 4 rows each.
 template <int D>
@@ -575,20 +598,20 @@ __global__ __launch_bounds__(256) void attn_docs_reduce_kernel(const DocsTiled p
                                                                unsigned gqx, unsigned gkx) {
   const DocsView& v = p.a.v;
   const int nq = p.a.nq, nkv = p.a.nkv, ld = (nq + 2 * nkv) * D;
-  if (!docs_fits(v, nq, nkv)) return;
   unsigned id = blockIdx.x;
   const bool q = id < nb_q;
   if (!q) id -= nb_q;
   const unsigned gx = q ? gqx : gkx, x = id % gx;
   const int h = id / gx, k = q ? x >> 4 : x >> 5, r0 = q ? (x & 15) * 8 : (x & 31) * 4, width = q ? D : 2 * D, heads = q ? nq : nkv;
-  if (k >= v.head[q ? DOCS_SPLIT_Q : DOCS_SPLIT_K]) return;
   const DocsSplit s = q ? v.split_q[k] : v.split_k[k];
+  if (!docs_fits(v, nq, nkv) || k >= v.head[q ? DOCS_SPLIT_Q : DOCS_SPLIT_K]) return;
   const float* part = q ? part_q : part_kv;
   const size_t unit = ((size_t)s.slot * heads + h) * DOCS_BLOCK, step = (size_t)heads * DOCS_BLOCK * width;
   const int e = threadIdx.x, row = r0 + e / (width / 4), c4 = (e % (width / 4)) * 4, i = s.block * DOCS_BLOCK + row;
   if (row >= r0 + (q ? 8 : 4) || i >= v.T || v.hi[i] <= v.lo[i]) return;
   f32x4 t = {0.f, 0.f, 0.f, 0.f};
   const float* from = part + (unit + row) * width + c4;
+#pragma unroll 8
   for (int c = 0; c < s.n; c++) t += __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + c * step));
   const float f = q ? p.a.scale : 1.f;
   bf16x4 out = {(bf16_t)(t[0] * f), (bf16_t)(t[1] * f), (bf16_t)(t[2] * f), (bf16_t)(t[3] * f)};
@@ -643,6 +666,10 @@ static DocsBwdLayout docs_bwd_layout(const DocsView& v, int nq, int nkv, int d) 
 }
 size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view_at(nullptr, T, nq, nkv), nq, nkv, d).total; }
 
+// Whether both halves of the backward pass go out as one launch.
+#define DOCS_ONE_LAUNCH 512  // 128-row blocks of all heads
+static bool docs_one_launch(int T, int nq, int nkv) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= DOCS_ONE_LAUNCH; }
+
 template <int D, bool CAP>
 static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, char* ws, hipStream_t stream) {
   static bool ready[DH_MAX_DEVICES] = {};
@@ -651,16 +678,24 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   if (!set) {
     if (int rc = set_lds(attn_docs_dq_bf16_kernel<D, CAP>, lds_dq)) return rc;
     if (int rc = set_lds(attn_docs_dkv_bf16_kernel<D, CAP>, lds_dkv)) return rc;
+    if (int rc = set_lds(attn_docs_bwd_bf16_kernel<D, CAP>, lds_dkv)) return rc;
     set = true;
   }
   const int nq = p.a.nq, nkv = p.a.nkv;
   const DocsCaps &q = p.a.v.q, &k = p.a.v.k;
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
-  attn_docs_dq_bf16_kernel<D, CAP><<<(unsigned)q.units * nq, AB_THREADS, lds_dq, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
-  DH_LAUNCH_CHECK();
-  attn_docs_dkv_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv, AB_THREADS, lds_dkv, stream>>>(p, qkv, dout, lse, lse2, delta, dqkv, part_kv);
-  DH_LAUNCH_CHECK();
+  if (docs_one_launch(p.a.v.T, nq, nkv)) {
+    attn_bwd_prep_kernel<D><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq);
+    DH_LAUNCH_CHECK();
+    attn_docs_bwd_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv + (unsigned)q.units * nq, AB_THREADS, lds_dkv, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q, part_kv);
+    DH_LAUNCH_CHECK();
+  } else {
+    attn_docs_dq_bf16_kernel<D, CAP><<<(unsigned)q.units * nq, AB_THREADS, lds_dq, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
+    DH_LAUNCH_CHECK();
+    attn_docs_dkv_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv, AB_THREADS, lds_dkv, stream>>>(p, qkv, dout, lse, lse2, delta, dqkv, part_kv);
+    DH_LAUNCH_CHECK();
+  }
   const unsigned gqx = 16 * q.splits, gkx = 32 * k.splits, nb_q = gqx * nq, nb_k = gkx * nkv;
   if (nb_q + nb_k > 0) {
     attn_docs_reduce_kernel<D><<<nb_q + nb_k, 256, 0, stream>>>(p, part_q, part_kv, dqkv, nb_q, gqx, gkx);
