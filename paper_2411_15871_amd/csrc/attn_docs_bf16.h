@@ -666,10 +666,6 @@ static DocsBwdLayout docs_bwd_layout(const DocsView& v, int nq, int nkv, int d) 
 }
 size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view_at(nullptr, T, nq, nkv), nq, nkv, d).total; }
 
-// Whether both halves of the backward pass go out as one launch.
-#define DOCS_ONE_LAUNCH 512  // 128-row blocks of all heads
-static bool docs_one_launch(int T, int nq, int nkv) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= DOCS_ONE_LAUNCH; }
-
 template <int D, bool CAP>
 static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, char* ws, hipStream_t stream) {
   static bool ready[DH_MAX_DEVICES] = {};

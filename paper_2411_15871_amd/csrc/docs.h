@@ -14,14 +14,24 @@
 enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_UNITS_Q, DOCS_SPLIT_Q, DOCS_UNITS_K, DOCS_SPLIT_K };  // head: the rows of documents are [live0, live1)
 #define DOCS_BLOCK 128
 #define DOCS_TILE 64
-// A chunk holds at least DOCS_CHUNK tiles, and so many that all heads' tiles together make DOCS_TARGET chunks.
+// A chunk holds so many tiles that all heads' tiles together make at most DOCS_TARGET chunks (room for partial results follows from that), and DOCS_CHUNK at least.
 #define DOCS_CHUNK_Q 4
-#define DOCS_CHUNK_K 6
-#define DOCS_TARGET_Q 512
-#define DOCS_TARGET_K 384
+#define DOCS_CHUNK_K 3
+#define DOCS_WHOLE_Q 10
+#define DOCS_WHOLE_K 4
+#define DOCS_TARGET_Q 1024
+#define DOCS_TARGET_K 512
+// 128-row blocks of all heads up to which both halves of the backward pass go out as one launch.
+#define DOCS_ONE_LAUNCH 1024
+__host__ __device__ static inline bool docs_one_launch(int T, int nq, int nkv) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= DOCS_ONE_LAUNCH; }
 struct DocsCaps { int blocks, units, slots, splits; };
 // With chunks of c > tiles of all blocks / (target / heads): sum of ceil(t / c) <= blocks + target / heads; blocks that are cut have t > c, and their units are
 // fewer than 2 t / c.  A block has at most tiles(T) + 1 tiles of each head of its group.
+// Tiles that a chunk holds at least: where a block cannot have more than `whole` tiles none is cut, and no launch is needed to merge.
+__host__ __device__ static inline int docs_least(int T, int grp, int chunk, int whole) {
+  const long long most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp;
+  return most <= whole ? whole : chunk;
+}
 static inline DocsCaps docs_caps(int T, int heads, int grp, int target, int chunk) {
   const long long blocks = ((long long)T + DOCS_BLOCK - 1) / DOCS_BLOCK, most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp, extra = target / heads + 1;
   const long long slots = most <= chunk ? 0 : blocks * ((most + chunk - 1) / chunk);
@@ -48,8 +58,8 @@ struct DocsView {
 static inline DocsView docs_view_at(const void* table, int T, int nq, int nkv) {
   DocsView v;
   v.T = T;
-  v.q = docs_caps(T, nq, 1, DOCS_TARGET_Q, DOCS_CHUNK_Q);
-  v.k = docs_caps(T, nkv, nq / nkv, DOCS_TARGET_K, DOCS_CHUNK_K);
+  v.q = docs_caps(T, nq, 1, DOCS_TARGET_Q, docs_least(T, 1, DOCS_CHUNK_Q, DOCS_WHOLE_Q));
+  v.k = docs_caps(T, nkv, nq / nkv, DOCS_TARGET_K, docs_least(T, nq / nkv, DOCS_CHUNK_K, DOCS_WHOLE_K));
   const char* p = (const char*)table;
   size_t at = 0;
   auto take = [&](size_t bytes) { const char* r = p + at; at = dh_align_up(at + bytes, 16); return r; };

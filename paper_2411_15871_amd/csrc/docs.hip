@@ -55,10 +55,45 @@ __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* st
   first = from / DOCS_TILE;
   return max(0, (to + DOCS_TILE - 1) / DOCS_TILE - first);
 }
+// The chunk length, between `shortest` and `longest`, whose launch is expected to be through first: 64 lengths in even ratios, a lane each.  In tiles of a block that shares its
+// unit of the chip with another (queries; 2.1 us at D = 128) or has it to itself (keys; 2.3 us): up to one round of resident blocks the longest unit counts, a fifth faster
+// alone; beyond, everything over all units (a unit's beginning and end count 1.5 tiles beside another's work) and a quarter of the longest one for the end.  A partial
+// result is written and read back (beyond 512 of them from memory), and the merge takes a while longer if there is any.  tiles[b]: of the first DOCS_BLOCKS blocks; longer
+// rows are cut at `shortest`.
+#define DOCS_BLOCKS 1024
+__device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, bool keys, int blocks, int shortest, int longest, float all, const int* tiles) {
+  __shared__ int units[4][64], cuts[4][64], tops[4][64];
+  if (blocks > DOCS_BLOCKS || shortest >= longest) return shortest;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = keys ? a.nkv : a.nq;
+  const int ch = max(shortest, (int)ceilf((float)longest * exp2f(-(float)lane / 63.f * log2f((float)longest / (float)shortest)) - 1e-3f));
+  const float inv = 1.f / (float)ch;
+  int n = 0, cut = 0, top = 0;
+  for (int b = wave; b < blocks; b += 4) {
+    const int t = tiles[b], k = (int)ceilf((float)t * inv - 1e-4f);
+    n += k;
+    cut += k > 1 ? k : 0;
+    top = max(top, min(t, ch));
+  }
+  units[wave][lane] = n;
+  cuts[wave][lane] = cut;
+  tops[wave][lane] = top;
+  __syncthreads();
+  const float N = (float)(units[0][lane] + units[1][lane] + units[2][lane] + units[3][lane]) * heads, C = (float)(cuts[0][lane] + cuts[1][lane] + cuts[2][lane] + cuts[3][lane]) * heads;
+  const float L = (float)max(max(tops[0][lane], tops[1][lane]), max(tops[2][lane], tops[3][lane]));
+  const float slots = !keys ? 512.f : docs_one_launch(a.T, a.nq, a.nkv) ? 144.f : 256.f;  // (in one launch the rest of the units has queries)
+  const float together = fmaxf(L, (all + 1.5f * N) / slots + 0.25f * L);
+  const float time = (N > slots ? together : keys ? L : L * (0.8f + 0.2f / 256.f * fmaxf(N - 256.f, 0.f))) + (C > 0.f ? 1.5f + 0.004f * C + 0.008f * fmaxf(C - 512.f, 0.f) : 0.f);
+  float best = time;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) best = fminf(best, __shfl_xor(best, d, 64));
+  const unsigned long long who = __ballot(time == best);
+  return __builtin_amdgcn_readlane(ch, who ? __builtin_ctzll(who) : 63);
+}
+
 template <class Start>
 __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* start, bool keys) {
   __shared__ unsigned long long wave_all[4], wave_cut[4];
-  __shared__ int wave_top[4], hist[64], from[64];
+  __shared__ int wave_top[4], hist[64], from[64], tiles[DOCS_BLOCKS];
   const int tid = threadIdx.x, grp = keys ? a.nq / a.nkv : 1, heads = keys ? a.nkv : a.nq;
   const DocsCaps cap = keys ? a.k : a.q;
   DocsUnit* units = keys ? a.units_k : a.units_q;
@@ -74,6 +109,7 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
   for (int b = tid; b < cap.blocks; b += 256) {
     const int t = docs_tiles(a, start, live0, live1, keys, b, first) * grp;
     if (b == tid) { tiles0 = t; first0 = first; }
+    if (b < DOCS_BLOCKS) tiles[b] = t;
     mine += t;
     top = max(top, t);
   }
@@ -87,9 +123,10 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
   const unsigned long long all = wave_all[0] + wave_all[1] + wave_all[2] + wave_all[3];
   const int longest = max(max(wave_top[0], wave_top[1]), max(wave_top[2], wave_top[3]));
   // all heads' tiles over the target, rounded up (float64 holds them exactly; a quotient off by a rounding still leaves the bounds of docs_caps: the next whole number is taken)
-  const int target = keys ? DOCS_TARGET_K : DOCS_TARGET_Q, least = keys ? DOCS_CHUNK_K : DOCS_CHUNK_Q;
+  const int target = keys ? DOCS_TARGET_K : DOCS_TARGET_Q, least = keys ? docs_least(a.T, grp, DOCS_CHUNK_K, DOCS_WHOLE_K) : docs_least(a.T, 1, DOCS_CHUNK_Q, DOCS_WHOLE_Q);
   const double want = floor((double)all * heads / target) + 1.0;
-  const int ch = (int)fmin(fmax(want, (double)least), (double)longest);
+  const int shortest = (int)fmin(fmax(want, (double)least), (double)longest);
+  const int ch = docs_chunk(a, keys, cap.blocks, shortest, longest, (float)all * heads, tiles);
   const float steps = 63.f / (float)ch;
   // Units longest first, counted by length in 64 steps, then placed.  A block of t tiles makes n = ceil(t / ch) units, t % n of them a tile longer than the others.
   auto bucket = [&](int len) { return min(max(63 - (int)((float)len * steps), 0), 63); };
