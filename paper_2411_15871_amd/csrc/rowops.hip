@@ -626,14 +626,17 @@ extern "C" int dh_rope_axes(int dtype, int pairing, int form, int T, int n_axes,
   if (((uintptr_t)t | (uintptr_t)out) & 15) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: t and out must be 16-byte aligned");
   if (t == out && t_stride != out_stride) DH_FAIL(DH_ERR_INVALID_ARG, "rope_axes: in place both strides are the same");
   const double l2b = log2((double)base);
-  const size_t per_row = (size_t)n_heads * (head_dim / 16), most = std::max<size_t>(1, ((size_t)1 << 31) / per_row);
+  const bool four = (size_t)T * n_heads * (head_dim / 16) >= (size_t)1 << 17 && !(dtype == DH_F32 && pairing == DH_ROPE_ADJACENT);  // as dh_rope_pairs
+  const size_t per_row = (size_t)(four ? (n_heads + 3) / 4 : n_heads) * (head_dim / 16), most = std::max<size_t>(1, ((size_t)1 << 31) / per_row);
   for (size_t row0 = 0; row0 < (size_t)T; row0 += most) {  // (a launch's threads are counted in 32 bits)
     const unsigned threads = (unsigned)(std::min(most, (size_t)T - row0) * per_row);
-#define GO(TT, ADJ)                                                                                                                                  \
-  rope_axes_kernel<TT, ADJ, 1><<<(threads + 255) / 256, 256, 0, (hipStream_t)stream>>>((const TT*)t, t_stride, (TT*)out, out_stride, row0, threads, n_heads, \
+#define GO(TT, ADJ, N)                                                                                                                                  \
+  rope_axes_kernel<TT, ADJ, N><<<(threads + 255) / 256, 256, 0, (hipStream_t)stream>>>((const TT*)t, t_stride, (TT*)out, out_stride, row0, threads, n_heads, \
                                                                                        head_dim, ax, form == DH_ROPE_AXES_OWN, l2b, pos, inverse)
-    if (dtype == DH_BF16) { if (pairing == DH_ROPE_ADJACENT) GO(bf16_t, true); else GO(bf16_t, false); }
-    else { if (pairing == DH_ROPE_ADJACENT) GO(float, true); else GO(float, false); }
+#define GO2(TT, ADJ) do { if (four) GO(TT, ADJ, 4); else GO(TT, ADJ, 1); } while (0)
+    if (dtype == DH_BF16) { if (pairing == DH_ROPE_ADJACENT) GO2(bf16_t, true); else GO2(bf16_t, false); }
+    else { if (pairing == DH_ROPE_ADJACENT) GO(float, true, 1); else GO2(float, false); }
+#undef GO2
 #undef GO
     DH_LAUNCH_CHECK();
   }
