@@ -63,7 +63,7 @@ __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* st
 #define DOCS_BLOCKS 1024
 __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, bool keys, int blocks, int shortest, int longest, float all, const int* tiles) {
   __shared__ int units[4][64], cuts[4][64], tops[4][64];
-  if (blocks > DOCS_BLOCKS || shortest >= longest) return shortest;
+  if (blocks > DOCS_BLOCKS || shortest >= longest || all <= 144.f) return shortest;  // (so few tiles: any cut fits)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = keys ? a.nkv : a.nq;
   const int ch = max(shortest, (int)ceilf((float)longest * exp2f(-(float)lane / 63.f * log2f((float)longest / (float)shortest)) - 1e-3f));
   const float inv = 1.f / (float)ch;
@@ -90,10 +90,20 @@ __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, bool keys, int 
   return __builtin_amdgcn_readlane(ch, who ? __builtin_ctzll(who) : 63);
 }
 
+__device__ __forceinline__ void docs_head(const DocsPlanArgs& a, bool keys, int live0, int live1, int units, int splits) {
+  a.head[keys ? DOCS_UNITS_K : DOCS_UNITS_Q] = units;
+  a.head[keys ? DOCS_SPLIT_K : DOCS_SPLIT_Q] = splits;
+  if (keys) return;
+  a.head[DOCS_LIVE0] = live0;
+  a.head[DOCS_LIVE1] = live1;
+  a.head[DOCS_T] = a.T;
+  a.head[DOCS_NQ] = a.nq;
+  a.head[DOCS_NKV] = a.nkv;
+}
 template <class Start>
 __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* start, bool keys) {
   __shared__ unsigned long long wave_all[4], wave_cut[4];
-  __shared__ int wave_top[4], hist[64], from[64], tiles[DOCS_BLOCKS];
+  __shared__ int wave_top[4], hist[64], from[64], tiles[DOCS_BLOCKS], all_units;
   const int tid = threadIdx.x, grp = keys ? a.nq / a.nkv : 1, heads = keys ? a.nkv : a.nq;
   const DocsCaps cap = keys ? a.k : a.q;
   DocsUnit* units = keys ? a.units_k : a.units_q;
@@ -112,6 +122,18 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
     if (b < DOCS_BLOCKS) tiles[b] = t;
     mine += t;
     top = max(top, t);
+  }
+  if (cap.slots == 0 && cap.blocks <= 64) {  // nothing is cut and everything is resident at once: one unit a block, in their order
+    const uint64_t have = __ballot(tiles0 > 0);
+    if (tid < 64) {
+      const int at = __popcll(have & ((1ull << tid) - 1));
+      if (tiles0 > 0) {
+        units[at] = {tid * 2 + 1, keys ? 0 : first0, (keys ? 0 : first0) + tiles0, -1};
+        if (keys) a.span_k[at] = {first0, tiles0 / grp, 0, 0};
+      }
+      if (tid == 0) docs_head(a, keys, live0, live1, __popcll(have), 0);
+    }
+    return;
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {  // (a lane's addition to one place of LDS after the other took 3 us)
@@ -146,7 +168,7 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
       if (tid >= d) upto += o;
     }
     from[tid] = upto - hist[tid];
-    if (tid == 63) a.head[keys ? DOCS_UNITS_K : DOCS_UNITS_Q] = min(upto, cap.units);
+    if (tid == 63) all_units = min(upto, cap.units);
   }
   unsigned long long cut = 0;  // slots and, in the upper half, blocks that are cut, before this round's
   for (int b0 = 0; b0 < cap.blocks; b0 += 256) {
@@ -182,16 +204,7 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
       f = end;
     }
   }
-  if (tid == 0) {
-    a.head[keys ? DOCS_SPLIT_K : DOCS_SPLIT_Q] = min((int)(cut >> 32), cap.splits);
-    if (!keys) {
-      a.head[DOCS_LIVE0] = live0;
-      a.head[DOCS_LIVE1] = live1;
-      a.head[DOCS_T] = a.T;
-      a.head[DOCS_NQ] = a.nq;
-      a.head[DOCS_NKV] = a.nkv;
-    }
-  }
+  if (tid == 0) docs_head(a, keys, live0, live1, all_units, min((int)(cut >> 32), cap.splits));
 }
 
 // Blocks 0 and 1 make the two work lists; in the others a wave takes 64 rows: the document of its first row, then, 64 starts at a time, how many more begin at or

@@ -245,3 +245,45 @@ def test_starts_out_of_order_touch_nothing_else(dh):
         torch.cuda.synchronize()
         pos = p.pos.cpu()
         assert bool(((pos >= 0) & (pos < 100)).all())
+
+
+@pytest.mark.parametrize("d,cap", [(128, 0.0), (64, 0.0), (128, 50.0), (64, 30.0)])
+def test_cut_rows(dh, d, cap):
+    """Long documents beside short ones on few heads: blocks of queries and of keys are cut into several units."""
+    p = Packed(dh, "bf16", T=2600, nq=2, nkv=1, d=d, lengths=[1900, 30, 600], first=17, cap=cap, seed=12).run()
+    head = p.table[:64].view(torch.int32).cpu()
+    assert int(head[6]) > 0 and int(head[8]) > 0  # blocks that were cut, of queries and of keys
+
+
+def test_cut_rows_beside_what_is_not_finite(dh):
+    """Units of a cut row in which keys that the row does not see are NaNs."""
+    def poison(qkv, dout):
+        qkv[1100:1130] = float("nan")
+        dout[1100:1130] = float("inf")
+
+    rows = torch.ones(2000, dtype=torch.bool)
+    rows[1100:1130] = False
+    Packed(dh, "bf16", T=2000, nq=2, nkv=1, d=128, lengths=[1100, 30, 870], seed=13).run(poison, rows)
+
+
+def test_two_launches(dh):
+    """More blocks of heads than the backward pass takes in one launch."""
+    Packed(dh, "bf16", T=1500, nq=96, nkv=32, d=64, lengths=[700, 100, 690], first=5, seed=14).run()
+
+
+def test_one_prefix_over_everything(dh):
+    """Every row sees every key."""
+    Packed(dh, "bf16", T=700, nq=2, nkv=1, d=128, lengths=[700], prefixes=[700], seed=15).run()
+    Packed(dh, "f32", T=130, nq=2, nkv=1, d=64, lengths=[130], prefixes=[130], seed=15).run()
+
+
+def test_a_table_for_other_sizes_is_left_alone(dh):
+    """Attention whose sizes are not those the table was made for writes nothing."""
+    p = Packed(dh, "bf16", T=300, nq=4, nkv=2, d=64, lengths=[300], seed=16)
+    p.qkv_d, p.dout_d = p.qkv.cuda(), p.dout.cuda()
+    p.buffers()
+    dh.dh_docs_plan(p.docs)
+    p.docs.nkv = 1  # the same buffers are large enough
+    p.forward()
+    torch.cuda.synchronize()
+    assert bool((p.o == MARK).all()) and bool((p.lse == MARK).all())
