@@ -8,7 +8,9 @@
 // Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN: a wave whose result is not finite makes the rows
 // concerned again, one at a time, over exactly what they see (docs_row_*).  Rows outside all documents are never read: transfers take the nearest row of a document.
 //
-// CAP: x = cap tanh(x / cap) as cap - 2 cap r with r = 1 / (1 + e^(2x/cap)), one exponential and one reciprocal more an element; its slope is 4 r (1 - r) = 4 e r r.
+// CAP: x = cap tanh(x / cap) as cap - 2 cap r with r = 1 / (1 + e^(2x/cap)), one exponential and one reciprocal more an element, whose limits (r = 0, 1) are right where the
+// exponential is infinite or zero; its slope is 4 (r - r r), off by at most 2^-22, of which the factor 4 waits for the end.  The exponent of 2 of a probability is
+// one multiply-add of r.
 #pragma once
 #include "docs.h"
 
@@ -52,12 +54,8 @@ __device__ __forceinline__ bool docs_not_finite(const f32x16 (&t)[N]) {
     for (int r = 0; r < 16; r++) m = max(m, __builtin_bit_cast(uint32_t, t[i][r]) & 0x7fffffffu);
   return m >= 0x7f800000u;
 }
-// A score as an exponent of 2 under the cap; e and r as above.
-__device__ __forceinline__ float docs_cap_exponent(float s, float k, float cap_log2, float& e, float& r) {
-  e = fast_exp2(fminf(s * k, 64.f));  // beyond 2^64 the tanh is 1 in float32, its slope 2^-62
-  r = __builtin_amdgcn_rcpf(1.f + e);
-  return fmaf(-2.f * cap_log2, r, cap_log2);
-}
+// r of a score under the cap, k = exp_scale.
+__device__ __forceinline__ float docs_cap_r(float s, float k) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k)); }
 // ================================================================================ forward
 // grid (units * nq)
 template <int D, bool CAP>
@@ -123,23 +121,21 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
 #pragma unroll
       for (int mt = 0; mt < 2; mt++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-          float e, q;
-          st[mt][r] = docs_cap_exponent(st[mt][r], p.exp_scale, p.cap_log2, e, q);
-        }
+        for (int r = 0; r < 16; r++) st[mt][r] = docs_cap_r(st[mt][r], p.exp_scale);
     }
     if (kb < see.all0 || kb + AB_KT > see.all1) {
 #pragma unroll
       for (int mt = 0; mt < 2; mt++)
 #pragma unroll
         for (int r = 0; r < 16; r++)
-          st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : -INFINITY;
+          st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : CAP ? INFINITY : -INFINITY;
     }
-    float mx = fmaxf(st[0][0], st[1][0]);
+    auto larger = [](float a, float b) { return CAP ? fminf(a, b) : fmaxf(a, b); };  // of the scores: the smaller r
+    float mx = larger(st[0][0], st[1][0]);
 #pragma unroll
-    for (int r = 1; r < 16; r++) mx = fmaxf(mx, fmaxf(st[0][r], st[1][r]));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float scale = CAP ? 1.f : p.exp_scale, mnew = mx * scale;
+    for (int r = 1; r < 16; r++) mx = larger(mx, larger(st[0][r], st[1][r]));
+    mx = larger(mx, __shfl_xor(mx, 32, 64));
+    const float scale = CAP ? -2.f * p.cap_log2 : p.exp_scale, mnew = CAP ? fmaf(scale, mx, p.cap_log2) : mx * scale;
     float rs = 0.f;
     if (__any(mnew > m + AF_TAU)) {  // the reference maximum moves where a row's probabilities would grow beyond 2^AF_TAU
       const float mn = fmaxf(m, mnew);
@@ -151,11 +147,12 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
 #pragma unroll
         for (int r = 0; r < 16; r++) ot[dt][r] *= alpha;
     }
+    const float off = CAP ? p.cap_log2 - m : -m;
 #pragma unroll
     for (int mt = 0; mt < 2; mt++)
 #pragma unroll
       for (int r = 0; r < 16; r++) {
-        const float x = CAP ? fast_exp2(st[mt][r] - m) : fast_exp2(fmaf(st[mt][r], scale, -m));
+        const float x = fast_exp2(fmaf(st[mt][r], scale, off));
         st[mt][r] = x;
         rs += x;
       }
@@ -259,7 +256,7 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
 
 // ================================================================================ backward: dQ
 // As attn_bwd_dq_block, unit id of head h.  STORE: the first unit of a block also stores its rows' delta and lse2 for the dK/dV launch behind it; otherwise
-// attn_bwd_prep_kernel has.
+// attn_docs_prep_kernel has.
 #define DOCS_DQ_RING 2
 template <int D, bool CAP, bool STORE>
 __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
@@ -310,7 +307,7 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
     dl += __shfl_xor(dl, 32, 64);
   }
   const bool live = iq < T && hi > lo;
-  l2 *= LOG2E;
+  l2 = CAP ? p.cap_log2 - l2 * LOG2E : l2 * LOG2E;  // with a cap: what the exponent adds to the multiple of r
   if (STORE && (u.block2 & 1) && kg == 0 && live) {
     delta[(size_t)h * T + row] = dl;
     lse2[(size_t)h * T + row] = l2;
@@ -343,9 +340,8 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
         const int x = j * N + i;
         const float s = st[x >> 4][x & 15];
         if constexpr (CAP) {
-          float e, r;
-          const float pr = fast_exp2(docs_cap_exponent(s, p.exp_scale, p.cap_log2, e, r) - l2);
-          st[x >> 4][x & 15] = pr * (4.f * e * r * r);  // times the slope at once: dQ needs no probability by itself
+          const float r = docs_cap_r(s, p.exp_scale);
+          st[x >> 4][x & 15] = fast_exp2(fmaf(-2.f * p.cap_log2, r, l2)) * fmaf(-r, r, r);  // times the slope at once: dQ needs no probability by itself
         } else {
           st[x >> 4][x & 15] = fast_exp2(fmaf(s, p.exp_scale, -l2));
         }
@@ -373,7 +369,7 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
   const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
   float* prow = part + (((size_t)u.slot * nq + h) * DOCS_BLOCK + wave * 32) * D;
   bf16_t* out = dqkv + (size_t)iw * ld + (size_t)h * D;
-  const float scale = p.a.scale;
+  const float scale = CAP ? 4.f * p.a.scale : p.a.scale;
   if (u.slot >= 0) {
     wave_rows_out_f32<D>(
         reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
@@ -389,11 +385,11 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
     const int r = __builtin_ctz(rest), i = iw + r, j0 = max(__builtin_amdgcn_readlane(lo, r), u.f0 * AB_KT), j1 = min(__builtin_amdgcn_readlane(end, r), u.f1 * AB_KT);
     const float dr = __shfl(dl, r, 64), lr = lse[(size_t)h * T + i];
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    docs_row_dq(qkv + (size_t)i * ld + (size_t)h * D, dout + ((size_t)i * nq + h) * D, kcol, kcol + (size_t)nkv * D, (size_t)ld, j0, j1, D, scale, p.a.cap, lr, dr, acc);
+    docs_row_dq(qkv + (size_t)i * ld + (size_t)h * D, dout + ((size_t)i * nq + h) * D, kcol, kcol + (size_t)nkv * D, (size_t)ld, j0, j1, D, p.a.scale, p.a.cap, lr, dr, acc);
 #pragma unroll
     for (int c = 0; c < D / 64; c++) {
-      if (u.slot >= 0) prow[(size_t)r * D + lane + 64 * c] = acc[c];
-      else out[(size_t)r * ld + lane + 64 * c] = (bf16_t)(acc[c] * scale);
+      if (u.slot >= 0) prow[(size_t)r * D + lane + 64 * c] = acc[c] * (CAP ? 0.25f : 1.f);
+      else out[(size_t)r * ld + lane + 64 * c] = (bf16_t)(acc[c] * p.a.scale);
     }
   }
 }
@@ -490,9 +486,9 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
         for (int e = 0; e < 4; e++) {
           const float s = st[mt][4 * q4 + e];
           if constexpr (CAP) {
-            float ex, r;
-            st[mt][4 * q4 + e] = fast_exp2(docs_cap_exponent(s, p.exp_scale, p.cap_log2, ex, r) - lv[x][e]);
-            slope[mt][4 * q4 + e] = 4.f * ex * r * r;
+            const float r = docs_cap_r(s, p.exp_scale);
+            st[mt][4 * q4 + e] = fast_exp2(fmaf(-2.f * p.cap_log2, r, lv[x][e]));
+            slope[mt][4 * q4 + e] = fmaf(-r, r, r);
           } else {
             st[mt][4 * q4 + e] = fast_exp2(fmaf(s, p.exp_scale, -lv[x][e]));
           }
@@ -527,7 +523,7 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   __syncthreads();  // every wave is done with the Q/dO rings: their LDS serves the output turn (dK, then dV)
   const uint64_t both = __ballot(live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt))), alive = __ballot(live);
   const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
-  const float scale = p.a.scale;
+  const float scale = CAP ? 4.f * p.a.scale : p.a.scale;
   auto dk_quad = [&](int dt, int q4) {
     return f32x4{dkt[dt][4 * q4] * scale, dkt[dt][4 * q4 + 1] * scale, dkt[dt][4 * q4 + 2] * scale, dkt[dt][4 * q4 + 3] * scale};
   };
@@ -552,22 +548,50 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
     for (int g = f0 / nt; g * nt < f1; g++) {  // the unit's run of tiles of each head
       const int t0 = span.first + max(f0 - g * nt, 0), t1 = span.first + min(f1 - g * nt, nt);
       docs_row_dkv(k, k + (size_t)nkv * D, qkv + (size_t)(hq + g) * D, (size_t)ld, dout + (size_t)(hq + g) * D, (size_t)ldo, lse + (size_t)(hq + g) * T, delta + (size_t)(hq + g) * T,
-                   max(a0, t0 * AB_KT), min(a1, t1 * AB_KT), D, scale, p.a.cap, dk, dv);
+                   max(a0, t0 * AB_KT), min(a1, t1 * AB_KT), D, p.a.scale, p.a.cap, dk, dv);
     }
 #pragma unroll
     for (int c = 0; c < D / 64; c++) {
       const int e = lane + 64 * c;
       if (u.slot >= 0) {
-        prow[(size_t)r * (2 * D) + e] = dk[c] * scale;
+        prow[(size_t)r * (2 * D) + e] = dk[c] * p.a.scale;
         prow[(size_t)r * (2 * D) + D + e] = dv[c];
       } else {
-        out[(size_t)r * ld + e] = (bf16_t)(dk[c] * scale);
+        out[(size_t)r * ld + e] = (bf16_t)(dk[c] * p.a.scale);
         out[(size_t)r * ld + (size_t)nkv * D + e] = (bf16_t)dv[c];
       }
     }
   }
 }
 
+// Delta and lse2 (with a cap: cap_log2 - lse2) of every row, as attn_bwd_prep_kernel: the numbers the dQ blocks use.
+template <int D, bool CAP>
+__global__ __launch_bounds__(64) void attn_docs_prep_kernel(const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout, const float* __restrict__ lse, float* __restrict__ lse2,
+                                                            float* __restrict__ delta, int T, int nq, float cap_log2) {
+  const size_t i = (size_t)blockIdx.x * 32 + (threadIdx.x >> 1);
+  if (i >= (size_t)T * nq) return;
+  const int kg = threadIdx.x & 1, h = (int)(i % nq);
+  const size_t t = i / nq, at = (size_t)h * T + t;
+  const bf16_t* orow = o + (t * nq + h) * D + kg * 8;
+  const bf16_t* drow = dout + (t * nq + h) * D + kg * 8;
+  const float l = lse[at] * LOG2E;
+  bf16x8 a[D / 16], b[D / 16];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) {
+    a[ks] = *reinterpret_cast<const bf16x8*>(drow + ks * 16);
+    b[ks] = *reinterpret_cast<const bf16x8*>(orow + ks * 16);
+  }
+  float half = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) half = fmaf((float)a[ks][e], (float)b[ks][e], half);
+  const float other = __shfl_xor(half, 1, 64);
+  if (kg == 0) {
+    delta[at] = half + other;
+    lse2[at] = CAP ? cap_log2 - l : l;
+  }
+}
 // The two as launches of their own (dQ first: it stores the rows' statistics that the dK/dV blocks read), grids (units * nq) and (units * nkv) ...
 template <int D, bool CAP>
 __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
@@ -581,7 +605,7 @@ __global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const Do
                                                                         float* __restrict__ part) {
   docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse, lse2, delta, dqkv, part);
 }
-// ... and as one, behind attn_bwd_prep_kernel, for grids that leave units of the chip idle: dK/dV units (the longer ones) first.  grid (units_k * nkv + units_q * nq)
+// ... and as one, behind attn_docs_prep_kernel, for grids that leave units of the chip idle: dK/dV units (the longer ones) first.  grid (units_k * nkv + units_q * nq)
 template <int D, bool CAP>
 __global__ __launch_bounds__(AB_THREADS) void attn_docs_bwd_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
                                                                         const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
@@ -613,7 +637,7 @@ __global__ __launch_bounds__(256) void attn_docs_reduce_kernel(const DocsTiled p
   const float* from = part + (unit + row) * width + c4;
 #pragma unroll 8
   for (int c = 0; c < s.n; c++) t += __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + c * step));
-  const float f = q ? p.a.scale : 1.f;
+  const float f = !q ? 1.f : p.a.cap > 0.f ? 4.f * p.a.scale : p.a.scale;
   bf16x4 out = {(bf16_t)(t[0] * f), (bf16_t)(t[1] * f), (bf16_t)(t[2] * f), (bf16_t)(t[3] * f)};
   bf16_t* dst = dqkv + (size_t)i * ld + (q ? (size_t)h * D + c4 : c4 < D ? (size_t)(nq + h) * D + c4 : (size_t)(nq + nkv + h) * D + (c4 - D));
   *reinterpret_cast<bf16x4*>(dst) = out;
@@ -682,7 +706,7 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
   if (docs_one_launch(p.a.v.T, nq, nkv)) {
-    attn_bwd_prep_kernel<D><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq);
+    attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
     DH_LAUNCH_CHECK();
     attn_docs_bwd_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv + (unsigned)q.units * nq, AB_THREADS, lds_dkv, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q, part_kv);
     DH_LAUNCH_CHECK();
