@@ -1157,6 +1157,194 @@ __device__ __forceinline__ void attn_bwd_dq_reduce_block(int bx, int by, int bz,
 }
 
 // ================================================================================ backward: dK, dV
+// The D = 128 tile loop of dK/dV: tiles [f0, f1) of the group's heads, nt query tiles from position q0 on of each, counted through; issue(slot) transfers the tile (gi, ti) and moves
+// on.  walk: the wave's tiles (idle: no query of the tile sees any of its keys; partial: some queries do not see some of them, a lane's key sees `rows` of them from position jk on;
+// ragged: the tile's transfer takes clamped rows, by issue).
+// One wave has a SIMD to itself: beside its matrix instructions runs only what stands between them.  A 32x32x16 one keeps the matrix cores 32 cycles, a
+// tile's 64 of them 2048; a tile's other instructions (32 exponentials, 130 more of the vector ALU, 112 LDS reads, 9 transfers, 70 scalar ones) fill about
+// as many issue cycles and fit in their shadows if every slot gets its share.  Left to the compiler, half of dP's products ended up
+// behind all exponentials, and a tile took 4500 cycles.  So the matrix instructions are volatile, each is followed by its share, and all of it is pinned; fragments are
+// requested six products ahead (transposed ones eight); the next tile is published beside this one's dK products and its first fragments are read
+// there, so that no tile begins with a wait.  The same bits as in phases.  The whole backward pass (us, before and after): 32:8 heads x 4096 tokens 492 -> 465, 8:1 x
+// 8192 497 -> 473, 4:1 x 4096 queries over 12288 keys 330 -> 305, 2 x 2048 x 8 heads 81.4 -> 72.5, 4:1 x 4096 92 -> 88; sequences of one tile pay for the longer
+// start (four of 64 tokens 9.8 -> 10.3).  (Accumulators that start from the rows' delta save the 32 subtractions, 0.6 % of these, and
+// round at delta's scale on the way: a score gradient that cancels loses the small terms.)
+template <class Walk, class Issue>
+__device__ __forceinline__ void dkv_pinned(const Walk& walk, Issue& issue, const lds_char* sm, const FragAddr<128>& fa, bf16x8 (&kf)[8], bf16x8 (&vf)[8], f32x16 (&dkt)[4], f32x16 (&dvt)[4],
+                                           const char* qbase, const char* obase, const float* srow, int T, size_t qstride, size_t ostride, const uint32_t (&vq)[4], const uint32_t (&vo)[4],
+                                           uint32_t ldsQ, uint32_t ldsS, int wave, int lane, int kg, int q0, int nt, int f0, int f1, int& gi, int& ti, int tc, float scale_log2) {
+  using TL = ATile<128>;
+  static_assert(AB_KT == 64 && AB_RING == 3, "slots below");
+  constexpr int D = 128, KS = D / 16, OFF1 = AB_RING * TL::BYTES;
+  const lds_char* dir[KS];
+  const lds_char* t0[D / 32];
+  const lds_char* t1[D / 32];
+  const lds_char* stp = sm + 2 * AB_RING * TL::BYTES + 4 * kg * sizeof(float);  // statistics of the lane's rows
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) dir[ks] = sm + fa.kdir[ks];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) { t0[dt] = sm + fa.tr0[dt]; t1[dt] = sm + fa.tr1[dt]; }
+  bf16x8 fr[4][2];         // score fragments of four k-steps
+  bf16x8 tr[3][D / 32];    // transposed fragments of three groups of 16 rows: dO's groups are 0-3, Q's 4-7
+  bf16x8 pf[2];            // packed P (groups 0-3), then dS (4-7)
+  f32x4 lv[8], dl[8];      // log sums and delta of rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
+  f32x16 st[2], dp[2];
+  auto row_stat = [&](int ring, int x) { return *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(stp + ring + x * 32); };
+  auto frag = [&](int step, int mt) {  // k-step `step` of the tile's S products, from KS on of its dP products
+    fr[step & 3][mt] = lds_frag(dir[step & (KS - 1)], (step < KS ? 0 : OFF1) + mt * 32 * TL::LD * 2);
+  };
+  auto trfrag = [&](int group, int dt) { tr[group % 3][dt] = lds_frag_tr(t0[dt], t1[dt], (group < 4 ? OFF1 : 0) + (group & 3) * 16 * TL::LD * 2); };
+  auto pack2 = [&](int group, int e) {  // elements 2e, 2e+1 of the group's fragment
+    const f32x16& t = st[(group & 3) >> 1];
+    pf[group & 1][2 * e] = (bf16_t)t[8 * (group & 1) + 2 * e];
+    pf[group & 1][2 * e + 1] = (bf16_t)t[8 * (group & 1) + 2 * e + 1];
+  };
+  auto pack_share = [&](int group, int i) {  // beside the i-th product of the group before: none beside the last, a product later than the vector ALU writes
+    if (i == 0) { pack2(group, 0); pack2(group, 1); }
+    else if (i < 3) pack2(group, i + 1);
+  };
+  issue(0);
+  if (f0 + 1 < f1) issue(1);
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) asm volatile("" : "+a"(kf[ks]), "+a"(vf[ks]));
+  const uint32_t ldsQw = ldsQ + wave * (TL::IPW * 1024), tile_bytes = TL::BYTES;
+  int slot = 0;
+  const char *qp, *op, *sp;  // of the tile to transfer next
+  auto sources = [&]() {
+    qp = qbase + ti * qstride + gi * (D * sizeof(bf16_t));
+    op = obase + ti * ostride + gi * (D * sizeof(bf16_t));
+    sp = reinterpret_cast<const char*>(srow + (size_t)gi * T + ti * AB_KT);
+  };
+  sources();
+  if (f0 + 1 < f1) dma_wait<2 * TL::IPW + 1>(); else dma_wait<0>();
+  __syncthreads();
+#pragma unroll
+  for (int step = 0; step < 3; step++) { frag(step, 0); frag(step, 1); }
+  for (int f = f0; f < f1; f++) {
+    const int next = slot == AB_RING - 1 ? 0 : slot + 1, free_slot = slot == 0 ? AB_RING - 1 : slot - 1;
+    const int step_tile = (next - slot) * TL::BYTES, step_stat = (next - slot) * AB_KT * (int)sizeof(float);
+    asm volatile("s_barrier" ::: "memory");  // every wave is done with tile f-1: its slot is filled next
+    const int qb = q0 + tc * AB_KT;
+    if (++tc == nt) tc = 0;
+    const bool more = f + 2 < f1, idle = walk.idle(qb);
+    const bool beside = more && !idle && !walk.ragged(ti);
+    if (more && !beside) { issue(free_slot); sources(); }
+    auto publish = [&]() {  // tile f+1, whose transfers are followed by tile f+2's
+      if (more) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * TL::IPW + 1) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    auto shift_dir = [&]() {
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) dir[ks] += step_tile;
+    };
+    auto shift_tr = [&]() {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++) { t0[dt] += step_tile; t1[dt] += step_tile; }
+    };
+    slot = next;
+    if (idle) {
+      publish();
+      shift_dir();
+      shift_tr();
+      stp += step_stat;
+#pragma unroll
+      for (int step = 0; step < 3; step++) { frag(step, 0); frag(step, 1); }
+      continue;
+    }
+    auto scores = [&](auto transfers) {
+      constexpr bool TRANSFERS = decltype(transfers)::value;
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        if (i < 2) mfma_first(st[i & 1], fr[(i >> 1) & 3][i & 1], kf[i >> 1]);
+        else mfma_next(st[i & 1], fr[(i >> 1) & 3][i & 1], kf[i >> 1]);
+        frag((i >> 1) + 3, i & 1);
+        if (i < 8) dl[i] = row_stat(AB_RING * AB_KT * sizeof(float), i);
+        else lv[i - 8] = row_stat(0, i - 8);
+        if (TRANSFERS) {
+          if (i == 2) m = dma_lds(ldsQw + free_slot * tile_bytes);
+          if (i == 6) m = dma_lds(ldsQw + free_slot * tile_bytes + AB_RING * tile_bytes);
+          if (i >= 2 && i < 6) dma16_at(m, qp, vq[i - 2], (i - 2) * 1024);
+          if (i >= 6 && i < 10) dma16_at(m, op, vo[i - 6], (i - 6) * 1024);
+          if (i == 10) dma4_base(sp, lane * sizeof(float), ldsS + free_slot * AB_KT * sizeof(float));
+          if (i == 12) {
+            qp += qstride;
+            op += ostride;
+            sp += AB_KT * sizeof(float);
+          }
+        }
+        AB_PIN();
+      }
+    };
+    if (beside) {
+      scores(std::true_type{});
+      if (++ti == nt) { ti = 0; gi++; sources(); }
+    } else {
+      scores(std::false_type{});
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      const int ks = i >> 1, mt = i & 1;
+      if (ks == 0) mfma_first(dp[mt], fr[KS & 3][mt], vf[0]);
+      else mfma_next(dp[mt], fr[(ks + KS) & 3][mt], vf[ks]);
+      if (ks + 3 < KS) frag(ks + KS + 3, mt);
+      if (i >= 8) trfrag((i - 8) >> 2, i & 3);
+      if (i >= 2) {  // P from S, 32 values over 14 slots
+#pragma unroll
+        for (int x = (i - 2) * 32 / 14; x < (i - 1) * 32 / 14; x++) st[x >> 4][x & 15] = fast_exp2(fmaf(st[x >> 4][x & 15], scale_log2, -lv[x >> 2][x & 3]));
+      }
+      AB_PIN();
+    }
+    if (walk.partial(qb)) {
+      const int first = qb + 4 * kg;
+      const uint32_t rows = walk.rows();
+#pragma unroll
+      for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          st[mt][r] = (uint32_t)(first + mt * 32 + 8 * (r >> 2) + (r & 3) - walk.jk) < rows ? st[mt][r] : 0.f;
+          if ((r & 3) == 3) AB_PIN();
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++) pack2(0, e);
+    frag_settle(pf[0]);
+    // dV^T += dO^T P; a group of P, once packed, becomes dS = P (dP - delta) in place
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      const int g = i >> 2, dt = i & 3;
+      mfma_grad(dvt[dt], tr[g % 3][dt], pf[g & 1]);
+      trfrag(g + 2, dt);
+#pragma unroll
+      for (int x = 8 * g + 2 * dt; x < 8 * g + 2 * dt + 2; x++) st[x >> 4][x & 15] *= dp[x >> 4][x & 15] - dl[x >> 2][x & 3];
+      pack_share(g + 1, dt);
+      if (i == 8) shift_dir();
+      AB_PIN();
+    }
+    // dK^T += Q^T dS
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      const int g = 4 + (i >> 2), dt = i & 3;
+      mfma_grad(dkt[dt], tr[g % 3][dt], pf[g & 1]);
+      if (g < 6) trfrag(g + 2, dt);
+      if (g < 7) pack_share(g + 1, dt);
+      if (i == 8) publish();
+      if (i == 9) shift_tr();
+      if (i >= 10) frag((i - 10) >> 1, i & 1);
+      AB_PIN();
+    }
+    stp += step_stat;
+  }
+}
+// The walk of plain causal attention.
+struct CausalWalk {
+  int jw, jk, seq, ragged_ti;  // ragged_ti: the tile of each head that is not whole
+  __device__ __forceinline__ bool idle(int qb) const { return qb + AB_KT - 1 < jw; }  // every query of the tile precedes every key of this wave
+  __device__ __forceinline__ bool partial(int qb) const { return qb < jw + 32 || qb + AB_KT > seq; }  // diagonal tile, or rows past the end of the sequence
+  __device__ __forceinline__ uint32_t rows() const { return (uint32_t)max(seq - jk, 0); }
+  __device__ __forceinline__ bool ragged(int ti) const { return ti == ragged_ti; }
+};
+
 // grid (pairs * nkv * batch): one block per (key block, chunk, key/value head); wave w owns keys
 // j0 + 32w .. +31 and keeps their K, V fragments and the dK^T, dV^T accumulators in registers while
 // 64-query tiles of Q and dO stream through LDS: those of the group's first query head, then those of the next, and so on
@@ -1237,177 +1425,8 @@ __device__ __forceinline__ void attn_bwd_dkv_block(const int bid, const AttnGeom
     if (++ti == nt) { ti = 0; gi++; }
   };
   if constexpr (D == 128) {
-    // One wave has a SIMD to itself: beside its matrix instructions runs only what stands between them.  A 32x32x16 one keeps the matrix cores 32 cycles, a
-    // tile's 64 of them 2048; a tile's other instructions (32 exponentials, 130 more of the vector ALU, 112 LDS reads, 9 transfers, 70 scalar ones) fill about
-    // as many issue cycles and fit in their shadows if every slot gets its share.  Left to the compiler, half of dP's products ended up
-    // behind all exponentials, and a tile took 4500 cycles.  So the matrix instructions are volatile, each is followed by its share, and all of it is pinned; fragments are
-    // requested six products ahead (transposed ones eight); the next tile is published beside this one's dK products and its first fragments are read
-    // there, so that no tile begins with a wait.  The same bits as in phases.  The whole backward pass (us, before and after): 32:8 heads x 4096 tokens 492 -> 465, 8:1 x
-    // 8192 497 -> 473, 4:1 x 4096 queries over 12288 keys 330 -> 305, 2 x 2048 x 8 heads 81.4 -> 72.5, 4:1 x 4096 92 -> 88; sequences of one tile pay for the longer
-    // start (four of 64 tokens 9.8 -> 10.3).  (Accumulators that start from the rows' delta save the 32 subtractions, 0.6 % of these, and
-    // round at delta's scale on the way: a score gradient that cancels loses the small terms.)
-    static_assert(AB_KT == 64 && AB_RING == 3, "slots below");
-    constexpr int KS = D / 16, OFF1 = AB_RING * TL::BYTES;
-    const lds_char* dir[KS];
-    const lds_char* t0[D / 32];
-    const lds_char* t1[D / 32];
-    const lds_char* stp = sm + 2 * AB_RING * TL::BYTES + 4 * kg * sizeof(float);  // statistics of the lane's rows
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) dir[ks] = sm + fa.kdir[ks];
-#pragma unroll
-    for (int dt = 0; dt < D / 32; dt++) { t0[dt] = sm + fa.tr0[dt]; t1[dt] = sm + fa.tr1[dt]; }
-    bf16x8 fr[4][2];         // score fragments of four k-steps
-    bf16x8 tr[3][D / 32];    // transposed fragments of three groups of 16 rows: dO's groups are 0-3, Q's 4-7
-    bf16x8 pf[2];            // packed P (groups 0-3), then dS (4-7)
-    f32x4 lv[8], dl[8];      // log sums and delta of rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
-    f32x16 st[2], dp[2];
-    auto row_stat = [&](int ring, int x) { return *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(stp + ring + x * 32); };
-    auto frag = [&](int step, int mt) {  // k-step `step` of the tile's S products, from KS on of its dP products
-      fr[step & 3][mt] = lds_frag(dir[step & (KS - 1)], (step < KS ? 0 : OFF1) + mt * 32 * TL::LD * 2);
-    };
-    auto trfrag = [&](int group, int dt) { tr[group % 3][dt] = lds_frag_tr(t0[dt], t1[dt], (group < 4 ? OFF1 : 0) + (group & 3) * 16 * TL::LD * 2); };
-    auto pack2 = [&](int group, int e) {  // elements 2e, 2e+1 of the group's fragment
-      const f32x16& t = st[(group & 3) >> 1];
-      pf[group & 1][2 * e] = (bf16_t)t[8 * (group & 1) + 2 * e];
-      pf[group & 1][2 * e + 1] = (bf16_t)t[8 * (group & 1) + 2 * e + 1];
-    };
-    auto pack_share = [&](int group, int i) {  // beside the i-th product of the group before: none beside the last, a product later than the vector ALU writes
-      if (i == 0) { pack2(group, 0); pack2(group, 1); }
-      else if (i < 3) pack2(group, i + 1);
-    };
-    issue(0);
-    if (f0 + 1 < f1) issue(1);
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) asm volatile("" : "+a"(kf[ks]), "+a"(vf[ks]));
-    const uint32_t ldsQw = ldsQ + wave * (TL::IPW * 1024), tile_bytes = TL::BYTES;
-    const int ragged_ti = (seq - q0) % AB_KT != 0 ? nt - 1 : nt;  // the tile of each head that is not whole
-    int slot = 0;
-    const char *qp, *op, *sp;  // of the tile to transfer next
-    auto sources = [&]() {
-      qp = qbase + ti * qstride + gi * (D * sizeof(bf16_t));
-      op = obase + ti * ostride + gi * (D * sizeof(bf16_t));
-      sp = reinterpret_cast<const char*>(srow + (size_t)gi * T + ti * AB_KT);
-    };
-    sources();
-    if (f0 + 1 < f1) dma_wait<2 * TL::IPW + 1>(); else dma_wait<0>();
-    __syncthreads();
-#pragma unroll
-    for (int step = 0; step < 3; step++) { frag(step, 0); frag(step, 1); }
-    for (int f = f0; f < f1; f++) {
-      const int next = slot == AB_RING - 1 ? 0 : slot + 1, free_slot = slot == 0 ? AB_RING - 1 : slot - 1;
-      const int step_tile = (next - slot) * TL::BYTES, step_stat = (next - slot) * AB_KT * (int)sizeof(float);
-      asm volatile("s_barrier" ::: "memory");  // every wave is done with tile f-1: its slot is filled next
-      const int qb = q0 + tc * AB_KT;
-      if (++tc == nt) tc = 0;
-      const bool more = f + 2 < f1, idle = qb + AB_KT - 1 < jw;  // idle: every query of the tile precedes every key of this wave
-      const bool beside = more && !idle && ti != ragged_ti;
-      if (more && !beside) { issue(free_slot); sources(); }
-      auto publish = [&]() {  // tile f+1, whose transfers are followed by tile f+2's
-        if (more) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * TL::IPW + 1) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-      };
-      auto shift_dir = [&]() {
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++) dir[ks] += step_tile;
-      };
-      auto shift_tr = [&]() {
-#pragma unroll
-        for (int dt = 0; dt < D / 32; dt++) { t0[dt] += step_tile; t1[dt] += step_tile; }
-      };
-      slot = next;
-      if (idle) {
-        publish();
-        shift_dir();
-        shift_tr();
-        stp += step_stat;
-#pragma unroll
-        for (int step = 0; step < 3; step++) { frag(step, 0); frag(step, 1); }
-        continue;
-      }
-      auto scores = [&](auto transfers) {
-        constexpr bool TRANSFERS = decltype(transfers)::value;
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-          if (i < 2) mfma_first(st[i & 1], fr[(i >> 1) & 3][i & 1], kf[i >> 1]);
-          else mfma_next(st[i & 1], fr[(i >> 1) & 3][i & 1], kf[i >> 1]);
-          frag((i >> 1) + 3, i & 1);
-          if (i < 8) dl[i] = row_stat(AB_RING * AB_KT * sizeof(float), i);
-          else lv[i - 8] = row_stat(0, i - 8);
-          if (TRANSFERS) {
-            if (i == 2) m = dma_lds(ldsQw + free_slot * tile_bytes);
-            if (i == 6) m = dma_lds(ldsQw + free_slot * tile_bytes + AB_RING * tile_bytes);
-            if (i >= 2 && i < 6) dma16_at(m, qp, vq[i - 2], (i - 2) * 1024);
-            if (i >= 6 && i < 10) dma16_at(m, op, vo[i - 6], (i - 6) * 1024);
-            if (i == 10) dma4_base(sp, lane * sizeof(float), ldsS + free_slot * AB_KT * sizeof(float));
-            if (i == 12) {
-              qp += qstride;
-              op += ostride;
-              sp += AB_KT * sizeof(float);
-            }
-          }
-          AB_PIN();
-        }
-      };
-      if (beside) {
-        scores(std::true_type{});
-        if (++ti == nt) { ti = 0; gi++; sources(); }
-      } else {
-        scores(std::false_type{});
-      }
-#pragma unroll
-      for (int i = 0; i < 16; i++) {
-        const int ks = i >> 1, mt = i & 1;
-        if (ks == 0) mfma_first(dp[mt], fr[KS & 3][mt], vf[0]);
-        else mfma_next(dp[mt], fr[(ks + KS) & 3][mt], vf[ks]);
-        if (ks + 3 < KS) frag(ks + KS + 3, mt);
-        if (i >= 8) trfrag((i - 8) >> 2, i & 3);
-        if (i >= 2) {  // P from S, 32 values over 14 slots
-#pragma unroll
-          for (int x = (i - 2) * 32 / 14; x < (i - 1) * 32 / 14; x++) st[x >> 4][x & 15] = fast_exp2(fmaf(st[x >> 4][x & 15], scale_log2, -lv[x >> 2][x & 3]));
-        }
-        AB_PIN();
-      }
-      if (qb < jw + 32 || qb + AB_KT > seq) {  // diagonal tile, or rows past the end of the sequence
-        const int first = qb + 4 * kg;
-        const uint32_t rows = (uint32_t)max(seq - jk, 0);
-#pragma unroll
-        for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-          for (int r = 0; r < 16; r++) {
-            st[mt][r] = (uint32_t)(first + mt * 32 + 8 * (r >> 2) + (r & 3) - jk) < rows ? st[mt][r] : 0.f;
-            if ((r & 3) == 3) AB_PIN();
-          }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; e++) pack2(0, e);
-      frag_settle(pf[0]);
-      // dV^T += dO^T P; a group of P, once packed, becomes dS = P (dP - delta) in place
-#pragma unroll
-      for (int i = 0; i < 16; i++) {
-        const int g = i >> 2, dt = i & 3;
-        mfma_grad(dvt[dt], tr[g % 3][dt], pf[g & 1]);
-        trfrag(g + 2, dt);
-#pragma unroll
-        for (int x = 8 * g + 2 * dt; x < 8 * g + 2 * dt + 2; x++) st[x >> 4][x & 15] *= dp[x >> 4][x & 15] - dl[x >> 2][x & 3];
-        pack_share(g + 1, dt);
-        if (i == 8) shift_dir();
-        AB_PIN();
-      }
-      // dK^T += Q^T dS
-#pragma unroll
-      for (int i = 0; i < 16; i++) {
-        const int g = 4 + (i >> 2), dt = i & 3;
-        mfma_grad(dkt[dt], tr[g % 3][dt], pf[g & 1]);
-        if (g < 6) trfrag(g + 2, dt);
-        if (g < 7) pack_share(g + 1, dt);
-        if (i == 8) publish();
-        if (i == 9) shift_tr();
-        if (i >= 10) frag((i - 10) >> 1, i & 1);
-        AB_PIN();
-      }
-      stp += step_stat;
-    }
+    const CausalWalk walk = {jw, jk, seq, (seq - q0) % AB_KT != 0 ? nt - 1 : nt};
+    dkv_pinned(walk, issue, sm, fa, kf, vf, dkt, dvt, qbase, obase, srow, T, qstride, ostride, vq, vo, ldsQ, ldsS, wave, lane, kg, q0, nt, f0, f1, gi, ti, tc, scale_log2);
   } else {
     issue(0);
     if (f0 + 1 < f1) issue(1);

@@ -395,12 +395,21 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
 }
 
 // ================================================================================ backward: dK, dV
-// As attn_bwd_dkv_block in phases: a block owns 128 keys of a key/value head and walks the query tiles of the group's heads, one head after the other.  Unit id of key/value head hk.
+// The walk of dkv_pinned.
+struct DocsWalk {
+  DocsSeen see;
+  int jk, live0, live1;  // whole tiles begin at live0 .. live1, from the first tile's row on
+  __device__ __forceinline__ bool idle(int qb) const { return qb >= see.any1 || qb + AB_KT <= see.any0; }
+  __device__ __forceinline__ bool partial(int qb) const { return qb < see.all0 || qb + AB_KT > see.all1; }
+  __device__ __forceinline__ uint32_t rows() const { return (uint32_t)see.n; }
+  __device__ __forceinline__ bool ragged(int ti) const { return ti * AB_KT < live0 || ti * AB_KT > live1; }
+};
+// As attn_bwd_dkv_block, at D = 128 without a cap with its pinned loop, otherwise in phases: a block owns 128 keys of a key/value head and walks the query tiles of the group's heads, one head after the other.  Unit id of key/value head hk.
 template <int D, bool CAP>
 __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int hk, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
                                                const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   using TL = ATile<D>;
-  constexpr bool AGPR = D == 128;
+  constexpr bool AGPR = D == 128, PINNED = D == 128 && !CAP;
   extern __shared__ __attribute__((aligned(1024))) char smem[];  // Q ring, dO ring, lse2 ring, delta ring
   const lds_char* sm = (const lds_char*)smem;
   const DocsView& v = p.a.v;
@@ -412,27 +421,30 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int jw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, jk = jw + l32, row = min(jk, T - 1);
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
-  const char* qbase = reinterpret_cast<const char*>(qkv + (size_t)hq * D);
-  const char* obase = reinterpret_cast<const char*>(dout + (size_t)hq * D);
+  const int q0 = span.first * AB_KT;  // tiles are counted from here
+  const char* qbase = reinterpret_cast<const char*>(qkv + (size_t)q0 * ld + (size_t)hq * D);
+  const char* obase = reinterpret_cast<const char*>(dout + (size_t)q0 * ldo + (size_t)hq * D);
   float* lse_s = reinterpret_cast<float*>(smem + 2 * AB_RING * TL::BYTES);
   float* del_s = lse_s + AB_RING * AB_KT;
   uint32_t vq[TL::IPW], vo[TL::IPW];
   tile_voff<D>(vq, ld, wave, lane, AB_KT);
   tile_voff<D>(vo, ldo, wave, lane, AB_KT);
+#pragma unroll
+  for (int j = 0; j < TL::IPW; j++) { vq[j] -= j * 1024; vo[j] -= j * 1024; }  // for tile_dma_at: transfer j moves rows from 512 j / D on, of at least 2 D bytes
   const uint32_t ldsQ = lds_address(smem), ldsO = ldsQ + AB_RING * TL::BYTES;
   const int nt = span.n, f0 = u.f0, f1 = u.f1;
   const size_t qstride = (size_t)AB_KT * ld * sizeof(bf16_t), ostride = (size_t)AB_KT * ldo * sizeof(bf16_t);
-  int gi = f0 / nt, ti = span.first + f0 - gi * nt;  // head of the group and tile to transfer next
-  int tc = ti;                                       // tile to work off next
+  int gi = f0 / nt, ti = f0 - gi * nt;  // head of the group and tile to transfer next
+  int tc = ti;                          // tile to work off next
   const uint32_t ldsS = ldsQ + 2 * AB_RING * TL::BYTES + (wave & 1) * AB_RING * AB_KT * sizeof(float);  // even waves transfer lse2, odd ones delta
-  const float* srow = ((wave & 1) ? delta : lse2) + (size_t)hq * T;
+  const float* srow = ((wave & 1) ? delta : lse2) + (size_t)hq * T + q0;
   auto issue = [&](int slot) {
-    const int first = max(0, live0 - ti * AB_KT), last = min(AB_KT - 1, live1 - 1 - ti * AB_KT);
+    const int first = max(0, live0 - q0 - ti * AB_KT), last = min(AB_KT - 1, live1 - 1 - q0 - ti * AB_KT);
     const char* qp = qbase + ti * qstride + gi * (D * sizeof(bf16_t));
     const char* op = obase + ti * ostride + gi * (D * sizeof(bf16_t));
     if (first == 0 && last == AB_KT - 1) {
-      tile_dma<D>(qp, vq, ldsQ + slot * TL::BYTES, wave);
-      tile_dma<D>(op, vo, ldsO + slot * TL::BYTES, wave);
+      tile_dma_at<D>(qp, vq, ldsQ + slot * TL::BYTES, wave);
+      tile_dma_at<D>(op, vo, ldsO + slot * TL::BYTES, wave);
     } else {
       uint32_t vc[TL::IPW];
       docs_voff<D>(vc, ld, wave, lane, first, last);
@@ -441,9 +453,9 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
       tile_dma<D>(op, vc, ldsO + slot * TL::BYTES, wave);
     }
     dma4_base(srow + (size_t)gi * T + (size_t)ti * AB_KT, (uint32_t)(max(first, min(lane, last)) * sizeof(float)), ldsS + slot * AB_KT * sizeof(float));
-    if (++ti == span.first + nt) { ti = span.first; gi++; }
+    if (++ti == nt) { ti = 0; gi++; }
   };
-  issue(0);  // the first tile, the key's table entries and its fragments are on their way together
+  if constexpr (!PINNED) issue(0);  // the first tile, the key's table entries and its fragments are on their way together
   const int lo = v.lo[row], end = v.hi[row], pre = v.pre[row];
   bf16x8 kf[D / 16], vf[D / 16];
   load_row_frags<D>(kf, kcol + (size_t)row * ld, jk < T, kg);
@@ -458,65 +470,70 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   const bool live = jk < T && end > lo;
   const int from = jk < pre ? lo : jk;
   const DocsSeen see = docs_seen(live, from, end);
-  if (f0 + 1 < f1) issue(1);
-  int slot = 0;
-  for (int f = f0; f < f1; f++, slot = slot == AB_RING - 1 ? 0 : slot + 1) {
-    if (f + 1 < f1) dma_wait<2 * TL::IPW + 1>(); else dma_wait<0>();
-    __syncthreads();
-    if (f + 2 < f1) issue(slot == 0 ? AB_RING - 1 : slot - 1);
-    const int qb = tc * AB_KT;
-    if (++tc == span.first + nt) tc = span.first;
-    if (qb >= see.any1 || qb + AB_KT <= see.any0) continue;  // no query of the tile sees any key of this wave
-    TilePtrs<D> Qp, Op;
-    Qp.set(sm + slot * TL::BYTES, fa);
-    Op.set(sm + (AB_RING + slot) * TL::BYTES, fa);
-    const float* ls = lse_s + slot * AB_KT;
-    const float* ds = del_s + slot * AB_KT;
-    f32x4 lv[8];  // rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
+  if constexpr (PINNED) {
+    const DocsWalk walk = {see, see.at, live0 - q0, live1 - q0 - AB_KT};
+    dkv_pinned(walk, issue, sm, fa, kf, vf, dkt, dvt, qbase, obase, srow, T, qstride, ostride, vq, vo, ldsQ, ldsS, wave, lane, kg, q0, nt, f0, f1, gi, ti, tc, p.exp_scale);
+  } else {
+    if (f0 + 1 < f1) issue(1);
+    int slot = 0;
+    for (int f = f0; f < f1; f++, slot = slot == AB_RING - 1 ? 0 : slot + 1) {
+      if (f + 1 < f1) dma_wait<2 * TL::IPW + 1>(); else dma_wait<0>();
+      __syncthreads();
+      if (f + 2 < f1) issue(slot == 0 ? AB_RING - 1 : slot - 1);
+      const int qb = q0 + tc * AB_KT;
+      if (++tc == nt) tc = 0;
+      if (qb >= see.any1 || qb + AB_KT <= see.any0) continue;  // no query of the tile sees any key of this wave
+      TilePtrs<D> Qp, Op;
+      Qp.set(sm + slot * TL::BYTES, fa);
+      Op.set(sm + (AB_RING + slot) * TL::BYTES, fa);
+      const float* ls = lse_s + slot * AB_KT;
+      const float* ds = del_s + slot * AB_KT;
+      f32x4 lv[8];  // rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
 #pragma unroll
-    for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ls + 8 * x + 4 * kg);
-    f32x16 st[2], dp[2], slope[CAP ? 2 : 1];
-    // P from S beside the dP products
-    score_tiles2<D, AB_RING * TL::BYTES, 3>(st, Qp, kf, dp, vf, [&](int j) {
-      constexpr int N = 8 / (D / 16) > 0 ? 8 / (D / 16) : 1;
+      for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ls + 8 * x + 4 * kg);
+      f32x16 st[2], dp[2], slope[CAP ? 2 : 1];
+      // P from S beside the dP products
+      score_tiles2<D, AB_RING * TL::BYTES, 3>(st, Qp, kf, dp, vf, [&](int j) {
+        constexpr int N = 8 / (D / 16) > 0 ? 8 / (D / 16) : 1;
 #pragma unroll
-      for (int i = 0; i < N; i++) {
-        const int x = j * N + i, mt = x >> 2, q4 = x & 3;
+        for (int i = 0; i < N; i++) {
+          const int x = j * N + i, mt = x >> 2, q4 = x & 3;
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const float s = st[mt][4 * q4 + e];
-          if constexpr (CAP) {
-            const float r = docs_cap_r(s, p.exp_scale);
-            st[mt][4 * q4 + e] = fast_exp2(fmaf(-2.f * p.cap_log2, r, lv[x][e]));
-            slope[mt][4 * q4 + e] = fmaf(-r, r, r);
-          } else {
-            st[mt][4 * q4 + e] = fast_exp2(fmaf(s, p.exp_scale, -lv[x][e]));
+          for (int e = 0; e < 4; e++) {
+            const float s = st[mt][4 * q4 + e];
+            if constexpr (CAP) {
+              const float r = docs_cap_r(s, p.exp_scale);
+              st[mt][4 * q4 + e] = fast_exp2(fmaf(-2.f * p.cap_log2, r, lv[x][e]));
+              slope[mt][4 * q4 + e] = fmaf(-r, r, r);
+            } else {
+              st[mt][4 * q4 + e] = fast_exp2(fmaf(s, p.exp_scale, -lv[x][e]));
+            }
           }
         }
+      });
+      TrFrags<D> fr;
+      tr_fetch<D>(fr, Op, 0);
+#pragma unroll
+      for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ds + 8 * x + 4 * kg);
+      if (qb < see.all0 || qb + AB_KT > see.all1) {
+        const int first = qb + 4 * kg - see.at;
+#pragma unroll
+        for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) {
+            st[mt][r] = (uint32_t)(first + mt * 32 + 8 * (r >> 2) + (r & 3)) < (uint32_t)see.n ? st[mt][r] : 0.f;
+            if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+          }
       }
-    });
-    TrFrags<D> fr;
-    tr_fetch<D>(fr, Op, 0);
+      acc_tile_tr<D, true, AGPR>(dvt, fr, Op, st, Qp, [&](int g) {
 #pragma unroll
-    for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ds + 8 * x + 4 * kg);
-    if (qb < see.all0 || qb + AB_KT > see.all1) {
-      const int first = qb + 4 * kg - see.at;
-#pragma unroll
-      for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-          st[mt][r] = (uint32_t)(first + mt * 32 + 8 * (r >> 2) + (r & 3)) < (uint32_t)see.n ? st[mt][r] : 0.f;
-          if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+        for (int r = 8 * (g & 1); r < 8 * (g & 1) + 8; r++) {
+          st[g >> 1][r] *= dp[g >> 1][r] - lv[4 * (g >> 1) + (r >> 2)][r & 3];
+          if constexpr (CAP) st[g >> 1][r] *= slope[g >> 1][r];
         }
+      });
+      acc_tile_tr<D, false, AGPR>(dkt, fr, Qp, st, Qp, [](int) {});
     }
-    acc_tile_tr<D, true, AGPR>(dvt, fr, Op, st, Qp, [&](int g) {
-#pragma unroll
-      for (int r = 8 * (g & 1); r < 8 * (g & 1) + 8; r++) {
-        st[g >> 1][r] *= dp[g >> 1][r] - lv[4 * (g >> 1) + (r >> 2)][r & 3];
-        if constexpr (CAP) st[g >> 1][r] *= slope[g >> 1][r];
-      }
-    });
-    acc_tile_tr<D, false, AGPR>(dkt, fr, Qp, st, Qp, [](int) {});
   }
   acc_settle<AGPR>(dkt);
   acc_settle<AGPR>(dvt);
