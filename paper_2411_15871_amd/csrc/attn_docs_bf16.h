@@ -67,8 +67,8 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = p.a.nq, nkv = p.a.nkv, h = blockIdx.x % nq, id = blockIdx.x / nq, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
-  const DocsUnit u = v.units_q[id];  // fetched beside the head
-  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
+  const DocsUnit u = v.q.units[id];  // fetched beside the head
+  if (!docs_fits(v, nq, nkv) || id >= v.head[v.q.counts]) return;
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int iw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, iq = iw + l32, row = min(iq, T - 1);
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
@@ -219,8 +219,8 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
                                                                 float* __restrict__ lse) {
   const DocsView& v = p.a.v;
   const int nq = p.a.nq, k = blockIdx.x >> 3, h = blockIdx.y;
-  const DocsSplit s = v.split_q[k];
-  if (!docs_fits(v, nq, p.a.nkv) || k >= v.head[DOCS_SPLIT_Q]) return;
+  const DocsSplit s = v.q.splits[k];
+  if (!docs_fits(v, nq, p.a.nkv) || k >= v.head[v.q.counts + 1]) return;
   const int r = (blockIdx.x & 7) * 16 + (threadIdx.x >> 4), i = s.block * DOCS_BLOCK + r;
   if (i >= v.T || v.hi[i] <= v.lo[i]) return;
   constexpr int CPT = D / 16;
@@ -267,8 +267,8 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = p.a.nq, nkv = p.a.nkv, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, T = v.T;
-  const DocsUnit u = v.units_q[id];  // fetched beside the head
-  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_Q]) return;
+  const DocsUnit u = v.q.units[id];  // fetched beside the head
+  if (!docs_fits(v, nq, nkv) || id >= v.head[v.q.counts]) return;
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int iw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, iq = iw + l32, row = min(iq, T - 1);
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
@@ -415,9 +415,9 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   const DocsView& v = p.a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = p.a.nq, nkv = p.a.nkv, grp = nq / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, T = v.T;
-  const DocsUnit u = v.units_k[id];  // fetched beside the head
-  const DocsSpan span = v.span_k[id];
-  if (!docs_fits(v, nq, nkv) || id >= v.head[DOCS_UNITS_K]) return;
+  const DocsUnit u = v.k.units[id];  // fetched beside the head
+  const DocsSpan span = v.k.spans[id];
+  if (!docs_fits(v, nq, nkv) || id >= v.head[v.k.counts]) return;
   const int live0 = v.head[DOCS_LIVE0], live1 = v.head[DOCS_LIVE1];
   const int jw = (u.block2 >> 1) * DOCS_BLOCK + wave * 32, jk = jw + l32, row = min(jk, T - 1);
   const bf16_t* kcol = qkv + (size_t)(nq + hk) * D;
@@ -627,7 +627,7 @@ template <int D, bool CAP>
 __global__ __launch_bounds__(AB_THREADS) void attn_docs_bwd_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
                                                                         const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
                                                                         float* __restrict__ part_q, float* __restrict__ part_kv) {
-  const unsigned n_k = (unsigned)p.a.v.k.units * p.a.nkv;
+  const unsigned n_k = (unsigned)p.a.v.k.cap.units * p.a.nkv;
   if (blockIdx.x < n_k) docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse, lse2, delta, dqkv, part_kv);
   else docs_dq_block<D, CAP, false>(p, (blockIdx.x - n_k) / p.a.nq, (blockIdx.x - n_k) % p.a.nq, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
 }
@@ -644,8 +644,9 @@ __global__ __launch_bounds__(256) void attn_docs_reduce_kernel(const DocsTiled p
   if (!q) id -= nb_q;
   const unsigned gx = q ? gqx : gkx, x = id % gx;
   const int h = id / gx, k = q ? x >> 4 : x >> 5, r0 = q ? (x & 15) * 8 : (x & 31) * 4, width = q ? D : 2 * D, heads = q ? nq : nkv;
-  const DocsSplit s = q ? v.split_q[k] : v.split_k[k];
-  if (!docs_fits(v, nq, nkv) || k >= v.head[q ? DOCS_SPLIT_Q : DOCS_SPLIT_K]) return;
+  const DocsList& list = q ? v.q : v.k;
+  const DocsSplit s = list.splits[k];
+  if (!docs_fits(v, nq, nkv) || k >= v.head[list.counts + 1]) return;
   const float* part = q ? part_q : part_kv;
   const size_t unit = ((size_t)s.slot * heads + h) * DOCS_BLOCK, step = (size_t)heads * DOCS_BLOCK * width;
   const int e = threadIdx.x, row = r0 + e / (width / 4), c4 = (e % (width / 4)) * 4, i = s.block * DOCS_BLOCK + row;
@@ -667,7 +668,7 @@ static DocsTiled docs_tiled(const DocsAttn& a) {
 }
 
 size_t dh_attn_docs_fwd_bf16_ws_bytes(int T, int nq, int nkv, int d) {
-  return (size_t)docs_view_at(nullptr, T, nq, nkv).q.slots * nq * DOCS_BLOCK * ((size_t)d + 2) * sizeof(float);
+  return (size_t)docs_view(nullptr, T, nq, nkv, d).q.cap.slots * nq * DOCS_BLOCK * ((size_t)d + 2) * sizeof(float);
 }
 
 template <int D, bool CAP>
@@ -679,7 +680,7 @@ static int docs_fwd(const DocsTiled& p, const bf16_t* qkv, bf16_t* o, float* lse
     if (int rc = set_lds(attn_docs_fwd_bf16_kernel<D, CAP>, lds)) return rc;
     set = true;
   }
-  const DocsCaps& q = p.a.v.q;
+  const DocsCaps& q = p.a.v.q.cap;
   float* part_ml = ws + (size_t)q.slots * p.a.nq * DOCS_BLOCK * D;
   attn_docs_fwd_bf16_kernel<D, CAP><<<(unsigned)q.units * p.a.nq, AB_THREADS, lds, stream>>>(p, qkv, o, lse, ws, part_ml);
   DH_LAUNCH_CHECK();
@@ -700,12 +701,12 @@ static DocsBwdLayout docs_bwd_layout(const DocsView& v, int nq, int nkv, int d) 
   DocsBwdLayout l;
   size_t at = 0;
   l.lse2 = at; at += dh_align_up((size_t)nq * v.T * sizeof(float), 256);
-  l.dkv = at; at += (size_t)v.k.slots * nkv * DOCS_BLOCK * 2 * d * sizeof(float);
-  l.dq = at; at += (size_t)v.q.slots * nq * DOCS_BLOCK * d * sizeof(float);
+  l.dkv = at; at += (size_t)v.k.cap.slots * nkv * DOCS_BLOCK * 2 * d * sizeof(float);
+  l.dq = at; at += (size_t)v.q.cap.slots * nq * DOCS_BLOCK * d * sizeof(float);
   l.total = at;
   return l;
 }
-size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view_at(nullptr, T, nq, nkv), nq, nkv, d).total; }
+size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view(nullptr, T, nq, nkv, d), nq, nkv, d).total; }
 
 template <int D, bool CAP>
 static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, char* ws, hipStream_t stream) {
@@ -719,7 +720,7 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
     set = true;
   }
   const int nq = p.a.nq, nkv = p.a.nkv;
-  const DocsCaps &q = p.a.v.q, &k = p.a.v.k;
+  const DocsCaps &q = p.a.v.q.cap, &k = p.a.v.k.cap;
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
   if (docs_one_launch(p.a.v.T, nq, nkv)) {

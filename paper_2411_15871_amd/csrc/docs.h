@@ -5,13 +5,15 @@
 // The table: a head of DOCS_HEAD ints, then three ints a row (arrays lo, hi, pre of T): the row's document is rows lo .. hi-1 and its prefix ends before row
 // `pre`.  Rows of no document have lo = hi = pre = their own index.  So row r sees keys lo[r] .. max(r + 1, pre[r]) - 1, and key j is seen by
 // rows (j < pre[j] ? lo[j] : j) .. hi[j] - 1.  All four borders ascend with the row.
-// Behind them the work of the tiled kernels, one list for blocks of 128 queries and one for blocks of 128 keys: units of a block and a run of the 64-row tiles it
+// Behind them the work of the tiled kernels, lists for blocks of 128 queries and for blocks of 128 keys: units of a block and a run of the 64-row tiles it
 // meets, longest first.  A block with more tiles than the list's chunk length is cut into units of even length, whose partial results get a slot of workspace each;
-// a second list names these blocks.  Lengths follow from the documents, on the device; room for them follows from T and the heads alone.
+// a second list names these blocks.  Lengths follow from the documents, on the device; room for them follows from T and the heads alone.  Either kind of list is made twice, for
+// heads of 128 and of 64, since that many blocks more of the shorter heads are resident at once.
 #define DOCS_MAX_T (1 << 28)  // tiles of a block, times the heads of a group, are counted in 32 bits
 #define DOCS_MAX_HEADS 1024
 #define DOCS_HEAD 16
-enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_UNITS_Q, DOCS_SPLIT_Q, DOCS_UNITS_K, DOCS_SPLIT_K };  // head: the rows of documents are [live0, live1)
+enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_COUNTS };  // head: the rows of documents are [live0, live1); from DOCS_COUNTS on, each list's units and cut blocks
+enum { DOCS_Q128, DOCS_Q64, DOCS_K128, DOCS_K64, DOCS_LISTS };
 #define DOCS_BLOCK 128
 #define DOCS_TILE 64
 // A chunk holds so many tiles that all heads' tiles together make at most DOCS_TARGET chunks (room for partial results follows from that), and DOCS_CHUNK at least.
@@ -46,36 +48,48 @@ static inline DocsCaps docs_caps(int T, int heads, int grp, int target, int chun
 struct DocsUnit { int block2, f0, f1, slot; };       // block * 2 + (1: its first unit); its run of tiles [f0, f1); slot of its partial result or -1
 struct DocsSpan { int first, n, pad0, pad1; };       // of a key block: its query tiles (first, count); f0 and f1 count through the heads of the group
 struct DocsSplit { int block, slot, n, pad; };       // a block that is cut: slots of its n units
-struct DocsView {
-  int T;
-  const int32_t *head, *lo, *hi, *pre;
-  const DocsUnit *units_q, *units_k;
-  const DocsSpan* span_k;
-  const DocsSplit *split_q, *split_k;
-  DocsCaps q, k;
+struct DocsList {
+  DocsUnit* units;
+  DocsSpan* spans;    // lists of keys: of each unit
+  DocsSplit* splits;
+  DocsCaps cap;
+  int counts;         // head[counts]: units; head[counts + 1]: splits
+};
+struct DocsTable {
+  int32_t *head, *lo, *hi, *pre;
+  DocsList list[DOCS_LISTS];
   size_t bytes;
 };
-static inline DocsView docs_view_at(const void* table, int T, int nq, int nkv) {
-  DocsView v;
-  v.T = T;
-  v.q = docs_caps(T, nq, 1, DOCS_TARGET_Q, docs_least(T, 1, DOCS_CHUNK_Q, DOCS_WHOLE_Q));
-  v.k = docs_caps(T, nkv, nq / nkv, DOCS_TARGET_K, docs_least(T, nq / nkv, DOCS_CHUNK_K, DOCS_WHOLE_K));
-  const char* p = (const char*)table;
+static inline DocsTable docs_table(void* table, int T, int nq, int nkv) {
+  DocsTable v;
   size_t at = 0;
-  auto take = [&](size_t bytes) { const char* r = p + at; at = dh_align_up(at + bytes, 16); return r; };
-  v.head = (const int32_t*)take(DOCS_HEAD * sizeof(int32_t));
-  v.lo = (const int32_t*)take((size_t)T * sizeof(int32_t));
-  v.hi = (const int32_t*)take((size_t)T * sizeof(int32_t));
-  v.pre = (const int32_t*)take((size_t)T * sizeof(int32_t));
-  v.units_q = (const DocsUnit*)take((size_t)v.q.units * sizeof(DocsUnit));
-  v.units_k = (const DocsUnit*)take((size_t)v.k.units * sizeof(DocsUnit));
-  v.span_k = (const DocsSpan*)take((size_t)v.k.units * sizeof(DocsSpan));
-  v.split_q = (const DocsSplit*)take((size_t)v.q.splits * sizeof(DocsSplit));
-  v.split_k = (const DocsSplit*)take((size_t)v.k.splits * sizeof(DocsSplit));
+  auto take = [&](size_t bytes) { char* r = (char*)table + at; at = dh_align_up(at + bytes, 16); return r; };
+  v.head = (int32_t*)take(DOCS_HEAD * sizeof(int32_t));
+  v.lo = (int32_t*)take((size_t)T * sizeof(int32_t));
+  v.hi = (int32_t*)take((size_t)T * sizeof(int32_t));
+  v.pre = (int32_t*)take((size_t)T * sizeof(int32_t));
+  for (int i = 0; i < DOCS_LISTS; i++) {
+    const bool keys = i >= DOCS_K128;
+    DocsList& l = v.list[i];
+    l.cap = keys ? docs_caps(T, nkv, nq / nkv, DOCS_TARGET_K, docs_least(T, nq / nkv, DOCS_CHUNK_K, DOCS_WHOLE_K)) : docs_caps(T, nq, 1, DOCS_TARGET_Q, docs_least(T, 1, DOCS_CHUNK_Q, DOCS_WHOLE_Q));
+    l.units = (DocsUnit*)take((size_t)l.cap.units * sizeof(DocsUnit));
+    l.spans = keys ? (DocsSpan*)take((size_t)l.cap.units * sizeof(DocsSpan)) : nullptr;
+    l.splits = (DocsSplit*)take((size_t)l.cap.splits * sizeof(DocsSplit));
+    l.counts = DOCS_COUNTS + 2 * i;
+  }
   v.bytes = at;
   return v;
 }
-static inline DocsView docs_view(const dh_docs* docs) { return docs_view_at(docs->table, docs->T, docs->nq, docs->nkv); }
+// What the kernels of one head width read.
+struct DocsView {
+  int T;
+  const int32_t *head, *lo, *hi, *pre;
+  DocsList q, k;
+};
+static inline DocsView docs_view(const void* table, int T, int nq, int nkv, int d) {
+  const DocsTable t = docs_table(const_cast<void*>(table), T, nq, nkv);
+  return {T, t.head, t.lo, t.hi, t.pre, t.list[d == 64 ? DOCS_Q64 : DOCS_Q128], t.list[d == 64 ? DOCS_K64 : DOCS_K128]};
+}
 // Whether the table was made for these sizes: a kernel that finds others does nothing.
 __device__ __forceinline__ bool docs_fits(const DocsView& v, int nq, int nkv) { return v.head[DOCS_T] == v.T && v.head[DOCS_NQ] == nq && v.head[DOCS_NKV] == nkv; }
 

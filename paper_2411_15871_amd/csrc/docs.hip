@@ -18,16 +18,13 @@ __device__ __forceinline__ int starts_upto(const int32_t* start, int n, int r) {
   return lo + __popcll(__ballot(lo + lane < hi && start[min(lo + lane, n - 1)] <= r));
 }
 
-// The work lists, by one block: thread b looks at block b (b + 256 ...) of 128 rows.  keys: the list of key blocks.
+// The work lists, a block each: thread b looks at block b (b + 256 ...) of 128 rows.  keys: a list of key blocks.
 #define DOCS_STARTS 4096
 struct DocsPlanArgs {
   int T, n_docs, nq, nkv;
   const int32_t *start, *prefix;
-  int32_t *head, *lo, *hi, *pre, *pos;
-  DocsUnit *units_q, *units_k;
-  DocsSpan* span_k;
-  DocsSplit *split_q, *split_k;
-  DocsCaps q, k;
+  int32_t* pos;
+  DocsTable t;
 };
 // The document of row r: its rows [s, e) and the end of its prefix; false: none.  start: a.start, or its copy in LDS.
 template <class Start>
@@ -61,10 +58,10 @@ __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* st
 // result is written and read back (beyond 512 of them from memory), and the merge takes a while longer if there is any.  tiles[b]: of the first DOCS_BLOCKS blocks; longer
 // rows are cut at `shortest`.
 #define DOCS_BLOCKS 1024
-__device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, bool keys, int blocks, int shortest, int longest, float all, const int* tiles) {
+__device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, int list, int blocks, int shortest, int longest, float all, const int* tiles) {
   __shared__ int units[4][64], cuts[4][64], tops[4][64];
   if (blocks > DOCS_BLOCKS || shortest >= longest || all <= 144.f) return shortest;  // (so few tiles: any cut fits)
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = keys ? a.nkv : a.nq;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = list >= DOCS_K128 ? a.nkv : a.nq;
   const int ch = max(shortest, (int)ceilf((float)longest * exp2f(-(float)lane / 63.f * log2f((float)longest / (float)shortest)) - 1e-3f));
   const float inv = 1.f / (float)ch;
   int n = 0, cut = 0, top = 0;
@@ -80,7 +77,8 @@ __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, bool keys, int 
   __syncthreads();
   const float N = (float)(units[0][lane] + units[1][lane] + units[2][lane] + units[3][lane]) * heads, C = (float)(cuts[0][lane] + cuts[1][lane] + cuts[2][lane] + cuts[3][lane]) * heads;
   const float L = (float)max(max(tops[0][lane], tops[1][lane]), max(tops[2][lane], tops[3][lane]));
-  const float slots = !keys ? 512.f : docs_one_launch(a.T, a.nq, a.nkv) ? 144.f : 256.f;  // (in one launch the rest of the units has queries)
+  const bool keys = list >= DOCS_K128, one = docs_one_launch(a.T, a.nq, a.nkv);  // (in one launch the rest of the chip has queries)
+  const float slots = !keys ? 512.f : list == DOCS_K64 ? (one ? 240.f : 400.f) : one ? 144.f : 256.f;
   const float together = fmaxf(L, (all + 1.5f * N) / slots + 0.25f * L);
   const float time = (N > slots ? together : keys ? L : L * (0.8f + 0.2f / 256.f * fmaxf(N - 256.f, 0.f))) + (C > 0.f ? 1.5f + 0.004f * C + 0.008f * fmaxf(C - 512.f, 0.f) : 0.f);
   float best = time;
@@ -90,24 +88,26 @@ __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, bool keys, int 
   return __builtin_amdgcn_readlane(ch, who ? __builtin_ctzll(who) : 63);
 }
 
-__device__ __forceinline__ void docs_head(const DocsPlanArgs& a, bool keys, int live0, int live1, int units, int splits) {
-  a.head[keys ? DOCS_UNITS_K : DOCS_UNITS_Q] = units;
-  a.head[keys ? DOCS_SPLIT_K : DOCS_SPLIT_Q] = splits;
-  if (keys) return;
-  a.head[DOCS_LIVE0] = live0;
-  a.head[DOCS_LIVE1] = live1;
-  a.head[DOCS_T] = a.T;
-  a.head[DOCS_NQ] = a.nq;
-  a.head[DOCS_NKV] = a.nkv;
+__device__ __forceinline__ void docs_head(const DocsPlanArgs& a, int list, int live0, int live1, int units, int splits) {
+  a.t.head[a.t.list[list].counts] = units;
+  a.t.head[a.t.list[list].counts + 1] = splits;
+  if (list != 0) return;
+  a.t.head[DOCS_LIVE0] = live0;
+  a.t.head[DOCS_LIVE1] = live1;
+  a.t.head[DOCS_T] = a.T;
+  a.t.head[DOCS_NQ] = a.nq;
+  a.t.head[DOCS_NKV] = a.nkv;
 }
 template <class Start>
-__device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* start, bool keys) {
+__device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* start, int list) {
   __shared__ unsigned long long wave_all[4], wave_cut[4];
   __shared__ int wave_top[4], hist[64], from[64], tiles[DOCS_BLOCKS], all_units;
+  const bool keys = list >= DOCS_K128;
   const int tid = threadIdx.x, grp = keys ? a.nq / a.nkv : 1, heads = keys ? a.nkv : a.nq;
-  const DocsCaps cap = keys ? a.k : a.q;
-  DocsUnit* units = keys ? a.units_k : a.units_q;
-  DocsSplit* splits = keys ? a.split_k : a.split_q;
+  const DocsCaps cap = a.t.list[list].cap;
+  DocsUnit* units = a.t.list[list].units;
+  DocsSpan* spans = a.t.list[list].spans;
+  DocsSplit* splits = a.t.list[list].splits;
   int live0 = 0, live1 = 0;
   if (a.n_docs > 0) {
     live0 = min(max(start[0], 0), a.T);
@@ -129,9 +129,9 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
       const int at = __popcll(have & ((1ull << tid) - 1));
       if (tiles0 > 0) {
         units[at] = {tid * 2 + 1, keys ? 0 : first0, (keys ? 0 : first0) + tiles0, -1};
-        if (keys) a.span_k[at] = {first0, tiles0 / grp, 0, 0};
+        if (keys) spans[at] = {first0, tiles0 / grp, 0, 0};
       }
-      if (tid == 0) docs_head(a, keys, live0, live1, __popcll(have), 0);
+      if (tid == 0) docs_head(a, list, live0, live1, __popcll(have), 0);
     }
     return;
   }
@@ -148,7 +148,7 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
   const int target = keys ? DOCS_TARGET_K : DOCS_TARGET_Q, least = keys ? docs_least(a.T, grp, DOCS_CHUNK_K, DOCS_WHOLE_K) : docs_least(a.T, 1, DOCS_CHUNK_Q, DOCS_WHOLE_Q);
   const double want = floor((double)all * heads / target) + 1.0;
   const int shortest = (int)fmin(fmax(want, (double)least), (double)longest);
-  const int ch = docs_chunk(a, keys, cap.blocks, shortest, longest, (float)all * heads, tiles);
+  const int ch = docs_chunk(a, list, cap.blocks, shortest, longest, (float)all * heads, tiles);
   const float steps = 63.f / (float)ch;
   // Units longest first, counted by length in 64 steps, then placed.  A block of t tiles makes n = ceil(t / ch) units, t % n of them a tile longer than the others.
   auto bucket = [&](int len) { return min(max(63 - (int)((float)len * steps), 0), 63); };
@@ -199,32 +199,32 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
       const int at = (u < more ? at0 : at1) + u, end = f + len + (u < more ? 1 : 0);
       if (at < cap.units) {
         units[at] = {b * 2 + (u == 0 ? 1 : 0), f, end, slot < 0 ? -1 : slot + u};
-        if (keys) a.span_k[at] = span;
+        if (keys) spans[at] = span;
       }
       f = end;
     }
   }
-  if (tid == 0) docs_head(a, keys, live0, live1, all_units, min((int)(cut >> 32), cap.splits));
+  if (tid == 0) docs_head(a, list, live0, live1, all_units, min((int)(cut >> 32), cap.splits));
 }
 
-// Blocks 0 and 1 make the two work lists; in the others a wave takes 64 rows: the document of its first row, then, 64 starts at a time, how many more begin at or
+// The first blocks make the work lists; in the others a wave takes 64 rows: the document of its first row, then, 64 starts at a time, how many more begin at or
 // before each lane's row.
 __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
-  if (blockIdx.x < 2) {  // a chain of searches, in LDS where the starts fit (17 documents, 4096 rows: 13 us from memory)
+  if (blockIdx.x < DOCS_LISTS) {  // a chain of searches, in LDS where the starts fit (17 documents, 4096 rows: 13 us from memory)
     __shared__ int copy[DOCS_STARTS];
-    const bool keys = blockIdx.x == 1;
+    const int list = blockIdx.x;
     if (a.n_docs >= DOCS_STARTS) {
-      docs_lists(a, a.start, keys);
+      docs_lists(a, a.start, list);
     } else {
       for (int i = threadIdx.x; i < (a.n_docs > 0 ? a.n_docs + 1 : 0); i += 256) copy[i] = a.start[i];
       __syncthreads();
-      docs_lists(a, (const __attribute__((address_space(3))) int*)copy, keys);
+      docs_lists(a, (const __attribute__((address_space(3))) int*)copy, list);
     }
     return;
   }
   const int T = a.T, n_docs = a.n_docs;
   const int32_t* start = a.start;
-  const int lane = threadIdx.x & 63, r0 = ((blockIdx.x - 2) * 4 + (threadIdx.x >> 6)) * 64, r = r0 + lane;
+  const int lane = threadIdx.x & 63, r0 = ((blockIdx.x - DOCS_LISTS) * 4 + (threadIdx.x >> 6)) * 64, r = r0 + lane;
   if (r0 >= T) return;
   int n = 0;  // starts at or before the lane's row
   if (n_docs > 0) {
@@ -248,9 +248,9 @@ __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
       pre = a.prefix ? s + min(max(a.prefix[n - 1], 0), e - s) : s;
     }
   }
-  a.lo[r] = lo;
-  a.hi[r] = hi;
-  a.pre[r] = pre;
+  a.t.lo[r] = lo;
+  a.t.hi[r] = hi;
+  a.t.pre[r] = pre;
   if (a.pos) a.pos[r] = r - lo;
 }
 
@@ -266,16 +266,14 @@ static int check_docs(const char* who, const dh_docs* docs) {
 
 extern "C" size_t dh_docs_table_bytes(int T, int nq, int nkv) {
   if (T <= 0 || nq <= 0 || nkv <= 0) return 0;
-  return docs_view_at(nullptr, T, nq, nkv).bytes;
+  return docs_table(nullptr, T, nq, nkv).bytes;
 }
 
 extern "C" int dh_docs_plan(const dh_docs* docs, void* stream) {
   if (int rc = check_docs("docs_plan", docs)) return rc;
   if (docs->T == 0) return DH_OK;
-  const DocsView v = docs_view(docs);
-  const DocsPlanArgs a = {docs->T, docs->n_docs, docs->nq, docs->nkv, docs->doc_start, docs->prefix, (int32_t*)v.head, (int32_t*)v.lo, (int32_t*)v.hi, (int32_t*)v.pre, docs->pos,
-                          (DocsUnit*)v.units_q, (DocsUnit*)v.units_k, (DocsSpan*)v.span_k, (DocsSplit*)v.split_q, (DocsSplit*)v.split_k, v.q, v.k};
-  docs_plan_kernel<<<2 + (unsigned)(((size_t)docs->T + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
+  const DocsPlanArgs a = {docs->T, docs->n_docs, docs->nq, docs->nkv, docs->doc_start, docs->prefix, docs->pos, docs_table(docs->table, docs->T, docs->nq, docs->nkv)};
+  docs_plan_kernel<<<DOCS_LISTS + (unsigned)(((size_t)docs->T + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
@@ -290,7 +288,7 @@ static int check_attn_docs(const char* who, int dtype, const dh_docs* docs, int 
   return DH_OK;
 }
 static bool unaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
-static DocsAttn attn_of(const dh_docs* docs, int d, float cap) { return {docs_view(docs), docs->nq, docs->nkv, d, (float)(1.0 / sqrt((double)d)), cap}; }
+static DocsAttn attn_of(const dh_docs* docs, int d, float cap) { return {docs_view(docs->table, docs->T, docs->nq, docs->nkv, d), docs->nq, docs->nkv, d, (float)(1.0 / sqrt((double)d)), cap}; }
 
 static bool sized(int dtype, int T, int nq, int nkv, int d) {
   return dtype == DH_BF16 && T > 0 && T <= DOCS_MAX_T && nkv > 0 && nq > 0 && nq <= DOCS_MAX_HEADS && nq % nkv == 0 && (d == 64 || d == 128);
