@@ -665,10 +665,10 @@ size_t dh_docs_table_bytes(int T, int nq, int nkv);
 int dh_docs_plan(const dh_docs* docs, void* stream);
 
 /* Grouped-query attention inside documents.  Layouts as dh_attn_fwd / dh_attn_bwd: qkv[T,(nq+2nkv)d] (already rotated), o[T,nq*d], lse[nq,T],
- * delta[nq,T]; docs as dh_docs_plan has filled it.  cap > 0: every scaled score x counts as cap * tanh(x / cap); 0: as it is.  Rows of no document are
+ * delta[nq,T]; docs as dh_docs_plan has filled it.  cap 0.001 to 1000: every scaled score x counts as cap * tanh(x / cap); 0: as it is.  Rows of no document are
  * left as they were, in o, lse and dqkv alike, whatever they hold.  What a row does not see does not reach its results, infinities and NaNs among it.
  * d: multiple of 8 up to 256 for DH_F32, 64 or 128 for DH_BF16.  qkv, o, dout, dqkv: 16-byte aligned.  ws: device workspace of the _workspace_bytes
- * queries (fewer bytes: DH_ERR_WORKSPACE_TOO_SMALL).  Backward writes dqkv (dk, dv summed over the query heads of a group in a fixed order) and delta. */
+ * queries, 16-byte aligned (fewer bytes: DH_ERR_WORKSPACE_TOO_SMALL); T up to 2^28, nq up to 1024.  Backward writes dqkv (dk, dv summed over the query heads of a group in a fixed order) and delta. */
 int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes,
                      void* stream);
 size_t dh_attn_docs_fwd_workspace_bytes(int dtype, int T, int nq, int nkv, int d);
@@ -694,7 +694,7 @@ typedef struct {
   int dtype;  /* dh_dtype */
 } dh_tensor;
 /* norm[0] = sqrt(sum of squares over all elements of all tensors), squared and added in float64 in a fixed order, rounded once to float32.
- * ws: dh_grad_norm_ws_bytes.  dh_grad_clip: out = data * c where c = max_norm / (norm + 1e-6) in float32 is below 1 and norm is finite, otherwise out = data
+ * ws: dh_grad_norm_ws_bytes, 8-byte aligned.  dh_grad_clip: out = data * c where c = max_norm / (norm + 1e-6) in float32 is below 1 and norm is finite, otherwise out = data
  * (nothing is written where out is data); norm: device float32, as dh_grad_norm has left it.  n_tensors >= 0; max_norm > 0. */
 int dh_grad_norm(int n_tensors, const dh_tensor* tensors, float* norm, void* ws, size_t ws_bytes, void* stream);
 size_t dh_grad_norm_ws_bytes(int n_tensors, const dh_tensor* tensors);
@@ -721,7 +721,7 @@ int dh_moe_route_bwd(int T, int E, const float* dprob, const int32_t* idx, const
  * A token whose logits are all minus infinity adds nothing to prob_mean and to loss[1]; N = 0 gives zeros.  lse of tokens that do not count is left as it was.
  * Backward: dlogits[t,e] = dloss[0] E/N p (counts[e]/(2N) - sum_e' counts[e']/(2N) p[t,e']) + dloss[1] 2/N lse[t] p (counts are constants), zero
  * for tokens that do not count; accumulate != 0 adds it to dlogits, e.g. to what dh_moe_route_bwd left there.  dloss: DEVICE [2].
- * logits, prob_mean, lse, loss, dloss, dlogits float32; 2 <= E <= 256; sums in a fixed order.  ws: dh_moe_balance_ws_bytes. */
+ * logits, prob_mean, lse, loss, dloss, dlogits float32; 2 <= E <= 256; sums in a fixed order.  ws: dh_moe_balance_ws_bytes, 4-byte aligned. */
 int dh_moe_balance_fwd(int T, int E, const float* logits, const int32_t* idx, const int32_t* n_live, int32_t* counts, float* prob_mean, float* lse,
                        float* loss, void* ws, size_t ws_bytes, void* stream);
 size_t dh_moe_balance_ws_bytes(int T, int E);

@@ -6,7 +6,8 @@
 // results merged in order by a launch behind.
 //
 // Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN: a wave whose result is not finite makes the rows
-// concerned again, one at a time, over exactly what they see (docs_row_*).  Rows outside all documents are never read: transfers take the nearest row of a document.
+// concerned again, one at a time, over exactly what they see (docs_row_*).  Rows outside all documents enter no tile, transfers take the nearest row of a document instead,
+// and what a lane makes of such a row of its own goes nowhere.
 //
 // CAP: x = cap tanh(x / cap) as cap - 2 cap r with r = 1 / (1 + e^(2x/cap)), one exponential and one reciprocal more an element, whose limits (r = 0, 1) are right where the
 // exponential is infinite or zero; its slope is 4 (r - r r), off by at most 2^-22, of which the factor 4 waits for the end.  The exponent of 2 of a probability is
@@ -723,7 +724,10 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   const DocsCaps &q = p.a.v.q.cap, &k = p.a.v.k.cap;
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
-  if (docs_one_launch(p.a.v.T, nq, nkv)) {
+  // One launch: the two halves' blocks fill each other's units.  Its blocks have those of dK/dV for neighbours and its registers, so that large grids of dQ blocks, two a unit
+  // by themselves, lose more than they gain at D = 128 (32:8 x 8192, 2560 blocks, 746 and 780 us; 16:8 x 4096 capped, 768, 172 and 166); at D = 64 two
+  // fit either way (16:4 x 8192, 1280, 239 and 216; 32 heads x 8192, 4096, 978 and 983).
+  if (docs_one_launch(p.a.v.T, nq, nkv) || (D == 64 && !CAP && docs_one_launch((p.a.v.T + 3) / 4, nq, nkv))) {
     attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
     DH_LAUNCH_CHECK();
     attn_docs_bwd_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv + (unsigned)q.units * nq, AB_THREADS, lds_dkv, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q, part_kv);

@@ -27,13 +27,13 @@ enum { DOCS_Q128, DOCS_Q64, DOCS_K128, DOCS_K64, DOCS_LISTS };
 #define DOCS_ONE_LAUNCH 1024
 __host__ __device__ static inline bool docs_one_launch(int T, int nq, int nkv) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= DOCS_ONE_LAUNCH; }
 struct DocsCaps { int blocks, units, slots, splits; };
-// With chunks of c > tiles of all blocks / (target / heads): sum of ceil(t / c) <= blocks + target / heads; blocks that are cut have t > c, and their units are
-// fewer than 2 t / c.  A block has at most tiles(T) + 1 tiles of each head of its group.
 // Tiles that a chunk holds at least: where a block cannot have more than `whole` tiles none is cut, and no launch is needed to merge.
 __host__ __device__ static inline int docs_least(int T, int grp, int chunk, int whole) {
   const long long most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp;
   return most <= whole ? whole : chunk;
 }
+// With chunks of c > tiles of all blocks / (target / heads): sum of ceil(t / c) <= blocks + target / heads; blocks that are cut have t > c, and their units are
+// fewer than 2 t / c.  A block has at most tiles(T) + 1 tiles of each head of its group.
 static inline DocsCaps docs_caps(int T, int heads, int grp, int target, int chunk) {
   const long long blocks = ((long long)T + DOCS_BLOCK - 1) / DOCS_BLOCK, most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp, extra = target / heads + 1;
   const long long slots = most <= chunk ? 0 : blocks * ((most + chunk - 1) / chunk);
@@ -151,7 +151,8 @@ __device__ __forceinline__ void docs_row_fwd(const T* q, const T* k, const T* v,
     const bool on = j + lane < j1;
     float slope, y = on ? docs_capped(docs_dot(q, k + (size_t)(j + lane) * ld, d) * scale, cap, slope) : -INFINITY;
     const float mn = fmaxf(m, wave_max(y));
-    const float a = mn == -INFINITY ? 1.f : expf(m - mn), p = on ? (mn == -INFINITY ? y - mn : expf(y - mn)) : 0.f;  // all scores minus infinity: no softmax
+    const float a = mn == -INFINITY ? 1.f : expf(m - mn);
+    const float p = __builtin_bit_cast(uint32_t, y) == 0xff800000u ? 0.f : expf(y - mn);  // minus infinity by its bits: some callers are built without comparisons of NaNs
     l = l * a + wave_sum(p);
 #pragma unroll
     for (int c = 0; c < 4; c++) acc[c] *= a;

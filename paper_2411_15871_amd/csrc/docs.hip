@@ -284,7 +284,7 @@ static int check_attn_docs(const char* who, int dtype, const dh_docs* docs, int 
   if (dtype != DH_F32 && dtype != DH_BF16) DH_FAIL(DH_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (dtype == DH_F32 && (d <= 0 || d % 8 || d > 256)) DH_FAIL(DH_ERR_SHAPE, "%s: head_dim %d must be a multiple of 8, at most 256", who, d);
   if (dtype == DH_BF16 && d != 64 && d != 128) DH_FAIL(DH_ERR_SHAPE, "%s: head_dim %d must be 64 or 128", who, d);
-  if (!(cap >= 0.f) || cap > 1e30f) DH_FAIL(DH_ERR_INVALID_ARG, "%s: cap %g must be 0 (none) or positive and finite", who, (double)cap);
+  if (cap != 0.f && !(cap >= 1e-3f && cap <= 1e3f)) DH_FAIL(DH_ERR_INVALID_ARG, "%s: cap %g must be 0 (none) or 0.001 to 1000", who, (double)cap);  // (bf16: off by 2^-22 cap)
   return DH_OK;
 }
 static bool unaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }

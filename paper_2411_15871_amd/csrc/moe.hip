@@ -512,6 +512,7 @@ extern "C" int dh_moe_balance_fwd(int T, int E, const float* logits, const int32
   if (!counts || !prob_mean || !loss || (T > 0 && (!logits || !idx || !lse))) DH_FAIL(DH_ERR_INVALID_ARG, "moe_balance_fwd: null pointer");
   const size_t need = dh_moe_balance_ws_bytes(T, E);
   if (!ws || ws_bytes < need) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "moe_balance_fwd: workspace %zu < %zu bytes", ws_bytes, need);
+  if ((uintptr_t)ws & 3) DH_FAIL(DH_ERR_INVALID_ARG, "moe_balance_fwd: ws must be 4-byte aligned");
   const bool vec = balance_vec(E, logits, nullptr);
   const int blocks = balance_blocks(T, E, vec);
   float* part_p = (float*)ws;

@@ -287,3 +287,59 @@ def test_a_table_for_other_sizes_is_left_alone(dh):
     p.forward()
     torch.cuda.synchronize()
     assert bool((p.o == MARK).all()) and bool((p.lse == MARK).all())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("cap", [0.001, 1000.0])
+def test_smallest_and_largest_cap(dh, dtype, d, cap):
+    Packed(dh, dtype, T=200, nq=2, nkv=1, d=d, lengths=[120, 75], cap=cap, seed=17).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 32)])
+def test_more_documents_than_the_plan_copies(dh, dtype, d):
+    """5000 documents of one token: a row is its own only key, so that o = v exactly, dv = dout and the rest of the gradient is zero."""
+    T = 5003
+    p = Packed(dh, dtype, T=T, nq=1, nkv=1, d=d, lengths=[1] * 5000, first=2, seed=18)
+    p.qkv_d, p.dout_d = p.qkv.cuda(), p.dout.cuda()
+    p.buffers()
+    dh.dh_docs_plan(p.docs)
+    p.forward()
+    p.backward()
+    torch.cuda.synchronize()
+    live = slice(2, 5002)
+    assert bool((p.pos == 0).all())
+    assert torch.equal(p.o.cpu()[live], p.qkv[live, 2 * d:])
+    # the score of the backward pass, its p = exp(score - lse), and dout . v - delta are sums of d products in another order than before: d + 8 times 2^-24 of their
+    # terms apart (the float32 kernels scale q in one pass and k in the other)
+    q, k, v, do = (t[live].double() for t in (p.qkv[:, :d], p.qkv[:, d:2 * d], p.qkv[:, 2 * d:], p.dout))
+    apart = (2 * (d + 8) * R.W * (q * k).abs().sum(1) / d ** 0.5)[:, None] + 2 ** -22
+    assert bool(((p.dqkv[live, 2 * d:].cpu().double() - do).abs() <= (1.01 * apart + (0 if p.bf16 else R.W)) * do.abs()).all())  # (bf16: p rounds to one)
+    off = (2 * (d + 8) * R.W * (do * v).abs().sum(1) / d ** 0.5)[:, None]
+    assert bool((p.dqkv[live, :d].cpu().double().abs() <= 1.01 * off * k.abs() + 1e-30).all())
+    assert bool((p.dqkv[live, d:2 * d].cpu().double().abs() <= 1.01 * off * q.abs() + 1e-30).all())
+    s = (q * k).sum(1) / d ** 0.5
+    assert bool(((p.lse[0, live].cpu().double() - s).abs() <= (d + 16) * R.W * ((q * k).abs().sum(1) / d ** 0.5) + 2 ** -22).all())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 32)])
+def test_more_blocks_than_the_plan_weighs(dh, dtype, d):
+    """2000 documents of 70 rows: 140000 rows, 1094 blocks."""
+    n, docs, T = 70, 2000, 140000
+    p = Packed(dh, dtype, T=T, nq=1, nkv=1, d=d, lengths=[n] * docs, seed=19)
+    p.qkv_d, p.dout_d = p.qkv.cuda(), p.dout.cuda()
+    p.buffers()
+    dh.dh_docs_plan(p.docs)
+    p.forward()
+    p.backward()
+    torch.cuda.synchronize()
+    q, k, v = (p.qkv_d[:, i * d:(i + 1) * d].double().view(docs, n, d).contiguous() for i in range(3))
+    do, sc = p.dout_d.double().view(docs, n, d), d ** -0.5
+    hidden = torch.ones((n, n), dtype=torch.bool, device="cuda").triu(1)
+    P = torch.softmax((torch.matmul(q, k.transpose(1, 2).contiguous()) * sc).masked_fill(hidden, float("-inf")), 2)
+    o = torch.matmul(P, v)
+    dS = P * (torch.matmul(do, v.transpose(1, 2).contiguous()) - (do * o).sum(2, keepdim=True)) * sc
+    want = torch.cat([torch.matmul(dS, k), torch.matmul(dS.transpose(1, 2).contiguous(), q), torch.matmul(P.transpose(1, 2).contiguous(), do)], 2).view(T, 3 * d)
+    # roundings of P, dS, o and the results, half a step each, add up to less than 3 half steps; float32 has its sums of up to 70 + d terms
+    tol = 3 * 2.0 ** -8 if p.bf16 else 200 * R.W
+    rel = lambda a, b: float((a.double() - b).norm() / b.norm())  # noqa: E731
+    assert rel(p.o, o.view(T, d)) <= tol and rel(p.dqkv, want) <= tol

@@ -22,7 +22,7 @@ def refused(code, fn, *args, **kw):
 
 @pytest.mark.parametrize("bad,code", [(dict(T=-1), dh.DH_ERR_SHAPE), (dict(n_docs=-1), dh.DH_ERR_SHAPE), (dict(nq=0), dh.DH_ERR_SHAPE), (dict(nkv=0), dh.DH_ERR_SHAPE),
                                       (dict(nkv=3), dh.DH_ERR_SHAPE), (dict(doc_start=None), dh.DH_ERR_INVALID_ARG), (dict(table=None), dh.DH_ERR_INVALID_ARG),
-                                      (dict(table=A + 8), dh.DH_ERR_INVALID_ARG)])
+                                      (dict(table=A + 8), dh.DH_ERR_INVALID_ARG), (dict(T=(1 << 28) + 1), dh.DH_ERR_SHAPE), (dict(nq=1026), dh.DH_ERR_SHAPE)])
 def test_documents(bad, code):
     big = 1 << 40
     refused(code, dh.dh_docs_plan, docs(**bad))
@@ -42,7 +42,7 @@ def test_attention():
         both(dh.DH_ERR_SHAPE, dim=dim)
     for dim in (4, 264, 0):
         both(dh.DH_ERR_SHAPE, dtype=dh.DH_F32, dim=dim)
-    for cap in (-1.0, float("nan"), float("inf")):
+    for cap in (-1.0, float("nan"), float("inf"), 1e-4, 1001.0):
         both(dh.DH_ERR_INVALID_ARG, cap=cap)
     for i in range(3):
         for bad in (None, A + 8):
@@ -92,7 +92,8 @@ def test_balance():
     need = dh.dh_moe_balance_ws_bytes(100, 16)
     ok = dict(T=100, E=16, logits=A, idx=A, n_live=None, counts=A, prob_mean=A, lse=A, loss=A, ws=A, ws_bytes=need)
     for bad, code in [(dict(T=-1), dh.DH_ERR_SHAPE), (dict(E=1), dh.DH_ERR_SHAPE), (dict(E=257), dh.DH_ERR_SHAPE), (dict(ws=None), dh.DH_ERR_WORKSPACE_TOO_SMALL),
-                      (dict(ws_bytes=need - 1), dh.DH_ERR_WORKSPACE_TOO_SMALL)] + [({k: None}, dh.DH_ERR_INVALID_ARG) for k in ("logits", "idx", "counts", "prob_mean", "lse", "loss")]:
+                      (dict(ws_bytes=need - 1), dh.DH_ERR_WORKSPACE_TOO_SMALL),
+                      (dict(ws=A + 2), dh.DH_ERR_INVALID_ARG)] + [({k: None}, dh.DH_ERR_INVALID_ARG) for k in ("logits", "idx", "counts", "prob_mean", "lse", "loss")]:
         refused(code, dh.dh_moe_balance_fwd, **{**ok, **bad})
     ok = dict(T=100, E=16, logits=A, lse=A, counts=A, n_live=None, dloss=A, accumulate=False, dlogits=A)
     for bad, code in [(dict(T=-1), dh.DH_ERR_SHAPE), (dict(E=1), dh.DH_ERR_SHAPE), (dict(E=300), dh.DH_ERR_SHAPE)] + [({k: None}, dh.DH_ERR_INVALID_ARG) for k in ("logits", "lse", "counts", "dloss", "dlogits")]:
