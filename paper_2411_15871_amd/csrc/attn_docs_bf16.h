@@ -628,9 +628,16 @@ template <int D, bool CAP>
 __global__ __launch_bounds__(AB_THREADS) void attn_docs_bwd_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
                                                                         const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
                                                                         float* __restrict__ part_q, float* __restrict__ part_kv) {
-  const unsigned n_k = (unsigned)p.a.v.k.cap.units * p.a.nkv;
-  if (blockIdx.x < n_k) docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse, lse2, delta, dqkv, part_kv);
-  else docs_dq_block<D, CAP, false>(p, (blockIdx.x - n_k) / p.a.nq, (blockIdx.x - n_k) % p.a.nq, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
+  const DocsView& v = p.a.v;
+  const int nq = p.a.nq, nkv = p.a.nkv;
+  // the units there are, not the room for them: blocks without work between the two kinds would hold up the second (17 documents in 4096 rows on 4:1 heads 40.6 -> 38.9 us, 1000 rows of 8 heads 29.3 -> 28.2)
+  const unsigned n_k = (unsigned)min(max(v.head[v.k.counts], 0), v.k.cap.units) * nkv;
+  if (blockIdx.x < n_k) {
+    docs_dkv_block<D, CAP>(p, blockIdx.x / nkv, blockIdx.x % nkv, qkv, dout, lse, lse2, delta, dqkv, part_kv);
+  } else {
+    const int id = (blockIdx.x - n_k) / nq;
+    if (id < v.q.cap.units) docs_dq_block<D, CAP, false>(p, id, (blockIdx.x - n_k) % nq, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
+  }
 }
 
 // Adds the units of the blocks that were cut, in order: rows of dQ (scaled here) and of [dK | dV].  The first nb_q blocks are (16 * blocks that may be cut, nq) of dQ, 8 rows
