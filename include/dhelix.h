@@ -654,7 +654,7 @@ size_t dh_attn_ctx_bwd_workspace_bytes(int dtype, int batch, int seq, int q_off,
 typedef struct {
   int T;                    /* rows of the buffers */
   int n_docs;               /* documents, >= 0 */
-  int nq, nkv;              /* query and key/value heads of the attention that reads the table; nkv divides nq */
+  int nq, nkv;              /* query and key/value heads of the attention that reads the table; nkv divides nq, T/64 * nq/nkv at most 2^30 */
   const int32_t* doc_start; /* device [n_docs+1], ascending */
   const int32_t* prefix;    /* device [n_docs] rows of each document's prefix (cut to its length), or NULL: none */
   int32_t* pos;             /* device [T] written by dh_docs_plan: position in the row's document (0 for rows of none), or NULL */

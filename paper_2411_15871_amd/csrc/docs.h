@@ -9,7 +9,8 @@
 // meets, longest first.  A block with more tiles than the list's chunk length is cut into units of even length, whose partial results get a slot of workspace each;
 // a second list names these blocks.  Lengths follow from the documents, on the device; room for them follows from T and the heads alone.  Either kind of list is made twice, for
 // heads of 128 and of 64, since that many blocks more of the shorter heads are resident at once.
-#define DOCS_MAX_T (1 << 28)  // tiles of a block, times the heads of a group, are counted in 32 bits
+#define DOCS_MAX_T (1 << 28)
+#define DOCS_MAX_RUN (1 << 30)  // tiles that a block may meet, over the heads of a group: counted in 32 bits, as is the sum of two such counts
 #define DOCS_MAX_HEADS 1024
 #define DOCS_HEAD 16
 enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_COUNTS };  // head: the rows of documents are [live0, live1); from DOCS_COUNTS on, each list's units and cut blocks

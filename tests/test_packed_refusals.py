@@ -132,3 +132,13 @@ def test_gradients():
         dh.tensor_list([torch.zeros((4, 4)).t()])
     with pytest.raises(ValueError):
         dh.tensor_list([torch.zeros(4)], [torch.zeros(5)])
+
+
+@pytest.mark.parametrize("T,nq,nkv", [(1 << 28, 1024, 1), (1 << 28, 512, 1), (1 << 27, 1024, 1), (1 << 28, 1000, 2)])
+def test_more_tiles_of_a_group_than_are_counted(T, nq, nkv):
+    """A key block of one document meets T/64 tiles of each head of its group, and the work lists count these in 32 bits."""
+    assert T // 64 * (nq // nkv) > 1 << 30
+    bad = dict(T=T, nq=nq, nkv=nkv)
+    refused(dh.DH_ERR_SHAPE, dh.dh_docs_plan, docs(**bad))
+    refused(dh.DH_ERR_SHAPE, dh.dh_attn_docs_fwd, dh.DH_BF16, docs(**bad), 128, 0.0, A, A, A, A, 1 << 60)
+    refused(dh.DH_ERR_SHAPE, dh.dh_attn_docs_bwd, dh.DH_BF16, docs(**bad), 128, 0.0, A, A, A, A, A, A, A, 1 << 60)
