@@ -689,7 +689,7 @@ int dh_rope_axes(int dtype, int pairing, int form, int T, int n_axes, const int*
 /* Tensors of one call over many: HOST array; data and out are device pointers, aligned to their elements. */
 typedef struct {
   const void* data;
-  void* out;  /* dh_grad_clip: where the result goes; NULL = data itself.  May not overlap another tensor, or data other than as a whole. */
+  void* out;  /* dh_grad_clip: where the result goes; NULL = data itself.  May not overlap another tensor, or data other than as a whole (DH_ERR_INVALID_ARG). */
   size_t n;   /* elements */
   int dtype;  /* dh_dtype */
 } dh_tensor;

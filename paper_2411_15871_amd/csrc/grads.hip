@@ -2,6 +2,8 @@
 // optimizer.  Bound by memory: the norm reads every element once, the clipped copy reads and writes it once.
 #include <algorithm>
 #include <cstdint>
+#include <memory>
+#include <new>
 #include "common.h"
 
 // A launch takes up to GR_TENSORS tensors as arguments (a launch's arguments hold 4 KiB), further ones go out in further launches.  A block works on one chunk
@@ -160,6 +162,29 @@ static int check_tensors(const char* who, int n, const dh_tensor* t) {
   }
   return DH_OK;
 }
+// Results that meet another tensor, or their own data other than as a whole: blocks would race, and an element be scaled twice or not at all.
+static int check_apart(const char* who, int n, const dh_tensor* t) {
+  struct Range { uintptr_t from, to; bool written; };
+  if (n == 0) return DH_OK;
+  std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[2 * (size_t)n]);
+  if (!ranges) DH_FAIL(DH_ERR_UNSUPPORTED, "%s: no host memory for %d tensors", who, n);
+  size_t k = 0;
+  for (int i = 0; i < n; i++) {
+    if (t[i].n == 0) continue;
+    const uintptr_t bytes = t[i].n * dh_elem_size(t[i].dtype), data = (uintptr_t)t[i].data, out = t[i].out ? (uintptr_t)t[i].out : data;
+    ranges[k++] = {out, out + bytes, true};
+    if (out != data) ranges[k++] = {data, data + bytes, false};
+  }
+  std::sort(ranges.get(), ranges.get() + k, [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t any = 0, written = 0;  // ends of all ranges before this one, and of those that are written
+  for (size_t i = 0; i < k; i++) {
+    const Range& r = ranges[i];
+    if (r.from < (r.written ? any : written)) DH_FAIL(DH_ERR_INVALID_ARG, "%s: a result overlaps another tensor, or its own in part", who);
+    any = std::max(any, r.to);
+    if (r.written) written = std::max(written, r.to);
+  }
+  return DH_OK;
+}
 // Vectors of a chunk: 4096 (64 KiB), more where that would make over 16384 chunks (1.7 GB of gradients, norm and copy: 4096 larger ones 914 us, these 893).
 static unsigned chunk_vecs(int n, const dh_tensor* t) {
   unsigned long long all = 0;
@@ -227,6 +252,7 @@ extern "C" int dh_grad_clip(int n_tensors, const dh_tensor* tensors, const float
   if (int rc = check_tensors("grad_clip", n_tensors, tensors)) return rc;
   if (!(max_norm > 0.f)) DH_FAIL(DH_ERR_INVALID_ARG, "grad_clip: max_norm %g must be positive", (double)max_norm);
   if (!norm) DH_FAIL(DH_ERR_INVALID_ARG, "grad_clip: null pointer");
+  if (int rc = check_apart("grad_clip", n_tensors, tensors)) return rc;
   return each_launch(n_tensors, tensors, [&](const GradArgs& a, unsigned, unsigned blocks) -> int {
     grad_scale_kernel<<<blocks, GR_THREADS, 0, (hipStream_t)stream>>>(a, norm, max_norm);
     DH_LAUNCH_CHECK();

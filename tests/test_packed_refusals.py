@@ -142,3 +142,14 @@ def test_more_tiles_of_a_group_than_are_counted(T, nq, nkv):
     refused(dh.DH_ERR_SHAPE, dh.dh_docs_plan, docs(**bad))
     refused(dh.DH_ERR_SHAPE, dh.dh_attn_docs_fwd, dh.DH_BF16, docs(**bad), 128, 0.0, A, A, A, A, 1 << 60)
     refused(dh.DH_ERR_SHAPE, dh.dh_attn_docs_bwd, dh.DH_BF16, docs(**bad), 128, 0.0, A, A, A, A, A, A, A, 1 << 60)
+
+
+@pytest.mark.parametrize("parts", [[(0, None, 100), (0, None, 100)],                   # a tensor twice, in place
+                                   [(0, None, 100), (396, None, 100)],                 # one element shared
+                                   [(0, 400, 100), (1000, 400, 100)],                  # two results in one place
+                                   [(0, 1200, 100), (1000, 2000, 100)],                # a result over another tensor
+                                   [(0, 4, 100)],                                      # a result shifted over its own tensor
+                                   [(0, 40000, 10000), (80000, None, 10), (80036, None, 10), (90000, None, 5)]])
+def test_clipping_what_overlaps(parts):
+    t = (dh.dh_tensor * len(parts))(*[dh.dh_tensor(A + d, None if o is None else A + o, n, dh.DH_F32) for d, o, n in parts])
+    refused(dh.DH_ERR_INVALID_ARG, dh.dh_grad_clip, t, A, 1.0)
