@@ -731,9 +731,9 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   const DocsCaps &q = p.a.v.q.cap, &k = p.a.v.k.cap;
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
-  // One launch: the two halves' blocks fill each other's units.  Its blocks have those of dK/dV for neighbours and its registers, so that large grids of dQ blocks, two a unit
-  // by themselves, lose more than they gain at D = 128 (32:8 x 8192, 2560 blocks, 746 and 780 us; 16:8 x 4096 capped, 768, 172 and 166); at D = 64 two
-  // fit either way (16:4 x 8192, 1280, 239 and 216; 32 heads x 8192, 4096, 978 and 983).
+  // One launch: the two halves' blocks fill each other's units (two launches and one, us: 1000 rows of 8 heads, 128 blocks, 43.7 and 28.5; 16:8 x 4096 capped, 768, 160 and 154).  Its
+  // blocks have the registers and LDS of dK/dV, so that large grids of dQ blocks, two a unit by themselves, lose more than they gain at D = 128 (32:8 x 8192, 2560 blocks, 745
+  // and 784; 8:2 x 16384, 1280, 752 and 740); at D = 64 two fit either way (16:4 x 8192, 1280, 240 and 219; 32 heads x 8192, 4096, 978 and 983).
   if (docs_one_launch(p.a.v.T, nq, nkv) || (D == 64 && !CAP && docs_one_launch((p.a.v.T + 3) / 4, nq, nkv))) {
     attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
     DH_LAUNCH_CHECK();

@@ -17,18 +17,24 @@ enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_COUNTS };  // hea
 enum { DOCS_Q128, DOCS_Q64, DOCS_K128, DOCS_K64, DOCS_LISTS };
 #define DOCS_BLOCK 128
 #define DOCS_TILE 64
-// A chunk holds so many tiles that all heads' tiles together make at most DOCS_TARGET chunks (room for partial results follows from that), and DOCS_CHUNK at least.
+// A chunk holds DOCS_CHUNK tiles at least: shorter ones cost more in beginnings, ends and merges than they share out, longer ones leave units of the chip idle.  us, D = 128:
+// Q 2, 4, 8: forward of 17 documents in 4096 rows on 4:1 heads 24.0, 22.0, 23.0, backward of 1000 rows of 8 heads 33.1, 28.5, 31.0 (of 2000 rows on 16:4 66.0, 65.5, 60.8);
+// K 2, 3, 6: backward of 500 rows on 8:2 23.6, 22.7, 24.3, of 100 rows there 17.2, 18.6, 20.2.
 #define DOCS_CHUNK_Q 4
 #define DOCS_CHUNK_K 3
+// Where no block can have more than DOCS_WHOLE tiles none is cut, and no launch is needed to merge.  us: Q 4 and 10: forward of 300 rows of 4 heads 14.9 and 10.6; 10 and 13: training step
+// of 700 39.5 and 46.7; K 4 and 8: backward of 440 rows of 4 heads 22.3 and 20.2; 8 and 12: of 100 rows on 8:2 18.6 and 22.9.
 #define DOCS_WHOLE_Q 10
-#define DOCS_WHOLE_K 4
+#define DOCS_WHOLE_K 8
+// All heads' tiles together make at most DOCS_TARGET chunks: room for partial results follows from that, two a chunk (at D = 128 135 MB for a target of 1024 of O or dQ, or of 512 of dK
+// and dV).  us: Q 512, 1024, 2048: forward of 16384 rows on 4:1 heads 331, 311, 309; K 256, 512, 1024: backward there 979, 969, 986, of 8192 rows on 32:8 736, 745, 757.
 #define DOCS_TARGET_Q 1024
 #define DOCS_TARGET_K 512
-// 128-row blocks of all heads up to which both halves of the backward pass go out as one launch.
+// 128-row blocks of all heads up to which both halves of the backward pass go out as one launch (figures where it is launched).
 #define DOCS_ONE_LAUNCH 1024
 __host__ __device__ static inline bool docs_one_launch(int T, int nq, int nkv) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= DOCS_ONE_LAUNCH; }
 struct DocsCaps { int blocks, units, slots, splits; };
-// Tiles that a chunk holds at least: where a block cannot have more than `whole` tiles none is cut, and no launch is needed to merge.
+// Tiles that a chunk holds at least, by the two rules above.
 __host__ __device__ static inline int docs_least(int T, int grp, int chunk, int whole) {
   const long long most = (((long long)T + DOCS_TILE - 1) / DOCS_TILE + 1) * grp;
   return most <= whole ? whole : chunk;
