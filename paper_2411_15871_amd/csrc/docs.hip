@@ -170,7 +170,7 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
     from[tid] = upto - hist[tid];
     if (tid == 63) all_units = min(upto, cap.units);
   }
-  unsigned long long cut = 0;  // slots and, in the upper half, blocks that are cut, before this round's
+  unsigned long long cut = 0;  // slots and, in the upper half, blocks that are cut, before these 256 blocks'
   for (int b0 = 0; b0 < cap.blocks; b0 += 256) {
     const int b = b0 + tid;
     first = first0;
