@@ -676,7 +676,7 @@ static DocsTiled docs_tiled(const DocsAttn& a) {
 }
 
 size_t dh_attn_docs_fwd_bf16_ws_bytes(int T, int nq, int nkv, int d) {
-  return (size_t)docs_view(nullptr, T, nq, nkv, d).q.cap.slots * nq * DOCS_BLOCK * ((size_t)d + 2) * sizeof(float);
+  return (size_t)docs_view(nullptr, T, nq, nkv, d, false).q.cap.slots * nq * DOCS_BLOCK * ((size_t)d + 2) * sizeof(float);
 }
 
 template <int D, bool CAP>
@@ -714,7 +714,7 @@ static DocsBwdLayout docs_bwd_layout(const DocsView& v, int nq, int nkv, int d) 
   l.total = at;
   return l;
 }
-size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view(nullptr, T, nq, nkv, d), nq, nkv, d).total; }
+size_t dh_attn_docs_bwd_bf16_ws_bytes(int T, int nq, int nkv, int d) { return docs_bwd_layout(docs_view(nullptr, T, nq, nkv, d, true), nq, nkv, d).total; }
 
 template <int D, bool CAP>
 static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, char* ws, hipStream_t stream) {
@@ -731,10 +731,11 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   const DocsCaps &q = p.a.v.q.cap, &k = p.a.v.k.cap;
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
-  // One launch: the two halves' blocks fill each other's units (two launches and one, us: 1000 rows of 8 heads, 128 blocks, 43.7 and 28.5; 16:8 x 4096 capped, 768, 160 and 154).  Its
-  // blocks have the registers and LDS of dK/dV, so that large grids of dQ blocks, two a unit by themselves, lose more than they gain at D = 128 (32:8 x 8192, 2560 blocks, 745
-  // and 784; 8:2 x 16384, 1280, 752 and 740); at D = 64 two fit either way (16:4 x 8192, 1280, 240 and 219; 32 heads x 8192, 4096, 978 and 983).
-  if (docs_one_launch(p.a.v.T, nq, nkv) || (D == 64 && !CAP && docs_one_launch((p.a.v.T + 3) / 4, nq, nkv))) {
+  // One launch: the two halves' blocks fill each other's units.  Its blocks have the registers and LDS of dK/dV, so that large grids of dQ blocks, two a unit by themselves, lose
+  // more than they gain at D = 128.  us, two launches and one, by blocks: D = 128: 128 (1000 rows of 8 heads) 43.6 and 28.4, 768 (16:8 x 4096 capped) 160 and 144, 1280 (16:4 x 8192) 427
+  // and 408, 1536 (8:4 x 16384) 1824 and 1842, 2560 (32:8 x 8192) 743 and 784.  D = 64, where two fit either way: 512 59.2 and 48.4, 1280 240 and 219, 4096 978 and 983; capped 512
+  // 59.8 and 52.4, 1024 95.7 and 100.6, 1280 240 and 257.
+  if (docs_one_launch(p.a.v.T, nq, nkv, D == 128 ? DOCS_ONE_128 : CAP ? DOCS_ONE_64 : 4 * DOCS_ONE_64)) {
     attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
     DH_LAUNCH_CHECK();
     attn_docs_bwd_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv + (unsigned)q.units * nq, AB_THREADS, lds_dkv, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q, part_kv);

@@ -7,19 +7,20 @@
 // rows (j < pre[j] ? lo[j] : j) .. hi[j] - 1.  All four borders ascend with the row.
 // Behind them the work of the tiled kernels, lists for blocks of 128 queries and for blocks of 128 keys: units of a block and a run of the 64-row tiles it
 // meets, longest first.  A block with more tiles than the list's chunk length is cut into units of even length, whose partial results get a slot of workspace each;
-// a second list names these blocks.  Lengths follow from the documents, on the device; room for them follows from T and the heads alone.  Either kind of list is made twice, for
-// heads of 128 and of 64, since that many blocks more of the shorter heads are resident at once.
+// a second list names these blocks.  Lengths follow from the documents, on the device; room for them follows from T and the heads alone.  There is one
+// list of the forward pass, and one of dQ and one of dK and dV for heads of 128 and of 64 each: more blocks of the shorter heads are resident at once, and where the backward pass is one
+// launch its two kinds share the chip.
 #define DOCS_MAX_T (1 << 28)
 #define DOCS_MAX_RUN (1 << 30)  // tiles that a block may meet, over the heads of a group: counted in 32 bits, as is the sum of two such counts
 #define DOCS_MAX_HEADS 1024
 #define DOCS_HEAD 16
 enum { DOCS_LIVE0, DOCS_LIVE1, DOCS_T, DOCS_NQ, DOCS_NKV, DOCS_COUNTS };  // head: the rows of documents are [live0, live1); from DOCS_COUNTS on, each list's units and cut blocks
-enum { DOCS_Q128, DOCS_Q64, DOCS_K128, DOCS_K64, DOCS_LISTS };
+enum { DOCS_Q, DOCS_DQ128, DOCS_DQ64, DOCS_K128, DOCS_K64, DOCS_LISTS };
 #define DOCS_BLOCK 128
 #define DOCS_TILE 64
 // A chunk holds DOCS_CHUNK tiles at least: shorter ones cost more in beginnings, ends and merges than they share out, longer ones leave units of the chip idle.  us, D = 128:
-// Q 2, 4, 8: forward of 17 documents in 4096 rows on 4:1 heads 24.0, 22.0, 23.0, backward of 1000 rows of 8 heads 33.1, 28.5, 31.0 (of 2000 rows on 16:4 66.0, 65.5, 60.8);
-// K 2, 3, 6: backward of 500 rows on 8:2 23.6, 22.7, 24.3, of 100 rows there 17.2, 18.6, 20.2.
+// Q 2, 4, 8: forward of 17 documents in 4096 rows on 4:1 heads 23.6, 22.2, 22.8, backward of 1000 rows of 8 heads 28.4, 28.4, 30.9;
+// K 2, 3, 6: backward of 500 rows on 8:2 23.9, 22.7, 24.4, of 100 rows there 17.2, 18.7, 20.0.
 #define DOCS_CHUNK_Q 4
 #define DOCS_CHUNK_K 3
 // Where no block can have more than DOCS_WHOLE tiles none is cut, and no launch is needed to merge.  us: Q 4 and 10: forward of 300 rows of 4 heads 14.9 and 10.6; 10 and 13: training step
@@ -30,9 +31,10 @@ enum { DOCS_Q128, DOCS_Q64, DOCS_K128, DOCS_K64, DOCS_LISTS };
 // and dV).  us: Q 512, 1024, 2048: forward of 16384 rows on 4:1 heads 331, 311, 309; K 256, 512, 1024: backward there 979, 969, 986, of 8192 rows on 32:8 736, 745, 757.
 #define DOCS_TARGET_Q 1024
 #define DOCS_TARGET_K 512
-// 128-row blocks of all heads up to which both halves of the backward pass go out as one launch (figures where it is launched).
-#define DOCS_ONE_LAUNCH 1024
-__host__ __device__ static inline bool docs_one_launch(int T, int nq, int nkv) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= DOCS_ONE_LAUNCH; }
+// Whether both halves of the backward pass go out as one launch: up to `most` 128-row blocks of all heads (figures where it is launched).
+#define DOCS_ONE_128 1280
+#define DOCS_ONE_64 1024
+__host__ __device__ static inline bool docs_one_launch(int T, int nq, int nkv, int most) { return (long long)((T + DOCS_BLOCK - 1) / DOCS_BLOCK) * (nq + nkv) <= most; }
 struct DocsCaps { int blocks, units, slots, splits; };
 // Tiles that a chunk holds at least, by the two rules above.
 __host__ __device__ static inline int docs_least(int T, int grp, int chunk, int whole) {
@@ -87,15 +89,15 @@ static inline DocsTable docs_table(void* table, int T, int nq, int nkv) {
   v.bytes = at;
   return v;
 }
-// What the kernels of one head width read.
+// What the kernels of one pass and head width read.
 struct DocsView {
   int T;
   const int32_t *head, *lo, *hi, *pre;
   DocsList q, k;
 };
-static inline DocsView docs_view(const void* table, int T, int nq, int nkv, int d) {
+static inline DocsView docs_view(const void* table, int T, int nq, int nkv, int d, bool bwd) {
   const DocsTable t = docs_table(const_cast<void*>(table), T, nq, nkv);
-  return {T, t.head, t.lo, t.hi, t.pre, t.list[d == 64 ? DOCS_Q64 : DOCS_Q128], t.list[d == 64 ? DOCS_K64 : DOCS_K128]};
+  return {T, t.head, t.lo, t.hi, t.pre, t.list[!bwd ? DOCS_Q : d == 64 ? DOCS_DQ64 : DOCS_DQ128], t.list[d == 64 ? DOCS_K64 : DOCS_K128]};
 }
 // Whether the table was made for these sizes: a kernel that finds others does nothing.
 __device__ __forceinline__ bool docs_fits(const DocsView& v, int nq, int nkv) { return v.head[DOCS_T] == v.T && v.head[DOCS_NQ] == nq && v.head[DOCS_NKV] == nkv; }

@@ -56,7 +56,7 @@ __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* st
 // unit of the chip with another (queries; 2.1 us at D = 128) or has it to itself (keys; 2.3 us): up to one round of resident blocks the longest unit counts, a fifth faster
 // alone; beyond, everything over all units (a unit's beginning and end count 1.5 tiles beside another's work) and a quarter of the longest one for the end.  A partial
 // result is written and read back (beyond 512 of them from memory), and the merge takes a while longer if there is any.  tiles[b]: of the first DOCS_BLOCKS blocks; longer
-// rows are cut at `shortest`.  (Always `shortest` and this, us: one document of 4096 rows on 4:1 heads, forward 49 and 39, backward 129 and 92; 32:8 x 8192 244 and 227, 771 and 745.)
+// rows are cut at `shortest`.  (Always `shortest` and this, us: one document of 4096 rows on 4:1 heads, forward 49 and 39, backward 131 and 91; 32:8 x 8192 248 and 230, 766 and 744.)
 #define DOCS_BLOCKS 1024
 __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, int list, int blocks, int shortest, int longest, float all, const int* tiles) {
   __shared__ int units[4][64], cuts[4][64], tops[4][64];
@@ -77,10 +77,13 @@ __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, int list, int b
   __syncthreads();
   const float N = (float)(units[0][lane] + units[1][lane] + units[2][lane] + units[3][lane]) * heads, C = (float)(cuts[0][lane] + cuts[1][lane] + cuts[2][lane] + cuts[3][lane]) * heads;
   const float L = (float)max(max(tops[0][lane], tops[1][lane]), max(tops[2][lane], tops[3][lane]));
-  const bool keys = list >= DOCS_K128, one = docs_one_launch(a.T, a.nq, a.nkv);  // (in one launch the rest of the chip has queries)
-  const float slots = !keys ? 512.f : list == DOCS_K64 ? (one ? 240.f : 400.f) : one ? 144.f : 256.f;
+  // Blocks resident at once; where the backward pass is one launch, each kind's share of them.  (dQ by the forward pass's list and by its own, us: 2000 rows on 16:4 66 and 55,
+  // 16:8 x 4096 capped 154 and 143, at D = 64 4001 rows of 8 heads 49.2 and 47.7.  Shares of dQ, D = 128, 80, 112, 200: 1500 rows on 8:2 44, 38, 40; D = 64, 272, 400: 2000 on 16:4 41,
+  // 39.  Of dK and dV, 112, 144, 176: 2000 rows 57, 55, 57, 1000 of 8 heads 28, 28, 36; D = 64, 180, 240, 300: 4001 rows 58, 48, 48, 2000 44, 39, 40.)
+  const bool one = docs_one_launch(a.T, a.nq, a.nkv, list == DOCS_DQ64 || list == DOCS_K64 ? DOCS_ONE_64 : DOCS_ONE_128), pairs = list == DOCS_Q || list == DOCS_DQ64 || (list == DOCS_DQ128 && !one);
+  const float slots = list == DOCS_Q ? 512.f : list == DOCS_DQ128 ? (one ? 112.f : 512.f) : list == DOCS_DQ64 ? (one ? 400.f : 512.f) : list == DOCS_K64 ? (one ? 240.f : 400.f) : one ? 144.f : 256.f;
   const float together = fmaxf(L, (all + 1.5f * N) / slots + 0.25f * L);
-  const float time = (N > slots ? together : keys ? L : L * (0.8f + 0.2f / 256.f * fmaxf(N - 256.f, 0.f))) + (C > 0.f ? 1.5f + 0.004f * C + 0.008f * fmaxf(C - 512.f, 0.f) : 0.f);
+  const float time = (N > slots ? together : !pairs ? L : L * (0.8f + 0.2f / 256.f * fmaxf(N - 256.f, 0.f))) + (C > 0.f ? 1.5f + 0.004f * C + 0.008f * fmaxf(C - 512.f, 0.f) : 0.f);
   float best = time;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) best = fminf(best, __shfl_xor(best, d, 64));
@@ -290,7 +293,7 @@ static int check_attn_docs(const char* who, int dtype, const dh_docs* docs, int 
   return DH_OK;
 }
 static bool unaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
-static DocsAttn attn_of(const dh_docs* docs, int d, float cap) { return {docs_view(docs->table, docs->T, docs->nq, docs->nkv, d), docs->nq, docs->nkv, d, (float)(1.0 / sqrt((double)d)), cap}; }
+static DocsAttn attn_of(const dh_docs* docs, int d, float cap, bool bwd) { return {docs_view(docs->table, docs->T, docs->nq, docs->nkv, d, bwd), docs->nq, docs->nkv, d, (float)(1.0 / sqrt((double)d)), cap}; }
 
 static bool sized(int dtype, int T, int nq, int nkv, int d) {
   return dtype == DH_BF16 && T > 0 && T <= DOCS_MAX_T && nkv > 0 && nq > 0 && nq <= DOCS_MAX_HEADS && nq % nkv == 0 && (d == 64 || d == 128);
@@ -306,7 +309,7 @@ extern "C" int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap
   const size_t need = dh_attn_docs_fwd_workspace_bytes(dtype, docs->T, docs->nq, docs->nkv, d);
   if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_docs_fwd: workspace %zu < %zu bytes", ws_bytes, need);
   if (unaligned16(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: ws must be 16-byte aligned");
-  const DocsAttn a = attn_of(docs, d, cap);
+  const DocsAttn a = attn_of(docs, d, cap, false);
   if (dtype == DH_BF16) return dh_launch_attn_docs_fwd_bf16(a, (const bf16_t*)qkv, (bf16_t*)o, lse, ws, ws_bytes, (hipStream_t)stream);
   return dh_launch_attn_docs_fwd_f32(a, (const float*)qkv, (float*)o, lse, (hipStream_t)stream);
 }
@@ -320,7 +323,7 @@ extern "C" int dh_attn_docs_bwd(int dtype, const dh_docs* docs, int d, float cap
   const size_t need = dh_attn_docs_bwd_workspace_bytes(dtype, docs->T, docs->nq, docs->nkv, d);
   if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_docs_bwd: workspace %zu < %zu bytes", ws_bytes, need);
   if (unaligned16(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: ws must be 16-byte aligned");
-  const DocsAttn a = attn_of(docs, d, cap);
+  const DocsAttn a = attn_of(docs, d, cap, true);
   if (dtype == DH_F32) return dh_launch_attn_docs_bwd_f32(a, (const float*)qkv, (const float*)o, (const float*)dout, lse, (float*)dqkv, delta, (hipStream_t)stream);
   return dh_launch_attn_docs_bwd_bf16(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)dout, lse, (bf16_t*)dqkv, delta, ws, ws_bytes, (hipStream_t)stream);
 }
