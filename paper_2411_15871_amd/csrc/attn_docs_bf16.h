@@ -489,9 +489,13 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
       Op.set(sm + (AB_RING + slot) * TL::BYTES, fa);
       const float* ls = lse_s + slot * AB_KT;
       const float* ds = del_s + slot * AB_KT;
-      f32x4 lv[8];  // rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
+      // With slopes besides, statistics are read where they are used: 248 registers let two blocks share a unit, 277 did not (5000 rows on 16:4 heads 360 us, 272 this way).
+      constexpr bool LATE = CAP && D == 64;
+      f32x4 lv[LATE ? 1 : 8];  // rows 32*mt + 8*q4 + 4*kg + e of the tile at [4*mt + q4]
+      if constexpr (!LATE) {
 #pragma unroll
-      for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ls + 8 * x + 4 * kg);
+        for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ls + 8 * x + 4 * kg);
+      }
       f32x16 st[2], dp[2], slope[CAP ? 2 : 1];
       // P from S beside the dP products
       score_tiles2<D, AB_RING * TL::BYTES, 3>(st, Qp, kf, dp, vf, [&](int j) {
@@ -499,12 +503,13 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
 #pragma unroll
         for (int i = 0; i < N; i++) {
           const int x = j * N + i, mt = x >> 2, q4 = x & 3;
+          if constexpr (LATE) lv[0] = *reinterpret_cast<const f32x4*>(ls + 8 * x + 4 * kg);
 #pragma unroll
           for (int e = 0; e < 4; e++) {
             const float s = st[mt][4 * q4 + e];
             if constexpr (CAP) {
               const float r = docs_cap_r(s, p.exp_scale);
-              st[mt][4 * q4 + e] = fast_exp2(fmaf(-2.f * p.cap_log2, r, lv[x][e]));
+              st[mt][4 * q4 + e] = fast_exp2(fmaf(-2.f * p.cap_log2, r, lv[LATE ? 0 : x][e]));
               slope[mt][4 * q4 + e] = fmaf(-r, r, r);
             } else {
               st[mt][4 * q4 + e] = fast_exp2(fmaf(s, p.exp_scale, -lv[x][e]));
@@ -514,8 +519,10 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
       });
       TrFrags<D> fr;
       tr_fetch<D>(fr, Op, 0);
+      if constexpr (!LATE) {
 #pragma unroll
-      for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ds + 8 * x + 4 * kg);
+        for (int x = 0; x < 8; x++) lv[x] = *reinterpret_cast<const f32x4*>(ds + 8 * x + 4 * kg);
+      }
       if (qb < see.all0 || qb + AB_KT > see.all1) {
         const int first = qb + 4 * kg - see.at;
 #pragma unroll
@@ -529,7 +536,8 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
       acc_tile_tr<D, true, AGPR>(dvt, fr, Op, st, Qp, [&](int g) {
 #pragma unroll
         for (int r = 8 * (g & 1); r < 8 * (g & 1) + 8; r++) {
-          st[g >> 1][r] *= dp[g >> 1][r] - lv[4 * (g >> 1) + (r >> 2)][r & 3];
+          if constexpr (LATE) { if ((r & 3) == 0) lv[0] = *reinterpret_cast<const f32x4*>(ds + 8 * (4 * (g >> 1) + (r >> 2)) + 4 * kg); }
+          st[g >> 1][r] *= dp[g >> 1][r] - lv[LATE ? 0 : 4 * (g >> 1) + (r >> 2)][r & 3];
           if constexpr (CAP) st[g >> 1][r] *= slope[g >> 1][r];
         }
       });
@@ -733,9 +741,9 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
   // One launch: the two halves' blocks fill each other's units.  Its blocks have the registers and LDS of dK/dV, so that large grids of dQ blocks, two a unit by themselves, lose
   // more than they gain at D = 128.  us, two launches and one, by blocks: D = 128: 128 (1000 rows of 8 heads) 43.6 and 28.4, 768 (16:8 x 4096 capped) 160 and 144, 1280 (16:4 x 8192) 427
-  // and 408, 1536 (8:4 x 16384) 1824 and 1842, 2560 (32:8 x 8192) 743 and 784.  D = 64, where two fit either way: 512 59.2 and 48.4, 1280 240 and 219, 4096 978 and 983; capped 512
-  // 59.8 and 52.4, 1024 95.7 and 100.6, 1280 240 and 257.
-  if (docs_one_launch(p.a.v.T, nq, nkv, D == 128 ? DOCS_ONE_128 : CAP ? DOCS_ONE_64 : 4 * DOCS_ONE_64)) {
+  // and 408, 1536 (8:4 x 16384) 1824 and 1842, 2560 (32:8 x 8192) 743 and 784.  D = 64, where two fit either way: 512 59.2 and 48.4, 1280 240 and 219, 4096 978 and 983; capped 1280 302
+  // and 273, 2500 318 and 296, 4000 433 and 434.
+  if (docs_one_launch(p.a.v.T, nq, nkv, D == 128 ? DOCS_ONE_128 : 4 * DOCS_ONE_64)) {
     attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
     DH_LAUNCH_CHECK();
     attn_docs_bwd_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv + (unsigned)q.units * nq, AB_THREADS, lds_dkv, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q, part_kv);
