@@ -45,6 +45,19 @@ __device__ __forceinline__ void docs_voff(uint32_t (&v)[ATile<D>::IPW], int ld, 
     v[j] = (uint32_t)(((size_t)max(first, min(row, last)) * ld + c * 8) * sizeof(bf16_t));
   }
 }
+// Moves a tile's lane pointers by a number of bytes, in the same registers: pointers that are formed anew for each tile need their offsets' registers as well, and where these do not
+// suffice the offsets come from scratch, in whose counter of loads the next tile's transfer stands ahead of them.
+template <int D>
+__device__ __forceinline__ void docs_shift(TilePtrs<D>& p, int bytes) {
+  auto by = [&](const lds_char*& q) {
+    q += bytes;
+    asm volatile("" : "+v"(q));
+  };
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) by(p.dir[ks]);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) { by(p.t0[dt]); by(p.t1[dt]); }
+}
 // Whether any of N accumulator tiles holds an infinity or a NaN.
 template <int N>
 __device__ __forceinline__ bool docs_not_finite(const f32x16 (&t)[N]) {
@@ -323,15 +336,15 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
   pin_frags(dof);
   pin_scalar(l2);
   pin_scalar(dl);
+  TilePtrs<D> Kp;
+  Kp.set(sm, fa);
   int slot = 0;
-  for (int t = u.f0; t < u.f1; t++, slot ^= 1) {
+  for (int t = u.f0; t < u.f1; t++, docs_shift<D>(Kp, slot ? -(int)TL::BYTES : (int)TL::BYTES), slot ^= 1) {
     dma_wait<0>();
     __syncthreads();
     if (t + 1 < u.f1) issue(t + 1, slot ^ 1);
     const int kb = t * AB_KT;
     if (kb >= see.any1 || kb + AB_KT <= see.any0) continue;
-    TilePtrs<D> Kp;
-    Kp.set(sm + slot * TL::BYTES, fa);
     f32x16 st[2], dp[2];
     // P^T from S^T beside the dP^T products
     score_tiles2<D, DOCS_DQ_RING * TL::BYTES, 1>(st, Kp, qf, dp, dof, [&](int j) {
