@@ -753,9 +753,9 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   const DocsBwdLayout l = docs_bwd_layout(p.a.v, nq, nkv, D);
   float *lse2 = (float*)(ws + l.lse2), *part_kv = (float*)(ws + l.dkv), *part_q = (float*)(ws + l.dq);
   // One launch: the two halves' blocks fill each other's units.  Its blocks have the registers and LDS of dK/dV, so that large grids of dQ blocks, two a unit by themselves, lose
-  // more than they gain at D = 128.  us, two launches and one, by blocks: D = 128: 128 (1000 rows of 8 heads) 43.6 and 28.4, 768 (16:8 x 4096 capped) 160 and 144, 1280 (16:4 x 8192) 427
-  // and 408, 1536 (8:4 x 16384) 1824 and 1842, 2560 (32:8 x 8192) 743 and 784.  D = 64, where two fit either way: 512 59.2 and 48.4, 1280 240 and 219, 4096 978 and 983; capped 1280 302
-  // and 273, 2500 318 and 296, 4000 433 and 434.
+  // more than they gain at D = 128.  us, two launches and one, by blocks: D = 128: 128 (1000 rows of 8 heads) 41 and 28, 512 (4096 rows of 8) 68 and 57, 768 (8:4 x 8192) 157 and 147,
+  // 960 (16:4 x 6144) 262 and 261, 1024 (8 x 8192) 149 and 151, capped 174 and 184, 1536 (8:4 x 16384) 1763 and 1820, 2560 (32:8 x 8192) 691 and 777.  D = 64, where two fit either
+  // way: 512 59.2 and 48.4, 1280 240 and 219, 4096 978 and 983; capped 1280 302 and 273, 2500 318 and 296, 4000 433 and 434.
   if (docs_one_launch(p.a.v.T, nq, nkv, D == 128 ? DOCS_ONE_128 : 4 * DOCS_ONE_64)) {
     attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
     DH_LAUNCH_CHECK();

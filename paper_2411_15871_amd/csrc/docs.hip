@@ -56,7 +56,7 @@ __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* st
 // unit of the chip with another (queries; 2.1 us at D = 128) or has it to itself (keys; 2.3 us): up to one round of resident blocks the longest unit counts, a fifth faster
 // alone; beyond, everything over all units (a unit's beginning and end count 1.5 tiles beside another's work) and a quarter of the longest one for the end.  A partial
 // result is written and read back (beyond 512 of them from memory), and the merge takes a while longer if there is any.  tiles[b]: of the first DOCS_BLOCKS blocks; longer
-// rows are cut at `shortest`.  (Always `shortest` and this, us: one document of 4096 rows on 4:1 heads, forward 49 and 39, backward 131 and 91; 32:8 x 8192 248 and 230, 766 and 744.)
+// rows are cut at `shortest`.  (Always `shortest` and this, us: one document of 4096 rows on 4:1 heads, forward 49 and 39, backward 131 and 91; 32:8 x 8192 forward 248 and 230.)
 #define DOCS_BLOCKS 1024
 __device__ __forceinline__ int docs_chunk(const DocsPlanArgs& a, int list, int blocks, int shortest, int longest, float all, const int* tiles) {
   __shared__ int units[4][64], cuts[4][64], tops[4][64];
