@@ -648,8 +648,9 @@ size_t dh_attn_ctx_bwd_workspace_bytes(int dtype, int batch, int seq, int q_off,
  * Packed micro-batches: one row of T tokens holds n_docs documents back to back and rows of padding around them.
  * Document n is rows doc_start[n] .. doc_start[n+1]-1; rows before doc_start[0] and from doc_start[n_docs] on belong to none.  A row
  * sees the rows of its document up to itself; with a prefix, the first prefix[n] rows of document n see one another whole.
- * doc_start and prefix are DEVICE arrays (they come with the micro-batch, no host round trip).  Documents may be empty.  Starts that do not ascend,
- * or lie outside 0..T, leave the rows they would give to two documents or none in an unspecified one of them or in none; nothing outside the buffers is touched.
+ * doc_start and prefix are DEVICE arrays (they come with the micro-batch, no host round trip).  Documents may be empty.  Starts that do not ascend
+ * leave it open which rows are of which document, and what these rows' results are; rows before doc_start[0] and from doc_start[n_docs] on are of none all the same, and nothing outside the
+ * buffers is touched.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
   int T;                    /* rows of the buffers */

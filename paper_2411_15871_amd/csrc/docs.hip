@@ -26,9 +26,15 @@ struct DocsPlanArgs {
   int32_t* pos;
   DocsTable t;
 };
+// The rows of documents, [live0, live1): whatever the starts are, no row outside is given to a document, and 0 <= live0 <= live1 <= T.
+template <class Start>
+__device__ __forceinline__ void docs_live(const DocsPlanArgs& a, const Start* start, int& live0, int& live1) {
+  live0 = a.n_docs > 0 ? min(max(start[0], 0), a.T) : 0;
+  live1 = a.n_docs > 0 ? min(max(start[a.n_docs], live0), a.T) : 0;
+}
 // The document of row r: its rows [s, e) and the end of its prefix; false: none.  start: a.start, or its copy in LDS.
 template <class Start>
-__device__ __forceinline__ bool docs_find(const DocsPlanArgs& a, const Start* start, int r, int& s, int& e, int& c) {
+__device__ __forceinline__ bool docs_find(const DocsPlanArgs& a, const Start* start, int live0, int live1, int r, int& s, int& e, int& c) {
   int lo = 0, hi = a.n_docs + 1;  // how many starts lie at or before r
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -36,8 +42,8 @@ __device__ __forceinline__ bool docs_find(const DocsPlanArgs& a, const Start* st
     else hi = mid;
   }
   if (lo < 1 || lo > a.n_docs) return false;
-  s = max(start[lo - 1], 0);
-  e = min(start[lo], a.T);
+  s = max(start[lo - 1], live0);
+  e = min(start[lo], live1);
   if (s > r || r >= e) return false;
   c = a.prefix ? s + min(max(a.prefix[lo - 1], 0), e - s) : s;
   return true;
@@ -47,7 +53,7 @@ template <class Start>
 __device__ __forceinline__ int docs_tiles(const DocsPlanArgs& a, const Start* start, int live0, int live1, bool keys, int b, int& first) {
   const int r0 = max(b * DOCS_BLOCK, live0), r1 = min(b * DOCS_BLOCK + DOCS_BLOCK, live1) - 1;
   int s0, e0, c0, s1, e1, c1;
-  if (r0 > r1 || !docs_find(a, start, r0, s0, e0, c0) || !docs_find(a, start, r1, s1, e1, c1)) return 0;
+  if (r0 > r1 || !docs_find(a, start, live0, live1, r0, s0, e0, c0) || !docs_find(a, start, live0, live1, r1, s1, e1, c1)) return 0;
   const int from = keys ? (r0 < c0 ? s0 : r0) : s0, to = keys ? e1 : max(r1 + 1, c1);
   first = from / DOCS_TILE;
   return max(0, (to + DOCS_TILE - 1) / DOCS_TILE - first);
@@ -111,11 +117,8 @@ __device__ __forceinline__ void docs_lists(const DocsPlanArgs& a, const Start* s
   DocsUnit* units = a.t.list[list].units;
   DocsSpan* spans = a.t.list[list].spans;
   DocsSplit* splits = a.t.list[list].splits;
-  int live0 = 0, live1 = 0;
-  if (a.n_docs > 0) {
-    live0 = min(max(start[0], 0), a.T);
-    live1 = min(max(start[a.n_docs], live0), a.T);
-  }
+  int live0, live1;
+  docs_live(a, start, live0, live1);
   if (tid < 64) hist[tid] = 0;
   unsigned long long mine = 0;
   int top = 1, first0 = 0, tiles0 = 0, first;
@@ -229,7 +232,8 @@ __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
   const int32_t* start = a.start;
   const int lane = threadIdx.x & 63, r0 = ((blockIdx.x - DOCS_LISTS) * 4 + (threadIdx.x >> 6)) * 64, r = r0 + lane;
   if (r0 >= T) return;
-  int n = 0;  // starts at or before the lane's row
+  int n = 0, live0, live1;  // n: starts at or before the lane's row
+  docs_live(a, start, live0, live1);
   if (n_docs > 0) {
     int base = starts_upto(start, n_docs + 1, r0);
     n = base;
@@ -244,7 +248,7 @@ __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
   if (r >= T) return;
   int lo = r, hi = r, pre = r;
   if (n >= 1 && n <= n_docs) {
-    const int s = max(start[n - 1], 0), e = min(start[n], T);
+    const int s = max(start[n - 1], live0), e = min(start[n], live1);
     if (s <= r && r < e) {
       lo = s;
       hi = e;
