@@ -648,13 +648,13 @@ size_t dh_attn_ctx_bwd_workspace_bytes(int dtype, int batch, int seq, int q_off,
  * Packed micro-batches: one row of T tokens holds n_docs documents back to back and rows of padding around them.
  * Document n is rows doc_start[n] .. doc_start[n+1]-1; rows before doc_start[0] and from doc_start[n_docs] on belong to none.  A row
  * sees the rows of its document up to itself; with a prefix, the first prefix[n] rows of document n see one another whole.
- * doc_start and prefix are DEVICE arrays (they come with the micro-batch, no host round trip).  Documents may be empty.  Starts that do not ascend
- * leave it open which rows are of which document, and what these rows' results are; rows before doc_start[0] and from doc_start[n_docs] on are of none all the same, and nothing outside the
+ * doc_start and prefix are DEVICE arrays (they come with the micro-batch, no host round trip).  Documents may be empty.  Starts that do not ascend, or lie outside
+ * 0..T, leave it open which rows are of which document, and what these rows' results are; rows before doc_start[0] and from doc_start[n_docs] on are of none all the same, and nothing outside the
  * buffers is touched.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
   int T;                    /* rows of the buffers */
-  int n_docs;               /* documents, >= 0 */
+  int n_docs;               /* documents, 0 to 2^28 */
   int nq, nkv;              /* query and key/value heads of the attention that reads the table; nkv divides nq, T/64 * nq/nkv at most 2^30 */
   const int32_t* doc_start; /* device [n_docs+1], ascending */
   const int32_t* prefix;    /* device [n_docs] rows of each document's prefix (cut to its length), or NULL: none */

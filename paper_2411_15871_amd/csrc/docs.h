@@ -11,6 +11,7 @@
 // list of the forward pass, and one of dQ and one of dK and dV for heads of 128 and of 64 each: more blocks of the shorter heads are resident at once, and where the backward pass is one
 // launch its two kinds share the chip.
 #define DOCS_MAX_T (1 << 28)
+#define DOCS_MAX_DOCS (1 << 28)  // the plan's searches add two places among the starts in 32 bits
 #define DOCS_MAX_RUN (1 << 30)  // tiles that a block may meet, over the heads of a group: counted in 32 bits, as is the sum of two such counts
 #define DOCS_MAX_HEADS 1024
 #define DOCS_HEAD 16

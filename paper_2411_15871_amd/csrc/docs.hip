@@ -266,6 +266,7 @@ static int check_docs(const char* who, const dh_docs* docs) {
   if (docs->T < 0 || docs->n_docs < 0 || docs->nq <= 0 || docs->nkv <= 0 || docs->nq % docs->nkv)
     DH_FAIL(DH_ERR_SHAPE, "%s: T=%d n_docs=%d nq=%d nkv=%d", who, docs->T, docs->n_docs, docs->nq, docs->nkv);
   if (docs->T > DOCS_MAX_T || docs->nq > DOCS_MAX_HEADS) DH_FAIL(DH_ERR_SHAPE, "%s: T=%d nq=%d (at most %d and %d)", who, docs->T, docs->nq, DOCS_MAX_T, DOCS_MAX_HEADS);
+  if (docs->n_docs > DOCS_MAX_DOCS) DH_FAIL(DH_ERR_SHAPE, "%s: %d documents (at most %d)", who, docs->n_docs, DOCS_MAX_DOCS);
   if (((long long)docs->T / DOCS_TILE + 2) * (docs->nq / docs->nkv) > DOCS_MAX_RUN)
     DH_FAIL(DH_ERR_SHAPE, "%s: T=%d with %d query heads a group (T/64 times these at most 2^30)", who, docs->T, docs->nq / docs->nkv);
   if (docs->T > 0 && (!docs->table || (docs->n_docs > 0 && !docs->doc_start))) DH_FAIL(DH_ERR_INVALID_ARG, "%s: null pointer", who);
