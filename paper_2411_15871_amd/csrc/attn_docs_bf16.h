@@ -603,10 +603,13 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   }
 }
 
-// Delta and lse2 (with a cap: cap_log2 - lse2) of every row, as attn_bwd_prep_kernel: the numbers the dQ blocks use.
+// Delta and lse2 (with a cap: cap_log2 - lse2) of every row of a document, as attn_bwd_prep_kernel: the numbers the dQ blocks use.  Like these it stores nothing if the table
+// was made for other sizes; the table's entries are fetched beside the rows.
 template <int D, bool CAP>
-__global__ __launch_bounds__(64) void attn_docs_prep_kernel(const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout, const float* __restrict__ lse, float* __restrict__ lse2,
-                                                            float* __restrict__ delta, int T, int nq, float cap_log2) {
+__global__ __launch_bounds__(64) void attn_docs_prep_kernel(const DocsTiled p, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout, const float* __restrict__ lse, float* __restrict__ lse2,
+                                                            float* __restrict__ delta) {
+  const DocsView& v = p.a.v;
+  const int T = v.T, nq = p.a.nq;
   const size_t i = (size_t)blockIdx.x * 32 + (threadIdx.x >> 1);
   if (i >= (size_t)T * nq) return;
   const int kg = threadIdx.x & 1, h = (int)(i % nq);
@@ -614,6 +617,7 @@ __global__ __launch_bounds__(64) void attn_docs_prep_kernel(const bf16_t* __rest
   const bf16_t* orow = o + (t * nq + h) * D + kg * 8;
   const bf16_t* drow = dout + (t * nq + h) * D + kg * 8;
   const float l = lse[at] * LOG2E;
+  const bool ours = docs_fits(v, nq, p.a.nkv) & (v.hi[t] > v.lo[t]);
   bf16x8 a[D / 16], b[D / 16];
 #pragma unroll
   for (int ks = 0; ks < D / 16; ks++) {
@@ -626,9 +630,9 @@ __global__ __launch_bounds__(64) void attn_docs_prep_kernel(const bf16_t* __rest
 #pragma unroll
     for (int e = 0; e < 8; e++) half = fmaf((float)a[ks][e], (float)b[ks][e], half);
   const float other = __shfl_xor(half, 1, 64);
-  if (kg == 0) {
+  if (kg == 0 && ours) {
     delta[at] = half + other;
-    lse2[at] = CAP ? cap_log2 - l : l;
+    lse2[at] = CAP ? p.cap_log2 - l : l;
   }
 }
 // The two as launches of their own (dQ first: it stores the rows' statistics that the dK/dV blocks read), grids (units * nq) and (units * nkv) ...
@@ -757,7 +761,7 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   // 960 (16:4 x 6144) 262 and 261, 1024 (8 x 8192) 149 and 151, capped 174 and 184, 1536 (8:4 x 16384) 1763 and 1820, 2560 (32:8 x 8192) 691 and 777.  D = 64, where two fit either
   // way: 512 59.2 and 48.4, 1280 240 and 219, 4096 978 and 983; capped 1280 302 and 273, 2500 318 and 296, 4000 433 and 434.
   if (docs_one_launch(p.a.v.T, nq, nkv, D == 128 ? DOCS_ONE_128 : 4 * DOCS_ONE_64)) {
-    attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(o, dout, lse, lse2, delta, p.a.v.T, nq, p.cap_log2);
+    attn_docs_prep_kernel<D, CAP><<<(unsigned)(((size_t)p.a.v.T * nq + 31) / 32), 64, 0, stream>>>(p, o, dout, lse, lse2, delta);
     DH_LAUNCH_CHECK();
     attn_docs_bwd_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv + (unsigned)q.units * nq, AB_THREADS, lds_dkv, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q, part_kv);
     DH_LAUNCH_CHECK();

@@ -1,0 +1,54 @@
+"""Attention inside packed documents in forms that its other tests do not take: every launch form of the backward pass, tables for other sizes, more rows than one launch counts."""
+import pytest
+import torch
+
+import docs_ref as R
+from test_gpu_docs_attn import MARK, Packed
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dh():
+    from paper_2411_15871_amd import dhelix
+    assert torch.cuda.is_available()
+    yield dhelix
+    torch.cuda.empty_cache()
+
+
+def prepared(p):
+    p.qkv_d, p.dout_d = p.qkv.cuda(), p.dout.cuda()
+    p.buffers()
+    return p
+
+
+@pytest.mark.parametrize("dtype,nq,nkv,d", [("bf16", 2, 1, 128), ("bf16", 2, 2, 64), ("bf16", 64, 16, 128), ("f32", 2, 1, 64), ("f32", 2, 1, 256)])
+def test_delta_of_rows_of_no_document_stays(dh, dtype, nq, nkv, d):
+    """In one launch and in two; delta of the others is rowsum(dout o), a sum of d products."""
+    p = prepared(Packed(dh, dtype, T=2100 if nq == 64 else 200, nq=nq, nkv=nkv, d=d, lengths=[30, 0, 70, 50], first=9, seed=21))
+    dh.dh_docs_plan(p.docs)
+    p.forward()
+    p.backward()
+    torch.cuda.synchronize()
+    delta = p.delta.cpu()
+    assert bool((delta[:, ~p.live] == MARK).all())
+    do, o = (t.double().cpu().view(p.T, nq, d).transpose(0, 1) for t in (p.dout, p.o))
+    assert bool((((delta.double() - (do * o).sum(2)).abs() <= (d + 8) * R.W * (do * o).abs().sum(2))[:, p.live]).all())
+
+
+@pytest.mark.parametrize("dtype,nq,nkv,d", [("bf16", 4, 2, 64), ("bf16", 4, 2, 128), ("bf16", 64, 32, 128), ("f32", 4, 2, 64), ("f32", 4, 2, 256)])
+@pytest.mark.parametrize("other", ["heads", "rows"])
+def test_a_table_for_other_sizes_changes_nothing(dh, dtype, nq, nkv, d, other):
+    """Both passes, in one launch and in two, with a table for other heads or other rows in a buffer that holds either: every output is as it was."""
+    T = 1500 if nq == 64 else 300
+    p = Packed(dh, dtype, T=T, nq=nq, nkv=nkv, d=d, lengths=[T], seed=22)
+    p.table = torch.zeros(max(dh.dh_docs_table_bytes(T, nq, k) for k in (1, nkv, nq)), dtype=torch.uint8, device="cuda")
+    made = dh.docs(T if other == "heads" else T - 64, 1, nq, 1 if other == "heads" else nkv, p.start, None, None, p.table)
+    p.docs = dh.docs(T, 1, nq, nkv, p.start, None, None, p.table)
+    prepared(p)
+    dh.dh_docs_plan(made)
+    p.forward()
+    p.backward()
+    torch.cuda.synchronize()
+    for t in (p.o, p.lse, p.dqkv, p.delta):
+        assert bool((t == MARK).all())
