@@ -36,15 +36,19 @@ __device__ __forceinline__ void docs32_cols(ColFrag<DT>& c, const float* base, s
   }
 }
 
+// Tiles of a launch, 16 rows each: a launch's threads along x are counted in 32 bits (2^23 tiles of 512 threads no longer fit).  A longer micro-batch takes several
+// launches, of tiles from tile0 on.
+#define A32_TILES (1 << 22)
+
 // grid (16-row tiles, nq)
 template <int DT>
-__global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_fwd_f32_kernel(const DocsAttn a, const float* __restrict__ qkv, float* __restrict__ o, float* __restrict__ lse) {
+__global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_fwd_f32_kernel(const DocsAttn a, int tile0, const float* __restrict__ qkv, float* __restrict__ o, float* __restrict__ lse) {
   constexpr int A32_WAVES = a32_waves<DT>(), LD = DT * 16 + 4;
   __shared__ float ms[A32_WAVES][16], ls[A32_WAVES][16];
   extern __shared__ float os[];  // [16 queries][LD]
   const DocsView& v = a.v;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4, d = a.d, nq = a.nq, nkv = a.nkv, T = v.T;
-  const int h = blockIdx.y, hk = h / (nq / nkv), i0 = (gridDim.x - 1 - blockIdx.x) * 16, iq = i0 + l16, row = min(iq, T - 1), ld = (nq + 2 * nkv) * d;
+  const int h = blockIdx.y, hk = h / (nq / nkv), i0 = (tile0 + (int)(gridDim.x - 1 - blockIdx.x)) * 16, iq = i0 + l16, row = min(iq, T - 1), ld = (nq + 2 * nkv) * d;
   if (!docs_fits(v, nq, nkv)) return;
   const int live0 = v.head[DOCS_LIVE0], key_last = v.head[DOCS_LIVE1] - 1;
   const int lo = v.lo[row], hi = v.hi[row], end = max(iq + 1, v.pre[row]);
@@ -278,14 +282,14 @@ __device__ __forceinline__ void docs32_dkv(const Docs32Bwd& b, int tile_k, int h
 }
 // The two as launches of their own, grids (tiles, nq) and (tiles, nkv), and as one, grid (tiles, nkv + nq); see bwd_f32.
 template <int DT>
-__global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_dq_f32_kernel(const Docs32Bwd b) {
+__global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_dq_f32_kernel(const Docs32Bwd b, int tile0) {
   extern __shared__ float os[];
-  if (docs_fits(b.a.v, b.a.nq, b.a.nkv)) docs32_dq<DT>(b, gridDim.x - 1 - blockIdx.x, blockIdx.y, os);
+  if (docs_fits(b.a.v, b.a.nq, b.a.nkv)) docs32_dq<DT>(b, tile0 + (int)gridDim.x - 1 - blockIdx.x, blockIdx.y, os);
 }
 template <int DT>
-__global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_dkv_f32_kernel(const Docs32Bwd b) {
+__global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_dkv_f32_kernel(const Docs32Bwd b, int tile0) {
   extern __shared__ float os[];
-  if (docs_fits(b.a.v, b.a.nq, b.a.nkv)) docs32_dkv<DT, false>(b, blockIdx.x, blockIdx.y, os);
+  if (docs_fits(b.a.v, b.a.nq, b.a.nkv)) docs32_dkv<DT, false>(b, tile0 + blockIdx.x, blockIdx.y, os);
 }
 template <int DT>
 __global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_bwd_f32_kernel(const Docs32Bwd b) {
@@ -298,8 +302,11 @@ __global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_bwd_f32_kernel
 // ------------------------------------------------------------------------------------ host side
 template <int DT>
 static int docs_fwd_f32(const DocsAttn& a, const float* qkv, float* o, float* lse, hipStream_t stream) {
-  attn_docs_fwd_f32_kernel<DT><<<dim3((a.v.T + 15) / 16, a.nq), 64 * a32_waves<DT>(), 16 * (DT * 16 + 4) * sizeof(float), stream>>>(a, qkv, o, lse);
-  DH_LAUNCH_CHECK();
+  const int tiles = (a.v.T + 15) / 16;
+  for (int t = 0; t < tiles; t += A32_TILES) {
+    attn_docs_fwd_f32_kernel<DT><<<dim3(std::min(tiles - t, A32_TILES), a.nq), 64 * a32_waves<DT>(), 16 * (DT * 16 + 4) * sizeof(float), stream>>>(a, t, qkv, o, lse);
+    DH_LAUNCH_CHECK();
+  }
   return DH_OK;
 }
 int dh_launch_attn_docs_fwd_f32(const DocsAttn& a, const float* qkv, float* o, float* lse, hipStream_t stream) {
@@ -319,10 +326,14 @@ static int docs_bwd_f32(const Docs32Bwd& b, hipStream_t stream) {
       return DH_OK;
     }
   }
-  attn_docs_dq_f32_kernel<DT><<<dim3(tiles, nq), 64 * a32_waves<DT>(), lds_q, stream>>>(b);
-  DH_LAUNCH_CHECK();
-  attn_docs_dkv_f32_kernel<DT><<<dim3(tiles, nkv), 64 * a32_waves<DT>(), lds_k, stream>>>(b);
-  DH_LAUNCH_CHECK();
+  for (int t = 0; t < tiles; t += A32_TILES) {
+    attn_docs_dq_f32_kernel<DT><<<dim3(std::min(tiles - t, A32_TILES), nq), 64 * a32_waves<DT>(), lds_q, stream>>>(b, t);
+    DH_LAUNCH_CHECK();
+  }
+  for (int t = 0; t < tiles; t += A32_TILES) {  // behind all of dQ, which leaves the rows' delta
+    attn_docs_dkv_f32_kernel<DT><<<dim3(std::min(tiles - t, A32_TILES), nkv), 64 * a32_waves<DT>(), lds_k, stream>>>(b, t);
+    DH_LAUNCH_CHECK();
+  }
   return DH_OK;
 }
 int dh_launch_attn_docs_bwd_f32(const DocsAttn& a, const float* qkv, const float* o, const float* dout, const float* lse, float* dqkv, float* delta, hipStream_t stream) {

@@ -52,3 +52,35 @@ def test_a_table_for_other_sizes_changes_nothing(dh, dtype, nq, nkv, d, other):
     torch.cuda.synchronize()
     for t in (p.o, p.lse, p.dqkv, p.delta):
         assert bool((t == MARK).all())
+
+
+@pytest.mark.parametrize("first", [2 ** 26 - 60, 2 ** 27 - 100])
+def test_more_rows_than_a_launch_counts(dh, first):
+    """Float32, 2^27 + 200 rows: a block of 512 threads for every 16 rows passes 32 bits.  Two documents across the border of two launches."""
+    T, S, d, lengths, base = 2 ** 27 + 200, 256, 8, [100, 70], first - 16
+    g = torch.Generator().manual_seed(23)
+    qkv, dout = torch.randn((S, 3 * d), generator=g), torch.randn((S, d), generator=g)
+    lo, hi = R.tables(S, lengths, None, 16)
+    rows, live = slice(base, base + S), slice(16, 16 + sum(lengths))
+    Q, D, O, DQ = (torch.empty((T, n), device="cuda") for n in (3 * d, d, d, 3 * d))
+    Q[rows], D[rows] = qkv.cuda(), dout.cuda()
+    lse, delta = torch.full((1, T), MARK, device="cuda"), torch.full((1, T), MARK, device="cuda")
+    for t in (O, DQ):
+        t.fill_(MARK)
+    start = torch.tensor([first, first + 100, first + 170], dtype=torch.int32, device="cuda")
+    table = torch.empty(dh.dh_docs_table_bytes(T, 1, 1), dtype=torch.uint8, device="cuda")
+    docs = dh.docs(T, 2, 1, 1, start, None, None, table)
+    dh.dh_docs_plan(docs)
+    dh.dh_attn_docs_fwd(dh.DH_F32, docs, d, 0.0, Q, O, lse)
+    dh.dh_attn_docs_bwd(dh.DH_F32, docs, d, 0.0, Q, O, D, lse, DQ, delta)
+    torch.cuda.synchronize()
+    o, l, dq = O[rows].cpu(), lse[:, rows].cpu(), DQ[rows].cpu()
+    u = 2.0 ** -24
+    r = R.attention(S, 1, 1, d, 0.0, lo, hi, qkv, u)
+    b = R.attention(S, 1, 1, d, 0.0, lo, hi, qkv, u, dout=dout, o_in=o, lse_in=l)
+    for got, pair in ((o, r["o"]), (dq[:, :d], b["dq"]), (dq[:, d:2 * d], b["dk"]), (dq[:, 2 * d:], b["dv"]), (l.t(), [t[:, :, None] for t in r["lse"]])):
+        val, err = (t.transpose(0, 1).reshape(S, -1)[live] for t in pair)
+        assert bool(((got[live].double() - val).abs() <= err).all())
+    for t, n in ((O, d), (DQ, 3 * d), (lse.view(T, 1), 1), (delta.view(T, 1), 1)):
+        others = sum(int((part != MARK).sum()) for part in t.split(1 << 24))
+        assert others <= 170 * n and int((t[first:first + 170] != MARK).sum()) == others  # nothing outside the documents changed
