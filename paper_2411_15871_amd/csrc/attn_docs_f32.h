@@ -106,8 +106,8 @@ __global__ __launch_bounds__(64 * a32_waves<DT>()) void attn_docs_fwd_f32_kernel
   for (int w = 1; w < A32_WAVES; w++) M = fmaxf(M, ms[w][l16]);
 #pragma unroll
   for (int w = 0; w < A32_WAVES; w++) L += ls[w][l16] == 0.f ? 0.f : ls[w][l16] * expf(ms[w][l16] - M);
-  if (M == -INFINITY) L = NAN;  // every score the row sees is minus infinity (or a NaN): no softmax
-  const float f = l == 0.f && L == L ? 0.f : expf(m - M) / L;
+  // every score the row sees is minus infinity (or a NaN, whose L is one): no softmax, o is a NaN; lse is minus infinity, the logarithm of no weight at all
+  const float f = M == -INFINITY ? NAN : l == 0.f ? 0.f : expf(m - M) / L;
   for (int w = 0; w < A32_WAVES; w++) {  // the waves' shares, added in wave order
     if (wave == w) {
 #pragma unroll

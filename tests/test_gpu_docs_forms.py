@@ -84,3 +84,26 @@ def test_more_rows_than_a_launch_counts(dh, first):
     for t, n in ((O, d), (DQ, 3 * d), (lse.view(T, 1), 1), (delta.view(T, 1), 1)):
         others = sum(int((part != MARK).sum()) for part in t.split(1 << 24))
         assert others <= 170 * n and int((t[first:first + 170] != MARK).sum()) == others  # nothing outside the documents changed
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 256), ("f32", 24)])
+@pytest.mark.parametrize("length", [40, 900])
+def test_rows_whose_scores_are_all_minus_infinity(dh, dtype, d, length):
+    """The second document's keys are minus infinities against queries of ones: lse is minus infinity, o a NaN, whatever the type and whether rows are cut.  With a finite score beside
+    them (the last key) a row has that key's value alone."""
+    T = length + 60
+    p = Packed(dh, dtype, T=T, nq=2, nkv=1, d=d, lengths=[50, length], seed=24)
+    p.qkv[50:, 2 * d] = float("-inf")  # one element of every key
+    p.qkv[:, :2 * d] = 1.0
+    p.qkv[49 + length, 2 * d] = 0.5
+    prepared(p)
+    dh.dh_docs_plan(p.docs)
+    p.forward()
+    torch.cuda.synchronize()
+    o, lse = p.o.cpu().view(T, 2, d).float(), p.lse.cpu()
+    assert bool((lse[:, 50:49 + length] == float("-inf")).all()) and bool(torch.isnan(o[50:49 + length]).all())
+    last = 49 + length
+    k, v = p.qkv[last, 2 * d:3 * d].double(), p.qkv[last, 3 * d:].float()
+    x, size = float(k.sum()) / d ** 0.5, float(k.abs().sum()) / d ** 0.5
+    assert bool(((lse[:, last].double() - x).abs() <= (d + 16) * R.W * size + 2 ** -22).all()) and torch.equal(o[last], v.expand(2, d))
+    assert bool(torch.isfinite(o[:50]).all()) and bool(torch.isfinite(lse[:, :50]).all())
