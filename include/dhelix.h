@@ -660,6 +660,7 @@ typedef struct {
   const int32_t* prefix;    /* device [n_docs] rows of each document's prefix (cut to its length), or NULL: none */
   int32_t* pos;             /* device [T] written by dh_docs_plan: position in the row's document (0 for rows of none), or NULL */
   void* table;              /* device, dh_docs_table_bytes(T, nq, nkv) bytes, 16-byte aligned, written by dh_docs_plan */
+  size_t table_bytes;       /* bytes behind table; fewer than a call reads or writes: DH_ERR_WORKSPACE_TOO_SMALL */
 } dh_docs;
 size_t dh_docs_table_bytes(int T, int nq, int nkv);
 /* Fills table (and pos) from doc_start and prefix: once for a micro-batch, whose layers all read it. */

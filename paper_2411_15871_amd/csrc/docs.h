@@ -69,7 +69,7 @@ struct DocsList {
 struct DocsTable {
   int32_t *head, *lo, *hi, *pre;
   DocsList list[DOCS_LISTS];
-  size_t bytes;
+  size_t bytes, fwd_bytes;  // of the whole table, and of what the forward pass reads
 };
 static inline DocsTable docs_table(void* table, int T, int nq, int nkv) {
   DocsTable v;
@@ -87,6 +87,7 @@ static inline DocsTable docs_table(void* table, int T, int nq, int nkv) {
     l.spans = keys ? (DocsSpan*)take((size_t)l.cap.units * sizeof(DocsSpan)) : nullptr;
     l.splits = (DocsSplit*)take((size_t)l.cap.splits * sizeof(DocsSplit));
     l.counts = DOCS_COUNTS + 2 * i;
+    if (i == DOCS_Q) v.fwd_bytes = at;
   }
   v.bytes = at;
   return v;

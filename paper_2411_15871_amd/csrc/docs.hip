@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
   if (a.pos) a.pos[r] = r - lo;
 }
 
-static int check_docs(const char* who, const dh_docs* docs) {
+static int check_docs(const char* who, const dh_docs* docs, bool fwd) {  // fwd: the call reads the forward pass's part of the table alone
   if (!docs) DH_FAIL(DH_ERR_INVALID_ARG, "%s: null pointer", who);
   if (docs->T < 0 || docs->n_docs < 0 || docs->nq <= 0 || docs->nkv <= 0 || docs->nq % docs->nkv)
     DH_FAIL(DH_ERR_SHAPE, "%s: T=%d n_docs=%d nq=%d nkv=%d", who, docs->T, docs->n_docs, docs->nq, docs->nkv);
@@ -271,6 +271,11 @@ static int check_docs(const char* who, const dh_docs* docs) {
     DH_FAIL(DH_ERR_SHAPE, "%s: T=%d with %d query heads a group (T/64 times these at most 2^30)", who, docs->T, docs->nq / docs->nkv);
   if (docs->T > 0 && (!docs->table || (docs->n_docs > 0 && !docs->doc_start))) DH_FAIL(DH_ERR_INVALID_ARG, "%s: null pointer", who);
   if ((uintptr_t)docs->table & 15) DH_FAIL(DH_ERR_INVALID_ARG, "%s: table must be 16-byte aligned", who);
+  if (docs->T > 0) {
+    const DocsTable t = docs_table(nullptr, docs->T, docs->nq, docs->nkv);
+    const size_t need = fwd ? t.fwd_bytes : t.bytes;
+    if (docs->table_bytes < need) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "%s: table of %zu < %zu bytes", who, docs->table_bytes, need);
+  }
   return DH_OK;
 }
 
@@ -280,7 +285,7 @@ extern "C" size_t dh_docs_table_bytes(int T, int nq, int nkv) {
 }
 
 extern "C" int dh_docs_plan(const dh_docs* docs, void* stream) {
-  if (int rc = check_docs("docs_plan", docs)) return rc;
+  if (int rc = check_docs("docs_plan", docs, false)) return rc;
   if (docs->T == 0) return DH_OK;
   const DocsPlanArgs a = {docs->T, docs->n_docs, docs->nq, docs->nkv, docs->doc_start, docs->prefix, docs->pos, docs_table(docs->table, docs->T, docs->nq, docs->nkv)};
   docs_plan_kernel<<<DOCS_LISTS + (unsigned)(((size_t)docs->T + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
@@ -289,8 +294,8 @@ extern "C" int dh_docs_plan(const dh_docs* docs, void* stream) {
 }
 
 // ------------------------------------------------------------------------------------ entry points
-static int check_attn_docs(const char* who, int dtype, const dh_docs* docs, int d, float cap) {
-  if (int rc = check_docs(who, docs)) return rc;
+static int check_attn_docs(const char* who, bool fwd, int dtype, const dh_docs* docs, int d, float cap) {
+  if (int rc = check_docs(who, docs, fwd)) return rc;
   if (dtype != DH_F32 && dtype != DH_BF16) DH_FAIL(DH_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (dtype == DH_F32 && (d <= 0 || d % 8 || d > 256)) DH_FAIL(DH_ERR_SHAPE, "%s: head_dim %d must be a multiple of 8, at most 256", who, d);
   if (dtype == DH_BF16 && d != 64 && d != 128) DH_FAIL(DH_ERR_SHAPE, "%s: head_dim %d must be 64 or 128", who, d);
@@ -307,7 +312,7 @@ extern "C" size_t dh_attn_docs_fwd_workspace_bytes(int dtype, int T, int nq, int
 extern "C" size_t dh_attn_docs_bwd_workspace_bytes(int dtype, int T, int nq, int nkv, int d) { return sized(dtype, T, nq, nkv, d) ? dh_attn_docs_bwd_bf16_ws_bytes(T, nq, nkv, d) : 0; }
 
 extern "C" int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
-  if (int rc = check_attn_docs("attn_docs_fwd", dtype, docs, d, cap)) return rc;
+  if (int rc = check_attn_docs("attn_docs_fwd", true, dtype, docs, d, cap)) return rc;
   if (docs->T == 0 || docs->n_docs == 0) return DH_OK;
   if (!qkv || !o || !lse) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: null pointer");
   if (unaligned16(qkv) || unaligned16(o)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_fwd: qkv and o must be 16-byte aligned");
@@ -321,7 +326,7 @@ extern "C" int dh_attn_docs_fwd(int dtype, const dh_docs* docs, int d, float cap
 
 extern "C" int dh_attn_docs_bwd(int dtype, const dh_docs* docs, int d, float cap, const void* qkv, const void* o, const void* dout, const float* lse, void* dqkv, float* delta,
                                 void* ws, size_t ws_bytes, void* stream) {
-  if (int rc = check_attn_docs("attn_docs_bwd", dtype, docs, d, cap)) return rc;
+  if (int rc = check_attn_docs("attn_docs_bwd", false, dtype, docs, d, cap)) return rc;
   if (docs->T == 0 || docs->n_docs == 0) return DH_OK;
   if (!qkv || !o || !dout || !lse || !dqkv || !delta) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: null pointer");
   if (unaligned16(qkv) || unaligned16(o) || unaligned16(dout) || unaligned16(dqkv)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_docs_bwd: qkv, o, dout and dqkv must be 16-byte aligned");

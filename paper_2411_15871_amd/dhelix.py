@@ -129,7 +129,7 @@ class dh_plan(C.Structure):
 _P, _I, _Z, _D, _F = C.c_void_p, C.c_int, C.c_size_t, C.c_double, C.c_float
 class dh_docs(C.Structure):
     _fields_ = [("T", C.c_int), ("n_docs", C.c_int), ("nq", C.c_int), ("nkv", C.c_int), ("doc_start", C.c_void_p), ("prefix", C.c_void_p),
-                ("pos", C.c_void_p), ("table", C.c_void_p)]
+                ("pos", C.c_void_p), ("table", C.c_void_p), ("table_bytes", C.c_size_t)]
 
 
 class dh_tensor(C.Structure):
@@ -822,9 +822,11 @@ FWD_OPS = op_names(DH_ARCH_LLAMA, 0)
 BWD_OPS = op_names(DH_ARCH_LLAMA, 1)
 
 
-def docs(T, n_docs, nq, nkv, doc_start, prefix, pos, table):
-    """dh_docs of a packed micro-batch; the tensors have to outlive it."""
-    return dh_docs(T, n_docs, nq, nkv, _ptr(doc_start), _ptr(prefix), _ptr(pos), _ptr(table))
+def docs(T, n_docs, nq, nkv, doc_start, prefix, pos, table, table_bytes=None):
+    """dh_docs of a packed micro-batch; the tensors have to outlive it.  table_bytes None: those of the tensor; behind a plain address as many as are needed."""
+    if table_bytes is None:
+        table_bytes = table.numel() * table.element_size() if isinstance(table, torch.Tensor) else lib.dh_docs_table_bytes(T, nq, nkv)
+    return dh_docs(T, n_docs, nq, nkv, _ptr(doc_start), _ptr(prefix), _ptr(pos), _ptr(table), table_bytes)
 
 
 def dh_docs_table_bytes(T, nq, nkv):
