@@ -20,8 +20,8 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument",
          "-Wno-unknown-warning-option", "-Wno-inline-asm"]
 # Per-source additions.  attn_bf16.hip: matrix instructions issued through the intrinsic write ordinary registers
-# (its long-lived accumulators are placed in AGPRs by hand); no NaN ever enters a max/min there.
-EXTRA_FLAGS = {"attn_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
+# (its long-lived accumulators are placed in AGPRs by hand).
+EXTRA_FLAGS = {"attn_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _deps_mtime():

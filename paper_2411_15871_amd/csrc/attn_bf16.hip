@@ -170,6 +170,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 
 #define LOG2E 1.4426950408889634f
+// The larger and the smaller of two, a NaN if either is one, in one instruction for two or three operands.  (fmaxf skips NaNs, and quiets its operands with an instruction
+// each unless the file is built on the promise that none is a NaN.  That cannot be promised, for tokens and gradients may hold NaNs, and under it a test for NaNs may be dropped.)
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float min_of(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 #define MFMA(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0)
 
 // acc += A * B with the accumulator held in the accumulation half of the register file (AGPRs) for the whole
@@ -625,10 +629,10 @@ __device__ __forceinline__ void attn_fwd_pinned(char* smem, const char* kbase, c
     pf[x >> 2][2 * (x & 3) + 1] = (bf16_t)s[x >> 3][2 * (x & 7) + 1];
   };
   auto max2 = [&](const Scores& s, int x) {
-    const float v = fmaxf(s[x >> 3][2 * (x & 7)], s[x >> 3][2 * (x & 7) + 1]);
-    mx = x == 0 ? v : fmaxf(mx, v);
+    const float v = max_of(s[x >> 3][2 * (x & 7)], s[x >> 3][2 * (x & 7) + 1]);
+    mx = x == 0 ? v : max_of(mx, v);
   };
-  auto larger = [](float a, float b) { return fmaxf(a, b); };
+  auto larger = [](float a, float b) { return max_of(a, b); };
   auto sum = [](float a, float b) { return a + b; };
   auto mask = [&](Scores& s, int t) {  // the tile crosses the diagonal for this wave: no key above the row
     if (t * AB_KT + AB_KT - 1 <= iw) return;
@@ -653,7 +657,7 @@ __device__ __forceinline__ void attn_fwd_pinned(char* smem, const char* kbase, c
 #pragma unroll
   for (int x = 0; x < 16; x++) max2(sa, x);
   mx = across_halves(mx, larger);
-  m = fmaxf(-INFINITY, mx * scale_log2);  // finite: the unit's first key is visible to every row
+  m = max_of(-INFINITY, mx * scale_log2);  // finite: the unit's first key is visible to every row
   l = 0.f;
   dma_wait<0>();
   __syncthreads();  // V(t0), K(t0+1)
@@ -671,7 +675,7 @@ __device__ __forceinline__ void attn_fwd_pinned(char* smem, const char* kbase, c
     const float mnew = mx * scale_log2;
     if (__any(mnew > m + AF_TAU)) {
       mfma_acc_settle(ot);
-      const float mn = fmaxf(m, mnew);
+      const float mn = max_of(m, mnew);
       const float alpha = fast_exp2(m - mn);
       l *= alpha;
       m = mn;
@@ -918,15 +922,15 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_fwd_bf16_kernel(const Attn
         for (int r = 0; r < 16; r++)
           if (kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) > iq) st[mt][r] = -INFINITY;
     }
-    float mx = fmaxf(st[0][0], st[1][0]);
+    float mx = max_of(st[0][0], st[1][0]);
 #pragma unroll
-    for (int r = 1; r < 16; r++) mx = fmaxf(mx, fmaxf(st[0][r], st[1][r]));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    for (int r = 1; r < 16; r++) mx = max_of(mx, max_of(st[0][r], st[1][r]));
+    mx = max_of(mx, __shfl_xor(mx, 32, 64));
     // The reference maximum moves as in attn_fwd_pinned.
     const float mnew = mx * scale_log2;  // finite from the unit's first tile on: its first key is visible to every row
     float rs = 0.f;
     if (__any(mnew > m + AF_TAU)) {
-      const float mn = fmaxf(m, mnew);
+      const float mn = max_of(m, mnew);
       const float alpha = fast_exp2(m - mn);
       l *= alpha;
       m = mn;
@@ -978,7 +982,7 @@ __global__ __launch_bounds__(256) void attn_fwd_combine_kernel(int seq, int q_of
   const int c0 = (threadIdx.x & 15) * CPT;
   const float* ml = part_ml + (unit0 * 128 + r) * 2;
   float M = -INFINITY;
-  for (int c = 0; c < nchunks; c++) M = fmaxf(M, ml[(size_t)c * 256]);
+  for (int c = 0; c < nchunks; c++) M = max_of(M, ml[(size_t)c * 256]);
   float L = 0.f, acc[CPT];
 #pragma unroll
   for (int i = 0; i < CPT; i++) acc[i] = 0.f;

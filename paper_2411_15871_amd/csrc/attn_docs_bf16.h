@@ -144,7 +144,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
         for (int r = 0; r < 16; r++)
           st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : CAP ? INFINITY : -INFINITY;
     }
-    auto larger = [](float a, float b) { return CAP ? fminf(a, b) : fmaxf(a, b); };  // of the scores: the smaller r
+    auto larger = [](float a, float b) { return CAP ? min_of(a, b) : max_of(a, b); };  // of the scores: the smaller r
     float mx = larger(st[0][0], st[1][0]);
 #pragma unroll
     for (int r = 1; r < 16; r++) mx = larger(mx, larger(st[0][r], st[1][r]));
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
     const float scale = CAP ? -2.f * p.cap_log2 : p.exp_scale, mnew = CAP ? fmaf(scale, mx, p.cap_log2) : mx * scale;
     float rs = 0.f;
     if (__any(mnew > m + AF_TAU)) {  // the reference maximum moves where a row's probabilities would grow beyond 2^AF_TAU
-      const float mn = fmaxf(m, mnew);
+      const float mn = max_of(m, mnew);
       const float alpha = fast_exp2(m - mn);
       l *= alpha;
       m = mn;
@@ -242,13 +242,13 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
   const size_t unit = ((size_t)s.slot * nq + h) * DOCS_BLOCK + r, step = (size_t)nq * DOCS_BLOCK;  // rows of the first unit's partial result, and to the next unit's
   float M = -3.0e38f;
 #pragma unroll 8
-  for (int c = 0; c < s.n; c++) M = fmaxf(M, part_ml[(unit + c * step) * 2]);
+  for (int c = 0; c < s.n; c++) M = max_of(M, part_ml[(unit + c * step) * 2]);
   float L = 0.f, acc[CPT];
 #pragma unroll
   for (int e = 0; e < CPT; e++) acc[e] = 0.f;
   for (int c = 0; c < s.n; c++) {
     const float lc = part_ml[(unit + c * step) * 2 + 1];
-    if (__builtin_bit_cast(uint32_t, lc) == 0) continue;  // this unit's tiles hold no key of the row (by its bits: this file is built without comparisons of NaNs)
+    if (lc == 0.f) continue;  // this unit's tiles hold no key of the row
     const float w = exp2f(part_ml[(unit + c * step) * 2] - M);
     L += w * lc;
     const float* po = part_o + (unit + c * step) * D + c0;

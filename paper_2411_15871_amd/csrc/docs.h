@@ -164,7 +164,7 @@ __device__ __forceinline__ void docs_row_fwd(const T* q, const T* k, const T* v,
     float slope, y = on ? docs_capped(docs_dot(q, k + (size_t)(j + lane) * ld, d) * scale, cap, slope) : -INFINITY;
     const float mn = fmaxf(m, wave_max(y));
     const float a = mn == -INFINITY ? 1.f : expf(m - mn);
-    const float p = __builtin_bit_cast(uint32_t, y) == 0xff800000u ? 0.f : expf(y - mn);  // minus infinity by its bits: some callers are built without comparisons of NaNs
+    const float p = y == -INFINITY ? 0.f : expf(y - mn);
     l = l * a + wave_sum(p);
 #pragma unroll
     for (int c = 0; c < 4; c++) acc[c] *= a;
