@@ -58,15 +58,15 @@ __device__ __forceinline__ void docs_shift(TilePtrs<D>& p, int bytes) {
 #pragma unroll
   for (int dt = 0; dt < D / 32; dt++) { by(p.t0[dt]); by(p.t1[dt]); }
 }
-// Whether any of N accumulator tiles holds an infinity or a NaN.
+// Whether any of N accumulator tiles holds an infinity or a NaN.  (__builtin_bit_cast of an element of a vector takes the vector's first one: elements are read as numbers.)
 template <int N>
 __device__ __forceinline__ bool docs_not_finite(const f32x16 (&t)[N]) {
-  uint32_t m = 0;
+  float m = 0.f;
 #pragma unroll
   for (int i = 0; i < N; i++)
 #pragma unroll
-    for (int r = 0; r < 16; r++) m = max(m, __builtin_bit_cast(uint32_t, t[i][r]) & 0x7fffffffu);
-  return m >= 0x7f800000u;
+    for (int r = 0; r < 16; r++) m = max_of(m, __builtin_fabsf(t[i][r]));
+  return !(m < INFINITY);
 }
 // r of a score under the cap, k = exp_scale.
 __device__ __forceinline__ float docs_cap_r(float s, float k) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k)); }
