@@ -669,7 +669,8 @@ int dh_docs_plan(const dh_docs* docs, void* stream);
 /* Grouped-query attention inside documents.  Layouts as dh_attn_fwd / dh_attn_bwd: qkv[T,(nq+2nkv)d] (already rotated), o[T,nq*d], lse[nq,T],
  * delta[nq,T]; docs as dh_docs_plan has filled it.  cap 0.001 to 1000: every scaled score x counts as cap * tanh(x / cap); 0: as it is.  Rows of no document are
  * left as they were, in o, lse, dqkv and delta alike, whatever they hold.  The host does not see the table: kernels that find one made for another T or other heads write nothing, and the
- * call is DH_OK.  What a row does not see does not reach its results, infinities and NaNs among it.
+ * call is DH_OK.  What a row does not see does not reach its results, infinities and NaNs among it (in
+ * results of which no element is finite it is open which of the two each holds).  DH_BF16: 32 rows next to such values take a second, slower walk over what they see.
  * A row all of whose scores are minus infinity has lse minus infinity and an o of NaNs.
  * d: multiple of 8 up to 256 for DH_F32, 64 or 128 for DH_BF16.  qkv, o, dout, dqkv: 16-byte aligned.  ws: device workspace of the _workspace_bytes
  * queries, 16-byte aligned (fewer bytes: DH_ERR_WORKSPACE_TOO_SMALL); T up to 2^28, nq up to 1024.  Backward writes dqkv (dk, dv summed over the query heads of a group in a fixed order) and delta. */

@@ -5,9 +5,9 @@
 // tiles that some row of the wave does not see whole are masked.  The runs come from the lists that dh_docs_plan has made (docs.h): longest first, long ones cut, partial
 // results merged in order by a launch behind.
 //
-// Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN: a wave whose result is not finite makes the rows
-// concerned again, one at a time, over exactly what they see (docs_row_*).  Rows outside all documents enter no tile, transfers take the nearest row of a document instead,
-// and what a lane makes of such a row of its own goes nowhere.
+// Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN.  A wave whose result is not finite looks whether its masked tiles hold any
+// such row; only then it walks its tiles again (docs_again_*), with the infinities and NaNs of masked tiles added to the rows that see them alone.  Rows outside all documents enter
+// no tile, transfers take the nearest row of a document instead, and what a lane makes of such a row of its own goes nowhere.
 //
 // CAP: x = cap tanh(x / cap) as cap - 2 cap r with r = 1 / (1 + e^(2x/cap)), one exponential and one reciprocal more an element, whose limits (r = 0, 1) are right where the
 // exponential is infinite or zero; its slope is 4 (r - r r), off by at most 2^-22, of which the factor 4 waits for the end.  The exponent of 2 of a probability is
@@ -68,9 +68,240 @@ __device__ __forceinline__ bool docs_not_finite(const f32x16 (&t)[N]) {
     for (int r = 0; r < 16; r++) m = max_of(m, __builtin_fabsf(t[i][r]));
   return !(m < INFINITY);
 }
+
+// ---- Results that are not finite.  What follows is a wave's own and stands behind its stores: it finds out which of its 32 rows may hold what they do not see, and makes these again.  One
+// tile at a time, in the LDS where the rows have left through.  Nothing of it may lengthen the tile loops: lane numbers are taken anew (docs_lane), accumulators are its own.
+#define DOCS_ODD 0x7f80u    // bits without the sign from which on a bf16 number is an infinity or a NaN
+#define DOCS_LARGE 0x5d80u  // 2^60: products of two smaller ones, summed over a head, are finite
+__device__ __forceinline__ int docs_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+// A scalar taken anew: with more vector arithmetic hanging off the tile loop's own, the compiler keeps those in vector registers, which transfers do not take.
+__device__ __forceinline__ int docs_scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// 64 rows of D columns from row0 on, clamped to [first, last]; base: their columns of row 0.
+struct DocsRows {
+  const bf16_t* base;
+  size_t ld;
+  int first, last;
+  __device__ __forceinline__ const bf16_t* row(int i) const { return base + (size_t)max(first, min(i, last)) * ld; }
+};
+// Bit r: row r of the 64 holds a number of bits `large` or more; holds nothing but infinities and NaNs.
+struct DocsOdd { uint64_t some, all; };
+template <int D>
+__device__ __forceinline__ DocsOdd docs_odd(const DocsRows& rows, int row0, uint32_t large) {
+  const uint4* x = reinterpret_cast<const uint4*>(rows.row(row0 + docs_lane()));
+  uint32_t top = 0, low = 0x7fffu;
+#pragma unroll 2
+  for (int c = 0; c < D / 8; c++) {
+    const uint4 v = x[c];
+    auto word = [&](uint32_t w) {
+      const uint32_t a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
+      top = max(top, max(a, b));
+      low = min(low, min(a, b));
+    };
+    word(v.x); word(v.y); word(v.z); word(v.w);
+  }
+  return {__ballot(top >= large), __ballot(low >= DOCS_ODD)};
+}
+// Of the 64 rows from row0 on: those in the lane's interval.
+__device__ __forceinline__ uint64_t docs_bits(const DocsSeen& see, int row0) {
+  const int a = max(see.at - row0, 0), b = min(see.at + see.n - row0, 64);
+  return a < b ? (~0ull >> (64 - (b - a))) << a : 0;
+}
+__device__ __forceinline__ bool docs_masked(const DocsSeen& see, int row0) { return row0 < see.all0 || row0 + AB_KT > see.all1; }
+// x where bit `bit` of `seen` is set, else zero, without a comparison (32 of these ahead of their use take more scalar registers than there are).
+__device__ __forceinline__ float docs_where(uint32_t seen, int bit, float x) {
+  return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & (uint32_t)__builtin_amdgcn_sbfe((int)seen, bit, 1));
+}
+// Between accesses to the wave's LDS in different layouts: they stay in order.
+__device__ __forceinline__ void docs_wave_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+// f(first row) for the tiles [f0, f1) that some row of the wave sees.
+template <class F>
+__device__ __forceinline__ void docs_again_tiles(const DocsSeen& see, int f0, int f1, F f) {
+#pragma unroll 1
+  for (int t = max(f0, see.any0 / AB_KT); t < f1 && t * AB_KT < see.any1; t++) f(t * AB_KT);
+}
+// 64 rows from row0 on to a tile as a transfer lays it out; clean: zeros in the place of infinities and NaNs.
+template <int D>
+__device__ __forceinline__ void docs_again_load(char* tile, const DocsRows& rows, int row0, bool clean) {
+  using TL = ATile<D>;
+  const uint32_t least = clean ? DOCS_ODD : 0x8000u;
+  docs_wave_order();
+#pragma unroll 2
+  for (int i = docs_lane(); i < AB_KT * TL::CPR; i += 64) {
+    const int r = i / TL::CPR, c = (i % TL::CPR) * 8;
+    uint4 v = *reinterpret_cast<const uint4*>(rows.row(row0 + r) + c);
+    auto word = [&](uint32_t w) { return ((w & 0x7fffu) >= least ? 0u : w & 0xffffu) | (((w >> 16) & 0x7fffu) >= least ? 0u : w & 0xffff0000u); };
+    v = make_uint4(word(v.x), word(v.y), word(v.z), word(v.w));
+    *reinterpret_cast<uint4*>(tile + TL::off(r, c) * 2) = v;
+  }
+  docs_wave_order();
+}
+// Score tiles of the 64 rows from row0 on against the lane's own row.
+template <int D>
+__device__ __forceinline__ void docs_again_scores(f32x16 (&st)[2], char* tile, const DocsRows& rows, int row0, const bf16_t* own, bool valid) {
+  docs_again_load<D>(tile, rows, row0, false);
+  const int lane = docs_lane(), l32 = lane & 31, kg = lane >> 5;
+  bf16x8 b[D / 16];
+  load_row_frags<D>(b, own, valid, kg);
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) st[mt][r] = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) {
+    const lds_char* at = (const lds_char*)tile + ATile<D>::off(l32, ks * 16 + kg * 8) * 2;
+    st[0] = MFMA(lds_frag(at, 0), b[ks], st[0]);
+    st[1] = MFMA(lds_frag(at, 32 * ATile<D>::LD * 2), b[ks], st[1]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// acc += rows^T w over 64 rows: w[mt][r] is the lane's weight of row 32 mt + 8 (r / 4) + 4 kg + r % 4.  In a masked tile the infinities and NaNs stay out of the products; those of its
+// rows are added to the lanes that see them, one row at a time.
+template <int D>
+__device__ __forceinline__ void docs_again_add(f32x16 (&acc)[D / 32], const f32x16 (&w)[2], char* tile, const DocsRows& rows, int row0, const DocsSeen& see) {
+  uint64_t odd = docs_masked(see, row0) ? docs_odd<D>(rows, row0, DOCS_ODD).some : 0;
+  docs_again_load<D>(tile, rows, row0, odd != 0);
+  const int lane = docs_lane(), kg = lane >> 5;
+  FragAddr<D> fa;
+  fa.init(lane);
+  const lds_char* sm = (const lds_char*)tile;
+#pragma unroll
+  for (int g = 0; g < 4; g++) {
+    const bf16x8 pf = pack_rows(w[g >> 1], g & 1);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++) acc[dt] = MFMA(lds_frag_tr(sm + fa.tr0[dt], sm + fa.tr1[dt], g * 16 * ATile<D>::LD * 2), pf, acc[dt]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (odd == 0) return;
+  docs_wave_order();
+  float* weights = reinterpret_cast<float*>(tile) + (lane & 31);  // [64 rows][32 lanes], in the place of the tile
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) weights[(32 * mt + 8 * (r >> 2) + 4 * kg + (r & 3)) * 32] = w[mt][r];
+  docs_wave_order();
+  const uint64_t seen = docs_bits(see, row0);
+#pragma unroll 1
+  for (; odd != 0; odd &= odd - 1) {
+    const int j = __builtin_ctzll(odd);
+    const float x = weights[j * 32];
+    const bool on = (seen >> j) & 1;
+    const bf16_t* row = rows.row(row0 + j) + 4 * kg;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++) {
+#pragma unroll
+      for (int q4 = 0; q4 < 4; q4++) {
+        const bf16x4 v = *reinterpret_cast<const bf16x4*>(row + dt * 32 + 8 * q4);
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          if (on && !__builtin_isfinite((float)v[e])) acc[dt][4 * q4 + e] = fmaf(x, (float)v[e], acc[dt][4 * q4 + e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+// The lane's row (its half of the columns) times f to `to`, float32 or bf16.
+template <int D, typename T>
+__device__ __forceinline__ void docs_again_out(const f32x16 (&acc)[D / 32], float f, T* to, bool on) {
+  to += 4 * (docs_lane() >> 5);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++)
+      if (on) to[dt * 32 + 8 * (r >> 2) + (r & 3)] = from_f32<T>(acc[dt][r] * f);
+}
 // r of a score under the cap, k = exp_scale.
 __device__ __forceinline__ float docs_cap_r(float s, float k) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k)); }
 // ================================================================================ forward
+// The tile's scores become probabilities; running maximum m, sum l and accumulators follow.
+template <int D, bool CAP, bool AGAIN>
+__device__ __forceinline__ void docs_softmax(const DocsTiled& p, const DocsSeen& see, int kb, int kg, f32x16 (&st)[2], f32x16 (&ot)[D / 32], float& m, float& l) {
+  if constexpr (CAP) {
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) st[mt][r] = docs_cap_r(st[mt][r], p.exp_scale);
+  }
+  if (docs_masked(see, kb)) {
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : CAP ? INFINITY : -INFINITY;
+        if constexpr (AGAIN || (CAP && D == 64)) { if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0); }  // (32 comparisons ahead of their use take more scalar registers than there are)
+      }
+  }
+  auto larger = [](float a, float b) { return CAP ? min_of(a, b) : max_of(a, b); };  // of the scores: the smaller r
+  float mx = larger(st[0][0], st[1][0]);
+#pragma unroll
+  for (int r = 1; r < 16; r++) mx = larger(mx, larger(st[0][r], st[1][r]));
+  mx = larger(mx, __shfl_xor(mx, 32, 64));
+  const float scale = CAP ? -2.f * p.cap_log2 : p.exp_scale, mnew = CAP ? fmaf(scale, mx, p.cap_log2) : mx * scale;
+  float rs = 0.f;
+  if (__any(mnew > m + AF_TAU)) {  // the reference maximum moves where a row's probabilities would grow beyond 2^AF_TAU
+    const float mn = max_of(m, mnew);
+    const float alpha = fast_exp2(m - mn);
+    l *= alpha;
+    m = mn;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) ot[dt][r] *= alpha;
+  }
+  const float off = CAP ? p.cap_log2 - m : -m;
+#pragma unroll
+  for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+      const float x = fast_exp2(fmaf(st[mt][r], scale, off));
+      st[mt][r] = x;
+      rs += x;
+    }
+  rs += __shfl_xor(rs, 32, 64);
+  l += rs;
+}
+// The rows `bad` of a wave again where they may hold what they do not see.  A row whose sum is a NaN has seen one among its scores (each of its results is one) and is not asked for; the
+// others are right as they are unless a masked tile holds an infinity or a NaN that they do not see, or a row sees there a key that makes each of its results one or the other.
+// q, o, lse: of the wave's first row, part_o, part_ml: likewise, of a unit with a slot.
+template <int D, bool CAP>
+__device__ __forceinline__ void docs_again_fwd(const DocsTiled& p, const DocsSeen& see, bool bad, const DocsUnit& u, const DocsRows& k, const DocsRows& v, const bf16_t* q, size_t ld, bf16_t* o,
+                                               size_t ldo, float* lse, float* part_o, float* part_ml, char* tile) {
+  bool arrives = false, none = false;
+  docs_again_tiles(see, u.f0, u.f1, [&](int kb) {
+    if (!docs_masked(see, kb)) return;
+    const DocsOdd odd = docs_odd<D>(v, kb, DOCS_ODD);
+    const uint64_t seen = docs_bits(see, kb);
+    arrives |= (odd.some & ~seen) != 0;
+    none |= (odd.all & seen) != 0;
+  });
+  const uint64_t rows = __ballot(bad && arrives && !none);
+  if (rows == 0) return;
+  const int lane = docs_lane(), r = lane & 31;
+  float m = -3.0e38f, l = 0.f;
+  f32x16 ot[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(ot[dt]);
+  docs_again_tiles(see, u.f0, u.f1, [&](int kb) {
+    f32x16 st[2];
+    docs_again_scores<D>(st, tile, k, kb, q + (see.n > 0 ? r : 0) * ld, see.n > 0);
+    docs_softmax<D, CAP, true>(p, see, kb, lane >> 5, st, ot, m, l);
+    docs_again_add<D>(ot, st, tile, v, kb, see);
+  });
+  const bool on = ((rows | rows >> 32) >> r) & 1;
+  if (u.slot >= 0) {
+    docs_again_out<D>(ot, 1.f, part_o + (size_t)r * D, on);
+    if (on) { part_ml[r * 2] = m; part_ml[r * 2 + 1] = l; }
+  } else {
+    docs_again_out<D>(ot, 1.f / l, o + r * ldo, on);
+    if (on) lse[r] = (m + log2f(l)) * 0.6931471805599453f;
+  }
+}
 // grid (units * nq)
 template <int D, bool CAP>
 __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o, float* __restrict__ lse,
@@ -131,47 +362,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
     Vp.set(sm + (AF_RING + slot) * TL::BYTES, fa);
     f32x16 st[2];
     score_tiles<D>(st, Kp, qf);
-    if constexpr (CAP) {
-#pragma unroll
-      for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) st[mt][r] = docs_cap_r(st[mt][r], p.exp_scale);
-    }
-    if (kb < see.all0 || kb + AB_KT > see.all1) {
-#pragma unroll
-      for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-        for (int r = 0; r < 16; r++)
-          st[mt][r] = (uint32_t)(kb + mt * 32 + 8 * (r >> 2) + 4 * kg + (r & 3) - see.at) < (uint32_t)see.n ? st[mt][r] : CAP ? INFINITY : -INFINITY;
-    }
-    auto larger = [](float a, float b) { return CAP ? min_of(a, b) : max_of(a, b); };  // of the scores: the smaller r
-    float mx = larger(st[0][0], st[1][0]);
-#pragma unroll
-    for (int r = 1; r < 16; r++) mx = larger(mx, larger(st[0][r], st[1][r]));
-    mx = larger(mx, __shfl_xor(mx, 32, 64));
-    const float scale = CAP ? -2.f * p.cap_log2 : p.exp_scale, mnew = CAP ? fmaf(scale, mx, p.cap_log2) : mx * scale;
-    float rs = 0.f;
-    if (__any(mnew > m + AF_TAU)) {  // the reference maximum moves where a row's probabilities would grow beyond 2^AF_TAU
-      const float mn = max_of(m, mnew);
-      const float alpha = fast_exp2(m - mn);
-      l *= alpha;
-      m = mn;
-#pragma unroll
-      for (int dt = 0; dt < D / 32; dt++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) ot[dt][r] *= alpha;
-    }
-    const float off = CAP ? p.cap_log2 - m : -m;
-#pragma unroll
-    for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        const float x = fast_exp2(fmaf(st[mt][r], scale, off));
-        st[mt][r] = x;
-        rs += x;
-      }
-    rs += __shfl_xor(rs, 32, 64);
-    l += rs;
+    docs_softmax<D, CAP, false>(p, see, kb, kg, st, ot, m, l);
 #pragma unroll
     for (int mt = 0; mt < 2; mt++)
 #pragma unroll
@@ -183,9 +374,8 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
       }
   }
   __syncthreads();  // every wave is done with the K/V rings: their LDS serves the output turn
-  const bool bad = live && (docs_not_finite<D / 32>(ot) || !(__builtin_bit_cast(uint32_t, l) < 0x7f800000u));
-  const uint64_t both = __ballot(bad), alive = __ballot(live);
-  const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
+  const bool bad = live && docs_not_finite<D / 32>(ot) && l < INFINITY;
+  const uint32_t store = (uint32_t)__ballot(live);
   float* prow = part_o + ((size_t)u.slot * nq + h) * DOCS_BLOCK * D + (size_t)wave * 32 * D;
   float* pml = part_ml + (((size_t)u.slot * nq + h) * DOCS_BLOCK + wave * 32) * 2;
   bf16_t* orow = o + (size_t)iw * nq * D + (size_t)h * D;
@@ -207,23 +397,11 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
         [&](int r) { return (store >> r) & 1 ? orow + (size_t)r * nq * D : nullptr; });
     if (lane < 32 && (store >> lane) & 1) lrow[l32] = (m + log2f(l)) * 0.6931471805599453f;
   }
-  for (uint32_t rest = again; rest != 0; rest &= rest - 1) {
-    const int r = __builtin_ctz(rest), i = iw + r, j0 = max(__builtin_amdgcn_readlane(lo, r), u.f0 * AB_KT), j1 = min(__builtin_amdgcn_readlane(end, r), u.f1 * AB_KT);
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, mr = -INFINITY, lr = 0.f;
-    docs_row_fwd(qkv + (size_t)i * ld + (size_t)h * D, kcol, kcol + (size_t)nkv * D, (size_t)ld, j0, j1, D, p.a.scale, p.a.cap, acc, mr, lr);
-#pragma unroll
-    for (int c = 0; c < D / 64; c++) {
-      if (u.slot >= 0) prow[(size_t)r * D + lane + 64 * c] = acc[c];
-      else orow[(size_t)r * nq * D + lane + 64 * c] = (bf16_t)(acc[c] / lr);
-    }
-    if (lane == 0) {
-      if (u.slot >= 0) {
-        pml[r * 2] = j0 < j1 ? mr * LOG2E : -3.0e38f;
-        pml[r * 2 + 1] = lr;
-      } else {
-        lrow[r] = mr + logf(lr);
-      }
-    }
+  if (__any(bad)) {
+    const int first = docs_scalar(live0), last = docs_scalar(live1) - 1;
+    const DocsUnit unit = {0, docs_scalar(u.f0), docs_scalar(u.f1), docs_scalar(u.slot)};
+    const DocsRows k = {kcol, (size_t)ld, first, last}, v = {kcol + (size_t)nkv * D, (size_t)ld, first, last};
+    docs_again_fwd<D, CAP>(p, see, bad, unit, k, v, qkv + (size_t)iw * ld + (size_t)h * D, ld, orow, (size_t)nq * D, lrow, prow, pml, smem + wave * (32 * D) * sizeof(float));
   }
 }
 
@@ -269,6 +447,45 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
 }
 
 // ================================================================================ backward: dQ
+// The rows `bad` of a wave again, as docs_again_fwd.  A row whose statistics are not finite has no finite result at all and is not asked for.  What is masked here is the gradient of a score, so that
+// no product over an unseen row counts; products that may pass float32's range are taken for infinities.  q, dout, dq: of the wave's first row, part: likewise, of a unit with a slot.
+template <int D, bool CAP>
+__device__ __forceinline__ void docs_again_dq(const DocsTiled& p, const DocsSeen& see, bool bad, float l2, float dl, const DocsUnit& u, const DocsRows& k, const DocsRows& v, const bf16_t* q,
+                                              size_t ld, const bf16_t* dout, size_t ldo, bf16_t* dq, float* part, float scale, char* tile) {
+  const int lane = docs_lane(), r = lane & 31, at = see.n > 0 ? r : 0;
+  bool arrives = (docs_odd<D>({dout + at * ldo, 0, 0, 0}, 0, DOCS_LARGE).some >> lane) & 1;
+  docs_again_tiles(see, u.f0, u.f1, [&](int kb) {
+    if (docs_masked(see, kb)) arrives |= ((docs_odd<D>(k, kb, DOCS_ODD).some | docs_odd<D>(v, kb, DOCS_LARGE).some) & ~docs_bits(see, kb)) != 0;
+  });
+  const uint64_t rows = __ballot(bad && arrives);
+  if (rows == 0) return;
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(acc[dt]);
+  docs_again_tiles(see, u.f0, u.f1, [&](int kb) {
+    f32x16 st[2], dp[2];
+    docs_again_scores<D>(st, tile, k, kb, q + at * ld, see.n > 0);
+    docs_again_scores<D>(dp, tile, v, kb, dout + at * ldo, see.n > 0);
+    const uint64_t seen = docs_bits(see, kb);
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        float x;
+        if constexpr (CAP) {
+          const float c = docs_cap_r(st[mt][i], p.exp_scale);
+          x = fast_exp2(fmaf(-2.f * p.cap_log2, c, l2)) * fmaf(-c, c, c);
+        } else {
+          x = fast_exp2(fmaf(st[mt][i], p.exp_scale, -l2));
+        }
+        st[mt][i] = docs_where((uint32_t)(seen >> (32 * mt)) >> (4 * (lane >> 5)), 8 * (i >> 2) + (i & 3), x * (dp[mt][i] - dl));
+      }
+    docs_again_add<D>(acc, st, tile, k, kb, see);
+  });
+  const bool on = ((rows | rows >> 32) >> r) & 1;
+  if (u.slot >= 0) docs_again_out<D>(acc, 1.f, part + (size_t)r * D, on);
+  else docs_again_out<D>(acc, scale, dq + r * ld, on);
+}
 // As attn_bwd_dq_block, unit id of head h.  STORE: the first unit of a block also stores its rows' delta and lse2 for the dK/dV launch behind it; otherwise
 // attn_docs_prep_kernel has.
 #define DOCS_DQ_RING 2
@@ -379,8 +596,8 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
     acc_tile_tr<D, false, false>(dqt, fr, Kp, st, Kp, [&](int g) { if (g + 1 < 4) ds_quarter(g + 1); });
   }
   __syncthreads();
-  const uint64_t both = __ballot(live && docs_not_finite<D / 32>(dqt)), alive = __ballot(live);
-  const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
+  const bool bad = live && docs_not_finite<D / 32>(dqt) && __builtin_isfinite(l2) && __builtin_isfinite(dl);
+  const uint32_t store = (uint32_t)__ballot(live);
   float* prow = part + (((size_t)u.slot * nq + h) * DOCS_BLOCK + wave * 32) * D;
   bf16_t* out = dqkv + (size_t)iw * ld + (size_t)h * D;
   const float scale = CAP ? 4.f * p.a.scale : p.a.scale;
@@ -395,16 +612,12 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
         [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4] * scale, dqt[dt][4 * q4 + 1] * scale, dqt[dt][4 * q4 + 2] * scale, dqt[dt][4 * q4 + 3] * scale}; },
         [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld : nullptr; });
   }
-  for (uint32_t rest = again; rest != 0; rest &= rest - 1) {
-    const int r = __builtin_ctz(rest), i = iw + r, j0 = max(__builtin_amdgcn_readlane(lo, r), u.f0 * AB_KT), j1 = min(__builtin_amdgcn_readlane(end, r), u.f1 * AB_KT);
-    const float dr = __shfl(dl, r, 64), lr = lse[(size_t)h * T + i];
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    docs_row_dq(qkv + (size_t)i * ld + (size_t)h * D, dout + ((size_t)i * nq + h) * D, kcol, kcol + (size_t)nkv * D, (size_t)ld, j0, j1, D, p.a.scale, p.a.cap, lr, dr, acc);
-#pragma unroll
-    for (int c = 0; c < D / 64; c++) {
-      if (u.slot >= 0) prow[(size_t)r * D + lane + 64 * c] = acc[c] * (CAP ? 0.25f : 1.f);
-      else out[(size_t)r * ld + lane + 64 * c] = (bf16_t)(acc[c] * p.a.scale);
-    }
+  if (__any(bad)) {
+    const int first = docs_scalar(live0), last = docs_scalar(live1) - 1;
+    const DocsUnit unit = {0, docs_scalar(u.f0), docs_scalar(u.f1), docs_scalar(u.slot)};
+    const DocsRows k = {kcol, (size_t)ld, first, last}, v = {kcol + (size_t)nkv * D, (size_t)ld, first, last};
+    docs_again_dq<D, CAP>(p, see, bad, l2, dl, unit, k, v, qkv + (size_t)iw * ld + (size_t)h * D, ld, dout + ((size_t)iw * nq + h) * D, (size_t)nq * D, out, prow, scale,
+                          smem + wave * (32 * D) * sizeof(float));
   }
 }
 
@@ -418,9 +631,80 @@ struct DocsWalk {
   __device__ __forceinline__ uint32_t rows() const { return (uint32_t)see.n; }
   __device__ __forceinline__ bool ragged(int ti) const { return ti * AB_KT < live0 || ti * AB_KT > live1; }
 };
+// The keys `bad` of a wave again, as docs_again_fwd.  Keys that see a row without finite statistics, or one whose gradient holds nothing but infinities and NaNs, have no finite result at all.
+// q, dout, lse2, delta: of the group's first head; k: of the wave's first key, v: so many columns behind; dk: likewise, part: likewise, of a unit with a slot.
+template <int D, bool CAP>
+__device__ __forceinline__ void docs_again_dkv(const DocsTiled& p, const DocsSeen& see, bool bad, const DocsUnit& u, const DocsSpan& span, const DocsRows& q0, const DocsRows& g0,
+                                               const float* lse2, const float* delta, const bf16_t* k, size_t ld, size_t v_off, bf16_t* dk, float* part, float scale, char* tile) {
+  const int lane = docs_lane(), r = lane & 31, T = p.a.v.T;
+  k += (see.n > 0 ? r : 0) * ld;
+  // f(rows of Q, rows of dO, statistics of the head, first row) for every tile of the unit that the wave sees, head after head
+  auto tiles = [&](auto f) {
+#pragma unroll 1
+    for (int h = 0; h * span.n < u.f1; h++) {
+      const DocsRows q = {q0.base + h * D, q0.ld, q0.first, q0.last}, g = {g0.base + h * D, g0.ld, g0.first, g0.last};
+      docs_again_tiles(see, span.first + max(u.f0 - h * span.n, 0), span.first + min(u.f1 - h * span.n, span.n), [&](int qb) { f(q, g, (size_t)h * T, qb); });
+    }
+  };
+  bool arrives = ((docs_odd<D>({k, 0, 0, 0}, 0, DOCS_LARGE).some | docs_odd<D>({k + v_off, 0, 0, 0}, 0, DOCS_LARGE).some) >> lane) & 1, none = false;
+  tiles([&](const DocsRows& q, const DocsRows& g, size_t head, int qb) {
+    if (!docs_masked(see, qb)) return;
+    const size_t at = head + max(q.first, min(qb + lane, q.last));
+    const DocsOdd odd = docs_odd<D>(g, qb, DOCS_LARGE);
+    const uint64_t no_sum = __ballot(!__builtin_isfinite(lse2[at])), no_delta = __ballot(!__builtin_isfinite(delta[at])), seen = docs_bits(see, qb);
+    arrives |= ((odd.some | docs_odd<D>(q, qb, DOCS_LARGE).some | no_sum | no_delta) & ~seen) != 0;
+    none |= ((odd.all | no_sum) & seen) != 0;
+  });
+  const uint64_t rows = __ballot(bad && arrives && !none);
+  if (rows == 0) return;
+  const bool on = ((rows | rows >> 32) >> r) & 1;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; pass++) {  // dV, then dK: both at once take more registers than the tile loop
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(acc[dt]);
+    tiles([&](const DocsRows& q, const DocsRows& g, size_t head, int qb) {
+      f32x16 st[2], dp[2];
+      docs_again_scores<D>(st, tile, q, qb, k, see.n > 0);
+      docs_again_scores<D>(dp, tile, g, qb, k + v_off, see.n > 0);
+      docs_wave_order();
+      float* stats = reinterpret_cast<float*>(tile);  // in the place of the tile: lse2 of the 64 rows, then delta
+      const size_t at = head + max(q.first, min(qb + lane, q.last));
+      stats[lane] = lse2[at];
+      stats[64 + lane] = delta[at];
+      docs_wave_order();
+      const uint64_t seen = docs_bits(see, qb);
+#pragma unroll
+      for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; q4++) {
+          const uint32_t word = (uint32_t)(seen >> (32 * mt)) >> (4 * (lane >> 5));
+          const float* of = stats + 32 * mt + 8 * q4 + 4 * (lane >> 5);
+          const f32x4 sums = *reinterpret_cast<const f32x4*>(of), deltas = *reinterpret_cast<const f32x4*>(of + 64);
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            float x, slope = 1.f;
+            if constexpr (CAP) {
+              const float c = docs_cap_r(st[mt][4 * q4 + e], p.exp_scale);
+              x = fast_exp2(fmaf(-2.f * p.cap_log2, c, sums[e]));
+              slope = fmaf(-c, c, c);
+            } else {
+              x = fast_exp2(fmaf(st[mt][4 * q4 + e], p.exp_scale, -sums[e]));
+            }
+            st[mt][4 * q4 + e] = docs_where(word, 8 * q4 + e, pass == 0 ? x : x * (dp[mt][4 * q4 + e] - deltas[e]) * slope);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      docs_again_add<D>(acc, st, tile, pass == 0 ? g : q, qb, see);
+    });
+    const int column = pass == 0 ? D : 0;
+    if (u.slot >= 0) docs_again_out<D>(acc, pass == 0 ? 1.f : scale, part + (size_t)r * (2 * D) + column, on);
+    else docs_again_out<D>(acc, pass == 0 ? 1.f : scale, dk + r * ld + (pass == 0 ? v_off : 0), on);
+  }
+}
 // As attn_bwd_dkv_block, at D = 128 without a cap with its pinned loop, otherwise in phases: a block owns 128 keys of a key/value head and walks the query tiles of the group's heads, one head after the other.  Unit id of key/value head hk.
 template <int D, bool CAP>
-__device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int hk, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+__device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int hk, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
                                                const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   using TL = ATile<D>;
   constexpr bool AGPR = D == 128, PINNED = D == 128 && !CAP;
@@ -560,8 +844,8 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   acc_settle<AGPR>(dkt);
   acc_settle<AGPR>(dvt);
   __syncthreads();  // every wave is done with the Q/dO rings: their LDS serves the output turn (dK, then dV)
-  const uint64_t both = __ballot(live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt))), alive = __ballot(live);
-  const uint32_t again = (uint32_t)(both | both >> 32), store = (uint32_t)alive & ~again;
+  const bool bad = live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt));
+  const uint32_t store = (uint32_t)__ballot(live);
   const float scale = CAP ? 4.f * p.a.scale : p.a.scale;
   auto dk_quad = [&](int dt, int q4) {
     return f32x4{dkt[dt][4 * q4] * scale, dkt[dt][4 * q4 + 1] * scale, dkt[dt][4 * q4 + 2] * scale, dkt[dt][4 * q4 + 3] * scale};
@@ -580,26 +864,13 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
     __builtin_amdgcn_wave_barrier();
     wave_rows_out_bf16<D>(reg, lane, dv_quad, [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld + (size_t)nkv * D : nullptr; });
   }
-  for (uint32_t rest = again; rest != 0; rest &= rest - 1) {
-    const int r = __builtin_ctz(rest), a0 = __builtin_amdgcn_readlane(from, r), a1 = __builtin_amdgcn_readlane(end, r);
-    const bf16_t* k = kcol + (size_t)(jw + r) * ld;
-    float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int g = f0 / nt; g * nt < f1; g++) {  // the unit's run of tiles of each head
-      const int t0 = span.first + max(f0 - g * nt, 0), t1 = span.first + min(f1 - g * nt, nt);
-      docs_row_dkv(k, k + (size_t)nkv * D, qkv + (size_t)(hq + g) * D, (size_t)ld, dout + (size_t)(hq + g) * D, (size_t)ldo, lse + (size_t)(hq + g) * T, delta + (size_t)(hq + g) * T,
-                   max(a0, t0 * AB_KT), min(a1, t1 * AB_KT), D, p.a.scale, p.a.cap, dk, dv);
-    }
-#pragma unroll
-    for (int c = 0; c < D / 64; c++) {
-      const int e = lane + 64 * c;
-      if (u.slot >= 0) {
-        prow[(size_t)r * (2 * D) + e] = dk[c] * p.a.scale;
-        prow[(size_t)r * (2 * D) + D + e] = dv[c];
-      } else {
-        out[(size_t)r * ld + e] = (bf16_t)(dk[c] * p.a.scale);
-        out[(size_t)r * ld + (size_t)nkv * D + e] = (bf16_t)dv[c];
-      }
-    }
+  if (__any(bad)) {
+    const int first = docs_scalar(live0), last = docs_scalar(live1) - 1, h0 = docs_scalar(hq), key = docs_scalar(jw);
+    const DocsUnit unit = {0, docs_scalar(u.f0), docs_scalar(u.f1), docs_scalar(u.slot)};
+    const DocsSpan run = {docs_scalar(span.first), docs_scalar(span.n), 0, 0};
+    const DocsRows q = {qkv + (size_t)h0 * D, (size_t)ld, first, last}, g = {dout + (size_t)h0 * D, (size_t)ldo, first, last};
+    docs_again_dkv<D, CAP>(p, see, bad, unit, run, q, g, lse2 + (size_t)h0 * T, delta + (size_t)h0 * T, qkv + (size_t)key * ld + (size_t)(nq + docs_scalar(hk)) * D, ld, (size_t)nkv * D, out, prow,
+                           scale, smem + wave * (32 * D) * sizeof(float));
   }
 }
 
@@ -643,10 +914,10 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_dq_bf16_kernel(const 
   docs_dq_block<D, CAP, true>(p, blockIdx.x / p.a.nq, blockIdx.x % p.a.nq, qkv, o, dout, lse, lse2, delta, dqkv, part);
 }
 template <int D, bool CAP>
-__global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+__global__ __launch_bounds__(AB_THREADS) void attn_docs_dkv_bf16_kernel(const DocsTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
                                                                         const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv,
                                                                         float* __restrict__ part) {
-  docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse, lse2, delta, dqkv, part);
+  docs_dkv_block<D, CAP>(p, blockIdx.x / p.a.nkv, blockIdx.x % p.a.nkv, qkv, dout, lse2, delta, dqkv, part);
 }
 // ... and as one, behind attn_docs_prep_kernel, for grids that leave units of the chip idle: dK/dV units (the longer ones) first.  grid (units_k * nkv + units_q * nq)
 template <int D, bool CAP>
@@ -658,7 +929,7 @@ __global__ __launch_bounds__(AB_THREADS) void attn_docs_bwd_bf16_kernel(const Do
   // the units there are, not the room for them: blocks without work between the two kinds would hold up the second (17 documents in 4096 rows on 4:1 heads 40.6 -> 38.9 us, 1000 rows of 8 heads 29.3 -> 28.2)
   const unsigned n_k = (unsigned)min(max(v.head[v.k.counts], 0), v.k.cap.units) * nkv;
   if (blockIdx.x < n_k) {
-    docs_dkv_block<D, CAP>(p, blockIdx.x / nkv, blockIdx.x % nkv, qkv, dout, lse, lse2, delta, dqkv, part_kv);
+    docs_dkv_block<D, CAP>(p, blockIdx.x / nkv, blockIdx.x % nkv, qkv, dout, lse2, delta, dqkv, part_kv);
   } else {
     const int id = (blockIdx.x - n_k) / nq;
     if (id < v.q.cap.units) docs_dq_block<D, CAP, false>(p, id, (blockIdx.x - n_k) % nq, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
@@ -768,7 +1039,7 @@ static int docs_bwd(const DocsTiled& p, const bf16_t* qkv, const bf16_t* o, cons
   } else {
     attn_docs_dq_bf16_kernel<D, CAP><<<(unsigned)q.units * nq, AB_THREADS, lds_dq, stream>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part_q);
     DH_LAUNCH_CHECK();
-    attn_docs_dkv_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv, AB_THREADS, lds_dkv, stream>>>(p, qkv, dout, lse, lse2, delta, dqkv, part_kv);
+    attn_docs_dkv_bf16_kernel<D, CAP><<<(unsigned)k.units * nkv, AB_THREADS, lds_dkv, stream>>>(p, qkv, dout, lse2, delta, dqkv, part_kv);
     DH_LAUNCH_CHECK();
   }
   const unsigned gqx = 16 * q.splits, gkx = 32 * k.splits, nb_q = gqx * nq, nb_k = gkx * nkv;
