@@ -58,14 +58,13 @@ __global__ void moe_route_bwd_kernel(int T, int E, const float* __restrict__ dpr
 #define BAL_BLOCKS 256
 #define BAL_TOKENS 4
 __device__ __forceinline__ int live_tokens(const int32_t* n_live, int T) { return n_live ? min(max(*n_live, 0), T) : T; }
-template <int L> __device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+// exp of a number below one by the hardware's exponential of 2: the rounding of its exponent h, up to 2^-24 |x|, is made good by the remainder x - h log 2.  Off by three half steps
+// and 2^-29 |h|.  (With expf the forward pass over 65536 x 256 was bound by its arithmetic, 21 us.)  Below -150 it is zero.
+__device__ __forceinline__ float bal_exp(float x) {
+  x = __builtin_elementwise_maximum(x, -150.f);
+  const float h = x * 1.4426950408889634f, e = __builtin_amdgcn_exp2f(h);
+  return fmaf(e, fmaf(h, -0.6931471805599453f, x), e);
 }
-// exp by the hardware's exponential of 2: off by 2^-24 |x| relatively for the product, one step for itself.  (With expf the forward pass over 65536 x 256 was bound by its
-// arithmetic, 21 us.)
-__device__ __forceinline__ float bal_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 template <int L, bool VEC> __device__ __forceinline__ int bal_expert(int el, int i) { return VEC ? el * 4 + i : el + L * i; }
 // A lane's logits of the row at l; -inf beyond E.
 template <int L, int NE, bool VEC>
@@ -109,9 +108,9 @@ __global__ __launch_bounds__(BAL_THREADS) void moe_balance_kernel(int T, int E, 
     const int e = idx[i];
     if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
   }
-  float p[NE], z = 0.f;
+  double p[NE], z = 0.0;  // a lane adds up to a few thousand tokens: BAL_TOKENS of them in float32, these in float64
 #pragma unroll
-  for (int i = 0; i < NE; i++) p[i] = 0.f;
+  for (int i = 0; i < NE; i++) p[i] = 0.0;
   // whole waves go round together: a group without a token repeats the last one and does not count it
   const size_t stride = (size_t)gridDim.x * GROUPS;
   for (size_t t0 = (size_t)blockIdx.x * GROUPS + (threadIdx.x & ~63) / L; t0 < (size_t)N; t0 += stride * BAL_TOKENS) {
@@ -144,39 +143,53 @@ __global__ __launch_bounds__(BAL_THREADS) void moe_balance_kernel(int T, int E, 
     for (int o = L / 2; o > 0; o >>= 1)
 #pragma unroll
       for (int k = 0; k < BAL_TOKENS; k++) sum[k] += __shfl_xor(sum[k], o, 64);
+    float share[NE], zs4 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NE; i++) share[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < BAL_TOKENS; k++) {
       const size_t t = t0 + k * stride + (threadIdx.x & 63) / L;
-      const float l = m[k] + __builtin_amdgcn_logf(sum[k]) * 0.69314718055994531f, inv = t < (size_t)N && sum[k] != 0.f ? 1.f / sum[k] : 0.f;
+      const float l = fmaf(__builtin_amdgcn_logf(sum[k]), 0.69314718055994531f, m[k]), inv = t < (size_t)N && sum[k] != 0.f ? 1.f / sum[k] : 0.f;
 #pragma unroll
-      for (int i = 0; i < NE; i++) p[i] = fmaf(v[k][i], inv, p[i]);
+      for (int i = 0; i < NE; i++) share[i] = fmaf(v[k][i], inv, share[i]);
       if (el == 0 && t < (size_t)N) {
         lse[t] = l;
-        z = sum[k] == 0.f ? z : fmaf(l, l, z);
+        zs4 = sum[k] == 0.f ? zs4 : fmaf(l, l, zs4);
       }
     }
+#pragma unroll
+    for (int i = 0; i < NE; i++) p[i] += (double)share[i];
+    z += (double)zs4;
   }
-  // the wave's groups, then the waves in order
+  // the wave's groups in float32
+  float q[NE];
+#pragma unroll
+  for (int i = 0; i < NE; i++) q[i] = (float)p[i];
 #pragma unroll
   for (int o = L; o < 64; o <<= 1) {
 #pragma unroll
-    for (int i = 0; i < NE; i++) p[i] += __shfl_xor(p[i], o, 64);
+    for (int i = 0; i < NE; i++) q[i] += __shfl_xor(q[i], o, 64);
   }
-  z = wave_sum(el == 0 ? z : 0.f);
+  const float zw = wave_sum(el == 0 ? (float)z : 0.f);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) < L) {
 #pragma unroll
-    for (int i = 0; i < NE; i++) sums[wave * (L * NE) + bal_expert<L, VEC>(el, i)] = p[i];
+    for (int i = 0; i < NE; i++) sums[wave * (L * NE) + bal_expert<L, VEC>(el, i)] = q[i];
   }
-  if ((threadIdx.x & 63) == 0) zs[wave] = z;
+  if ((threadIdx.x & 63) == 0) zs[wave] = zw;
   __syncthreads();
-  float pe = 0.f, ze = 0.f;
-  if ((int)threadIdx.x < L * NE) {
+  // the 16 waves' sums, in pairs of pairs
+  auto waves = [](const float* of, int step) {
+    float x[BAL_THREADS / 64];
 #pragma unroll
-    for (int w = 0; w < BAL_THREADS / 64; w++) pe += sums[w * (L * NE) + threadIdx.x];
-  }
+    for (int w = 0; w < BAL_THREADS / 64; w++) x[w] = of[w * step];
 #pragma unroll
-  for (int w = 0; w < BAL_THREADS / 64; w++) ze += zs[w];
+    for (int n = BAL_THREADS / 128; n > 0; n /= 2)
+#pragma unroll
+      for (int w = 0; w < n; w++) x[w] += x[w + n];
+    return x[0];
+  };
+  const float pe = (int)threadIdx.x < L * NE ? waves(sums + threadIdx.x, L * NE) : 0.f, ze = waves(zs, 1);
   const int e = threadIdx.x;
   if (gridDim.x == 1) {
     const float b = bal_result(0, E, E, N, pe, e < E ? hist[e] : 0, fp, counts, prob_mean);
@@ -199,10 +212,12 @@ __global__ __launch_bounds__(BAL_THREADS) void moe_balance_kernel(int T, int E, 
 __global__ __launch_bounds__(256) void moe_balance_finish_kernel(int T, int E, int blocks, const int32_t* __restrict__ n_live, const float* __restrict__ part_p,
                                                                  const int32_t* __restrict__ part_n, const float* __restrict__ part_z, int* __restrict__ done, float* __restrict__ part_b,
                                                                  int32_t* __restrict__ counts, float* __restrict__ prob_mean, float* __restrict__ loss) {
-  __shared__ float ps[256], terms[BAL_FINISH], zz[4];
+  __shared__ double ps[256], zz[4];
+  __shared__ float terms[BAL_FINISH];
   __shared__ int ns[256], last;
   const int N = live_tokens(n_live, T), e0 = blockIdx.x * BAL_FINISH, e1 = min(E, e0 + BAL_FINISH), c = threadIdx.x % BAL_FINISH, slice = threadIdx.x / BAL_FINISH;
-  float p = 0.f, x[BAL_BLOCKS / BAL_FINISH];
+  double p = 0.0;
+  float x[BAL_BLOCKS / BAL_FINISH];
   int n = 0, y[BAL_BLOCKS / BAL_FINISH];
   const int per = (blocks + 15) / 16, b0 = slice * per, e = min(e0 + c, E - 1);
 #pragma unroll
@@ -213,17 +228,17 @@ __global__ __launch_bounds__(256) void moe_balance_finish_kernel(int T, int E, i
   }
 #pragma unroll
   for (int u = 0; u < BAL_BLOCKS / 16; u++)
-    if (u < per && b0 + u < blocks) { p += x[u]; n += y[u]; }
+    if (u < per && b0 + u < blocks) { p += (double)x[u]; n += y[u]; }
   ps[threadIdx.x] = p;
   ns[threadIdx.x] = n;
   __syncthreads();
-  p = 0.f;
+  p = 0.0;
   n = 0;
   if (threadIdx.x < BAL_FINISH) {
 #pragma unroll
     for (int k = 0; k < 16; k++) { p += ps[k * BAL_FINISH + threadIdx.x]; n += ns[k * BAL_FINISH + threadIdx.x]; }
   }
-  const float b = bal_result(e0, e1, E, N, p, n, terms, counts, prob_mean);
+  const float b = bal_result(e0, e1, E, N, (float)p, n, terms, counts, prob_mean);
   if (threadIdx.x == 0) {
     part_b[blockIdx.x] = b;
     __threadfence();
@@ -232,17 +247,20 @@ __global__ __launch_bounds__(256) void moe_balance_finish_kernel(int T, int E, i
   __syncthreads();
   if (!last) return;
   __threadfence();
-  float z = wave_sum((int)threadIdx.x < blocks ? part_z[threadIdx.x] : 0.f);
+  double z = (int)threadIdx.x < blocks ? (double)part_z[threadIdx.x] : 0.0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
   if ((threadIdx.x & 63) == 0) zz[threadIdx.x >> 6] = z;
   __syncthreads();
   if (threadIdx.x == 0) {
     float sum = 0.f;
     for (unsigned k = 0; k < gridDim.x; k++) sum += __hip_atomic_load(part_b + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     loss[0] = sum;
-    loss[1] = N > 0 ? (zz[0] + zz[1] + zz[2] + zz[3]) / (float)N : 0.f;
+    loss[1] = N > 0 ? (float)((zz[0] + zz[1] + zz[2] + zz[3]) / (double)N) : 0.f;
   }
 }
-// dlogits, in the groups of the forward pass: one read and one write of the logits' size.
+// dlogits, in the groups of the forward pass: one read and one write of the logits' size.  Probabilities are exponentials of the logits less the whole number next to lse, over their own sum:
+// logits less lse itself would be off by its rounding and by their difference's.
 template <int L, int NE, bool VEC>
 __global__ __launch_bounds__(256) void moe_balance_bwd_kernel(int T, int E, const float* __restrict__ logits, const float* __restrict__ lse, const int32_t* __restrict__ counts,
                                                               const int32_t* __restrict__ n_live, const float* __restrict__ dloss, int accumulate, float* __restrict__ dlogits) {
@@ -259,18 +277,26 @@ __global__ __launch_bounds__(256) void moe_balance_bwd_kernel(int T, int E, cons
     const size_t t = t0 + (threadIdx.x & 63) / L;
     const bool live = t < (size_t)N;
     const float l = live ? lse[t] : 0.f;
-    float p[NE], s = 0.f;
+    const float near = rintf(l);
+    float p[NE], s = 0.f, sum = 0.f;
     bal_load<L, NE, VEC>(p, logits + (t < (size_t)T ? t : T - 1) * E, el, E);
 #pragma unroll
     for (int i = 0; i < NE; i++) {
-      p[i] = live && l != -INFINITY && bal_expert<L, VEC>(el, i) < E ? bal_exp(p[i] - l) : 0.f;
+      p[i] = live && l != -INFINITY && bal_expert<L, VEC>(el, i) < E ? bal_exp(p[i] - near) : 0.f;
+      sum += p[i];
       s = fmaf(p[i], f[i], s);
     }
-    s = lanes_sum<L>(s);
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) {
+      sum += __shfl_xor(sum, o, 64);
+      s += __shfl_xor(s, o, 64);
+    }
+    const float r = live && l != -INFINITY ? 1.f / sum : 0.f;
+    s *= r;
     if (t < (size_t)T && (live || !accumulate)) {
       float g[NE];
 #pragma unroll
-      for (int i = 0; i < NE; i++) g[i] = live && l != -INFINITY ? p[i] * fmaf(gb, f[i] - s, gz * l) : 0.f;
+      for (int i = 0; i < NE; i++) g[i] = live && l != -INFINITY ? p[i] * r * fmaf(gb, f[i] - s, gz * l) : 0.f;
       float* to = dlogits + t * E;
       if constexpr (VEC) {
         if (el * 4 < E) {
