@@ -1,4 +1,7 @@
 """Attention inside packed documents in forms that its other tests do not take: every launch form of the backward pass, tables for other sizes, more rows than one launch counts."""
+import os
+import re
+
 import pytest
 import torch
 
@@ -107,3 +110,41 @@ def test_rows_whose_scores_are_all_minus_infinity(dh, dtype, d, length):
     x, size = float(k.sum()) / d ** 0.5, float(k.abs().sum()) / d ** 0.5
     assert bool(((lse[:, last].double() - x).abs() <= (d + 16) * R.W * size + 2 ** -22).all()) and torch.equal(o[last], v.expand(2, d))
     assert bool(torch.isfinite(o[:50]).all()) and bool(torch.isfinite(lse[:, :50]).all())
+
+
+@pytest.mark.parametrize("T,nq,nkv,d", [(17000, 24, 8, 64), (10000, 12, 4, 128)])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_two_launches_with_cut_blocks(dh, T, nq, nkv, d, cap):
+    """More blocks than the backward pass takes in one launch, so that dQ leaves the statistics for dK and dV, and a document of 3000 rows among short ones, whose blocks of queries and of keys are cut.
+    Checked: that document's first and last group of heads, and the first and the last short document's."""
+    from paper_2411_15871_amd import build as B
+    table_h, attn_h = (open(os.path.join(B.CSRC, f)).read() for f in ("docs.h", "attn_docs_bf16.h"))
+    assert "D == 128 ? DOCS_ONE_128 : 4 * DOCS_ONE_64)) {" in attn_h  # the limits that this test is to pass
+    limit = {n: int(re.search(r"#define DOCS_ONE_%d (\d+)" % n, table_h).group(1)) for n in (64, 128)}
+    assert (T + 127) // 128 * (nq + nkv) > (limit[128] if d == 128 else 4 * limit[64])
+    short = (T - 3000 - 90) // 100
+    lengths = [90] + [3000] + [100] * short
+    p = prepared(Packed(dh, "bf16", T=T, nq=nq, nkv=nkv, d=d, lengths=lengths, first=0, cap=cap, seed=25))
+    dh.dh_docs_plan(p.docs)
+    p.forward()
+    p.backward()
+    torch.cuda.synchronize()
+    cut = p.table[:64].view(torch.int32).cpu()[6::2].tolist()  # forward, dQ of heads of 128 and of 64, dK and dV
+    assert cut[0] > 0 and cut[2 if d == 64 else 1] > 0 and cut[4 if d == 64 else 3] > 0
+    o, lse, dqkv, delta = p.o.cpu(), p.lse.cpu(), p.dqkv.cpu(), p.delta.cpu()
+    assert bool(torch.isfinite(dqkv[p.live].float()).all()) and bool((dqkv[~p.live] == MARK).all()) and bool((delta[:, ~p.live] == MARK).all())
+    grp = nq // nkv
+    for a, n, groups in ((90, 3000, (0, nkv - 1)), (0, 90, range(nkv)), (3090, 100, range(nkv)), (3090 + 100 * (short - 1), 100, range(nkv))):
+        rows, lo = slice(a, a + n), torch.zeros(n, dtype=torch.long)
+        for g in groups:
+            hs = slice(g * grp, (g + 1) * grp)
+            x = [p.qkv[rows, i * d:j * d] for i, j in ((g * grp, (g + 1) * grp), (nq + g, nq + g + 1), (nq + nkv + g, nq + nkv + g + 1))]
+            args = (n, grp, 1, d, cap, lo, torch.arange(1, n + 1), torch.cat(x, 1), p.u)
+            fwd = R.attention(*args)
+            bwd = R.attention(*args, dout=p.dout[rows, g * grp * d:(g + 1) * grp * d], o_in=o[rows, g * grp * d:(g + 1) * grp * d], lse_in=lse[hs, rows])
+            got = {"o": o[rows, g * grp * d:(g + 1) * grp * d], "dq": dqkv[rows, g * grp * d:(g + 1) * grp * d], "dk": dqkv[rows, (nq + g) * d:(nq + g + 1) * d],
+                   "dv": dqkv[rows, (nq + nkv + g) * d:(nq + nkv + g + 1) * d]}
+            for name, t in got.items():
+                val, err = (z.transpose(0, 1).reshape(n, -1) for z in (fwd if name == "o" else bwd)[name])
+                assert bool(((t.double() - val).abs() <= err).all()), (name, a, g)
+            assert bool(((lse[hs, rows].double() - fwd["lse"][0]).abs() <= fwd["lse"][1]).all()), (a, g)
