@@ -282,6 +282,7 @@ __device__ __forceinline__ void docs_again_fwd(const DocsTiled& p, const DocsSee
   });
   const uint64_t rows = __ballot(bad && arrives && !none);
   if (rows == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first results of these rows, which other lanes have stored, are in place
   const int lane = docs_lane(), r = lane & 31;
   float m = -3.0e38f, l = 0.f;
   f32x16 ot[D / 32];
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(256) void attn_docs_combine_kernel(const DocsTiled 
 }
 
 // ================================================================================ backward: dQ
-// The rows `bad` of a wave again, as docs_again_fwd.  A row whose statistics are not finite has no finite result at all and is not asked for.  What is masked here is the gradient of a score, so that
+// The rows `bad` of a wave again, as docs_again_fwd.  A row whose lse is a NaN, or whose delta is not finite, has no finite result at all and is not asked for.  What is masked here is the gradient of a score, so that
 // no product over an unseen row counts; products that may pass float32's range are taken for infinities.  q, dout, dq: of the wave's first row, part: likewise, of a unit with a slot.
 template <int D, bool CAP>
 __device__ __forceinline__ void docs_again_dq(const DocsTiled& p, const DocsSeen& see, bool bad, float l2, float dl, const DocsUnit& u, const DocsRows& k, const DocsRows& v, const bf16_t* q,
@@ -459,6 +460,7 @@ __device__ __forceinline__ void docs_again_dq(const DocsTiled& p, const DocsSeen
   });
   const uint64_t rows = __ballot(bad && arrives);
   if (rows == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first results of these rows, which other lanes have stored, are in place
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(acc[dt]);
@@ -596,7 +598,7 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
     acc_tile_tr<D, false, false>(dqt, fr, Kp, st, Kp, [&](int g) { if (g + 1 < 4) ds_quarter(g + 1); });
   }
   __syncthreads();
-  const bool bad = live && docs_not_finite<D / 32>(dqt) && __builtin_isfinite(l2) && __builtin_isfinite(dl);
+  const bool bad = live && docs_not_finite<D / 32>(dqt) && l2 == l2 && __builtin_isfinite(dl);
   const uint32_t store = (uint32_t)__ballot(live);
   float* prow = part + (((size_t)u.slot * nq + h) * DOCS_BLOCK + wave * 32) * D;
   bf16_t* out = dqkv + (size_t)iw * ld + (size_t)h * D;
@@ -631,7 +633,7 @@ struct DocsWalk {
   __device__ __forceinline__ uint32_t rows() const { return (uint32_t)see.n; }
   __device__ __forceinline__ bool ragged(int ti) const { return ti * AB_KT < live0 || ti * AB_KT > live1; }
 };
-// The keys `bad` of a wave again, as docs_again_fwd.  Keys that see a row without finite statistics, or one whose gradient holds nothing but infinities and NaNs, have no finite result at all.
+// The keys `bad` of a wave again, as docs_again_fwd.  Keys that see a row whose lse is a NaN, or one whose gradient holds nothing but infinities and NaNs, have no finite result at all.
 // q, dout, lse2, delta: of the group's first head; k: of the wave's first key, v: so many columns behind; dk: likewise, part: likewise, of a unit with a slot.
 template <int D, bool CAP>
 __device__ __forceinline__ void docs_again_dkv(const DocsTiled& p, const DocsSeen& see, bool bad, const DocsUnit& u, const DocsSpan& span, const DocsRows& q0, const DocsRows& g0,
@@ -651,12 +653,14 @@ __device__ __forceinline__ void docs_again_dkv(const DocsTiled& p, const DocsSee
     if (!docs_masked(see, qb)) return;
     const size_t at = head + max(q.first, min(qb + lane, q.last));
     const DocsOdd odd = docs_odd<D>(g, qb, DOCS_LARGE);
-    const uint64_t no_sum = __ballot(!__builtin_isfinite(lse2[at])), no_delta = __ballot(!__builtin_isfinite(delta[at])), seen = docs_bits(see, qb);
-    arrives |= ((odd.some | docs_odd<D>(q, qb, DOCS_LARGE).some | no_sum | no_delta) & ~seen) != 0;
-    none |= ((odd.all | no_sum) & seen) != 0;
+    const float sum = lse2[at];
+    const uint64_t no_delta = __ballot(!__builtin_isfinite(delta[at])), seen = docs_bits(see, qb);
+    arrives |= ((odd.some | docs_odd<D>(q, qb, DOCS_LARGE).some | __ballot(!__builtin_isfinite(sum)) | no_delta) & ~seen) != 0;
+    none |= ((odd.all | __ballot(sum != sum)) & seen) != 0;
   });
   const uint64_t rows = __ballot(bad && arrives && !none);
   if (rows == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first results of these rows, which other lanes have stored, are in place
   const bool on = ((rows | rows >> 32) >> r) & 1;
 #pragma unroll 1
   for (int pass = 0; pass < 2; pass++) {  // dV, then dK: both at once take more registers than the tile loop

@@ -60,13 +60,14 @@ def same(got, want, size, what, rows, any_kind):
     assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[0].tolist(), got[bad][0].item(), want[bad][0].item())
 
 
-@pytest.mark.parametrize("d,nq,nkv,lengths", [(128, 2, 1, [70, 90, 30]), (64, 2, 2, [70, 90, 30]), (128, 1, 1, [700, 200]), (64, 1, 1, [900, 40])])
+@pytest.mark.parametrize("dtype,d,nq,nkv,lengths", [("bf16", 128, 2, 1, [70, 90, 30]), ("bf16", 64, 2, 2, [70, 90, 30]), ("bf16", 128, 1, 1, [700, 200]), ("bf16", 64, 1, 1, [900, 40]),
+                                                    ("f32", 64, 2, 1, [70, 90, 30]), ("f32", 24, 1, 1, [70, 90, 30]), ("f32", 256, 1, 1, [70, 90, 30])])
 @pytest.mark.parametrize("cap", [0.0, 50.0])
 @pytest.mark.parametrize("where", ["v", "k", "dout"])
-def test_single_elements(dh, d, nq, nkv, lengths, cap, where):
+def test_single_elements(dh, dtype, d, nq, nkv, lengths, cap, where):
     """One element of the first document's middle row is an infinity, which later rows see in that column; beside it a row of NaNs at the document's end, which the rows before do not see, and
     the second document is NaNs altogether."""
-    p = Packed(dh, "bf16", T=sum(lengths) + 3, nq=nq, nkv=nkv, d=d, lengths=lengths, first=2, cap=cap, seed=31)
+    p = Packed(dh, dtype, T=sum(lengths) + 3, nq=nq, nkv=nkv, d=d, lengths=lengths, first=2, cap=cap, seed=31)
     a, mid = 2 + lengths[0], 2 + lengths[0] - 25
     kc, vc = nq * d, (nq + nkv) * d
     p.qkv[:a, :nq * d] *= 0.2  # no probability falls below what the kernels hold
@@ -156,6 +157,32 @@ def test_a_nan_that_is_seen_arrives(dh, dtype, d, which):
     o, lse = p.o.float().cpu(), p.lse.cpu()[0]
     assert bool(torch.isnan(o[sees]).all()) and bool(torch.isfinite(o[~sees]).all())
     assert torch.equal(torch.isnan(lse), sees if which != "v" else torch.zeros_like(sees))
+
+
+@pytest.mark.parametrize("d,cap", [(128, 0.0), (128, 30.0), (64, 0.0), (64, 30.0)])
+def test_a_row_without_weight(dh, d, cap):
+    """lse of plus infinity, as a caller may pass for a row that is to count for nothing: its dq is zero and it adds nothing to dk and dv, beside a document of NaNs in the same tile."""
+    p = Packed(dh, "bf16", T=200, nq=1, nkv=1, d=d, lengths=[100, 90], first=0, cap=cap, seed=36)
+    for t in (p.qkv, p.dout):
+        t[100:190] = NAN
+    p.qkv_d, p.dout_d = p.qkv.cuda(), p.dout.cuda()
+    p.buffers()
+    dh.dh_docs_plan(p.docs)
+    p.forward()
+    p.lse[:, 80] = INF
+    p.backward()
+    torch.cuda.synchronize()
+    got = p.dqkv[:100].float().cpu()
+    clean = Packed(dh, "bf16", T=200, nq=1, nkv=1, d=d, lengths=[100, 90], first=0, cap=cap, seed=36)
+    clean.dout[80] = 0.0  # the same as a row of no gradient, whose delta is zero
+    o = torch.nan_to_num(p.o.cpu())
+    lse = torch.nan_to_num(p.lse.cpu(), posinf=0.0)
+    lse[:, 80] = 1e4  # exp(score - lse) = 0
+    r = clean.ref(dout=clean.dout, o_in=o, lse_in=lse)
+    assert not bool(got[80, :d].any())
+    for i, name in enumerate(("dq", "dk", "dv")):
+        val, err = (t[0, :100] for t in r[name])
+        assert bool(((got[:, i * d:(i + 1) * d].double() - val).abs() <= err).all()), name
 
 
 def microseconds(f):
