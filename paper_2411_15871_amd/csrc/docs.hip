@@ -239,10 +239,17 @@ __global__ __launch_bounds__(256) void docs_plan_kernel(const DocsPlanArgs a) {
     n = base;
     for (bool more = true; more;) {
       const int s = base + lane <= n_docs ? start[base + lane] : INT32_MAX;
+      const int s0 = __builtin_amdgcn_readlane(s, 0), s63 = __builtin_amdgcn_readlane(s, 63);
+      if (s0 == s63 && s0 < r0 + 64) {  // empty documents at one place, at least 63: all that lie there (starts padded to 4096 behind the last document: 77 us one by one, 9 this way)
+        const int next = max(starts_upto(start, n_docs + 1, s0), base + 64);
+        n += s0 <= r ? next - base : 0;
+        base = next;
+      } else {
 #pragma unroll 8
-      for (int i = 0; i < 64; i++) n += __builtin_amdgcn_readlane(s, i) <= r ? 1 : 0;
-      base += 64;
-      more = base <= n_docs && __builtin_amdgcn_readlane(s, 63) < r0 + 64;
+        for (int i = 0; i < 64; i++) n += __builtin_amdgcn_readlane(s, i) <= r ? 1 : 0;
+        base += 64;
+      }
+      more = base <= n_docs && s63 < r0 + 64;
     }
   }
   if (r >= T) return;

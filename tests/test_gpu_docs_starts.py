@@ -76,3 +76,51 @@ def test_nothing_around_the_buffers_is_written(dh, dtype, d, cap, T, starts):
     words = b["table"][1][64:64 + 8 * T].view(torch.int32).view(2, T)
     dead = words[0] == words[1]
     assert not bool(b["o"][1].view(T, -1)[dead].any()) and not bool(b["dqkv"][1].view(T, -1)[dead].any()) and not bool(b["lse"][1].view(torch.int32).view(nq, T)[:, dead].any())
+
+
+def table_of(dh, T, starts):
+    table, pos = torch.empty(dh.dh_docs_table_bytes(T, 2, 1), dtype=torch.uint8, device="cuda"), torch.empty(T, dtype=torch.int32, device="cuda")
+    start = torch.as_tensor(starts, dtype=torch.int32).cuda()
+    docs = dh.docs(T, len(starts) - 1, 2, 1, start, None, pos, table)
+    docs.keep = (table, pos, start)
+    return docs
+
+
+@pytest.mark.parametrize("T,places", [(1000, {0: 1, 5: 300, 70: 64, 130: 63, 131: 65, 200: 1, 700: 5000, 900: 1}), (1000, {0: 70000, 1: 64, 2: 128, 3: 1, 63: 200, 64: 200, 65: 200, 990: 100000}),
+                                      (1000, {10: 1, 11: 4097, 1000: 9000}), (64, {3: 64, 40: 1000})])
+def test_many_empty_documents(dh, T, places):
+    """places: row -> how many documents begin there; all but the last of them are empty."""
+    starts = [r for r, n in sorted(places.items()) for _ in range(n)]
+    docs = table_of(dh, T, starts)
+    dh.dh_docs_plan(docs)
+    torch.cuda.synchronize()
+    table, pos, _ = docs.keep
+    words = table[:64 + 12 * T].view(torch.int32).cpu().long()
+    lo, hi, pre = words[16:].view(3, T)
+    rows = sorted(places)
+    want_lo, want_hi = torch.arange(T), torch.arange(T)
+    for a, z in zip(rows, rows[1:]):
+        want_lo[a:z], want_hi[a:z] = a, z
+    assert torch.equal(lo, want_lo) and torch.equal(hi, want_hi) and torch.equal(pre, want_lo) and torch.equal(pos.cpu().long(), torch.arange(T) - want_lo)
+
+
+@pytest.mark.parametrize("n", [4000, 1 << 20])
+def test_starts_padded_to_a_capacity(dh, n):
+    """Starts behind the last document, all at its end: a micro-batch of few documents takes little longer to plan (one by one, a million starts took 2700 times as long)."""
+    T, few = 8192, [0, 900, 4000, 8100]
+    plain, padded = table_of(dh, T, few), table_of(dh, T, few + [8100] * (n - len(few)))
+
+    def microseconds(docs):
+        best = float("inf")
+        for _ in range(5):
+            dh.dh_docs_plan(docs)
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(5):
+                dh.dh_docs_plan(docs)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) * 200)
+        return best
+
+    assert microseconds(padded) <= 8 * microseconds(plain)
