@@ -29,7 +29,7 @@ enum { DOCS_Q, DOCS_DQ128, DOCS_DQ64, DOCS_K128, DOCS_K64, DOCS_LISTS };
 #define DOCS_WHOLE_Q 10
 #define DOCS_WHOLE_K 8
 // All heads' tiles together make at most DOCS_TARGET chunks: room for partial results follows from that, two a chunk (at D = 128 135 MB for a target of 1024 of O or dQ, or of 512 of dK
-// and dV).  us: Q 512, 1024, 2048: forward of 16384 rows on 4:1 heads 331, 311, 309; K 256, 512, 1024: backward there 979, 969, 986, of 8192 rows on 32:8 736, 745, 757 (before dQ took 10 % less).
+// and dV).  us: Q 512, 1024, 2048: forward of 16384 rows on 4:1 heads 327, 303, 302; K 256, 512, 1024: backward there 927, 921, 940, of 8192 rows on 32:8 668, 676, 693.
 #define DOCS_TARGET_Q 1024
 #define DOCS_TARGET_K 512
 // Whether both halves of the backward pass go out as one launch: up to `most` 128-row blocks of all heads (figures where it is launched; at D = 64 up to four times as many, where

@@ -53,7 +53,7 @@ __global__ void moe_route_bwd_kernel(int T, int E, const float* __restrict__ dpr
 // the address allow it), otherwise expert = lane of the group + L * i.  A lane's experts are the same for all its tokens: it adds their probabilities in registers,
 // and the block's lanes meet in LDS once at the end, in order.  The counts are integers added in LDS, in any order.  Each block leaves its sums in the
 // workspace: [blocks][E] probabilities, [blocks][E] counts, [blocks] z; a block that is alone goes on to the results.  Bound by memory where there are many tokens: BAL_TOKENS
-// rows a group are in flight (65536 x 256: 16.6 us, 4 TB/s).
+// rows a group are in flight (65536 x 256: 17.8 us, 3.8 TB/s).
 #define BAL_THREADS 1024
 #define BAL_BLOCKS 256
 #define BAL_TOKENS 4
@@ -520,8 +520,8 @@ static int balance_lanes(int E, bool vec) {  // of a group, as above
   return l;
 }
 static bool balance_vec(int E, const void* a, const void* b) { return E % 4 == 0 && (((uintptr_t)a | (uintptr_t)b) & 15) == 0; }
-// Blocks of the forward launch: one up to BAL_ALONE rounds of its groups (it goes on to the results: 1500 x 16, 6 rounds, 9.4 us by several blocks and 7.1 by one; 4000 x 16, 16
-// rounds, 9.6 and 11.5), else two rounds a block.
+// Blocks of the forward launch: one up to BAL_ALONE rounds of its groups (it goes on to the results: 1500 x 16, 6 rounds, 10.1 us by several blocks and 7.9 by one; 4000 x 16, 16
+// rounds, 10.8 and 13.2), else two rounds a block.
 #define BAL_ALONE 8
 static int balance_blocks(int T, int E, bool vec) {
   const size_t groups = BAL_THREADS / balance_lanes(E, vec), rounds = ((size_t)T + groups - 1) / groups;
