@@ -706,6 +706,59 @@ size_t dh_grad_norm_ws_bytes(int n_tensors, const dh_tensor* tensors);
 int dh_grad_clip(int n_tensors, const dh_tensor* tensors, const float* norm, float max_norm, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Token mixers whose cost grows linearly with the length of a row, for training (forward and backward over equal sequences, layouts as dh_attn_fwd: qkv[T,(nq+2nkv)d],
+ * T = batch*seq, sequence-major) and for single tokens (one of each of `batch` sequences, which carry a cache or a state along); and the dropout that joins a
+ * mixer's result to the residual stream.  Device pointers, 16-byte aligned unless stated; d: multiple of 8 up to 128 for DH_F32, 64 or 128 for DH_BF16; nq up to 1024, a
+ * multiple of nkv; batch up to 65535, seq up to 2^26, batch*seq up to 2^28; empty batches and sequences are DH_OK.  Sums in a fixed order: the same inputs give the same bits.  What a row does
+ * not see does not reach its results, infinities and NaNs among it (which of the two a result that is not finite holds is left open).
+ * ------------------------------------------------------------------------------------------ */
+
+/* Causal attention in which the token at position i of its sequence sees the positions j <= i with j > i - window or j < sinks (the first tokens stay visible).
+ * window >= 1, sinks >= 0, either may pass seq.  Scores are scaled by 1/sqrt(d); o[T,nq*d], lse[nq,T] (4-byte aligned), delta[nq,T] as in dh_attn_fwd / dh_attn_bwd, whose results these are where
+ * window >= seq.  A row all of whose scores are minus infinity has lse minus infinity and an o of NaNs.  ws: the _workspace_bytes queries. */
+int dh_attn_window_fwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes,
+                       void* stream);
+size_t dh_attn_window_fwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d);
+int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, const void* o, const void* dout, const float* lse,
+                       void* dqkv, float* delta, void* ws, size_t ws_bytes, void* stream);
+size_t dh_attn_window_bwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d);
+/* One token of each sequence: qkv[batch,(nq+2nkv)d] (rotated), at position pos[b] (DEVICE int32, 4-byte aligned; negative: the slot is not in use, its row of o and its cache are
+ * left as they are).  kv: device [batch, cache_rows, 2*nkv*d], rows [k heads | v heads]: the cache, which holds position p in row p while p < cache_rows, and from there on in row
+ * sinks + (p - sinks) mod (cache_rows - sinks), so that cache_rows >= window + sinks rows serve rows of any length.  The call puts the token's key and value into its row and
+ * writes o[batch, nq*d]. */
+int dh_attn_window_step(int dtype, int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d, const int32_t* pos, const void* qkv, void* kv, void* o, void* ws,
+                        size_t ws_bytes, void* stream);
+size_t dh_attn_window_step_workspace_bytes(int dtype, int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d);
+
+/* Linear attention with a decay: each key/value head has a state S of d x d (key index first), S_t = lambda S_(t-1) + k_t v_t^T with lambda = exp(log_decay[head]), and each query
+ * head reads its group's, o_t = scale S_t^T q_t.  log_decay: DEVICE float32 [nkv], constants, at most 0 (minus infinity: no memory).  state_in: device float32 [batch,nkv,d,d], what the
+ * sequences begin with (NULL: zeros); state_out: likewise, S behind the last token (NULL: not wanted; seq = 0: state_in); the two may not overlap.  States are float32 and are summed in float32, also
+ * for DH_BF16, whose products with a state take it rounded to bf16.
+ * Backward: dqkv (dk, dv summed over the query heads of a group in a fixed order) from dout[T,nq*d] and dstate_out, the gradient of state_out (NULL: none); dstate_in: that of
+ * state_in (NULL: not wanted); the two may not overlap. */
+int dh_linattn_fwd(int dtype, int batch, int seq, int nq, int nkv, int d, float scale, const float* log_decay, const void* qkv, const float* state_in, void* o, float* state_out,
+                   void* ws, size_t ws_bytes, void* stream);
+size_t dh_linattn_fwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d);
+int dh_linattn_bwd(int dtype, int batch, int seq, int nq, int nkv, int d, float scale, const float* log_decay, const void* qkv, const float* state_in, const void* dout,
+                   const float* dstate_out, void* dqkv, float* dstate_in, void* ws, size_t ws_bytes, void* stream);
+size_t dh_linattn_bwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d);
+/* One token of each sequence, qkv[batch,(nq+2nkv)d] -> o[batch,nq*d]: state_out = lambda state_in + k v^T (state_out == state_in: in place; otherwise they may not overlap).  pos: DEVICE int32
+ * [batch] or NULL; a negative one leaves its sequence's o and state_out as they are, 0 begins a sequence: state_in counts as zeros, whatever it holds. */
+int dh_linattn_step(int dtype, int batch, int nq, int nkv, int d, float scale, const float* log_decay, const int32_t* pos, const void* qkv, const float* state_in,
+                    float* state_out, void* o, void* stream);
+
+/* Bias-dropout-add with p > 0: out[t,:] = a[t,:] + keep * (b[t,:] + bias[:]) * f, one rounding at the end (a NULL: zeros, bias NULL: none; out may be a or b).  Elements are dropped where
+ * their 16 random bits are below n = round(65536 p), 0 <= p <= 1, and f = 65536 / (65536 - n) (p = 1: out = a).  The mask is stored nowhere: the bits of element e = t*H + h are half e % 2 (low half
+ * first) of word e % 8 / 2 of Philox4x32-10 (Salmon et al., SC 2011) with the counter words (v mod 2^32, v / 2^32, rng[1] mod 2^32, site), v = e / 8, and the key rng[0] (low
+ * word first).  rng: DEVICE uint64 [2], a key and a step, 8-byte aligned, so that replays of a captured graph draw anew where the program moves the step; site: tells the calls of one step apart.
+ * Backward, with the rng and site of the forward call: dx = keep * dout * f (dx may be dout); dbias (NULL: not wanted) float32 [H], column sums of the unrounded products, accumulate != 0 adds them to dbias.
+ * H multiple of 8; ws: dh_dropout_add_bwd_ws_bytes (0 bytes are enough without dbias).  out and dx may otherwise not overlap an input. */
+int dh_dropout_add_fwd(int dtype, int T, int H, const void* a, const void* b, const void* bias, float p, const uint64_t* rng, uint32_t site, void* out, void* stream);
+int dh_dropout_add_bwd(int dtype, int T, int H, const void* dout, float p, const uint64_t* rng, uint32_t site, void* dx, float* dbias, int accumulate, void* ws, size_t ws_bytes,
+                       void* stream);
+size_t dh_dropout_add_bwd_ws_bytes(int T, int H);
+
+/* ------------------------------------------------------------------------------------------
  * Mixture-of-experts operators (Sec. 6.1, top-2 gating; operator bases Router, Permute, AlltoAll and
  * Group-GEMM of Table 2).  Expert parallelism on one GPU: the E logical experts are
  * e = source_rank * n_local + local_expert; this GPU holds the n_local local experts and receives

@@ -1,0 +1,274 @@
+// Causal attention with a sliding window and sinks: entry points, the kernels of a wave a row, and the form for single tokens.
+#include <algorithm>
+#include "window_rows.h"
+
+#define WR_THREADS 256
+// grid (rows / 4, heads, batch)
+template <typename T>
+__global__ __launch_bounds__(WR_THREADS) void window_rows_fwd_kernel(const WindowGeom g, const T* __restrict__ qkv, T* __restrict__ o, float* __restrict__ lse) {
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
+  if (i >= g.seq) return;
+  const size_t t0 = (size_t)blockIdx.z * g.seq, ld = (size_t)(g.nq + 2 * g.nkv) * g.d;
+  window_row_fwd(g, qkv + t0 * ld, h, i, o + ((t0 + i) * g.nq + h) * g.d, lse + (size_t)h * g.batch * g.seq + t0 + i);
+}
+template <typename T>
+__global__ __launch_bounds__(WR_THREADS) void window_rows_dq_kernel(const WindowGeom g, const T* __restrict__ qkv, const T* __restrict__ o, const T* __restrict__ dout,
+                                                                    const float* __restrict__ lse, T* __restrict__ dqkv, float* __restrict__ delta) {
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, lane = threadIdx.x & 63;
+  if (i >= g.seq) return;
+  const size_t t0 = (size_t)blockIdx.z * g.seq, ld = (size_t)(g.nq + 2 * g.nkv) * g.d, at = ((t0 + i) * g.nq + h) * g.d, st = (size_t)h * g.batch * g.seq + t0 + i;
+  float dl = 0.f;
+  for (int x = lane; x < g.d; x += 64) dl = fmaf(to_f32(o[at + x]), to_f32(dout[at + x]), dl);
+  dl = wave_sum(dl);
+  if (lane == 0) delta[st] = dl;
+  window_row_dq(g, qkv + t0 * ld, dout + at, lse[st], dl, h, i, dqkv + (t0 + i) * ld + (size_t)h * g.d);
+}
+template <typename T>
+__global__ __launch_bounds__(WR_THREADS) void window_rows_dkv_kernel(const WindowGeom g, const T* __restrict__ qkv, const T* __restrict__ dout, const float* __restrict__ lse,
+                                                                     const float* __restrict__ delta, T* __restrict__ dqkv) {
+  const int j = blockIdx.x * 4 + (threadIdx.x >> 6), hk = blockIdx.y;
+  if (j >= g.seq) return;
+  const size_t t0 = (size_t)blockIdx.z * g.seq, ld = (size_t)(g.nq + 2 * g.nkv) * g.d;
+  T* dk = dqkv + (t0 + j) * ld + (size_t)(g.nq + hk) * g.d;
+  window_row_dkv(g, qkv + t0 * ld, dout + t0 * g.nq * g.d, lse + t0, delta + t0, (size_t)g.batch * g.seq, hk, j, dk, dk + (size_t)g.nkv * g.d);
+}
+
+// ------------------------------------------------------------------------------------ single tokens
+// Bound by memory: each visible row of the cache is read once.  `lanes` lanes (a power of two) read a row of a head, 8 elements each, so that a wave has 64 / lanes rows in
+// flight a load; each such group keeps a running maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.
+struct WindowStep {
+  WindowGeom g;  // seq: rows of the cache
+  int chunk;     // keys of a block
+  int splits;    // blocks that share a sequence's keys
+};
+#define WS_THREADS 256
+#define WS_ROWS 4  // rows a lane has in flight
+template <typename T, int LANES, int GH>
+__global__ __launch_bounds__(WS_THREADS) void window_step_kernel(const WindowStep a, const int32_t* __restrict__ pos, const T* __restrict__ qkv, T* __restrict__ kv, T* __restrict__ o,
+                                                                 float* __restrict__ part) {
+  constexpr int GROUPS = WS_THREADS / LANES;
+  extern __shared__ float sm[];  // [GROUPS][GH][2 + LANES * 8]
+  const WindowGeom& g = a.g;
+  const int b = blockIdx.z, hk = blockIdx.y, split = blockIdx.x % a.splits, h0 = blockIdx.x / a.splits * GH, grp = g.nq / g.nkv, d = g.d, p = pos[b];
+  const int group = threadIdx.x / LANES, l = threadIdx.x % LANES, heads = min(GH, grp - h0), c0 = l * 8;
+  if (p < 0) return;
+  const int lo = max(0, p - g.window + 1), ns = min(g.sinks, lo), n = ns + p + 1 - lo, turn = g.seq - g.sinks;
+  const int from = split * a.chunk, to = min(n, from + a.chunk);
+  const size_t ld = (size_t)2 * g.nkv * d;
+  const T* token = qkv + (size_t)b * (g.nq + 2 * g.nkv) * d;
+  T* cache = kv + (size_t)b * g.seq * ld + (size_t)hk * d;
+  const T* now = token + (size_t)(g.nq + hk) * d;
+  const bool on = c0 < d;
+  auto row = [&](int j) { return j < g.seq ? j : g.sinks + (j - g.sinks) % turn; };
+  if (from < n && to == n && h0 == 0 && group == 0 && on) {  // the token's own key and value
+    T* at = cache + row(p) * ld + c0;
+    Vec8<T> x, y;
+    x.load(now + c0);
+    y.load(now + (size_t)g.nkv * d + c0);
+    x.store(at);
+    y.store(at + (size_t)g.nkv * d);
+  }
+  float q[GH][8], acc[GH][8], m[GH], sum[GH];
+#pragma unroll
+  for (int h = 0; h < GH; h++) {
+    m[h] = -INFINITY;
+    sum[h] = 0.f;
+    Vec8<T> x;
+    if (on && h < heads) x.load(token + (size_t)(hk * grp + h0 + h) * d + c0);
+#pragma unroll
+    for (int e = 0; e < 8; e++) { q[h][e] = on && h < heads ? x.v[e] * g.scale : 0.f; acc[h][e] = 0.f; }
+  }
+  for (int c = from + group; c < to; c += GROUPS * WS_ROWS) {
+    Raw8<T> rk[WS_ROWS], rv[WS_ROWS];
+#pragma unroll
+    for (int u = 0; u < WS_ROWS; u++) {
+      const int cu = min(c + u * GROUPS, to - 1), j = cu < ns ? cu : lo + cu - ns;
+      const T* at = j == p ? now : cache + row(j) * ld;
+      if (on) { rk[u].load(at + c0); rv[u].load(at + (size_t)g.nkv * d + c0); }
+    }
+#pragma unroll
+    for (int u = 0; u < WS_ROWS; u++) {
+      if (c + u * GROUPS >= to) continue;
+#pragma unroll
+      for (int h = 0; h < GH; h++) {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) s = on ? fmaf(q[h][e], rk[u].get(e), s) : s;
+#pragma unroll
+        for (int x = 1; x < LANES; x <<= 1) s += __shfl_xor(s, x, 64);
+        if (!(s <= m[h])) {  // a larger score, or a NaN, which stays one
+          const float ref = s;
+          const float alpha = m[h] == -INFINITY ? 0.f : expf(m[h] - ref);
+          sum[h] *= alpha;
+#pragma unroll
+          for (int e = 0; e < 8; e++) acc[h][e] *= alpha;
+          m[h] = ref;
+        }
+        const float w = m[h] == -INFINITY ? 0.f : expf(s - m[h]);
+        sum[h] += w;
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[h][e] = on ? fmaf(w, rv[u].get(e), acc[h][e]) : 0.f;
+      }
+    }
+  }
+  constexpr int PER = 2 + LANES * 8;
+#pragma unroll
+  for (int h = 0; h < GH; h++) {
+    float* to_s = sm + (group * GH + h) * PER;
+    if (l == 0) { to_s[0] = m[h]; to_s[1] = sum[h]; }
+#pragma unroll
+    for (int e = 0; e < 8; e++) to_s[2 + c0 + e] = acc[h][e];
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < heads * d; x += WS_THREADS) {
+    const int h = x / d, c = x % d, hq = hk * grp + h0 + h;
+    float M = -INFINITY, L = 0.f, A = 0.f;
+    for (int w = 0; w < GROUPS; w++) { const float mw = sm[(w * GH + h) * PER]; M = mw > M || mw != mw ? mw : M; }
+    const float ref = M == -INFINITY ? 0.f : M;
+    for (int w = 0; w < GROUPS; w++) {
+      const float* of = sm + (w * GH + h) * PER;
+      if (of[0] == -INFINITY) continue;
+      const float f = expf(of[0] - ref);
+      L = fmaf(f, of[1], L);
+      A = fmaf(f, of[2 + c], A);
+    }
+    if (a.splits == 1) {
+      o[((size_t)b * g.nq + hq) * d + c] = from_f32<T>(A / L);  // no weight at all: 0 / 0
+    } else {
+      float* to_p = part + (((size_t)b * g.nq + hq) * a.splits + split) * (d + 2);
+      if (c == 0) { to_p[0] = M; to_p[1] = L; }
+      to_p[2 + c] = A;
+    }
+  }
+}
+// grid (nq, batch), d threads
+template <typename T>
+__global__ void window_step_merge_kernel(const WindowStep a, const int32_t* __restrict__ pos, const float* __restrict__ part, T* __restrict__ o) {
+  const int b = blockIdx.y, h = blockIdx.x, d = a.g.d, c = threadIdx.x;
+  if (pos[b] < 0) return;
+  const float* of = part + ((size_t)b * a.g.nq + h) * a.splits * (d + 2);
+  float M = -INFINITY, L = 0.f, A = 0.f;
+  for (int s = 0; s < a.splits; s++) { const float ms = of[(size_t)s * (d + 2)]; M = ms > M || ms != ms ? ms : M; }
+  for (int s = 0; s < a.splits; s++) {
+    const float* at = of + (size_t)s * (d + 2);
+    if (at[0] == -INFINITY) continue;
+    const float f = expf(at[0] - M);
+    L = fmaf(f, at[1], L);
+    A = fmaf(f, at[2 + c], A);
+  }
+  o[((size_t)b * a.g.nq + h) * d + c] = from_f32<T>(A / L);
+}
+
+// ------------------------------------------------------------------------------------ host side
+static WindowGeom window_geom(int batch, int seq, int window, int sinks, int nq, int nkv, int d) { return {batch, seq, window, sinks, nq, nkv, d, (float)(1.0 / sqrt((double)d))}; }
+static int check_window(const char* who, int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) {
+  if (int rc = mix_check(who, dtype, batch, seq, nq, nkv, d)) return rc;
+  if (window < 1 || sinks < 0) DH_FAIL(DH_ERR_SHAPE, "%s: window=%d sinks=%d (at least 1 and 0)", who, window, sinks);
+  return DH_OK;
+}
+extern "C" size_t dh_attn_window_fwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) { return 0; }
+extern "C" size_t dh_attn_window_bwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) { return 0; }
+
+template <typename T>
+static int window_fwd(const WindowGeom& g, const void* qkv, void* o, float* lse, hipStream_t s) {
+  window_rows_fwd_kernel<T><<<dim3((g.seq + 3) / 4, g.nq, g.batch), WR_THREADS, 0, s>>>(g, (const T*)qkv, (T*)o, lse);
+  DH_LAUNCH_CHECK();
+  return DH_OK;
+}
+template <typename T>
+static int window_bwd(const WindowGeom& g, const void* qkv, const void* o, const void* dout, const float* lse, void* dqkv, float* delta, hipStream_t s) {
+  window_rows_dq_kernel<T><<<dim3((g.seq + 3) / 4, g.nq, g.batch), WR_THREADS, 0, s>>>(g, (const T*)qkv, (const T*)o, (const T*)dout, lse, (T*)dqkv, delta);
+  DH_LAUNCH_CHECK();
+  window_rows_dkv_kernel<T><<<dim3((g.seq + 3) / 4, g.nkv, g.batch), WR_THREADS, 0, s>>>(g, (const T*)qkv, (const T*)dout, lse, delta, (T*)dqkv);
+  DH_LAUNCH_CHECK();
+  return DH_OK;
+}
+extern "C" int dh_attn_window_fwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  if (int rc = check_window("attn_window_fwd", dtype, batch, seq, window, sinks, nq, nkv, d)) return rc;
+  if (batch == 0 || seq == 0) return DH_OK;
+  if (!qkv || !o || !lse) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_fwd: null pointer");
+  if (mix_unaligned(qkv) || mix_unaligned(o)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_fwd: qkv and o must be 16-byte aligned");
+  const size_t need = dh_attn_window_fwd_workspace_bytes(dtype, batch, seq, window, sinks, nq, nkv, d);
+  if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_window_fwd: workspace %zu < %zu bytes", ws_bytes, need);
+  if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_fwd: ws must be 16-byte aligned");
+  const WindowGeom g = window_geom(batch, seq, window, sinks, nq, nkv, d);
+  return dtype == DH_BF16 ? window_fwd<bf16_t>(g, qkv, o, lse, (hipStream_t)stream) : window_fwd<float>(g, qkv, o, lse, (hipStream_t)stream);
+}
+extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, const void* o, const void* dout, const float* lse,
+                                  void* dqkv, float* delta, void* ws, size_t ws_bytes, void* stream) {
+  if (int rc = check_window("attn_window_bwd", dtype, batch, seq, window, sinks, nq, nkv, d)) return rc;
+  if (batch == 0 || seq == 0) return DH_OK;
+  if (!qkv || !o || !dout || !lse || !dqkv || !delta) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_bwd: null pointer");
+  if (mix_unaligned(qkv) || mix_unaligned(o) || mix_unaligned(dout) || mix_unaligned(dqkv)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_bwd: qkv, o, dout and dqkv must be 16-byte aligned");
+  const size_t need = dh_attn_window_bwd_workspace_bytes(dtype, batch, seq, window, sinks, nq, nkv, d);
+  if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_window_bwd: workspace %zu < %zu bytes", ws_bytes, need);
+  if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_bwd: ws must be 16-byte aligned");
+  const WindowGeom g = window_geom(batch, seq, window, sinks, nq, nkv, d);
+  return dtype == DH_BF16 ? window_bwd<bf16_t>(g, qkv, o, dout, lse, dqkv, delta, (hipStream_t)stream) : window_bwd<float>(g, qkv, o, dout, lse, dqkv, delta, (hipStream_t)stream);
+}
+
+// Query heads that a block takes at once: up to 8; a group of more is shared out evenly over blocks, which read the cache again.
+static int step_heads(int grp) { return grp >= 8 ? 8 : grp > 4 ? 8 : grp > 2 ? 4 : grp; }
+// Blocks that share a sequence's keys: none holds fewer than 128, and there are no more blocks than the chip takes at a time by far.
+static WindowStep window_step_of(int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d) {
+  WindowStep a = {window_geom(batch, cache_rows, window, sinks, nq, nkv, d), 0, 1};
+  const long long most = std::min((long long)window + sinks, (long long)cache_rows), grp = nq / nkv, blocks = (long long)batch * nkv * ((grp + step_heads(grp) - 1) / step_heads(grp));
+  a.splits = (int)std::max(1ll, std::min({(most + 127) / 128, (1024 + blocks - 1) / blocks, 256ll}));
+  a.chunk = (int)((most + a.splits - 1) / a.splits);
+  return a;
+}
+extern "C" size_t dh_attn_window_step_workspace_bytes(int dtype, int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d) {
+  if (!mix_sized(dtype, batch, 1, nq, nkv, d) || cache_rows < 1 || window < 1 || sinks < 0) return 0;
+  const WindowStep a = window_step_of(batch, cache_rows, window, sinks, nq, nkv, d);
+  return a.splits == 1 ? 0 : (size_t)batch * nq * a.splits * (d + 2) * sizeof(float);
+}
+template <typename T, int LANES, int GH>
+static int window_step_launch(const WindowStep& a, const int32_t* pos, const T* qkv, T* kv, T* o, float* part, hipStream_t s) {
+  const int grp = a.g.nq / a.g.nkv;
+  const size_t lds = (size_t)(WS_THREADS / LANES) * GH * (2 + LANES * 8) * sizeof(float);
+  if (lds > 65536) {
+    static bool ready[DH_MAX_DEVICES] = {};
+    bool& set = ready[dh_device_index()];
+    if (!set) {
+      DH_HIP(hipFuncSetAttribute((const void*)window_step_kernel<T, LANES, GH>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+      set = true;
+    }
+  }
+  window_step_kernel<T, LANES, GH><<<dim3((unsigned)a.splits * ((grp + GH - 1) / GH), a.g.nkv, a.g.batch), WS_THREADS, lds, s>>>(a, pos, qkv, kv, o, part);
+  DH_LAUNCH_CHECK();
+  if (a.splits > 1) {
+    window_step_merge_kernel<T><<<dim3(a.g.nq, a.g.batch), a.g.d, 0, s>>>(a, pos, part, o);
+    DH_LAUNCH_CHECK();
+  }
+  return DH_OK;
+}
+template <typename T, int LANES>
+static int window_step_heads(const WindowStep& a, const int32_t* pos, const T* qkv, T* kv, T* o, float* part, hipStream_t s) {
+  switch (step_heads(a.g.nq / a.g.nkv)) {
+    case 1: return window_step_launch<T, LANES, 1>(a, pos, qkv, kv, o, part, s);
+    case 2: return window_step_launch<T, LANES, 2>(a, pos, qkv, kv, o, part, s);
+    case 4: return window_step_launch<T, LANES, 4>(a, pos, qkv, kv, o, part, s);
+    default: return window_step_launch<T, LANES, 8>(a, pos, qkv, kv, o, part, s);
+  }
+}
+template <typename T>
+static int window_step(const WindowStep& a, const int32_t* pos, const void* qkv, void* kv, void* o, void* ws, hipStream_t s) {
+  const int d = a.g.d;
+  if (d > 64) return window_step_heads<T, 16>(a, pos, (const T*)qkv, (T*)kv, (T*)o, (float*)ws, s);
+  return window_step_heads<T, 8>(a, pos, (const T*)qkv, (T*)kv, (T*)o, (float*)ws, s);
+}
+extern "C" int dh_attn_window_step(int dtype, int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d, const int32_t* pos, const void* qkv, void* kv, void* o, void* ws,
+                                   size_t ws_bytes, void* stream) {
+  if (int rc = check_window("attn_window_step", dtype, batch, 1, window, sinks, nq, nkv, d)) return rc;
+  if (cache_rows < 1 || (long long)window + sinks > cache_rows)
+    DH_FAIL(DH_ERR_SHAPE, "attn_window_step: %d rows of cache hold no window of %d behind %d sinks", cache_rows, window, sinks);
+  if (batch == 0) return DH_OK;
+  if (!pos || !qkv || !kv || !o) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_step: null pointer");
+  if (mix_unaligned(qkv) || mix_unaligned(kv) || mix_unaligned(o) || mix_unaligned(pos, 4)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_step: qkv, kv and o must be 16-byte aligned, pos 4-byte");
+  const size_t need = dh_attn_window_step_workspace_bytes(dtype, batch, cache_rows, window, sinks, nq, nkv, d);
+  if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_window_step: workspace %zu < %zu bytes", ws_bytes, need);
+  if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_step: ws must be 16-byte aligned");
+  const WindowStep a = window_step_of(batch, cache_rows, window, sinks, nq, nkv, d);
+  return dtype == DH_BF16 ? window_step<bf16_t>(a, pos, qkv, kv, o, ws, (hipStream_t)stream) : window_step<float>(a, pos, qkv, kv, o, ws, (hipStream_t)stream);
+}

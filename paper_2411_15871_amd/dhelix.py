@@ -240,6 +240,20 @@ SIGNATURES = {
     "dh_attn_docs_bwd": (_I, [_I, C.POINTER(dh_docs), _I, _F, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "dh_attn_docs_bwd_workspace_bytes": (_Z, [_I, _I, _I, _I, _I]),
     "dh_rope_axes": (_I, [_I, _I, _I, _I, _I, C.POINTER(C.c_int), _P, _I, _I, _F, _I, _P, _I, _P, _I, _P]),
+    "dh_attn_window_fwd": (_I, [_I] * 8 + [_P, _P, _P, _P, _Z, _P]),
+    "dh_attn_window_fwd_workspace_bytes": (_Z, [_I] * 8),
+    "dh_attn_window_bwd": (_I, [_I] * 8 + [_P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dh_attn_window_bwd_workspace_bytes": (_Z, [_I] * 8),
+    "dh_attn_window_step": (_I, [_I] * 8 + [_P, _P, _P, _P, _P, _Z, _P]),
+    "dh_attn_window_step_workspace_bytes": (_Z, [_I] * 8),
+    "dh_linattn_fwd": (_I, [_I] * 6 + [_F, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dh_linattn_fwd_workspace_bytes": (_Z, [_I] * 6),
+    "dh_linattn_bwd": (_I, [_I] * 6 + [_F, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dh_linattn_bwd_workspace_bytes": (_Z, [_I] * 6),
+    "dh_linattn_step": (_I, [_I] * 5 + [_F, _P, _P, _P, _P, _P, _P, _P]),
+    "dh_dropout_add_fwd": (_I, [_I, _I, _I, _P, _P, _P, _F, _P, C.c_uint32, _P, _P]),
+    "dh_dropout_add_bwd": (_I, [_I, _I, _I, _P, _F, _P, C.c_uint32, _P, _P, _I, _P, _Z, _P]),
+    "dh_dropout_add_bwd_ws_bytes": (_Z, [_I, _I]),
     "dh_grad_norm": (_I, [_I, C.POINTER(dh_tensor), _P, _P, _Z, _P]),
     "dh_grad_norm_ws_bytes": (_Z, [_I, C.POINTER(dh_tensor)]),
     "dh_grad_clip": (_I, [_I, C.POINTER(dh_tensor), _P, _F, _P]),
@@ -897,3 +911,64 @@ def dh_moe_balance_ws_bytes(T, E):
 def dh_moe_balance_bwd(T, E, logits, lse, counts, n_live, dloss, accumulate, dlogits, stream=None):
     _check(lib.dh_moe_balance_bwd(T, E, _ptr(logits), _ptr(lse), _ptr(counts), _ptr(n_live), _ptr(dloss), 1 if accumulate else 0, _ptr(dlogits),
                                   _stream(stream)))
+
+
+def dh_attn_window_fwd(dtype, batch, seq, window, sinks, nq, nkv, d, qkv, o, lse, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_attn_window_fwd(dtype, batch, seq, window, sinks, nq, nkv, d, _ptr(qkv), _ptr(o), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dh_attn_window_fwd_workspace_bytes(dtype, batch, seq, window, sinks, nq, nkv, d):
+    return lib.dh_attn_window_fwd_workspace_bytes(dtype, batch, seq, window, sinks, nq, nkv, d)
+
+
+def dh_attn_window_bwd(dtype, batch, seq, window, sinks, nq, nkv, d, qkv, o, dout, lse, dqkv, delta, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_attn_window_bwd(dtype, batch, seq, window, sinks, nq, nkv, d, _ptr(qkv), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dqkv), _ptr(delta), _ptr(ws),
+                                  ws_bytes, _stream(stream)))
+
+
+def dh_attn_window_bwd_workspace_bytes(dtype, batch, seq, window, sinks, nq, nkv, d):
+    return lib.dh_attn_window_bwd_workspace_bytes(dtype, batch, seq, window, sinks, nq, nkv, d)
+
+
+def dh_attn_window_step(dtype, batch, cache_rows, window, sinks, nq, nkv, d, pos, qkv, kv, o, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_attn_window_step(dtype, batch, cache_rows, window, sinks, nq, nkv, d, _ptr(pos), _ptr(qkv), _ptr(kv), _ptr(o), _ptr(ws), ws_bytes,
+                                   _stream(stream)))
+
+
+def dh_attn_window_step_workspace_bytes(dtype, batch, cache_rows, window, sinks, nq, nkv, d):
+    return lib.dh_attn_window_step_workspace_bytes(dtype, batch, cache_rows, window, sinks, nq, nkv, d)
+
+
+def dh_linattn_fwd(dtype, batch, seq, nq, nkv, d, scale, log_decay, qkv, state_in, o, state_out, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_linattn_fwd(dtype, batch, seq, nq, nkv, d, scale, _ptr(log_decay), _ptr(qkv), _ptr(state_in), _ptr(o), _ptr(state_out), _ptr(ws), ws_bytes,
+                              _stream(stream)))
+
+
+def dh_linattn_fwd_workspace_bytes(dtype, batch, seq, nq, nkv, d):
+    return lib.dh_linattn_fwd_workspace_bytes(dtype, batch, seq, nq, nkv, d)
+
+
+def dh_linattn_bwd(dtype, batch, seq, nq, nkv, d, scale, log_decay, qkv, state_in, dout, dstate_out, dqkv, dstate_in, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_linattn_bwd(dtype, batch, seq, nq, nkv, d, scale, _ptr(log_decay), _ptr(qkv), _ptr(state_in), _ptr(dout), _ptr(dstate_out), _ptr(dqkv),
+                              _ptr(dstate_in), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dh_linattn_bwd_workspace_bytes(dtype, batch, seq, nq, nkv, d):
+    return lib.dh_linattn_bwd_workspace_bytes(dtype, batch, seq, nq, nkv, d)
+
+
+def dh_linattn_step(dtype, batch, nq, nkv, d, scale, log_decay, pos, qkv, state_in, state_out, o, stream=None):
+    _check(lib.dh_linattn_step(dtype, batch, nq, nkv, d, scale, _ptr(log_decay), _ptr(pos), _ptr(qkv), _ptr(state_in), _ptr(state_out), _ptr(o), _stream(stream)))
+
+
+def dh_dropout_add_fwd(dtype, T, H, a, b, bias, p, rng, site, out, stream=None):
+    _check(lib.dh_dropout_add_fwd(dtype, T, H, _ptr(a), _ptr(b), _ptr(bias), p, _ptr(rng), site, _ptr(out), _stream(stream)))
+
+
+def dh_dropout_add_bwd(dtype, T, H, dout, p, rng, site, dx, dbias, accumulate, ws=None, ws_bytes=0, stream=None):
+    _check(lib.dh_dropout_add_bwd(dtype, T, H, _ptr(dout), p, _ptr(rng), site, _ptr(dx), _ptr(dbias), 1 if accumulate else 0, _ptr(ws), ws_bytes,
+                                  _stream(stream)))
+
+
+def dh_dropout_add_bwd_ws_bytes(T, H):
+    return lib.dh_dropout_add_bwd_ws_bytes(T, H)
