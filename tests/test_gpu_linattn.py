@@ -1,0 +1,235 @@
+"""Linear attention with a decay through the C ABI, against float64 (tests/mixers_ref.py holds the formulas and the bounds)."""
+import math
+
+import pytest
+import torch
+
+import mixers_ref as R
+
+pytestmark = pytest.mark.gpu
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def dh():
+    from paper_2411_15871_amd import dhelix
+    assert torch.cuda.is_available()
+    return dhelix
+
+
+class Case:
+    def __init__(self, dh, tt, batch, seq, nq, nkv, d, state=True, decays=None, seed=1):
+        self.dh, self.tt, self.batch, self.seq, self.nq, self.nkv, self.d, self.T = dh, tt, batch, seq, nq, nkv, d, batch * seq
+        g = torch.Generator().manual_seed(seed)
+        self.dt, self.scale = dh.DH_BF16 if tt == BF else dh.DH_F32, 1.0 / math.sqrt(d)
+        self.qkv, self.dout = torch.randn((self.T, (nq + 2 * nkv) * d), generator=g).to(tt), torch.randn((self.T, nq * d), generator=g).to(tt)
+        self.log_decay = torch.tensor(decays if decays else [-2.0 ** -(2 + 8.0 * i / nkv) for i in range(nkv)])
+        self.state = torch.randn((batch, nkv, d, d), generator=g) if state else None
+        self.dstate = torch.randn((batch, nkv, d, d), generator=g) if state else None
+
+    def upload(self):
+        dev = lambda t: None if t is None else t.cuda()  # noqa: E731
+        self.qkv_d, self.dout_d, self.decay_d, self.state_d, self.dstate_d = (dev(t) for t in (self.qkv, self.dout, self.log_decay, self.state, self.dstate))
+        nan = lambda *shape, t=self.tt: torch.full(shape, math.nan, dtype=t, device="cuda")  # noqa: E731
+        s = (self.batch, self.nkv, self.d, self.d)
+        self.o, self.dqkv, self.state_out, self.dstate_in = nan(self.T, self.nq * self.d), nan(*self.qkv.shape), nan(*s, t=F), nan(*s, t=F)
+        a = (self.dt, self.batch, self.seq, self.nq, self.nkv, self.d)
+        self.wsb = max(self.dh.dh_linattn_fwd_workspace_bytes(*a), self.dh.dh_linattn_bwd_workspace_bytes(*a))
+        self.ws = torch.full((max(16, self.wsb),), 0xff, dtype=torch.uint8, device="cuda")
+        self.args = (*a, self.scale, self.decay_d)
+        return self
+
+    def forward(self, stream=None, state_out=True):
+        self.dh.dh_linattn_fwd(*self.args, self.qkv_d, self.state_d, self.o, self.state_out if state_out else None, self.ws, self.wsb, stream)
+
+    def backward(self, stream=None, dstate_in=True):
+        self.dh.dh_linattn_bwd(*self.args, self.qkv_d, self.state_d, self.dout_d, self.dstate_d, self.dqkv, self.dstate_in if dstate_in else None, self.ws, self.wsb, stream)
+
+    def results(self):
+        return [t.clone() for t in (self.o, self.state_out, self.dqkv, self.dstate_in)]
+
+    def ref(self):
+        a = (self.batch, self.seq, self.nq, self.nkv, self.d, self.scale, self.log_decay, self.qkv, self.state)
+        return {**R.linear(*a), **R.linear(*a, self.dout, self.dstate)}
+
+    def check(self, which=("o", "state", "dq", "dk", "dv", "dstate"), where=None):
+        a, b, r = self.nq * self.d, (self.nq + self.nkv) * self.d, self.ref()
+        got = {"o": self.o, "state": self.state_out, "dq": self.dqkv[:, :a], "dk": self.dqkv[:, a:b], "dv": self.dqkv[:, b:], "dstate": self.dstate_in}
+        for name in which:
+            R.check(got[name], r[name], name, where)
+
+
+@pytest.mark.parametrize("batch,seq", [(1, 1), (2, 2), (1, 15), (3, 63), (1, 64), (2, 65), (1, 128), (1, 200), (2, 513), (1, 1000)])
+@pytest.mark.parametrize("tt,nq,nkv,d", [(BF, 2, 2, 64), (BF, 4, 1, 128), (BF, 6, 2, 64), (F, 2, 2, 64), (F, 3, 1, 40)])
+@pytest.mark.parametrize("state", [True, False])
+def test_both_passes(dh, tt, nq, nkv, d, batch, seq, state):
+    c = Case(dh, tt, batch, seq, nq, nkv, d, state, seed=seq).upload()
+    c.forward()
+    c.backward()
+    c.check()
+
+
+@pytest.mark.parametrize("tt,nq,nkv,d", [(F, 1, 1, 8), (F, 4, 2, 128), (F, 5, 5, 24), (F, 2, 1, 32), (BF, 16, 1, 64), (BF, 8, 8, 128), (BF, 12, 4, 128)])
+def test_head_layouts(dh, tt, nq, nkv, d):
+    c = Case(dh, tt, 2, 150, nq, nkv, d).upload()
+    c.forward()
+    c.backward()
+    c.check()
+
+
+@pytest.mark.parametrize("tt", [BF, F])
+@pytest.mark.parametrize("decay", [0.0, -1e-6, -0.01, -1.0, -30.0, -200.0, -math.inf])
+def test_decays(dh, tt, decay):
+    c = Case(dh, tt, 1, 300, 2, 2, 64, decays=[decay, -0.1]).upload()
+    c.forward()
+    c.backward()
+    c.check()
+
+
+@pytest.mark.parametrize("tt", [BF, F])
+def test_results_that_are_not_wanted(dh, tt):
+    c = Case(dh, tt, 1, 270, 4, 2, 64).upload()
+    c.forward(state_out=False)
+    c.backward(dstate_in=False)
+    c.check(("o", "dq", "dk", "dv"))
+    assert torch.isnan(c.state_out).all() and torch.isnan(c.dstate_in).all()
+
+
+@pytest.mark.parametrize("tt,d", [(BF, 64), (BF, 128), (F, 64)])
+def test_pieces_of_a_row(dh, tt, d):
+    """A row in two pieces, the state passed on, and the gradient of it passed back."""
+    nq, nkv, cut, seq = 4, 2, 130, 300
+    whole = Case(dh, tt, 1, seq, nq, nkv, d).upload()
+    a, b = (Case(dh, tt, 1, n, nq, nkv, d) for n in (cut, seq - cut))
+    a.qkv, a.dout, a.state = whole.qkv[:cut], whole.dout[:cut], whole.state
+    b.qkv, b.dout, b.dstate = whole.qkv[cut:], whole.dout[cut:], whole.dstate
+    a.upload().forward()
+    b.upload()
+    b.state_d = a.state_out
+    b.forward()
+    b.backward()
+    a.dstate_d = b.dstate_in
+    a.backward()
+    r, x, y = whole.ref(), nq * d, (nq + nkv) * d
+    R.check(torch.cat([a.o, b.o]), r["o"], "o")
+    R.check(b.state_out, r["state"], "state")
+    R.check(a.dstate_in, r["dstate"], "dstate")
+    dqkv = torch.cat([a.dqkv, b.dqkv])
+    for name, part in (("dq", dqkv[:, :x]), ("dk", dqkv[:, x:y]), ("dv", dqkv[:, y:])):
+        R.check(part, r[name], name)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("tt,nq,nkv,d", [(BF, 4, 2, 128), (BF, 2, 2, 64), (F, 2, 1, 64)])
+def test_later_tokens_do_not_reach_earlier_ones(dh, tt, nq, nkv, d, bad):
+    seq, a, b = 330, nq * d, (nq + nkv) * d
+    for what in ("k", "v", "q"):
+        c = Case(dh, tt, 2, seq, nq, nkv, d)
+        first, second = seq + 100, seq + 103  # of the second sequence, twice in one piece of 64
+        for t in (first, second):
+            c.qkv[t, {"k": slice(a + 2, a + 3), "v": slice(b + 7, b + 8), "q": slice(0, 1)}[what]] = bad
+        c.upload()
+        c.forward()
+        c.backward()
+        i = torch.arange(2 * seq)
+        before = (i < first)[:, None]
+        r = c.ref()
+        R.check(c.o, r["o"], "o", before if what != "q" else ((i != first) & (i != second))[:, None])
+        R.check(c.dqkv[:, :a], r["dq"], "dq", before if what != "q" else None)
+        behind = ((i > second) | (i < seq))[:, None]
+        R.check(c.dqkv[:, a:b], r["dk"], "dk", behind)  # a later token's gradients know of the earlier ones nothing
+        R.check(c.dqkv[:, b:], r["dv"], "dv", behind)
+        R.check(c.state_out[0], tuple(t[0] for t in r["state"]), "state")
+        assert not torch.isfinite(c.o[first].float()).all()
+        if what == "v":  # one column of a state
+            cols = (torch.arange(nq * d) % d != 7)[None, :]
+            R.check(c.o, r["o"], "o", cols.expand(2 * seq, -1))
+
+
+@pytest.mark.parametrize("tt,d", [(BF, 64), (BF, 128), (F, 64)])
+def test_bits_streams_and_graphs(dh, tt, d):
+    c = Case(dh, tt, 2, 530, 8, 2, d).upload()
+    other = Case(dh, tt, 2, 530, 8, 2, d, seed=5).upload()
+    c.forward()
+    c.backward()
+    first = c.results()
+    st = torch.cuda.Stream()
+    c.upload()
+    torch.cuda.synchronize()
+    c.forward(st)
+    c.backward(st)
+    st.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(first, c.results()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward(torch.cuda.current_stream())
+        c.backward(torch.cuda.current_stream())
+    for _ in range(3):
+        for t in (c.o, c.state_out, c.dqkv, c.dstate_in):
+            t.fill_(3.0)
+        other.forward()
+        other.backward()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(first, c.results()))
+
+
+def test_gradients_against_differences(dh):
+    c = Case(dh, F, 1, 90, 2, 1, 16).upload()
+    c.forward()
+    c.backward()
+    g = torch.Generator().manual_seed(4)
+    lam = torch.exp(c.log_decay.double())
+    for _ in range(3):
+        step, sstep = torch.randn(c.qkv.shape, generator=g, dtype=torch.float64), torch.randn(c.state.shape, generator=g, dtype=torch.float64)
+        sides = []
+        for s in (1e-5, -1e-5):
+            r = R._linear(1, 90, 2, 1, 16, c.scale, lam, c.qkv.double() + s * step, c.state.double() + s * sstep, None, None)
+            sides.append(float((r["o"] * c.dout.double()).sum() + (r["state"] * c.dstate.double()).sum()))
+        want = (sides[0] - sides[1]) / 2e-5
+        terms = [(c.dqkv.double().cpu() * step), (c.dstate_in.double().cpu() * sstep)]
+        got, size = sum(float(t.sum()) for t in terms), sum(float(t.abs().sum()) for t in terms)
+        assert abs(got - want) <= 1e-5 * size  # float32 results; the difference itself is good to 1e-9
+
+
+def test_no_tokens(dh):
+    for tt in (BF, F):
+        c = Case(dh, tt, 2, 0, 2, 1, 64).upload()
+        c.forward()
+        c.backward()
+        assert torch.equal(c.state_out, c.state_d) and torch.equal(c.dstate_in, c.dstate_d)
+        c = Case(dh, tt, 2, 0, 2, 1, 64, state=False).upload()
+        c.forward()
+        c.backward()
+        assert (c.state_out == 0).all() and (c.dstate_in == 0).all()
+
+
+# ------------------------------------------------------------------------------------ single tokens
+@pytest.mark.parametrize("tt,nq,nkv,d", [(BF, 4, 1, 128), (BF, 8, 8, 64), (F, 4, 2, 64), (F, 3, 1, 40), (F, 2, 2, 8), (BF, 16, 2, 64), (F, 2, 2, 128)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_single_tokens(dh, tt, nq, nkv, d, in_place):
+    pos = [5, -1, 0, 17]
+    c = Case(dh, tt, len(pos), 1, nq, nkv, d).upload()
+    c.state_d[2] = math.nan  # begins: whatever it holds
+    c.state[2] = 0.0
+    before = c.state_d[1].clone()
+    out = c.state_d if in_place else torch.full_like(c.state_d, 3.0)
+    c.o.fill_(3.0)
+    dh.dh_linattn_step(c.dt, len(pos), nq, nkv, d, c.scale, c.decay_d, torch.tensor(pos, dtype=torch.int32, device="cuda"), c.qkv_d, c.state_d, out, c.o)
+    r = c.ref()
+    on = torch.tensor([p >= 0 for p in pos])
+    R.check(c.o, r["o"], "o", on[:, None])
+    R.check(out, r["state"], "state", on[:, None, None, None])
+    assert (c.o[1] == 3.0).all() and (torch.equal(out[1], before) if in_place else (out[1] == 3.0).all())
+
+
+def test_steps_follow_the_forward_pass(dh):
+    c = Case(dh, F, 1, 70, 4, 2, 64, state=False).upload()
+    c.forward()
+    state, o = torch.full((1, 2, 64, 64), math.nan, device="cuda"), torch.zeros((1, 256), device="cuda")
+    for t in range(70):
+        dh.dh_linattn_step(dh.DH_F32, 1, 4, 2, 64, c.scale, c.decay_d, torch.tensor([t], dtype=torch.int32, device="cuda"), c.qkv_d[t:t + 1], state, state, o)
+        assert torch.allclose(o[0], c.o[t], rtol=1e-4, atol=1e-4), t
+    assert torch.allclose(state, c.state_out, rtol=1e-4, atol=1e-4)
+    dh.dh_linattn_step(dh.DH_F32, 1, 4, 2, 64, c.scale, c.decay_d, None, c.qkv_d[:1], state, state, o)  # without positions every slot is in use
+    assert torch.isfinite(o).all()
