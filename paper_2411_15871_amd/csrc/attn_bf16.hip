@@ -32,11 +32,10 @@
 #include <queue>
 #include <tuple>
 #include <vector>
-#include "common.h"
+#include "attn_tiles.h"
 #include "dma.h"
 
 #define AB_THREADS 256
-#define AB_KT 64   // tokens per LDS tile
 #define AB_RING 3  // tile slots
 // Tile slots of the dQ kernel in a launch of its own: two at D = 128, so that two of its blocks fit a compute unit (64 KiB each,
 // 256 registers a lane).  The arithmetic of one block's waves then runs beside the products of the other's: 32 heads x 4096
@@ -166,15 +165,10 @@ __device__ __forceinline__ ChunkMap map_dkv(int id, int seq, int q_off, int c, i
   return m;
 }
 
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
-
-#define LOG2E 1.4426950408889634f
 // The larger and the smaller of two, a NaN if either is one, in one instruction for two or three operands.  (fmaxf skips NaNs, and quiets its operands with an instruction
 // each unless the file is built on the promise that none is a NaN.  That cannot be promised, for tokens and gradients may hold NaNs, and under it a test for NaNs may be dropped.)
 __device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float min_of(float a, float b) { return __builtin_elementwise_minimum(a, b); }
-#define MFMA(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0)
 
 // acc += A * B with the accumulator held in the accumulation half of the register file (AGPRs) for the whole
 // tile loop: the long-lived gradient accumulators then cost no ordinary registers and no copies.  (This file
@@ -239,18 +233,6 @@ __device__ __forceinline__ void mfma_settle(f32x16 (&a)[2]) {
   asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0]), "+v"(a[1]));
 }
 
-template <int D>
-struct ATile {
-  static constexpr int LD = D;
-  static constexpr int ELEMS = AB_KT * D;
-  static constexpr int BYTES = ELEMS * 2;
-  static constexpr int CPR = D / 8;   // 16-byte chunks per row
-  static constexpr int IPW = D / 32;  // transfers per wave per tile (4 waves)
-  __device__ static __forceinline__ int swz(int r) { return (((r & 3) << 2) | ((r >> 2) & 3)) & (CPR - 1); }
-  // element offset of (row r, column c), c a multiple of 4
-  __device__ static __forceinline__ int off(int r, int c) { return r * LD + ((((c >> 3) ^ swz(r)) << 3) | (c & 7)); }
-};
-
 // Per-lane byte offsets (relative to the tile's first row in global memory, row stride ld elements)
 // of the chunks this wave transfers; rows >= rows_valid are clamped to the last valid row.
 template <int D>
@@ -277,39 +259,6 @@ __device__ __forceinline__ void tile_dma_at(const char* base, const uint32_t (&v
   for (int j = 0; j < ATile<D>::IPW; j++) dma16_at(m, base, v[j], j * 1024);
 }
 
-// Byte offsets inside a tile of the two kinds of fragment reads, precomputed per lane.
-//   direct: row l32 (+32*mt), columns ks*16 + kg*8 .. +7              -> kdir[ks] (+ mt*32*LD*2)
-//   transposed: rows 4*kg + s/4 (+8 for the second read) (+ mt*32 + 16*c), column dt*32 + h16*16 + (s%4)*4
-//                                                                      -> tr0[dt], tr1[dt] (+ (mt*32+16c)*LD*2)
-// The swizzle of a row only depends on row%16 through bits that the added multiples of 16 (and, for
-// the direct reads, 32) leave untouched, so the additions are plain constants.
-template <int D>
-struct FragAddr {
-  int kdir[D / 16], tr0[D / 32], tr1[D / 32];
-  __device__ __forceinline__ void init(int lane) {
-    using TL = ATile<D>;
-    const int l32 = lane & 31, kg = lane >> 5, s16 = lane & 15, h16 = (lane >> 4) & 1;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ks++) kdir[ks] = TL::off(l32, ks * 16 + kg * 8) * 2;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; dt++) {
-      tr0[dt] = TL::off(4 * kg + (s16 >> 2), dt * 32 + h16 * 16 + ((s16 & 3) << 2)) * 2;
-      tr1[dt] = TL::off(8 + 4 * kg + (s16 >> 2), dt * 32 + h16 * 16 + ((s16 & 3) << 2)) * 2;
-    }
-  }
-};
-// Fragment reads take a per-lane pointer (tile base + precomputed lane offset) and a compile-time
-// constant byte offset, which the compiler folds into the offset field of the LDS instruction.
-typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
-__device__ __forceinline__ bf16x8 lds_frag(const lds_char* lane_ptr, int const_off) {
-  return *reinterpret_cast<const lds_bf16x8*>(lane_ptr + const_off);
-}
-__device__ __forceinline__ bf16x8 lds_frag_tr(const lds_char* lane_ptr0, const lds_char* lane_ptr1, int const_off) {
-  s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lane_ptr0 + const_off));
-  s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lane_ptr1 + const_off));
-  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-}
 // Per-tile lane pointers for one LDS tile.
 template <int D>
 struct TilePtrs {
@@ -323,15 +272,6 @@ struct TilePtrs {
     for (int dt = 0; dt < D / 32; dt++) { t0[dt] = tile + fa.tr0[dt]; t1[dt] = tile + fa.tr1[dt]; }
   }
 };
-// Registers 8c..8c+7 of a 32x32 result tile as a bf16 B fragment (k-slots = rows 16c+4g+{0..3}, 16c+8+4g+{0..3}).
-__device__ __forceinline__ bf16x8 pack_rows(const f32x16& t, int c) {
-  bf16x8 f;
-#pragma unroll
-  for (int i = 0; i < 8; i++) f[i] = (bf16_t)t[8 * c + i];
-  return f;
-}
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-
 // Score tiles of a 64-token LDS tile: acc[mt] = sum over k of T[rows 32 mt .. 32 mt + 31][k] * b[k] (direct fragments
 // of the tile behind P against the D-long register fragments b).  A matrix instruction that accumulates into the
 // result of the one just before it has to wait for that result, so the products of the two independent tiles are

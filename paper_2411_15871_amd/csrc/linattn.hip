@@ -1,12 +1,6 @@
 // Linear attention with a decay for each head: S_t = lambda S_(t-1) + k_t v_t^T, o_t = scale S_t^T q_t.
 #include <algorithm>
-#include "mixers.h"
-
-struct LinGeom {
-  int batch, seq, nq, nkv, d;
-  float scale;
-  const float* log_decay;
-};
+#include "linattn.h"
 
 // The recurrence as it stands, a token at a time: a block has a state, a thread one column (or row) of it in registers.
 // grid (nkv, batch), 128 threads
@@ -156,8 +150,12 @@ __global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, c
 }
 
 // ------------------------------------------------------------------------------------ host side
-extern "C" size_t dh_linattn_fwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d) { return 0; }
-extern "C" size_t dh_linattn_bwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d) { return 0; }
+extern "C" size_t dh_linattn_fwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d) {
+  return dtype == DH_BF16 && mix_sized(dtype, batch, seq, nq, nkv, d) ? dh_linattn_bf16_ws_bytes({batch, seq, nq, nkv, d, 1.f, nullptr}, false) : 0;
+}
+extern "C" size_t dh_linattn_bwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d) {
+  return dtype == DH_BF16 && mix_sized(dtype, batch, seq, nq, nkv, d) ? dh_linattn_bf16_ws_bytes({batch, seq, nq, nkv, d, 1.f, nullptr}, true) : 0;
+}
 
 static bool lin_overlap(const void* a, const void* b, size_t bytes) { return a && b && (const char*)a < (const char*)b + bytes && (const char*)b < (const char*)a + bytes; }
 extern "C" int dh_linattn_fwd(int dtype, int batch, int seq, int nq, int nkv, int d, float scale, const float* log_decay, const void* qkv, const float* state_in, void* o, float* state_out,
@@ -173,8 +171,8 @@ extern "C" int dh_linattn_fwd(int dtype, int batch, int seq, int nq, int nkv, in
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "linattn_fwd: ws must be 16-byte aligned");
   const LinGeom g = {batch, seq, nq, nkv, d, scale, log_decay};
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == DH_BF16) lin_rec_fwd_kernel<bf16_t><<<dim3(nkv, batch), LR_THREADS, 0, s>>>(g, (const bf16_t*)qkv, state_in, (bf16_t*)o, state_out);
-  else lin_rec_fwd_kernel<float><<<dim3(nkv, batch), LR_THREADS, 0, s>>>(g, (const float*)qkv, state_in, (float*)o, state_out);
+  if (dtype == DH_BF16 && seq > 0) return dh_launch_linattn_fwd_bf16(g, (const bf16_t*)qkv, state_in, (bf16_t*)o, state_out, ws, s);
+  lin_rec_fwd_kernel<float><<<dim3(nkv, batch), LR_THREADS, 0, s>>>(g, (const float*)qkv, state_in, (float*)o, state_out);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
@@ -191,10 +189,8 @@ extern "C" int dh_linattn_bwd(int dtype, int batch, int seq, int nq, int nkv, in
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "linattn_bwd: ws must be 16-byte aligned");
   const LinGeom g = {batch, seq, nq, nkv, d, scale, log_decay};
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == DH_BF16)
-    lin_rec_bwd_kernel<bf16_t><<<dim3(nkv, batch, 3), LR_THREADS, 0, s>>>(g, (const bf16_t*)qkv, state_in, (const bf16_t*)dout, dstate_out, (bf16_t*)dqkv, dstate_in);
-  else
-    lin_rec_bwd_kernel<float><<<dim3(nkv, batch, 3), LR_THREADS, 0, s>>>(g, (const float*)qkv, state_in, (const float*)dout, dstate_out, (float*)dqkv, dstate_in);
+  if (dtype == DH_BF16 && seq > 0) return dh_launch_linattn_bwd_bf16(g, (const bf16_t*)qkv, state_in, (const bf16_t*)dout, dstate_out, (bf16_t*)dqkv, dstate_in, ws, s);
+  lin_rec_bwd_kernel<float><<<dim3(nkv, batch, 3), LR_THREADS, 0, s>>>(g, (const float*)qkv, state_in, (const float*)dout, dstate_out, (float*)dqkv, dstate_in);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
