@@ -15,10 +15,14 @@
 //
 // Bound by memory: q, k, v, o once, k and v again for the pieces' states.
 #include <algorithm>
+#include <type_traits>
 #include "attn_tiles.h"
 #include "dma.h"
 #include "linattn.h"
 
+#ifndef LIN_OCC
+#define LIN_OCC 2
+#endif
 #define LC 32  // tokens of a chunk
 
 // One pass in the form above.
@@ -72,7 +76,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), heads = GROUPED || OUT ? grp : 1;
   const size_t t0 = (size_t)b * g.seq;
   const float l2 = g.log_decay[hk] * LOG2E;
-  // LDS: two slots each of Q, K, V tiles
+  // LDS: two slots each of Q, K, V tiles.  (A third, with transfers two steps ahead, brings nothing: 131 -> 133 us for 8192 tokens x 32 heads.)
   const uint32_t lds = lds_address(smem);
   uint32_t off[3][IPW];
   auto offsets = [&](uint32_t (&v)[IPW], int ld, int last) {
@@ -127,23 +131,33 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   }
   // powers: of a score, of the state a token reads, of a row on its way into the state (fragment 1; fragment 0 of a whole chunk: 16 tokens further from the end, or nearer)
   const float f_score = g.scale, f_read = GROUPED ? 1.f : g.scale, f_in = GROUPED ? g.scale : 1.f;
-  float weight[OUT ? 16 : 1], into[8];
-  uint32_t seen = 0;
-  if constexpr (OUT) {
+  float weight[OUT ? 16 : 1], into[2][8], whole, read;
+  uint32_t seen;
+  auto powers = [&](int left) {  // of a chunk of so many tokens: rows behind them are copies of the last one, which count for nothing
+    seen = 0;
 #pragma unroll
     for (int r = 0; r < 16; r++) {
-      const int j = 8 * (r >> 2) + 4 * kg + (r & 3), m = REV ? j - l32 : l32 - j;
-      weight[r] = m >= 0 ? f_score * lin_pow(l2, m) : 0.f;
-      seen |= m >= 0 ? 1u << r : 0u;
+      const int j = lin_token(r >> 3, r & 7, kg);
+      seen |= (REV ? j >= l32 && j < left : j <= l32) ? 1u << r : 0u;
     }
-  }
 #pragma unroll
-  for (int e = 0; e < 8; e++) into[e] = f_in * lin_pow(l2, REV ? 1 + lin_token(0, e, kg) : LC - 1 - lin_token(1, e, kg));
-  const float far = lin_pow(l2, 16);  // of the other fragment
-  float whole = lin_pow(l2, LC);
-  float read = f_read * lin_pow(l2, REV ? LC - 1 - l32 : l32 + 1);
+    for (int c = 0; c < 2; c++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int t = lin_token(c, e, kg);
+        into[c][e] = t < left ? f_in * lin_pow(l2, REV ? 1 + t : left - 1 - t) : 0.f;
+      }
+    whole = lin_pow(l2, left);
+    read = f_read * (REV ? l32 < left ? lin_pow(l2, left - 1 - l32) : 0.f : lin_pow(l2, l32 + 1));
+  };
+  if constexpr (OUT) {
+#pragma unroll
+    for (int r = 0; r < 16; r++) weight[r] = f_score * lin_pow(l2, max(0, REV ? lin_token(r >> 3, r & 7, kg) - l32 : l32 - lin_token(r >> 3, r & 7, kg)));
+  }
+  int known = LC;  // tokens of the chunk that the powers are for
+  powers(LC);
   f32x16 ot;
-  bf16x8 Sp[OUT ? KS : 1], qf[OUT ? KS : 1];
+  bf16x8 qf[OUT ? KS : 1];
   int n = 0, h = 0;
   for (int s = 0; s < steps; s++) {
     // this step's tiles are here once the transfers before the last step's stores are through
@@ -153,87 +167,83 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     if (s + 1 < steps) issue();
     const int chunk = chunk_of(n), left = min(LC, g.seq - chunk * LC), slot_s = s & 1, slot_c = n & 1, slot_q = GROUPED ? slot_c : slot_s, slot_k = GROUPED ? slot_s : slot_c;
     const lds_char *Qt = sm + slot_q * TILE, *Kt = sm + (2 + slot_k) * TILE, *Vt = sm + (4 + slot_k) * TILE;
+    if (left != known) powers(known = left);
     bf16x8 vf[2];
 #pragma unroll
     for (int c = 0; c < 2; c++) vf[c] = lds_frag_tr(Vt + fa.tr[0], Vt + fa.tr[1], c * 16 * TL::LD * 2);
     if constexpr (OUT) {
-      if (h == 0) {
-#pragma unroll
-        for (int dt = 0; dt < W; dt++)
-#pragma unroll
-          for (int c = 0; c < 2; c++) Sp[2 * dt + c] = pack_rows(S[dt], c);
-      }
       if (!GROUPED || h == 0) {
 #pragma unroll
         for (int ks = 0; ks < KS; ks++) qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
-#pragma unroll
-        for (int r = 0; r < 16; r++) ot[r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++) ot = MFMA(Sp[ks], qf[ks], ot);
-        float rd = read;
-        if (REV && left < LC) rd = f_read * (l32 < left ? lin_pow(l2, left - 1 - l32) : 0.f);
-#pragma unroll
-        for (int r = 0; r < 16; r++) ot[r] *= rd;
       }
-      f32x16 st;
-#pragma unroll
-      for (int r = 0; r < 16; r++) st[r] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ks++) st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
-      uint32_t see = seen;
-      if (REV && left < LC) {  // rows behind the end are copies of the last one
-#pragma unroll
-        for (int r = 0; r < 16; r++) see &= 8 * (r >> 2) + 4 * kg + (r & 3) < left ? ~0u : ~(1u << r);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; r++) st[r] = (see >> r) & 1 ? st[r] * weight[r] : 0.f;
-      const bf16x8 pf[2] = {pack_rows(st, 0), pack_rows(st, 1)};
-      // Tokens whose value holds an infinity or a NaN in this wave's columns: a zero times it would reach the tokens that do not see it.
+      // Tokens whose value holds an infinity or a NaN in this wave's columns: a zero times it would reach the tokens that do not see it.  They stay out of the product and are added
+      // one by one.
       uint32_t odd = 0;
+      bf16x8 vs[2] = {vf[0], vf[1]};
       {
         typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
         const u16x8 m0 = __builtin_bit_cast(u16x8, vf[0]) & (unsigned short)0x7fff, m1 = __builtin_bit_cast(u16x8, vf[1]) & (unsigned short)0x7fff;
         const u16x8 m = __builtin_elementwise_max(m0, m1);
-        bool any = false;
-#pragma unroll
-        for (int e = 0; e < 8; e++) any |= m[e] >= 0x7f80;
-        if (__any(any)) {
+        const auto m4 = __builtin_elementwise_max(__builtin_shufflevector(m, m, 0, 1, 2, 3), __builtin_shufflevector(m, m, 4, 5, 6, 7));
+        const auto m2 = __builtin_elementwise_max(__builtin_shufflevector(m4, m4, 0, 1), __builtin_shufflevector(m4, m4, 2, 3));
+        if (__any(m2[0] >= 0x7f80 || m2[1] >= 0x7f80)) {
 #pragma unroll
           for (int e = 0; e < 8; e++) {
             const uint64_t x = __ballot(m0[e] >= 0x7f80), y = __ballot(m1[e] >= 0x7f80);
             odd |= ((uint32_t)x ? 1u << lin_token(0, e, 0) : 0) | ((uint32_t)(x >> 32) ? 1u << lin_token(0, e, 1) : 0);
             odd |= ((uint32_t)y ? 1u << lin_token(1, e, 0) : 0) | ((uint32_t)(y >> 32) ? 1u << lin_token(1, e, 1) : 0);
           }
-        }
-      }
-      if (odd == 0) {
-        ot = MFMA(vf[0], pf[0], ot);
-        ot = MFMA(vf[1], pf[1], ot);
-      } else {  // a token adds what it sees: once for each number of such tokens that a token may see, with the others' values taken as zeros
-        const uint32_t mine = odd & (REV ? ~0u << l32 : ~0u >> (31 - l32));
-#pragma unroll 1
-        for (int x = 0; x <= __popc(odd); x++) {
-          uint32_t zap = odd;  // not seen by tokens that see x
-          for (int k = 0; k < x; k++) zap &= REV ? ~(1u << (31 - __clz(zap))) : zap - 1;
-          bf16x8 v0 = vf[0], v1 = vf[1];
 #pragma unroll
           for (int e = 0; e < 8; e++) {
-            v0[e] = (zap >> lin_token(0, e, kg)) & 1 ? (bf16_t)0.f : v0[e];
-            v1[e] = (zap >> lin_token(1, e, kg)) & 1 ? (bf16_t)0.f : v1[e];
+            vs[0][e] = (odd >> lin_token(0, e, kg)) & 1 ? (bf16_t)0.f : vf[0][e];
+            vs[1][e] = (odd >> lin_token(1, e, kg)) & 1 ? (bf16_t)0.f : vf[1][e];
           }
-          f32x16 add = MFMA(v0, pf[0], ot);
-          add = MFMA(v1, pf[1], add);
-          const bool here = __popc(mine) == x;
+        }
+      }
+      f32x16 st;
 #pragma unroll
-          for (int r = 0; r < 16; r++) ot[r] = here ? add[r] : ot[r];
+      for (int r = 0; r < 16; r++) st[r] = 0.f;
+      if (!GROUPED || h == 0) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) ot[r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks], ot);
+#pragma unroll
+        for (int r = 0; r < 16; r++) ot[r] *= read;
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
+#pragma unroll
+      for (int r = 0; r < 16; r++)  // what is not seen becomes a zero whatever it is
+        st[r] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, st[r] * weight[r]) & (uint32_t)__builtin_amdgcn_sbfe((int)seen, r, 1));
+      const bf16x8 pf[2] = {pack_rows(st, 0), pack_rows(st, 1)};
+      ot = MFMA(vs[0], pf[0], ot);
+      ot = MFMA(vs[1], pf[1], ot);
+      if (odd != 0) {
+#pragma unroll 1
+        for (; odd != 0; odd &= odd - 1) {
+          const int j = __builtin_ctz(odd);
+          bf16x8 v0, v1;
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            v0[e] = lin_token(0, e, kg) == j ? vf[0][e] : (bf16_t)0.f;
+            v1[e] = lin_token(1, e, kg) == j ? vf[1][e] : (bf16_t)0.f;
+          }
+          f32x16 add;
+#pragma unroll
+          for (int r = 0; r < 16; r++) add[r] = 0.f;
+          add = MFMA(v0, pf[0], add);
+          add = MFMA(v1, pf[1], add);
+          const bool here = REV ? j >= l32 : j <= l32;
+#pragma unroll
+          for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
         }
       }
       if (!GROUPED || h == heads - 1) {  // a lane has a token's columns 8 q4 + 4 kg .. of 32; halves are exchanged so that it stores 16 bytes
         bf16_t* row = p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(GROUPED ? hk : hk * grp + h) * D + wave * 32 + 8 * kg;
 #pragma unroll
         for (int c = 0; c < 2; c++) {
-          const bf16x8 f = pack_rows(ot, c);
-          const uint4 u = __builtin_bit_cast(uint4, f);
+          const uint4 u = __builtin_bit_cast(uint4, pack_rows(ot, c));
           const auto x = __builtin_amdgcn_permlane32_swap(u.x, u.z, false, false);
           const auto y = __builtin_amdgcn_permlane32_swap(u.y, u.w, false, false);
           if (l32 < left) *reinterpret_cast<uint4*>(row + 16 * c) = make_uint4((uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]);
@@ -242,30 +252,20 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     }
     if (GROUPED || h == heads - 1) {  // into the state
       if (!GROUPED || h == 0) {
-        const float f = left == LC ? whole : lin_pow(l2, left);
 #pragma unroll
         for (int dt = 0; dt < W; dt++)
 #pragma unroll
-          for (int r = 0; r < 16; r++) S[dt][r] *= f;
+          for (int r = 0; r < 16; r++) S[dt][r] *= whole;
       }
 #pragma unroll
       for (int c = 0; c < 2; c++) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          float w = c == (REV ? 0 : 1) ? into[e] : into[e] * far;
-          if (left < LC) {
-            const int t = lin_token(c, e, kg);
-            w = t < left ? f_in * lin_pow(l2, REV ? 1 + t : left - 1 - t) : 0.f;
-          }
-          x[e] = (float)vf[c][e] * w;
-        }
         bf16x8 hi, mid, lo;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          hi[e] = (bf16_t)x[e];
+          const float x = (float)vf[c][e] * into[c][e];
+          hi[e] = (bf16_t)x;
           if constexpr (EXACT) {
-            const float y = x[e] - (float)hi[e];
+            const float y = x - (float)hi[e];
             mid[e] = (bf16_t)y;
             lo[e] = (bf16_t)(y - (float)mid[e]);
           }
@@ -295,13 +295,13 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
 
 // The forward pass: OUT its results, otherwise the pieces' contributions to the states.  grid (pieces, nkv, batch)
 template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
+__global__ __launch_bounds__(2 * D, LIN_OCC) void lin_fwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lin_walk<D, false, false, EXACT, OUT>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
 // The backward pass: dq, dk and dv (OUT), otherwise the pieces' contributions to S and R.  grid (pieces, nkv * (OUT ? 3 : 2), batch)
 template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, 2) void lin_bwd_kernel(const LinArgs a) {
+__global__ __launch_bounds__(2 * D, LIN_OCC) void lin_bwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int nkv = a.g.nkv, y = blockIdx.y, b = blockIdx.z;
   if (y < nkv) lin_walk<D, false, false, EXACT && !OUT, OUT>(a, a.pass[0], blockIdx.x, y, b, smem);
@@ -338,7 +338,9 @@ __global__ __launch_bounds__(256) void lin_carry_kernel(const LinArgs a, const L
 // ------------------------------------------------------------------------------------ host side
 // Pieces of a row: enough that the chip's units have two blocks each, none below LIN_LEAST chunks.
 #define LIN_LEAST 4
+#ifndef LIN_BLOCKS
 #define LIN_BLOCKS 512
+#endif
 struct LinCut { int pieces, per; };
 static LinCut lin_cut(const LinGeom& g, bool bwd) {
   const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 3 : 1);
