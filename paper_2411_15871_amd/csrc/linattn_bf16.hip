@@ -20,9 +20,6 @@
 #include "dma.h"
 #include "linattn.h"
 
-#ifndef LIN_OCC
-#define LIN_OCC 2
-#endif
 #define LC 32  // tokens of a chunk
 
 // One pass in the form above.
@@ -37,7 +34,14 @@ struct LinPass {
 struct LinArgs {
   LinGeom g;
   int pieces, per;  // per: chunks of a piece
-  LinPass pass[3];
+  LinPass pass[2];
+};
+// dk and dv together.
+struct LinGrads {
+  const bf16_t *qkv, *dout;
+  bf16_t* dqkv;
+  const float* state;  // R behind each piece
+  float* sum;          // EXACT: the gradient of the state before the row (or nullptr)
 };
 
 // Fragments of 32-token tiles.  tr: as FragAddr's transposed reads; tp: the same with bits 2 and 3 of the column exchanged, so that accumulator row 8a + 4b + e (of 16) of a product with it holds
@@ -64,54 +68,211 @@ __device__ __forceinline__ int lin_token(int c, int e, int kg) { return 16 * c +
 // lambda^m; log2 of lambda may be minus infinity
 __device__ __forceinline__ float lin_pow(float l2, int m) { return m == 0 ? 1.f : fast_exp2(l2 * (float)m); }
 
-// GROUPED: the query role is shared by the group's heads and the other two come from each of them (dk, dv and the states R), otherwise the other way
-// round.  REV: from the row's end.
+// What a chunk's arithmetic multiplies by.  Powers of lambda: of a score, of the state that a token reads, of a row on its way into the state.  REV: the row is walked from its end.
+template <bool REV>
+struct LinPowers {
+  float weight[16], into[2][8], whole, read;
+  uint32_t seen;  // bit r: the lane's token sees that of score register r
+  int left;       // tokens of the chunk
+  __device__ __forceinline__ void scores(float l2, float f, int lane) {
+    const int l32 = lane & 31, kg = lane >> 5;
+#pragma unroll
+    for (int r = 0; r < 16; r++) weight[r] = f * lin_pow(l2, max(0, REV ? lin_token(r >> 3, r & 7, kg) - l32 : l32 - lin_token(r >> 3, r & 7, kg)));
+  }
+  __device__ __forceinline__ void chunk(int n, float l2, float f_read, float f_in, int lane) {  // rows behind the chunk's n are copies of its last one, which count for nothing
+    const int l32 = lane & 31, kg = lane >> 5;
+    left = n;
+    seen = 0;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+      const int j = lin_token(r >> 3, r & 7, kg);
+      seen |= (REV ? j >= l32 && j < n : j <= l32) ? 1u << r : 0u;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; c++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int t = lin_token(c, e, kg);
+        into[c][e] = t < n ? f_in * lin_pow(l2, REV ? 1 + t : n - 1 - t) : 0.f;
+      }
+    whole = lin_pow(l2, n);
+    read = f_read * (REV ? l32 < n ? lin_pow(l2, n - 1 - l32) : 0.f : lin_pow(l2, l32 + 1));
+  }
+};
+// The values of 32 tokens in a wave's columns, as the matrix instruction takes them.
+struct LinValues {
+  bf16x8 all[2], kept[2];  // kept: zeros in the place of tokens that hold an infinity or a NaN, which a zero's product would carry to tokens that do not see them
+  uint32_t odd;            // those tokens
+  __device__ __forceinline__ void load(const lds_char* t0, const lds_char* t1, int row_bytes) {
+#pragma unroll
+    for (int c = 0; c < 2; c++) all[c] = lds_frag_tr(t0, t1, c * 16 * row_bytes);
+  }
+  __device__ __forceinline__ void look(int kg) {
+    typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
+    kept[0] = all[0];
+    kept[1] = all[1];
+    odd = 0;
+    const u16x8 m0 = __builtin_bit_cast(u16x8, all[0]) & (unsigned short)0x7fff, m1 = __builtin_bit_cast(u16x8, all[1]) & (unsigned short)0x7fff;
+    const u16x8 m = __builtin_elementwise_max(m0, m1);
+    const auto m4 = __builtin_elementwise_max(__builtin_shufflevector(m, m, 0, 1, 2, 3), __builtin_shufflevector(m, m, 4, 5, 6, 7));
+    const auto m2 = __builtin_elementwise_max(__builtin_shufflevector(m4, m4, 0, 1), __builtin_shufflevector(m4, m4, 2, 3));
+    if (!__any(m2[0] >= 0x7f80 || m2[1] >= 0x7f80)) return;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const uint64_t x = __ballot(m0[e] >= 0x7f80), y = __ballot(m1[e] >= 0x7f80);
+      odd |= ((uint32_t)x ? 1u << lin_token(0, e, 0) : 0) | ((uint32_t)(x >> 32) ? 1u << lin_token(0, e, 1) : 0);
+      odd |= ((uint32_t)y ? 1u << lin_token(1, e, 0) : 0) | ((uint32_t)(y >> 32) ? 1u << lin_token(1, e, 1) : 0);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      kept[0][e] = (odd >> lin_token(0, e, kg)) & 1 ? (bf16_t)0.f : all[0][e];
+      kept[1][e] = (odd >> lin_token(1, e, kg)) & 1 ? (bf16_t)0.f : all[1][e];
+    }
+  }
+};
+__device__ __forceinline__ void lin_zero(f32x16& t) {
+#pragma unroll
+  for (int r = 0; r < 16; r++) t[r] = 0.f;
+}
+// ot += values * (weighted scores st); what is not seen becomes a zero whatever it is.
+template <bool REV>
+__device__ __forceinline__ void lin_inside(f32x16& ot, f32x16& st, const LinPowers<REV>& p, const LinValues& v, int lane) {
+  const int l32 = lane & 31, kg = lane >> 5;
+#pragma unroll
+  for (int r = 0; r < 16; r++)
+    st[r] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, st[r] * p.weight[r]) & (uint32_t)__builtin_amdgcn_sbfe((int)p.seen, r, 1));
+  const bf16x8 pf[2] = {pack_rows(st, 0), pack_rows(st, 1)};
+  ot = MFMA(v.kept[0], pf[0], ot);
+  ot = MFMA(v.kept[1], pf[1], ot);
+#pragma unroll 1
+  for (uint32_t odd = v.odd; odd != 0; odd &= odd - 1) {  // token by token, to those that see it
+    const int j = __builtin_ctz(odd);
+    bf16x8 v0, v1;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      v0[e] = lin_token(0, e, kg) == j ? v.all[0][e] : (bf16_t)0.f;
+      v1[e] = lin_token(1, e, kg) == j ? v.all[1][e] : (bf16_t)0.f;
+    }
+    f32x16 add;
+    lin_zero(add);
+    add = MFMA(v0, pf[0], add);
+    add = MFMA(v1, pf[1], add);
+    const bool here = REV ? j >= l32 : j <= l32;
+#pragma unroll
+    for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
+  }
+}
+// S += rows^T * (values on their way into the state).  EXACT: their weighted values in three terms.
+template <int D, bool EXACT>
+__device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& fa, const lds_char* rows, const bf16x8 (&v)[2], const float (&into)[2][8]) {
+#pragma unroll
+  for (int c = 0; c < 2; c++) {
+    bf16x8 hi, mid, lo;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const float x = (float)v[c][e] * into[c][e];
+      hi[e] = (bf16_t)x;
+      if constexpr (EXACT) {
+        const float y = x - (float)hi[e];
+        mid[e] = (bf16_t)y;
+        lo[e] = (bf16_t)(y - (float)mid[e]);
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++) {
+      const bf16x8 kf = lds_frag_tr(rows + fa.tp[dt][0], rows + fa.tp[dt][1], c * 16 * D * 2);
+      S[dt] = MFMA(kf, hi, S[dt]);
+      if constexpr (EXACT) {
+        S[dt] = MFMA(kf, mid, S[dt]);
+        S[dt] = MFMA(kf, lo, S[dt]);
+      }
+    }
+  }
+}
+// The state a wave begins with (its 32 columns; transposed: of the transposed one), and the one it leaves.
+template <int D>
+__device__ __forceinline__ void lin_state_load(f32x16 (&S)[D / 32], const float* from, bool transposed, int wave, int lane) {
+  const int l32 = lane & 31, kg = lane >> 5, y = wave * 32 + l32;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+      const int x = lin_row(dt, r, kg);
+      S[dt][r] = from ? from[transposed ? (size_t)y * D + x : (size_t)x * D + y] : 0.f;
+    }
+}
+template <int D>
+__device__ __forceinline__ void lin_state_store(const f32x16 (&S)[D / 32], float* to, int wave, int lane) {
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) to[(size_t)lin_row(dt, r, lane >> 5) * D + wave * 32 + (lane & 31)] = S[dt][r];
+}
+// A lane has a token's columns 8 q4 + 4 kg .. of 32: halves are exchanged so that it stores 16 bytes twice.  row: of the lane's token, from the wave's columns on.
+__device__ __forceinline__ void lin_out(const f32x16& ot, bf16_t* row, bool on, int lane) {
+#pragma unroll
+  for (int c = 0; c < 2; c++) {
+    const uint4 u = __builtin_bit_cast(uint4, pack_rows(ot, c));
+    const auto x = __builtin_amdgcn_permlane32_swap(u.x, u.z, false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(u.y, u.w, false, false);
+    if (on) *reinterpret_cast<uint4*>(row + 8 * (lane >> 5) + 16 * c) = make_uint4((uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]);
+  }
+}
+// Transfers of 32-token tiles to LDS, D / 16 KiB a tile, two a wave.
+template <int D>
+struct LinTransfer {
+  static constexpr int TILE = LC * D * 2;
+  __device__ static __forceinline__ void offsets(uint32_t (&v)[2], int ld, int last, int wave, int lane) {
+    using TL = ATile<D>;
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      const int x = (wave * 2 + j) * 64 + lane, row = x / TL::CPR, c = (x % TL::CPR) ^ TL::swz(row);
+      v[j] = (uint32_t)((min(row, last) * (size_t)ld + c * 8) * sizeof(bf16_t));
+    }
+  }
+  // rows from `base` on; rows behind row `last` are copies of it.  off: offsets of a whole tile.
+  __device__ static __forceinline__ void go(const bf16_t* base, int ld, const uint32_t (&off)[2], int last, uint32_t to, int wave, int lane) {
+    to += wave * 2048;
+    if (last == LC - 1) {
+#pragma unroll
+      for (int j = 0; j < 2; j++) dma16_base(base, off[j], to + j * 1024);
+    } else {
+      uint32_t v[2];
+      offsets(v, ld, last, wave, lane);
+#pragma unroll
+      for (int j = 0; j < 2; j++) dma16_base(base, v[j], to + j * 1024);
+    }
+  }
+};
+
+// The pass in its first form, a state for the group and a query row for each of its heads (o, dq); or, with !OUT, sums for the states alone: GROUPED and REV: of R, over the group's heads, from
+// the row's end.  LDS: two slots each of Q, K, V tiles.  (A third, with transfers two steps ahead, brings nothing: 131 -> 133 us for 8192 tokens x 32 heads.)
 template <int D, bool GROUPED, bool REV, bool EXACT, bool OUT>
 __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int piece, int hk, int b, char* smem) {
-  using TL = ATile<D>;
-  constexpr int W = D / 32, KS = D / 16, TILE = LC * D * 2, IPW = 2;
+  static_assert(!(GROUPED && OUT), "lin_walk_kv");
+  using TR = LinTransfer<D>;
+  constexpr int W = D / 32, KS = D / 16;
   const lds_char* sm = (const lds_char*)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const LinGeom& g = a.g;
   const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), heads = GROUPED || OUT ? grp : 1;
   const size_t t0 = (size_t)b * g.seq;
-  const float l2 = g.log_decay[hk] * LOG2E;
-  // LDS: two slots each of Q, K, V tiles.  (A third, with transfers two steps ahead, brings nothing: 131 -> 133 us for 8192 tokens x 32 heads.)
+  const float l2 = g.log_decay[hk] * LOG2E, f_in = GROUPED ? g.scale : 1.f;
   const uint32_t lds = lds_address(smem);
-  uint32_t off[3][IPW];
-  auto offsets = [&](uint32_t (&v)[IPW], int ld, int last) {
-#pragma unroll
-    for (int j = 0; j < IPW; j++) {
-      const int x = (wave * IPW + j) * 64 + lane, row = x / TL::CPR, c = (x % TL::CPR) ^ TL::swz(row);
-      v[j] = (uint32_t)((min(row, last) * (size_t)ld + c * 8) * sizeof(bf16_t));
-    }
-  };
-  offsets(off[0], p.ldq, LC - 1);
-  offsets(off[1], p.ldk, LC - 1);
-  offsets(off[2], p.ldv, LC - 1);
-  auto transfer = [&](int which, const bf16_t* base, int ld, int head, int chunk, int slot) {
-    const char* at = reinterpret_cast<const char*>(base + (t0 + (size_t)chunk * LC) * ld + (size_t)head * D);
-    const int last = min(LC, g.seq - chunk * LC) - 1;
-    const uint32_t to = lds + (which * 2 + slot) * TILE + wave * IPW * 1024;
-    if (last == LC - 1) {
-#pragma unroll
-      for (int j = 0; j < IPW; j++) dma16_base(at, off[which][j], to + j * 1024);
-    } else {
-      uint32_t v[IPW];
-      offsets(v, ld, last);
-#pragma unroll
-      for (int j = 0; j < IPW; j++) dma16_base(at, v[j], to + j * 1024);
-    }
-  };
-  const int nc = c1 - c0, steps = nc * heads;
+  uint32_t off[3][2];
+  TR::offsets(off[0], p.ldq, LC - 1, wave, lane);
+  TR::offsets(off[1], p.ldk, LC - 1, wave, lane);
+  TR::offsets(off[2], p.ldv, LC - 1, wave, lane);
+  const int steps = (c1 - c0) * heads;
   auto chunk_of = [&](int n) { return REV ? c1 - 1 - n : c0 + n; };
   int in = 0, ih = 0;  // of the step to transfer next
   auto issue = [&]() {
-    const int chunk = chunk_of(in), slot_s = (in * heads + ih) & 1, slot_c = in & 1;
-    if (OUT && (!GROUPED || ih == 0)) transfer(0, p.q, p.ldq, GROUPED ? hk : hk * grp + ih, chunk, GROUPED ? slot_c : slot_s);
+    const int chunk = chunk_of(in), slot_s = (in * heads + ih) & 1, slot_k = GROUPED ? slot_s : in & 1, last = min(LC, g.seq - chunk * LC) - 1, hkv = GROUPED ? hk * grp + ih : hk;
+    const size_t row = t0 + (size_t)chunk * LC;
+    if (OUT) TR::go(p.q + row * p.ldq + (size_t)(hk * grp + ih) * D, p.ldq, off[0], last, lds + slot_s * TR::TILE, wave, lane);
     if (GROUPED || ih == 0) {
-      transfer(1, p.k, p.ldk, GROUPED ? hk * grp + ih : hk, chunk, GROUPED ? slot_s : slot_c);
-      transfer(2, p.v, p.ldv, GROUPED ? hk * grp + ih : hk, chunk, GROUPED ? slot_s : slot_c);
+      TR::go(p.k + row * p.ldk + (size_t)hkv * D, p.ldk, off[1], last, lds + (2 + slot_k) * TR::TILE, wave, lane);
+      TR::go(p.v + row * p.ldv + (size_t)hkv * D, p.ldv, off[2], last, lds + (4 + slot_k) * TR::TILE, wave, lane);
     }
     if (++ih == heads) { ih = 0; in++; }
   };
@@ -119,194 +280,171 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   LinFrag<D> fa;
   fa.init(lane, wave);
   f32x16 S[W];
-  {
-    const float* from = OUT ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr;
-#pragma unroll
-    for (int dt = 0; dt < W; dt++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        const int x = lin_row(dt, r, kg), y = wave * 32 + l32;
-        S[dt][r] = OUT && p.state ? from[p.transposed ? (size_t)y * D + x : (size_t)x * D + y] : 0.f;
-      }
-  }
-  // powers: of a score, of the state a token reads, of a row on its way into the state (fragment 1; fragment 0 of a whole chunk: 16 tokens further from the end, or nearer)
-  const float f_score = g.scale, f_read = GROUPED ? 1.f : g.scale, f_in = GROUPED ? g.scale : 1.f;
-  float weight[OUT ? 16 : 1], into[2][8], whole, read;
-  uint32_t seen;
-  auto powers = [&](int left) {  // of a chunk of so many tokens: rows behind them are copies of the last one, which count for nothing
-    seen = 0;
-#pragma unroll
-    for (int r = 0; r < 16; r++) {
-      const int j = lin_token(r >> 3, r & 7, kg);
-      seen |= (REV ? j >= l32 && j < left : j <= l32) ? 1u << r : 0u;
-    }
-#pragma unroll
-    for (int c = 0; c < 2; c++)
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int t = lin_token(c, e, kg);
-        into[c][e] = t < left ? f_in * lin_pow(l2, REV ? 1 + t : left - 1 - t) : 0.f;
-      }
-    whole = lin_pow(l2, left);
-    read = f_read * (REV ? l32 < left ? lin_pow(l2, left - 1 - l32) : 0.f : lin_pow(l2, l32 + 1));
-  };
-  if constexpr (OUT) {
-#pragma unroll
-    for (int r = 0; r < 16; r++) weight[r] = f_score * lin_pow(l2, max(0, REV ? lin_token(r >> 3, r & 7, kg) - l32 : l32 - lin_token(r >> 3, r & 7, kg)));
-  }
-  int known = LC;  // tokens of the chunk that the powers are for
-  powers(LC);
-  f32x16 ot;
-  bf16x8 qf[OUT ? KS : 1];
+  lin_state_load<D>(S, OUT && p.state ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr, p.transposed, wave, lane);
+  LinPowers<REV> pw;
+  if constexpr (OUT) pw.scores(l2, g.scale, lane);
+  pw.chunk(LC, l2, g.scale, f_in, lane);
   int n = 0, h = 0;
   for (int s = 0; s < steps; s++) {
-    // this step's tiles are here once the transfers before the last step's stores are through
-    if constexpr (OUT && !GROUPED) { if (s > 0) dma_wait<2>(); else dma_wait<0>(); }
+    // this step's tiles are here once the transfers before the last step's two stores are through
+    if constexpr (OUT) { if (s > 0) dma_wait<2>(); else dma_wait<0>(); }
     else dma_wait<0>();
     __syncthreads();  // and every wave is done with the step before, whose slots the next one takes
     if (s + 1 < steps) issue();
-    const int chunk = chunk_of(n), left = min(LC, g.seq - chunk * LC), slot_s = s & 1, slot_c = n & 1, slot_q = GROUPED ? slot_c : slot_s, slot_k = GROUPED ? slot_s : slot_c;
-    const lds_char *Qt = sm + slot_q * TILE, *Kt = sm + (2 + slot_k) * TILE, *Vt = sm + (4 + slot_k) * TILE;
-    if (left != known) powers(known = left);
-    bf16x8 vf[2];
-#pragma unroll
-    for (int c = 0; c < 2; c++) vf[c] = lds_frag_tr(Vt + fa.tr[0], Vt + fa.tr[1], c * 16 * TL::LD * 2);
+    const int chunk = chunk_of(n), left = min(LC, g.seq - chunk * LC), slot_s = s & 1, slot_k = GROUPED ? slot_s : n & 1;
+    const lds_char *Qt = sm + slot_s * TR::TILE, *Kt = sm + (2 + slot_k) * TR::TILE, *Vt = sm + (4 + slot_k) * TR::TILE;
+    if (left != pw.left) pw.chunk(left, l2, g.scale, f_in, lane);
+    LinValues v;
+    v.load(Vt + fa.tr[0], Vt + fa.tr[1], D * 2);
     if constexpr (OUT) {
-      if (!GROUPED || h == 0) {
+      bf16x8 qf[KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ks++) qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
-      }
-      // Tokens whose value holds an infinity or a NaN in this wave's columns: a zero times it would reach the tokens that do not see it.  They stay out of the product and are added
-      // one by one.
-      uint32_t odd = 0;
-      bf16x8 vs[2] = {vf[0], vf[1]};
-      {
-        typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
-        const u16x8 m0 = __builtin_bit_cast(u16x8, vf[0]) & (unsigned short)0x7fff, m1 = __builtin_bit_cast(u16x8, vf[1]) & (unsigned short)0x7fff;
-        const u16x8 m = __builtin_elementwise_max(m0, m1);
-        const auto m4 = __builtin_elementwise_max(__builtin_shufflevector(m, m, 0, 1, 2, 3), __builtin_shufflevector(m, m, 4, 5, 6, 7));
-        const auto m2 = __builtin_elementwise_max(__builtin_shufflevector(m4, m4, 0, 1), __builtin_shufflevector(m4, m4, 2, 3));
-        if (__any(m2[0] >= 0x7f80 || m2[1] >= 0x7f80)) {
+      for (int ks = 0; ks < KS; ks++) qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
+      v.look(kg);
+      f32x16 ot, st;
+      lin_zero(ot);
+      lin_zero(st);
 #pragma unroll
-          for (int e = 0; e < 8; e++) {
-            const uint64_t x = __ballot(m0[e] >= 0x7f80), y = __ballot(m1[e] >= 0x7f80);
-            odd |= ((uint32_t)x ? 1u << lin_token(0, e, 0) : 0) | ((uint32_t)(x >> 32) ? 1u << lin_token(0, e, 1) : 0);
-            odd |= ((uint32_t)y ? 1u << lin_token(1, e, 0) : 0) | ((uint32_t)(y >> 32) ? 1u << lin_token(1, e, 1) : 0);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; e++) {
-            vs[0][e] = (odd >> lin_token(0, e, kg)) & 1 ? (bf16_t)0.f : vf[0][e];
-            vs[1][e] = (odd >> lin_token(1, e, kg)) & 1 ? (bf16_t)0.f : vf[1][e];
-          }
-        }
-      }
-      f32x16 st;
-#pragma unroll
-      for (int r = 0; r < 16; r++) st[r] = 0.f;
-      if (!GROUPED || h == 0) {
-#pragma unroll
-        for (int r = 0; r < 16; r++) ot[r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ks++) ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks], ot);
-#pragma unroll
-        for (int r = 0; r < 16; r++) ot[r] *= read;
+      for (int ks = 0; ks < KS; ks++) {  // in turn: a product waits for one before it that adds to the same registers
+        st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
+        ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks], ot);
       }
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
-#pragma unroll
-      for (int r = 0; r < 16; r++)  // what is not seen becomes a zero whatever it is
-        st[r] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, st[r] * weight[r]) & (uint32_t)__builtin_amdgcn_sbfe((int)seen, r, 1));
-      const bf16x8 pf[2] = {pack_rows(st, 0), pack_rows(st, 1)};
-      ot = MFMA(vs[0], pf[0], ot);
-      ot = MFMA(vs[1], pf[1], ot);
-      if (odd != 0) {
-#pragma unroll 1
-        for (; odd != 0; odd &= odd - 1) {
-          const int j = __builtin_ctz(odd);
-          bf16x8 v0, v1;
-#pragma unroll
-          for (int e = 0; e < 8; e++) {
-            v0[e] = lin_token(0, e, kg) == j ? vf[0][e] : (bf16_t)0.f;
-            v1[e] = lin_token(1, e, kg) == j ? vf[1][e] : (bf16_t)0.f;
-          }
-          f32x16 add;
-#pragma unroll
-          for (int r = 0; r < 16; r++) add[r] = 0.f;
-          add = MFMA(v0, pf[0], add);
-          add = MFMA(v1, pf[1], add);
-          const bool here = REV ? j >= l32 : j <= l32;
-#pragma unroll
-          for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
-        }
-      }
-      if (!GROUPED || h == heads - 1) {  // a lane has a token's columns 8 q4 + 4 kg .. of 32; halves are exchanged so that it stores 16 bytes
-        bf16_t* row = p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(GROUPED ? hk : hk * grp + h) * D + wave * 32 + 8 * kg;
-#pragma unroll
-        for (int c = 0; c < 2; c++) {
-          const uint4 u = __builtin_bit_cast(uint4, pack_rows(ot, c));
-          const auto x = __builtin_amdgcn_permlane32_swap(u.x, u.z, false, false);
-          const auto y = __builtin_amdgcn_permlane32_swap(u.y, u.w, false, false);
-          if (l32 < left) *reinterpret_cast<uint4*>(row + 16 * c) = make_uint4((uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]);
-        }
-      }
+      for (int r = 0; r < 16; r++) ot[r] *= pw.read;
+      lin_inside<REV>(ot, st, pw, v, lane);
+      lin_out(ot, p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(hk * grp + h) * D + wave * 32, l32 < left, lane);
     }
-    if (GROUPED || h == heads - 1) {  // into the state
+    if (GROUPED || h == heads - 1) {
       if (!GROUPED || h == 0) {
 #pragma unroll
         for (int dt = 0; dt < W; dt++)
 #pragma unroll
-          for (int r = 0; r < 16; r++) S[dt][r] *= whole;
+          for (int r = 0; r < 16; r++) S[dt][r] *= pw.whole;
       }
-#pragma unroll
-      for (int c = 0; c < 2; c++) {
-        bf16x8 hi, mid, lo;
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const float x = (float)vf[c][e] * into[c][e];
-          hi[e] = (bf16_t)x;
-          if constexpr (EXACT) {
-            const float y = x - (float)hi[e];
-            mid[e] = (bf16_t)y;
-            lo[e] = (bf16_t)(y - (float)mid[e]);
-          }
-        }
-#pragma unroll
-        for (int dt = 0; dt < W; dt++) {
-          const bf16x8 kf = lds_frag_tr(Kt + fa.tp[dt][0], Kt + fa.tp[dt][1], c * 16 * TL::LD * 2);
-          S[dt] = MFMA(kf, hi, S[dt]);
-          if constexpr (EXACT) {
-            S[dt] = MFMA(kf, mid, S[dt]);
-            S[dt] = MFMA(kf, lo, S[dt]);
-          }
-        }
-      }
+      lin_into<D, EXACT>(S, fa, Kt, v.all, pw.into);
     }
     if (++h == heads) { h = 0; n++; }
   }
   if constexpr (EXACT) {
-    if (!p.sum) return;
-    float* to = p.sum + (OUT ? ((size_t)b * g.nkv + hk) : ((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D;
+    if (p.sum) lin_state_store<D>(S, p.sum + (OUT ? (size_t)b * g.nkv + hk : ((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D, wave, lane);
+  }
+}
+
+// dk and dv, from the row's end, over the group's heads: a wave holds its columns of R (for dv) and of its transpose (for dk), so that q and dout are read once.  LDS: two slots each of K, V, Q, dO tiles.
+template <int D, bool EXACT>
+__device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p, int piece, int hk, int b, char* smem) {
+  using TR = LinTransfer<D>;
+  constexpr int W = D / 32, KS = D / 16;
+  const lds_char* sm = (const lds_char*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
+  const LinGeom& g = a.g;
+  const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), ld = (g.nq + 2 * g.nkv) * D, ldo = g.nq * D;
+  const size_t t0 = (size_t)b * g.seq;
+  const float l2 = g.log_decay[hk] * LOG2E;
+  const uint32_t lds = lds_address(smem);
+  uint32_t off[2][2];
+  TR::offsets(off[0], ld, LC - 1, wave, lane);
+  TR::offsets(off[1], ldo, LC - 1, wave, lane);
+  const int steps = (c1 - c0) * grp;
+  int in = 0, ih = 0;
+  auto issue = [&]() {
+    const int chunk = c1 - 1 - in, slot_s = (in * grp + ih) & 1, slot_c = in & 1, last = min(LC, g.seq - chunk * LC) - 1;
+    const bf16_t* row = p.qkv + (t0 + (size_t)chunk * LC) * ld;
+    if (ih == 0) {
+      TR::go(row + (size_t)(g.nq + hk) * D, ld, off[0], last, lds + slot_c * TR::TILE, wave, lane);
+      TR::go(row + (size_t)(g.nq + g.nkv + hk) * D, ld, off[0], last, lds + (2 + slot_c) * TR::TILE, wave, lane);
+    }
+    TR::go(row + (size_t)(hk * grp + ih) * D, ld, off[0], last, lds + (4 + slot_s) * TR::TILE, wave, lane);
+    TR::go(p.dout + (t0 + (size_t)chunk * LC) * ldo + (size_t)(hk * grp + ih) * D, ldo, off[1], last, lds + (6 + slot_s) * TR::TILE, wave, lane);
+    if (++ih == grp) { ih = 0; in++; }
+  };
+  issue();
+  LinFrag<D> fa;
+  fa.init(lane, wave);
+  f32x16 R[W], Rt[W];
+  const float* state = p.state ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr;
+  lin_state_load<D>(R, state, false, wave, lane);
+  lin_state_load<D>(Rt, state, true, wave, lane);
+  LinPowers<true> pw;
+  pw.scores(l2, g.scale, lane);
+  pw.chunk(LC, l2, 1.f, g.scale, lane);
+  f32x16 dk, dv;
+  bf16x8 kf[KS], vf[KS];
+  int n = 0, h = 0;
+  for (int s = 0; s < steps; s++) {
+    dma_wait<0>();
+    __syncthreads();
+    if (s + 1 < steps) issue();
+    const int chunk = c1 - 1 - n, left = min(LC, g.seq - chunk * LC);
+    const lds_char *Kt = sm + (n & 1) * TR::TILE, *Vt = sm + (2 + (n & 1)) * TR::TILE, *Qt = sm + (4 + (s & 1)) * TR::TILE, *Gt = sm + (6 + (s & 1)) * TR::TILE;
+    if (left != pw.left) pw.chunk(left, l2, 1.f, g.scale, lane);
+    LinValues q, e;
+    q.load(Qt + fa.tr[0], Qt + fa.tr[1], D * 2);
+    e.load(Gt + fa.tr[0], Gt + fa.tr[1], D * 2);
+    q.look(kg);
+    e.look(kg);
+    if (h == 0) {
+      lin_zero(dk);
+      lin_zero(dv);
 #pragma unroll
-    for (int dt = 0; dt < W; dt++)
+      for (int ks = 0; ks < KS; ks++) {
+        kf[ks] = lds_frag(Kt + fa.dir[ks], 0);
+        vf[ks] = lds_frag(Vt + fa.dir[ks], 0);
+        dv = MFMA(pack_rows(R[ks >> 1], ks & 1), kf[ks], dv);
+        dk = MFMA(pack_rows(Rt[ks >> 1], ks & 1), vf[ks], dk);
+      }
 #pragma unroll
-      for (int r = 0; r < 16; r++) to[(size_t)lin_row(dt, r, kg) * D + wave * 32 + l32] = S[dt][r];
+      for (int r = 0; r < 16; r++) { dk[r] *= pw.read; dv[r] *= pw.read; }
+#pragma unroll
+      for (int dt = 0; dt < W; dt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) { R[dt][r] *= pw.whole; Rt[dt][r] *= pw.whole; }
+    }
+    f32x16 sv, sk;
+    lin_zero(sv);
+    lin_zero(sk);
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) {
+      sv = MFMA(lds_frag(Qt + fa.dir[ks], 0), kf[ks], sv);
+      sk = MFMA(lds_frag(Gt + fa.dir[ks], 0), vf[ks], sk);
+    }
+    lin_inside<true>(dv, sv, pw, e, lane);
+    lin_inside<true>(dk, sk, pw, q, lane);
+    lin_into<D, EXACT>(R, fa, Qt, e.all, pw.into);
+    lin_into<D, false>(Rt, fa, Gt, q.all, pw.into);
+    if (++h < grp) continue;
+    bf16_t* row = p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + wave * 32;
+    lin_out(dk, row + (size_t)(g.nq + hk) * D, l32 < left, lane);
+    lin_out(dv, row + (size_t)(g.nq + g.nkv + hk) * D, l32 < left, lane);
+    h = 0;
+    n++;
+  }
+  if constexpr (EXACT) {
+    if (p.sum) lin_state_store<D>(R, p.sum + ((size_t)b * g.nkv + hk) * D * D, wave, lane);
   }
 }
 
 // The forward pass: OUT its results, otherwise the pieces' contributions to the states.  grid (pieces, nkv, batch)
 template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, LIN_OCC) void lin_fwd_kernel(const LinArgs a) {
+__global__ __launch_bounds__(2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lin_walk<D, false, false, EXACT, OUT>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
-// The backward pass: dq, dk and dv (OUT), otherwise the pieces' contributions to S and R.  grid (pieces, nkv * (OUT ? 3 : 2), batch)
-template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, LIN_OCC) void lin_bwd_kernel(const LinArgs a) {
+// The backward pass: dk and dv (grid rows y < nkv, the longer ones), then dq.  grid (pieces, 2 * nkv, batch)
+template <int D, bool EXACT>
+__global__ __launch_bounds__(2 * D, 1) void lin_bwd_kernel(const LinArgs a, const LinGrads k) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int nkv = a.g.nkv, y = blockIdx.y, b = blockIdx.z;
-  if (y < nkv) lin_walk<D, false, false, EXACT && !OUT, OUT>(a, a.pass[0], blockIdx.x, y, b, smem);
-  else if (y < 2 * nkv) lin_walk<D, true, true, EXACT && !OUT, OUT>(a, a.pass[1], blockIdx.x, y - nkv, b, smem);
-  else if constexpr (OUT) lin_walk<D, true, true, EXACT, OUT>(a, a.pass[2], blockIdx.x, y - 2 * nkv, b, smem);
+  const int nkv = a.g.nkv, y = blockIdx.y;
+  if (y < nkv) lin_walk_kv<D, EXACT>(a, k, blockIdx.x, y, blockIdx.z, smem);
+  else lin_walk<D, false, false, false, true>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
+}
+// The pieces' contributions to R (y < nkv) and to S.  grid (pieces, 2 * nkv, batch)
+template <int D>
+__global__ __launch_bounds__(2 * D, 2) void lin_bwd_sums_kernel(const LinArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int nkv = a.g.nkv, y = blockIdx.y;
+  if (y < nkv) lin_walk<D, true, true, true, false>(a, a.pass[1], blockIdx.x, y, blockIdx.z, smem);
+  else lin_walk<D, false, false, true, false>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
 }
 // Carries the states along the pieces: each piece's contribution gives place to the state before it.  REV: from the end, after the same of the S of a backward pass.
 // grid (D * D / 1024, nkv * passes, batch), four elements a thread
@@ -338,12 +476,10 @@ __global__ __launch_bounds__(256) void lin_carry_kernel(const LinArgs a, const L
 // ------------------------------------------------------------------------------------ host side
 // Pieces of a row: enough that the chip's units have two blocks each, none below LIN_LEAST chunks.
 #define LIN_LEAST 4
-#ifndef LIN_BLOCKS
 #define LIN_BLOCKS 512
-#endif
 struct LinCut { int pieces, per; };
 static LinCut lin_cut(const LinGeom& g, bool bwd) {
-  const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 3 : 1);
+  const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 2 : 1);
   const long long want = std::max(1ll, std::min((LIN_BLOCKS + blocks - 1) / blocks, chunks / LIN_LEAST));
   const int per = (int)((chunks + want - 1) / want);
   return {(int)((chunks + per - 1) / per), per};
@@ -389,28 +525,24 @@ static int lin_bwd(const LinGeom& g, const bf16_t* qkv, const float* state_in, c
   const LinCut c = lin_cut(g, true);
   LinArgs a = {g, c.pieces, c.per, {}};
   a.pass[0] = {dout, v, k, dqkv, ldo, ld, ld, ld, state_in, nullptr, 1};
-  a.pass[1] = {v, dout, q, dqkv + kc, ld, ldo, ld, ld, dstate_out, nullptr, 1};
-  a.pass[2] = {k, q, dout, dqkv + vc, ld, ld, ldo, ld, dstate_out, dstate_in, 0};
-  const size_t lds = 6 * LC * D * 2;
-  const dim3 grid(c.pieces, g.nkv * 3, g.batch);
+  LinGrads kv = {qkv, dout, dqkv, dstate_out, dstate_in};
+  const dim3 grid(c.pieces, g.nkv * 2, g.batch);
   if (c.pieces > 1) {
     float* R = ws + lin_states(g, c.pieces);
     LinArgs f = a;
     f.pass[0] = {nullptr, k, v, nullptr, 0, ld, ld, 0, nullptr, ws, 0};
     f.pass[1] = {nullptr, q, dout, nullptr, 0, ld, ldo, 0, nullptr, R, 0};
-    lin_bwd_kernel<D, true, false><<<dim3(c.pieces, g.nkv * 2, g.batch), 2 * D, lds, s>>>(f);
+    lin_bwd_sums_kernel<D><<<grid, 2 * D, 6 * LC * D * 2, s>>>(f);
     DH_LAUNCH_CHECK();
     lin_carry_kernel<D><<<dim3(D * D / 1024, g.nkv * 2, g.batch), 256, 0, s>>>(a, {ws, state_in, nullptr, 0}, {R, dstate_out, dstate_in, 1});
     DH_LAUNCH_CHECK();
     a.pass[0].state = ws;
-    a.pass[1].state = a.pass[2].state = R;
-    a.pass[2].sum = nullptr;
-  } else if (dstate_in) {
-    lin_bwd_kernel<D, true, true><<<grid, 2 * D, lds, s>>>(a);
-    DH_LAUNCH_CHECK();
-    return DH_OK;
+    kv.state = R;
+    kv.sum = nullptr;
   }
-  lin_bwd_kernel<D, false, true><<<grid, 2 * D, lds, s>>>(a);
+  const size_t lds = 8 * LC * D * 2;
+  if (kv.sum) lin_bwd_kernel<D, true><<<grid, 2 * D, lds, s>>>(a, kv);
+  else lin_bwd_kernel<D, false><<<grid, 2 * D, lds, s>>>(a, kv);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
