@@ -1972,3 +1972,4 @@ int dh_launch_attn_bwd_bf16(int batch, int seq_q, int nq, int nkv, int d, const 
 }
 
 #include "attn_docs_bf16.h"
+#include "attn_window_bf16.h"

@@ -1,0 +1,8 @@
+// Attention with a sliding window and sinks: what its sources share.
+#pragma once
+#include "window_rows.h"
+
+int dh_launch_window_fwd_bf16(const WindowGeom& g, const bf16_t* qkv, bf16_t* o, float* lse, void* ws, hipStream_t stream);
+size_t dh_window_fwd_bf16_ws_bytes(const WindowGeom& g);
+int dh_launch_window_bwd_bf16(const WindowGeom& g, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, void* ws, hipStream_t stream);
+size_t dh_window_bwd_bf16_ws_bytes(const WindowGeom& g);

@@ -1,6 +1,6 @@
 // Causal attention with a sliding window and sinks: entry points, the kernels of a wave a row, and the form for single tokens.
 #include <algorithm>
-#include "window_rows.h"
+#include "window.h"
 
 #define WR_THREADS 256
 // grid (rows / 4, heads, batch)
@@ -166,8 +166,13 @@ static int check_window(const char* who, int dtype, int batch, int seq, int wind
   if (window < 1 || sinks < 0) DH_FAIL(DH_ERR_SHAPE, "%s: window=%d sinks=%d (at least 1 and 0)", who, window, sinks);
   return DH_OK;
 }
-extern "C" size_t dh_attn_window_fwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) { return 0; }
-extern "C" size_t dh_attn_window_bwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) { return 0; }
+static bool window_sized(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) { return mix_sized(dtype, batch, seq, nq, nkv, d) && window >= 1 && sinks >= 0; }
+extern "C" size_t dh_attn_window_fwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) {
+  return dtype == DH_BF16 && window_sized(dtype, batch, seq, window, sinks, nq, nkv, d) ? dh_window_fwd_bf16_ws_bytes(window_geom(batch, seq, window, sinks, nq, nkv, d)) : 0;
+}
+extern "C" size_t dh_attn_window_bwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d) {
+  return dtype == DH_BF16 && window_sized(dtype, batch, seq, window, sinks, nq, nkv, d) ? dh_window_bwd_bf16_ws_bytes(window_geom(batch, seq, window, sinks, nq, nkv, d)) : 0;
+}
 
 template <typename T>
 static int window_fwd(const WindowGeom& g, const void* qkv, void* o, float* lse, hipStream_t s) {
@@ -193,7 +198,7 @@ extern "C" int dh_attn_window_fwd(int dtype, int batch, int seq, int window, int
   if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_window_fwd: workspace %zu < %zu bytes", ws_bytes, need);
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_fwd: ws must be 16-byte aligned");
   const WindowGeom g = window_geom(batch, seq, window, sinks, nq, nkv, d);
-  return dtype == DH_BF16 ? window_fwd<bf16_t>(g, qkv, o, lse, (hipStream_t)stream) : window_fwd<float>(g, qkv, o, lse, (hipStream_t)stream);
+  return dtype == DH_BF16 ? dh_launch_window_fwd_bf16(g, (const bf16_t*)qkv, (bf16_t*)o, lse, ws, (hipStream_t)stream) : window_fwd<float>(g, qkv, o, lse, (hipStream_t)stream);
 }
 extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, const void* o, const void* dout, const float* lse,
                                   void* dqkv, float* delta, void* ws, size_t ws_bytes, void* stream) {
@@ -205,7 +210,9 @@ extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int
   if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_window_bwd: workspace %zu < %zu bytes", ws_bytes, need);
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_bwd: ws must be 16-byte aligned");
   const WindowGeom g = window_geom(batch, seq, window, sinks, nq, nkv, d);
-  return dtype == DH_BF16 ? window_bwd<bf16_t>(g, qkv, o, dout, lse, dqkv, delta, (hipStream_t)stream) : window_bwd<float>(g, qkv, o, dout, lse, dqkv, delta, (hipStream_t)stream);
+  if (dtype == DH_BF16)
+    return dh_launch_window_bwd_bf16(g, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)dout, lse, (bf16_t*)dqkv, delta, ws, (hipStream_t)stream);
+  return window_bwd<float>(g, qkv, o, dout, lse, dqkv, delta, (hipStream_t)stream);
 }
 
 // Query heads that a block takes at once: up to 8; a group of more is shared out evenly over blocks, which read the cache again.
