@@ -2,99 +2,31 @@
 #include <algorithm>
 #include "linattn.h"
 
-// The recurrence as it stands, a token at a time: a block has a state, a thread one column (or row) of it in registers.
-// grid (nkv, batch), 128 threads
-#define LR_THREADS 128
-template <typename T>
-__global__ __launch_bounds__(LR_THREADS) void lin_rec_fwd_kernel(const LinGeom g, const T* __restrict__ qkv, const float* __restrict__ state_in, T* __restrict__ o,
-                                                                 float* __restrict__ state_out) {
-  __shared__ float ks[LR_THREADS], qs[LR_THREADS];
-  const int hk = blockIdx.x, b = blockIdx.y, y = threadIdx.x, d = g.d, grp = g.nq / g.nkv;
-  const size_t ld = (size_t)(g.nq + 2 * g.nkv) * d, st = ((size_t)b * g.nkv + hk) * d * d;
-  const float lam = expf(g.log_decay[hk]);
-  const bool on = y < d;
-  float S[LR_THREADS];
-#pragma unroll
-  for (int x = 0; x < LR_THREADS; x++) S[x] = on && x < d && state_in ? state_in[st + (size_t)x * d + y] : 0.f;
-  for (int t = 0; t < g.seq; t++) {
-    const T* row = qkv + ((size_t)b * g.seq + t) * ld;
-    __syncthreads();
-    ks[y] = on ? to_f32(row[(size_t)(g.nq + hk) * d + y]) : 0.f;
-    const float v = on ? to_f32(row[(size_t)(g.nq + g.nkv + hk) * d + y]) : 0.f;
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < LR_THREADS; x++) S[x] = x < d ? fmaf(ks[x], v, lam * S[x]) : 0.f;
-    for (int h = hk * grp; h < (hk + 1) * grp; h++) {
-      __syncthreads();
-      qs[y] = on ? to_f32(row[(size_t)h * d + y]) : 0.f;
-      __syncthreads();
-      float s = 0.f;
-#pragma unroll
-      for (int x = 0; x < LR_THREADS; x++) s = x < d ? fmaf(qs[x], S[x], s) : s;
-      if (on) o[(((size_t)b * g.seq + t) * g.nq + h) * d + y] = from_f32<T>(s * g.scale);
-    }
+// ------------------------------------------------------------------------------------ states along the pieces of a row
+// grid (ceil(d * d / 1024), nkv * passes, batch), four elements a thread
+__global__ __launch_bounds__(256) void lin_carry_kernel(const LinGeom g, int pieces, int tokens, const LinCarry c0, const LinCarry c1) {
+  const int b = blockIdx.z, hk = blockIdx.y % g.nkv, e = (blockIdx.x * 256 + threadIdx.x) * 4, dd = g.d * g.d;
+  if (e >= dd) return;
+  const LinCarry& c = (int)blockIdx.y >= g.nkv ? c1 : c0;
+  const size_t head = (size_t)b * g.nkv + hk;
+  const float l2 = g.log_decay[hk] * 1.4426950408889634f, f = lin_pow(l2, tokens), f_last = lin_pow(l2, g.seq - (pieces - 1) * tokens);
+  f32x4 run = {0.f, 0.f, 0.f, 0.f};
+  if (c.first) run = *reinterpret_cast<const f32x4*>(c.first + head * dd + e);
+  float* at = c.sums + head * pieces * dd + e;
+#pragma unroll 4
+  for (int i = 0; i < pieces; i++) {
+    const int s = c.rev ? pieces - 1 - i : i;
+    f32x4* x = reinterpret_cast<f32x4*>(at + (size_t)s * dd);
+    const f32x4 sum = *x;
+    *x = run;
+    run = run * (s == pieces - 1 ? f_last : f) + sum;
   }
-  if (state_out && on)
-#pragma unroll
-    for (int x = 0; x < LR_THREADS; x++)
-      if (x < d) state_out[st + (size_t)x * d + y] = S[x];
+  if (c.last) *reinterpret_cast<f32x4*>(c.last + head * dd + e) = run;
 }
-// grid (nkv, batch, 3): dq (forward in time), dk and dstate_in, dv (backward in time).  A thread holds M[.] = S[y][.] (dq), R[y][.] (dk) or R[.][y] (dv).
-template <typename T>
-__global__ __launch_bounds__(LR_THREADS) void lin_rec_bwd_kernel(const LinGeom g, const T* __restrict__ qkv, const float* __restrict__ state_in, const T* __restrict__ dout,
-                                                                 const float* __restrict__ dstate_out, T* __restrict__ dqkv, float* __restrict__ dstate_in) {
-  __shared__ float ws[LR_THREADS];
-  const int hk = blockIdx.x, b = blockIdx.y, kind = blockIdx.z, y = threadIdx.x, d = g.d, grp = g.nq / g.nkv;
-  const size_t ld = (size_t)(g.nq + 2 * g.nkv) * d, st = ((size_t)b * g.nkv + hk) * d * d;
-  const float lam = expf(g.log_decay[hk]);
-  const bool on = y < d;
-  const float* from = kind == 0 ? state_in : dstate_out;
-  float M[LR_THREADS];
-#pragma unroll
-  for (int x = 0; x < LR_THREADS; x++) M[x] = on && x < d && from ? from[st + (kind == 2 ? (size_t)x * d + y : (size_t)y * d + x)] : 0.f;
-  auto share = [&](const T* p) {
-    __syncthreads();
-    ws[y] = on ? to_f32(p[y]) : 0.f;
-    __syncthreads();
-  };
-  auto update = [&](float f, float own) {  // M = f M + own * (shared vector)
-#pragma unroll
-    for (int x = 0; x < LR_THREADS; x++) M[x] = x < d ? fmaf(own, ws[x], f * M[x]) : 0.f;
-  };
-  auto dot = [&]() {
-    float s = 0.f;
-#pragma unroll
-    for (int x = 0; x < LR_THREADS; x++) s = x < d ? fmaf(ws[x], M[x], s) : s;
-    return s;
-  };
-  for (int n = 0; n < g.seq; n++) {
-    const int t = kind == 0 ? n : g.seq - 1 - n;
-    const size_t tok = (size_t)b * g.seq + t;
-    const T *row = qkv + tok * ld, *k = row + (size_t)(g.nq + hk) * d, *v = k + (size_t)g.nkv * d, *dor = dout + tok * g.nq * d;
-    T* out = dqkv + tok * ld;
-    if (kind == 0) {
-      share(v);
-      update(lam, on ? to_f32(k[y]) : 0.f);
-      for (int h = hk * grp; h < (hk + 1) * grp; h++) {
-        share(dor + (size_t)h * d);
-        const float s = dot();
-        if (on) out[(size_t)h * d + y] = from_f32<T>(s * g.scale);
-      }
-      continue;
-    }
-    for (int h = hk * grp; h < (hk + 1) * grp; h++) {
-      const T *q = row + (size_t)h * d, *e = dor + (size_t)h * d;
-      share(kind == 1 ? e : q);
-      update(h == hk * grp && n > 0 ? lam : 1.f, on ? g.scale * to_f32((kind == 1 ? q : e)[y]) : 0.f);
-    }
-    share(kind == 1 ? v : k);
-    const float s = dot();
-    if (on) out[(size_t)(g.nq + (kind == 1 ? 0 : g.nkv) + hk) * d + y] = from_f32<T>(s);
-  }
-  if (kind == 1 && dstate_in && on)
-#pragma unroll
-    for (int x = 0; x < LR_THREADS; x++)
-      if (x < d) dstate_in[st + (size_t)y * d + x] = g.seq > 0 ? lam * M[x] : M[x];
+int dh_launch_lin_carry(const LinGeom& g, int pieces, int tokens, const LinCarry& c0, const LinCarry* c1, hipStream_t s) {
+  lin_carry_kernel<<<dim3((g.d * g.d + 1023) / 1024, g.nkv * (c1 ? 2 : 1), g.batch), 256, 0, s>>>(g, pieces, tokens, c0, c1 ? *c1 : LinCarry{});
+  DH_LAUNCH_CHECK();
+  return DH_OK;
 }
 
 // ------------------------------------------------------------------------------------ single tokens
@@ -150,11 +82,15 @@ __global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, c
 }
 
 // ------------------------------------------------------------------------------------ host side
+static size_t lin_ws_bytes(int dtype, const LinGeom& g, bool bwd) {
+  if (!mix_sized(dtype, g.batch, g.seq, g.nq, g.nkv, g.d)) return 0;
+  return dtype == DH_BF16 ? dh_linattn_bf16_ws_bytes(g, bwd) : dh_linattn_f32_ws_bytes(g, bwd);
+}
 extern "C" size_t dh_linattn_fwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d) {
-  return dtype == DH_BF16 && mix_sized(dtype, batch, seq, nq, nkv, d) ? dh_linattn_bf16_ws_bytes({batch, seq, nq, nkv, d, 1.f, nullptr}, false) : 0;
+  return lin_ws_bytes(dtype, {batch, seq, nq, nkv, d, 1.f, nullptr}, false);
 }
 extern "C" size_t dh_linattn_bwd_workspace_bytes(int dtype, int batch, int seq, int nq, int nkv, int d) {
-  return dtype == DH_BF16 && mix_sized(dtype, batch, seq, nq, nkv, d) ? dh_linattn_bf16_ws_bytes({batch, seq, nq, nkv, d, 1.f, nullptr}, true) : 0;
+  return lin_ws_bytes(dtype, {batch, seq, nq, nkv, d, 1.f, nullptr}, true);
 }
 
 static bool lin_overlap(const void* a, const void* b, size_t bytes) { return a && b && (const char*)a < (const char*)b + bytes && (const char*)b < (const char*)a + bytes; }
@@ -171,10 +107,9 @@ extern "C" int dh_linattn_fwd(int dtype, int batch, int seq, int nq, int nkv, in
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "linattn_fwd: ws must be 16-byte aligned");
   const LinGeom g = {batch, seq, nq, nkv, d, scale, log_decay};
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == DH_BF16 && seq > 0) return dh_launch_linattn_fwd_bf16(g, (const bf16_t*)qkv, state_in, (bf16_t*)o, state_out, ws, s);
-  lin_rec_fwd_kernel<float><<<dim3(nkv, batch), LR_THREADS, 0, s>>>(g, (const float*)qkv, state_in, (float*)o, state_out);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
+  if (seq == 0) return state_out ? dh_launch_lin_carry(g, 0, 0, {nullptr, state_in, state_out, 0}, nullptr, s) : DH_OK;
+  if (dtype == DH_BF16) return dh_launch_linattn_fwd_bf16(g, (const bf16_t*)qkv, state_in, (bf16_t*)o, state_out, ws, s);
+  return dh_launch_linattn_fwd_f32(g, (const float*)qkv, state_in, (float*)o, state_out, ws, s);
 }
 extern "C" int dh_linattn_bwd(int dtype, int batch, int seq, int nq, int nkv, int d, float scale, const float* log_decay, const void* qkv, const float* state_in, const void* dout,
                               const float* dstate_out, void* dqkv, float* dstate_in, void* ws, size_t ws_bytes, void* stream) {
@@ -189,10 +124,9 @@ extern "C" int dh_linattn_bwd(int dtype, int batch, int seq, int nq, int nkv, in
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "linattn_bwd: ws must be 16-byte aligned");
   const LinGeom g = {batch, seq, nq, nkv, d, scale, log_decay};
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == DH_BF16 && seq > 0) return dh_launch_linattn_bwd_bf16(g, (const bf16_t*)qkv, state_in, (const bf16_t*)dout, dstate_out, (bf16_t*)dqkv, dstate_in, ws, s);
-  lin_rec_bwd_kernel<float><<<dim3(nkv, batch, 3), LR_THREADS, 0, s>>>(g, (const float*)qkv, state_in, (const float*)dout, dstate_out, (float*)dqkv, dstate_in);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
+  if (seq == 0) return dstate_in ? dh_launch_lin_carry(g, 0, 0, {nullptr, dstate_out, dstate_in, 0}, nullptr, s) : DH_OK;
+  if (dtype == DH_BF16) return dh_launch_linattn_bwd_bf16(g, (const bf16_t*)qkv, state_in, (const bf16_t*)dout, dstate_out, (bf16_t*)dqkv, dstate_in, ws, s);
+  return dh_launch_linattn_bwd_f32(g, (const float*)qkv, state_in, (const float*)dout, dstate_out, (float*)dqkv, dstate_in, ws, s);
 }
 extern "C" int dh_linattn_step(int dtype, int batch, int nq, int nkv, int d, float scale, const float* log_decay, const int32_t* pos, const void* qkv, const float* state_in,
                                float* state_out, void* o, void* stream) {

@@ -20,7 +20,6 @@
 #include "dma.h"
 #include "linattn.h"
 
-#define LC 32  // tokens of a chunk
 
 // One pass in the form above.
 struct LinPass {
@@ -65,8 +64,6 @@ struct LinFrag {
 __device__ __forceinline__ int lin_row(int dt, int r, int kg) { return 32 * dt + 16 * (r >> 3) + 8 * kg + (r & 7); }  // state row of accumulator register r
 __device__ __forceinline__ int lin_token(int c, int e, int kg) { return 16 * c + 8 * (e >> 2) + 4 * kg + (e & 3); }    // token of element e of fragment c
 
-// lambda^m; log2 of lambda may be minus infinity
-__device__ __forceinline__ float lin_pow(float l2, int m) { return m == 0 ? 1.f : fast_exp2(l2 * (float)m); }
 
 // What a chunk's arithmetic multiplies by.  Powers of lambda: of a score, of the state that a token reads, of a row on its way into the state.  REV: the row is walked from its end.
 template <bool REV>
@@ -446,38 +443,10 @@ __global__ __launch_bounds__(2 * D, 2) void lin_bwd_sums_kernel(const LinArgs a)
   if (y < nkv) lin_walk<D, true, true, true, false>(a, a.pass[1], blockIdx.x, y, blockIdx.z, smem);
   else lin_walk<D, false, false, true, false>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
 }
-// Carries the states along the pieces: each piece's contribution gives place to the state before it.  REV: from the end, after the same of the S of a backward pass.
-// grid (D * D / 1024, nkv * passes, batch), four elements a thread
-struct LinCarry { float* sums; const float* first; float* last; int rev; };
-template <int D>
-__global__ __launch_bounds__(256) void lin_carry_kernel(const LinArgs a, const LinCarry c0, const LinCarry c1) {
-  const LinGeom& g = a.g;
-  const int b = blockIdx.z, hk = blockIdx.y % g.nkv, e = (blockIdx.x * 256 + threadIdx.x) * 4;
-  const LinCarry& c = (int)blockIdx.y >= g.nkv ? c1 : c0;
-  const size_t head = (size_t)b * g.nkv + hk;
-  const float l2 = g.log_decay[hk] * LOG2E;
-  const int len = a.per * LC;
-  f32x4 run = {0.f, 0.f, 0.f, 0.f};
-  if (c.first) run = *reinterpret_cast<const f32x4*>(c.first + head * D * D + e);
-  const float f = lin_pow(l2, len), f_last = lin_pow(l2, g.seq - (a.pieces - 1) * len);
-  float* at = c.sums + head * a.pieces * D * D + e;
-#pragma unroll 4
-  for (int i = 0; i < a.pieces; i++) {
-    const int s = c.rev ? a.pieces - 1 - i : i;
-    f32x4* x = reinterpret_cast<f32x4*>(at + (size_t)s * D * D);
-    const f32x4 sum = *x;
-    *x = run;
-    const float w = s == a.pieces - 1 ? f_last : f;
-    run = run * w + sum;
-  }
-  if (c.last) *reinterpret_cast<f32x4*>(c.last + head * D * D + e) = run;
-}
-
 // ------------------------------------------------------------------------------------ host side
 // Pieces of a row: enough that the chip's units have two blocks each, none below LIN_LEAST chunks.
 #define LIN_LEAST 4
 #define LIN_BLOCKS 512
-struct LinCut { int pieces, per; };
 static LinCut lin_cut(const LinGeom& g, bool bwd) {
   const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 2 : 1);
   const long long want = std::max(1ll, std::min((LIN_BLOCKS + blocks - 1) / blocks, chunks / LIN_LEAST));
@@ -502,8 +471,7 @@ static int lin_fwd(const LinGeom& g, const bf16_t* qkv, const float* state_in, b
     a.pass[0].sum = ws;
     lin_fwd_kernel<D, true, false><<<grid, 2 * D, lds, s>>>(a);
     DH_LAUNCH_CHECK();
-    lin_carry_kernel<D><<<dim3(D * D / 1024, g.nkv, g.batch), 256, 0, s>>>(a, {ws, state_in, state_out, 0}, {});
-    DH_LAUNCH_CHECK();
+    if (int rc = dh_launch_lin_carry(g, c.pieces, c.per * LC, {ws, state_in, state_out, 0}, nullptr, s)) return rc;
     a.pass[0].state = ws;
   } else if (state_out) {
     lin_fwd_kernel<D, true, true><<<grid, 2 * D, lds, s>>>(a);
@@ -534,8 +502,8 @@ static int lin_bwd(const LinGeom& g, const bf16_t* qkv, const float* state_in, c
     f.pass[1] = {nullptr, q, dout, nullptr, 0, ld, ldo, 0, nullptr, R, 0};
     lin_bwd_sums_kernel<D><<<grid, 2 * D, 6 * LC * D * 2, s>>>(f);
     DH_LAUNCH_CHECK();
-    lin_carry_kernel<D><<<dim3(D * D / 1024, g.nkv * 2, g.batch), 256, 0, s>>>(a, {ws, state_in, nullptr, 0}, {R, dstate_out, dstate_in, 1});
-    DH_LAUNCH_CHECK();
+    const LinCarry back = {R, dstate_out, dstate_in, 1};
+    if (int rc = dh_launch_lin_carry(g, c.pieces, c.per * LC, {ws, state_in, nullptr, 0}, &back, s)) return rc;
     a.pass[0].state = ws;
     kv.state = R;
     kv.sum = nullptr;
