@@ -34,15 +34,30 @@ __global__ __launch_bounds__(WR_THREADS) void window_rows_dkv_kernel(const Windo
 }
 
 // ------------------------------------------------------------------------------------ single tokens
-// Bound by memory: each visible row of the cache is read once.  `lanes` lanes (a power of two) read a row of a head, 8 elements each, so that a wave has 64 / lanes rows in
-// flight a load; each such group keeps a running maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.
+// Bound by memory: each visible row of the cache is read once.  LANES lanes read a row of a head, 8 elements each, so that a wave has 64 / LANES rows in flight a load; each such
+// group keeps a reference maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.
 struct WindowStep {
   WindowGeom g;  // seq: rows of the cache
   int chunk;     // keys of a block
   int splits;    // blocks that share a sequence's keys
 };
 #define WS_THREADS 256
-#define WS_ROWS 4  // rows a lane has in flight
+#define WS_ROWS 4    // rows a lane has in flight
+#define WS_TAU 8.0f  // log2 of the headroom that weights may take over the reference maximum before it moves
+// Sum over 8 or 16 neighbouring lanes, in all of them, by lane permutations inside the vector ALU.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+  x = dpp_add<0xb1>(x);   // lane ^ 1
+  x = dpp_add<0x4e>(x);   // lane ^ 2
+  x = dpp_add<0x141>(x);  // 8 lanes mirrored: the other four
+  if constexpr (LANES == 16) x = dpp_add<0x140>(x);  // 16 lanes mirrored
+  return x;
+}
+// grid (splits * head groups, nkv, batch)
 template <typename T, int LANES, int GH>
 __global__ __launch_bounds__(WS_THREADS) void window_step_kernel(const WindowStep a, const int32_t* __restrict__ pos, const T* __restrict__ qkv, T* __restrict__ kv, T* __restrict__ o,
                                                                  float* __restrict__ part) {
@@ -58,56 +73,90 @@ __global__ __launch_bounds__(WS_THREADS) void window_step_kernel(const WindowSte
   const T* token = qkv + (size_t)b * (g.nq + 2 * g.nkv) * d;
   T* cache = kv + (size_t)b * g.seq * ld + (size_t)hk * d;
   const T* now = token + (size_t)(g.nq + hk) * d;
-  const bool on = c0 < d;
-  auto row = [&](int j) { return j < g.seq ? j : g.sinks + (j - g.sinks) % turn; };
+  const bool on = c0 < d, ring = p >= g.seq;
+  // Row of the c-th key that the token sees: sinks, then positions from lo on.  Behind the first turn lo lies behind the sinks, and the window wraps once at most.
+  const int first = ring ? g.sinks + (lo - g.sinks) % turn : lo;
+  auto row = [&](int c) {
+    const int r = first + c - ns;
+    return c < ns ? c : r < g.seq ? r : r - turn;
+  };
   if (from < n && to == n && h0 == 0 && group == 0 && on) {  // the token's own key and value
-    T* at = cache + row(p) * ld + c0;
+    T* at = cache + row(n - 1) * ld + c0;
     Vec8<T> x, y;
     x.load(now + c0);
     y.load(now + (size_t)g.nkv * d + c0);
     x.store(at);
     y.store(at + (size_t)g.nkv * d);
   }
-  float q[GH][8], acc[GH][8], m[GH], sum[GH];
+  float q[GH][8], acc[GH][8], m[GH], sum[GH];  // scores in log2
 #pragma unroll
   for (int h = 0; h < GH; h++) {
-    m[h] = -INFINITY;
+    m[h] = -3.0e38f;
     sum[h] = 0.f;
     Vec8<T> x;
     if (on && h < heads) x.load(token + (size_t)(hk * grp + h0 + h) * d + c0);
 #pragma unroll
-    for (int e = 0; e < 8; e++) { q[h][e] = on && h < heads ? x.v[e] * g.scale : 0.f; acc[h][e] = 0.f; }
+    for (int e = 0; e < 8; e++) { q[h][e] = on && h < heads ? x.v[e] * (g.scale * 1.4426950408889634f) : 0.f; acc[h][e] = 0.f; }
   }
-  for (int c = from + group; c < to; c += GROUPS * WS_ROWS) {
-    Raw8<T> rk[WS_ROWS], rv[WS_ROWS];
+  Raw8<T> rk[WS_ROWS], rv[WS_ROWS];
+  auto fetch = [&](int c) {
 #pragma unroll
     for (int u = 0; u < WS_ROWS; u++) {
-      const int cu = min(c + u * GROUPS, to - 1), j = cu < ns ? cu : lo + cu - ns;
-      const T* at = j == p ? now : cache + row(j) * ld;
-      if (on) { rk[u].load(at + c0); rv[u].load(at + (size_t)g.nkv * d + c0); }
+      const int cu = min(c + u * GROUPS, to - 1);
+      const T* at = (cu == n - 1 ? now : cache + row(cu) * ld) + (on ? c0 : 0);  // lanes behind the head read its first columns, which count for nothing
+      rk[u].load(at);
+      rv[u].load(at + (size_t)g.nkv * d);
+    }
+  };
+  if (from + group < to) fetch(from + group);
+  for (int c = from + group; c < to; c += GROUPS * WS_ROWS) {
+    float s[GH][WS_ROWS];
+#pragma unroll
+    for (int u = 0; u < WS_ROWS; u++)
+#pragma unroll
+      for (int h = 0; h < GH; h++) {
+        float x = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) x = fmaf(q[h][e], rk[u].get(e), x);
+        s[h][u] = on ? x : 0.f;
+      }
+    float v[WS_ROWS][8];
+#pragma unroll
+    for (int u = 0; u < WS_ROWS; u++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[u][e] = rv[u].get(e);
+    if (c + GROUPS * WS_ROWS < to) fetch(c + GROUPS * WS_ROWS);
+    bool move = false;
+    float top[GH];
+#pragma unroll
+    for (int h = 0; h < GH; h++) {
+#pragma unroll
+      for (int u = 0; u < WS_ROWS; u++) {
+        const float x = lanes_sum<LANES>(s[h][u]);
+        s[h][u] = c + u * GROUPS < to ? x : -INFINITY;
+        top[h] = u == 0 ? x : __builtin_elementwise_maximum(top[h], s[h][u]);
+      }
+      move |= !(top[h] <= m[h] + WS_TAU);
+    }
+    if (__any(move)) {
+#pragma unroll
+      for (int h = 0; h < GH; h++) {
+        const float mn = __builtin_elementwise_maximum(m[h], top[h]), alpha = __builtin_amdgcn_exp2f(m[h] - mn);
+        sum[h] *= alpha;
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[h][e] *= alpha;
+        m[h] = mn;
+      }
     }
 #pragma unroll
     for (int u = 0; u < WS_ROWS; u++) {
-      if (c + u * GROUPS >= to) continue;
+      const bool in = c + u * GROUPS < to;  // rows behind the block's last are copies of it, which may hold an infinity
 #pragma unroll
       for (int h = 0; h < GH; h++) {
-        float s = 0.f;
+        const float w = __builtin_amdgcn_exp2f(s[h][u] - m[h]);
+        sum[h] += in ? w : 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; e++) s = on ? fmaf(q[h][e], rk[u].get(e), s) : s;
-#pragma unroll
-        for (int x = 1; x < LANES; x <<= 1) s += __shfl_xor(s, x, 64);
-        if (!(s <= m[h])) {  // a larger score, or a NaN, which stays one
-          const float ref = s;
-          const float alpha = m[h] == -INFINITY ? 0.f : expf(m[h] - ref);
-          sum[h] *= alpha;
-#pragma unroll
-          for (int e = 0; e < 8; e++) acc[h][e] *= alpha;
-          m[h] = ref;
-        }
-        const float w = m[h] == -INFINITY ? 0.f : expf(s - m[h]);
-        sum[h] += w;
-#pragma unroll
-        for (int e = 0; e < 8; e++) acc[h][e] = on ? fmaf(w, rv[u].get(e), acc[h][e]) : 0.f;
+        for (int e = 0; e < 8; e++) acc[h][e] = fmaf(w, in ? v[u][e] : 0.f, acc[h][e]);
       }
     }
   }
@@ -122,13 +171,12 @@ __global__ __launch_bounds__(WS_THREADS) void window_step_kernel(const WindowSte
   __syncthreads();
   for (int x = threadIdx.x; x < heads * d; x += WS_THREADS) {
     const int h = x / d, c = x % d, hq = hk * grp + h0 + h;
-    float M = -INFINITY, L = 0.f, A = 0.f;
-    for (int w = 0; w < GROUPS; w++) { const float mw = sm[(w * GH + h) * PER]; M = mw > M || mw != mw ? mw : M; }
-    const float ref = M == -INFINITY ? 0.f : M;
+    float M = -3.0e38f, L = 0.f, A = 0.f;
+    for (int w = 0; w < GROUPS; w++) M = __builtin_elementwise_maximum(M, sm[(w * GH + h) * PER]);
     for (int w = 0; w < GROUPS; w++) {
       const float* of = sm + (w * GH + h) * PER;
-      if (of[0] == -INFINITY) continue;
-      const float f = expf(of[0] - ref);
+      if (of[1] == 0.f) continue;  // no key, or none of any weight
+      const float f = __builtin_amdgcn_exp2f(of[0] - M);
       L = fmaf(f, of[1], L);
       A = fmaf(f, of[2 + c], A);
     }
@@ -147,12 +195,12 @@ __global__ void window_step_merge_kernel(const WindowStep a, const int32_t* __re
   const int b = blockIdx.y, h = blockIdx.x, d = a.g.d, c = threadIdx.x;
   if (pos[b] < 0) return;
   const float* of = part + ((size_t)b * a.g.nq + h) * a.splits * (d + 2);
-  float M = -INFINITY, L = 0.f, A = 0.f;
-  for (int s = 0; s < a.splits; s++) { const float ms = of[(size_t)s * (d + 2)]; M = ms > M || ms != ms ? ms : M; }
+  float M = -3.0e38f, L = 0.f, A = 0.f;
+  for (int s = 0; s < a.splits; s++) M = __builtin_elementwise_maximum(M, of[(size_t)s * (d + 2)]);
   for (int s = 0; s < a.splits; s++) {
     const float* at = of + (size_t)s * (d + 2);
-    if (at[0] == -INFINITY) continue;
-    const float f = expf(at[0] - M);
+    if (at[1] == 0.f) continue;
+    const float f = __builtin_amdgcn_exp2f(at[0] - M);
     L = fmaf(f, at[1], L);
     A = fmaf(f, at[2 + c], A);
   }
