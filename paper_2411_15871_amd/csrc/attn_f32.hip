@@ -488,3 +488,4 @@ int dh_launch_attn_bwd_f32(int batch, int seq, int nq, int nkv, int d, const flo
 }
 
 #include "attn_docs_f32.h"
+#include "attn_window_f32.h"

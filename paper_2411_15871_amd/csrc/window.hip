@@ -1,37 +1,6 @@
-// Causal attention with a sliding window and sinks: entry points, the kernels of a wave a row, and the form for single tokens.
+// Causal attention with a sliding window and sinks: entry points, and the form for single tokens.
 #include <algorithm>
 #include "window.h"
-
-#define WR_THREADS 256
-// grid (rows / 4, heads, batch)
-template <typename T>
-__global__ __launch_bounds__(WR_THREADS) void window_rows_fwd_kernel(const WindowGeom g, const T* __restrict__ qkv, T* __restrict__ o, float* __restrict__ lse) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
-  if (i >= g.seq) return;
-  const size_t t0 = (size_t)blockIdx.z * g.seq, ld = (size_t)(g.nq + 2 * g.nkv) * g.d;
-  window_row_fwd(g, qkv + t0 * ld, h, i, o + ((t0 + i) * g.nq + h) * g.d, lse + (size_t)h * g.batch * g.seq + t0 + i);
-}
-template <typename T>
-__global__ __launch_bounds__(WR_THREADS) void window_rows_dq_kernel(const WindowGeom g, const T* __restrict__ qkv, const T* __restrict__ o, const T* __restrict__ dout,
-                                                                    const float* __restrict__ lse, T* __restrict__ dqkv, float* __restrict__ delta) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, lane = threadIdx.x & 63;
-  if (i >= g.seq) return;
-  const size_t t0 = (size_t)blockIdx.z * g.seq, ld = (size_t)(g.nq + 2 * g.nkv) * g.d, at = ((t0 + i) * g.nq + h) * g.d, st = (size_t)h * g.batch * g.seq + t0 + i;
-  float dl = 0.f;
-  for (int x = lane; x < g.d; x += 64) dl = fmaf(to_f32(o[at + x]), to_f32(dout[at + x]), dl);
-  dl = wave_sum(dl);
-  if (lane == 0) delta[st] = dl;
-  window_row_dq(g, qkv + t0 * ld, dout + at, lse[st], dl, h, i, dqkv + (t0 + i) * ld + (size_t)h * g.d);
-}
-template <typename T>
-__global__ __launch_bounds__(WR_THREADS) void window_rows_dkv_kernel(const WindowGeom g, const T* __restrict__ qkv, const T* __restrict__ dout, const float* __restrict__ lse,
-                                                                     const float* __restrict__ delta, T* __restrict__ dqkv) {
-  const int j = blockIdx.x * 4 + (threadIdx.x >> 6), hk = blockIdx.y;
-  if (j >= g.seq) return;
-  const size_t t0 = (size_t)blockIdx.z * g.seq, ld = (size_t)(g.nq + 2 * g.nkv) * g.d;
-  T* dk = dqkv + (t0 + j) * ld + (size_t)(g.nq + hk) * g.d;
-  window_row_dkv(g, qkv + t0 * ld, dout + t0 * g.nq * g.d, lse + t0, delta + t0, (size_t)g.batch * g.seq, hk, j, dk, dk + (size_t)g.nkv * g.d);
-}
 
 // ------------------------------------------------------------------------------------ single tokens
 // Bound by memory: each visible row of the cache is read once.  LANES lanes read a row of a head, 8 elements each, so that a wave has 64 / LANES rows in flight a load; each such
@@ -222,20 +191,6 @@ extern "C" size_t dh_attn_window_bwd_workspace_bytes(int dtype, int batch, int s
   return dtype == DH_BF16 && window_sized(dtype, batch, seq, window, sinks, nq, nkv, d) ? dh_window_bwd_bf16_ws_bytes(window_geom(batch, seq, window, sinks, nq, nkv, d)) : 0;
 }
 
-template <typename T>
-static int window_fwd(const WindowGeom& g, const void* qkv, void* o, float* lse, hipStream_t s) {
-  window_rows_fwd_kernel<T><<<dim3((g.seq + 3) / 4, g.nq, g.batch), WR_THREADS, 0, s>>>(g, (const T*)qkv, (T*)o, lse);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
-}
-template <typename T>
-static int window_bwd(const WindowGeom& g, const void* qkv, const void* o, const void* dout, const float* lse, void* dqkv, float* delta, hipStream_t s) {
-  window_rows_dq_kernel<T><<<dim3((g.seq + 3) / 4, g.nq, g.batch), WR_THREADS, 0, s>>>(g, (const T*)qkv, (const T*)o, (const T*)dout, lse, (T*)dqkv, delta);
-  DH_LAUNCH_CHECK();
-  window_rows_dkv_kernel<T><<<dim3((g.seq + 3) / 4, g.nkv, g.batch), WR_THREADS, 0, s>>>(g, (const T*)qkv, (const T*)dout, lse, delta, (T*)dqkv);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
-}
 extern "C" int dh_attn_window_fwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes,
                                   void* stream) {
   if (int rc = check_window("attn_window_fwd", dtype, batch, seq, window, sinks, nq, nkv, d)) return rc;
@@ -246,7 +201,8 @@ extern "C" int dh_attn_window_fwd(int dtype, int batch, int seq, int window, int
   if (need > 0 && (!ws || ws_bytes < need)) DH_FAIL(DH_ERR_WORKSPACE_TOO_SMALL, "attn_window_fwd: workspace %zu < %zu bytes", ws_bytes, need);
   if (mix_unaligned(ws)) DH_FAIL(DH_ERR_INVALID_ARG, "attn_window_fwd: ws must be 16-byte aligned");
   const WindowGeom g = window_geom(batch, seq, window, sinks, nq, nkv, d);
-  return dtype == DH_BF16 ? dh_launch_window_fwd_bf16(g, (const bf16_t*)qkv, (bf16_t*)o, lse, ws, (hipStream_t)stream) : window_fwd<float>(g, qkv, o, lse, (hipStream_t)stream);
+  return dtype == DH_BF16 ? dh_launch_window_fwd_bf16(g, (const bf16_t*)qkv, (bf16_t*)o, lse, ws, (hipStream_t)stream) 
+                          : dh_launch_window_fwd_f32(g, (const float*)qkv, (float*)o, lse, (hipStream_t)stream);
 }
 extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, const void* o, const void* dout, const float* lse,
                                   void* dqkv, float* delta, void* ws, size_t ws_bytes, void* stream) {
@@ -260,7 +216,7 @@ extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int
   const WindowGeom g = window_geom(batch, seq, window, sinks, nq, nkv, d);
   if (dtype == DH_BF16)
     return dh_launch_window_bwd_bf16(g, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)dout, lse, (bf16_t*)dqkv, delta, ws, (hipStream_t)stream);
-  return window_bwd<float>(g, qkv, o, dout, lse, dqkv, delta, (hipStream_t)stream);
+  return dh_launch_window_bwd_f32(g, (const float*)qkv, (const float*)o, (const float*)dout, lse, (float*)dqkv, delta, (hipStream_t)stream);
 }
 
 // Query heads that a block takes at once: up to 8; a group of more is shared out evenly over blocks, which read the cache again.
