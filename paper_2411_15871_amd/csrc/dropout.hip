@@ -99,6 +99,43 @@ __global__ __launch_bounds__(DB_COLS * DB_LANES) void dropout_bwd_bias_kernel(co
     *reinterpret_cast<f32x4*>(to + 4) = f32x4{s[4], s[5], s[6], s[7]};
   }
 }
+// Few rows: all of them by one block for 32 columns, so that nothing is left to add behind it.  4 vectors x 256 rows side by side, which meet in the wave and then in LDS, in order.
+#define DD_COLS 4
+template <typename T>
+__global__ __launch_bounds__(1024) void dropout_bwd_direct_kernel(const DropArgs d, int rows, const T* dout, T* dx, int accumulate, float* __restrict__ dbias) {
+  __shared__ float red[16][DD_COLS][8];
+  const uint64_t key = d.rng[0];
+  const uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32), step = (uint32_t)d.rng[1];
+  const int c = threadIdx.x % DD_COLS, col = blockIdx.x * DD_COLS + c, wave = threadIdx.x >> 6;
+  float s[8] = {};
+  if (col < d.vrow)
+    for (int r = threadIdx.x / DD_COLS; r < rows; r += 1024 / DD_COLS) {
+      const size_t i = (size_t)r * d.vrow + col;
+      Vec8<T> x;
+      x.load(dout + i * 8);
+      const Words w = philox(i, step, d.site, k0, k1);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        x.v[e] = bits16(w, e) >= d.below ? x.v[e] * d.factor : 0.f;
+        s[e] += x.v[e];
+      }
+      x.store(dx + i * 8);
+    }
+#pragma unroll
+  for (int e = 0; e < 8; e++)
+#pragma unroll
+    for (int o = DD_COLS; o < 64; o <<= 1) s[e] += __shfl_xor(s[e], o, 64);
+  if ((threadIdx.x & 63) < DD_COLS)
+#pragma unroll
+    for (int e = 0; e < 8; e++) red[wave][c][e] = s[e];
+  __syncthreads();
+  if (threadIdx.x < DD_COLS * 8 && blockIdx.x * DD_COLS + threadIdx.x / 8 < (unsigned)d.vrow) {
+    float t = 0.f;
+    for (int w = 0; w < 16; w++) t += red[w][threadIdx.x / 8][threadIdx.x % 8];
+    float* to = dbias + (size_t)blockIdx.x * DD_COLS * 8 + threadIdx.x;
+    *to = accumulate ? *to + t : t;
+  }
+}
 // dbias from n partial rows, in their order by threads and then in the threads' order.  A block has 32 columns, 8 threads each.
 __global__ __launch_bounds__(256) void dropout_bias_finish_kernel(const float* __restrict__ partial, int n, int H, int accumulate, float* __restrict__ dbias) {
   __shared__ float red[8][33];
@@ -129,6 +166,7 @@ static DropArgs drop_args(int T, int H, float p, const uint64_t* rng, uint32_t s
   return {(size_t)T * (H / 8), H / 8, below, below >= 65536 ? 0.f : (float)(65536.0 / (65536 - below)), site, rng};
 }
 static unsigned drop_blocks(size_t vecs) { return (unsigned)std::min((vecs + DROP_THREADS - 1) / DROP_THREADS, (size_t)4096); }
+static bool drop_direct(int T, int H) { return T > 0 && T <= 2048 && (long long)T * H <= 8 << 20; }
 static int drop_groups(int T, int H) {
   const int cols = (H / 8 + DB_COLS - 1) / DB_COLS;
   return std::max(1, std::min((T + 15) / 16, (2048 + cols - 1) / cols));
@@ -153,7 +191,7 @@ extern "C" int dh_dropout_add_fwd(int dtype, int T, int H, const void* a, const 
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
-extern "C" size_t dh_dropout_add_bwd_ws_bytes(int T, int H) { return T <= 0 || H <= 0 || H % 8 ? 0 : (size_t)drop_groups(T, H) * H * sizeof(float); }
+extern "C" size_t dh_dropout_add_bwd_ws_bytes(int T, int H) { return T <= 0 || H <= 0 || H % 8 || drop_direct(T, H) ? 0 : (size_t)drop_groups(T, H) * H * sizeof(float); }
 extern "C" int dh_dropout_add_bwd(int dtype, int T, int H, const void* dout, float p, const uint64_t* rng, uint32_t site, void* dx, float* dbias, int accumulate, void* ws, size_t ws_bytes,
                                   void* stream) {
   if (int rc = check_drop("dropout_add_bwd", dtype, T, H, p, rng)) return rc;
@@ -167,6 +205,13 @@ extern "C" int dh_dropout_add_bwd(int dtype, int T, int H, const void* dout, flo
   if (!dbias) {
     if (dtype == DH_BF16) dropout_bwd_kernel<bf16_t><<<drop_blocks(d.vecs), DROP_THREADS, 0, s>>>(d, (const bf16_t*)dout, (bf16_t*)dx);
     else dropout_bwd_kernel<float><<<drop_blocks(d.vecs), DROP_THREADS, 0, s>>>(d, (const float*)dout, (float*)dx);
+    DH_LAUNCH_CHECK();
+    return DH_OK;
+  }
+  if (drop_direct(T, H)) {
+    const unsigned n = (H / 8 + DD_COLS - 1) / DD_COLS;
+    if (dtype == DH_BF16) dropout_bwd_direct_kernel<bf16_t><<<n, 1024, 0, s>>>(d, T, (const bf16_t*)dout, (bf16_t*)dx, accumulate, dbias);
+    else dropout_bwd_direct_kernel<float><<<n, 1024, 0, s>>>(d, T, (const float*)dout, (float*)dx, accumulate, dbias);
     DH_LAUNCH_CHECK();
     return DH_OK;
   }

@@ -142,9 +142,9 @@ def test_dropout():
         bwd(INVALID, **{k: None})
     bwd(INVALID, dbias=A + 2)
     bwd(INVALID, ws=A + 8)
-    need = dh.dh_dropout_add_bwd_ws_bytes(4, 64)
-    bwd(SMALL, n=need - 1)
-    bwd(SMALL, ws=None)
+    need = dh.dh_dropout_add_bwd_ws_bytes(4096, 64)
+    bwd(SMALL, T=4096, n=need - 1)
+    bwd(SMALL, T=4096, ws=None)
 
 
 def test_nothing_to_do_is_no_error():
