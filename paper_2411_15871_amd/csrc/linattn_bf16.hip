@@ -159,9 +159,22 @@ __device__ __forceinline__ void lin_inside(f32x16& ot, f32x16& st, const LinPowe
     for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
   }
 }
-// S += rows^T * (values on their way into the state).  EXACT: their weighted values in three terms.
+// Left to the compiler, each fragment is read right before the product that takes it, which then waits for LDS: fragments are asked for ahead, and what is asked for stays in its place.
+#define LIN_PIN() __builtin_amdgcn_sched_barrier(0)
+template <int D>
+struct LinRows {  // a tile's transposed fragments of 16 tokens
+  bf16x8 f[D / 32];
+  __device__ __forceinline__ void load(const LinFrag<D>& fa, const lds_char* rows, int c) {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++) f[dt] = lds_frag_tr(rows + fa.tp[dt][0], rows + fa.tp[dt][1], c * 16 * D * 2);
+  }
+};
+// S += rows^T * (values on their way into the state).  first: the fragments of the first 16 tokens.  EXACT: their weighted values in three terms.
 template <int D, bool EXACT>
-__device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& fa, const lds_char* rows, const bf16x8 (&v)[2], const float (&into)[2][8]) {
+__device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& fa, const lds_char* rows, const LinRows<D>& first, const bf16x8 (&v)[2], const float (&into)[2][8]) {
+  LinRows<D> second;
+  second.load(fa, rows, 1);
+  LIN_PIN();
 #pragma unroll
   for (int c = 0; c < 2; c++) {
     bf16x8 hi, mid, lo;
@@ -176,13 +189,12 @@ __device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& 
       }
     }
 #pragma unroll
-    for (int dt = 0; dt < D / 32; dt++) {
-      const bf16x8 kf = lds_frag_tr(rows + fa.tp[dt][0], rows + fa.tp[dt][1], c * 16 * D * 2);
-      S[dt] = MFMA(kf, hi, S[dt]);
-      if constexpr (EXACT) {
-        S[dt] = MFMA(kf, mid, S[dt]);
-        S[dt] = MFMA(kf, lo, S[dt]);
-      }
+    for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(c ? second.f[dt] : first.f[dt], hi, S[dt]);
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(c ? second.f[dt] : first.f[dt], mid, S[dt]);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(c ? second.f[dt] : first.f[dt], lo, S[dt]);
     }
   }
 }
@@ -292,33 +304,50 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     const lds_char *Qt = sm + slot_s * TR::TILE, *Kt = sm + (2 + slot_k) * TR::TILE, *Vt = sm + (4 + slot_k) * TR::TILE;
     if (left != pw.left) pw.chunk(left, l2, g.scale, f_in, lane);
     LinValues v;
+    LinRows<D> kr;
+    const bool last_head = GROUPED || h == heads - 1;
     v.load(Vt + fa.tr[0], Vt + fa.tr[1], D * 2);
     if constexpr (OUT) {
-      bf16x8 qf[KS];
+      constexpr int AHEAD = 4;
+      bf16x8 qf[AHEAD], kf[AHEAD];
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
+      for (int ks = 0; ks < AHEAD; ks++) {
+        qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
+        kf[ks] = lds_frag(Kt + fa.dir[ks], 0);
+      }
+      LIN_PIN();
       v.look(kg);
       f32x16 ot, st;
       lin_zero(ot);
       lin_zero(st);
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) {  // in turn: a product waits for one before it that adds to the same registers
-        st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
-        ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks], ot);
+        st = MFMA(kf[ks % AHEAD], qf[ks % AHEAD], st);
+        ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks % AHEAD], ot);
+        if (ks + AHEAD < KS) {
+          qf[ks % AHEAD] = lds_frag(Qt + fa.dir[ks + AHEAD], 0);
+          kf[ks % AHEAD] = lds_frag(Kt + fa.dir[ks + AHEAD], 0);
+        }
+        LIN_PIN();
       }
+      if (last_head) kr.load(fa, Kt, 0);
+      LIN_PIN();
 #pragma unroll
       for (int r = 0; r < 16; r++) ot[r] *= pw.read;
       lin_inside<REV>(ot, st, pw, v, lane);
       lin_out(ot, p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(hk * grp + h) * D + wave * 32, l32 < left, lane);
+    } else {
+      kr.load(fa, Kt, 0);
+      LIN_PIN();
     }
-    if (GROUPED || h == heads - 1) {
+    if (last_head) {
       if (!GROUPED || h == 0) {
 #pragma unroll
         for (int dt = 0; dt < W; dt++)
 #pragma unroll
           for (int r = 0; r < 16; r++) S[dt][r] *= pw.whole;
       }
-      lin_into<D, EXACT>(S, fa, Kt, v.all, pw.into);
+      lin_into<D, EXACT>(S, fa, Kt, kr, v.all, pw.into);
     }
     if (++h == heads) { h = 0; n++; }
   }
@@ -378,15 +407,24 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
     LinValues q, e;
     q.load(Qt + fa.tr[0], Qt + fa.tr[1], D * 2);
     e.load(Gt + fa.tr[0], Gt + fa.tr[1], D * 2);
-    q.look(kg);
-    e.look(kg);
+    constexpr int AHEAD = 4;
+    bf16x8 qd[AHEAD], ed[AHEAD];
+#pragma unroll
+    for (int ks = 0; ks < AHEAD; ks++) {
+      qd[ks] = lds_frag(Qt + fa.dir[ks], 0);
+      ed[ks] = lds_frag(Gt + fa.dir[ks], 0);
+    }
     if (h == 0) {
-      lin_zero(dk);
-      lin_zero(dv);
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) {
         kf[ks] = lds_frag(Kt + fa.dir[ks], 0);
         vf[ks] = lds_frag(Vt + fa.dir[ks], 0);
+      }
+      LIN_PIN();
+      lin_zero(dk);
+      lin_zero(dv);
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) {
         dv = MFMA(pack_rows(R[ks >> 1], ks & 1), kf[ks], dv);
         dk = MFMA(pack_rows(Rt[ks >> 1], ks & 1), vf[ks], dk);
       }
@@ -397,18 +435,30 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
 #pragma unroll
         for (int r = 0; r < 16; r++) { R[dt][r] *= pw.whole; Rt[dt][r] *= pw.whole; }
     }
+    LIN_PIN();
+    q.look(kg);
+    e.look(kg);
     f32x16 sv, sk;
     lin_zero(sv);
     lin_zero(sk);
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) {
-      sv = MFMA(lds_frag(Qt + fa.dir[ks], 0), kf[ks], sv);
-      sk = MFMA(lds_frag(Gt + fa.dir[ks], 0), vf[ks], sk);
+      sv = MFMA(qd[ks % AHEAD], kf[ks], sv);
+      sk = MFMA(ed[ks % AHEAD], vf[ks], sk);
+      if (ks + AHEAD < KS) {
+        qd[ks % AHEAD] = lds_frag(Qt + fa.dir[ks + AHEAD], 0);
+        ed[ks % AHEAD] = lds_frag(Gt + fa.dir[ks + AHEAD], 0);
+      }
+      LIN_PIN();
     }
+    LinRows<D> qr, er;
+    qr.load(fa, Qt, 0);
+    er.load(fa, Gt, 0);
+    LIN_PIN();
     lin_inside<true>(dv, sv, pw, e, lane);
     lin_inside<true>(dk, sk, pw, q, lane);
-    lin_into<D, EXACT>(R, fa, Qt, e.all, pw.into);
-    lin_into<D, false>(Rt, fa, Gt, q.all, pw.into);
+    lin_into<D, EXACT>(R, fa, Qt, qr, e.all, pw.into);
+    lin_into<D, false>(Rt, fa, Gt, er, q.all, pw.into);
     if (++h < grp) continue;
     bf16_t* row = p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + wave * 32;
     lin_out(dk, row + (size_t)(g.nq + hk) * D, l32 < left, lane);
@@ -423,7 +473,7 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
 
 // The forward pass: OUT its results, otherwise the pieces' contributions to the states.  grid (pieces, nkv, batch)
 template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
+__global__ __launch_bounds__(2 * D, OUT && D == 128 ? 1 : 2) void lin_fwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lin_walk<D, false, false, EXACT, OUT>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
