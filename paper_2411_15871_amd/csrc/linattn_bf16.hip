@@ -159,7 +159,8 @@ __device__ __forceinline__ void lin_inside(f32x16& ot, f32x16& st, const LinPowe
     for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
   }
 }
-// Left to the compiler, each fragment is read right before the product that takes it, which then waits for LDS: fragments are asked for ahead, and what is asked for stays in its place.
+// Where a wave has a SIMD to itself fragments are asked for ahead, and what is asked for stays in its place: left to the compiler each is read right before the product that takes it, which
+// then waits for LDS.  With two waves a SIMD these cover such waits, and registers count for more.
 #define LIN_PIN() __builtin_amdgcn_sched_barrier(0)
 template <int D>
 struct LinRows {  // a tile's transposed fragments of 16 tokens
@@ -169,12 +170,9 @@ struct LinRows {  // a tile's transposed fragments of 16 tokens
     for (int dt = 0; dt < D / 32; dt++) f[dt] = lds_frag_tr(rows + fa.tp[dt][0], rows + fa.tp[dt][1], c * 16 * D * 2);
   }
 };
-// S += rows^T * (values on their way into the state).  first: the fragments of the first 16 tokens.  EXACT: their weighted values in three terms.
-template <int D, bool EXACT>
-__device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& fa, const lds_char* rows, const LinRows<D>& first, const bf16x8 (&v)[2], const float (&into)[2][8]) {
-  LinRows<D> second;
-  second.load(fa, rows, 1);
-  LIN_PIN();
+// S += rows^T * (values on their way into the state).  PIN: the fragments are in `ahead` already.  EXACT: the weighted values in three terms.
+template <int D, bool EXACT, bool PIN>
+__device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& fa, const lds_char* rows, const LinRows<D> (&ahead)[2], const bf16x8 (&v)[2], const float (&into)[2][8]) {
 #pragma unroll
   for (int c = 0; c < 2; c++) {
     bf16x8 hi, mid, lo;
@@ -188,13 +186,16 @@ __device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& 
         lo[e] = (bf16_t)(y - (float)mid[e]);
       }
     }
+    LinRows<D> k;
+    if constexpr (PIN) k = ahead[c];
+    else k.load(fa, rows, c);
 #pragma unroll
-    for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(c ? second.f[dt] : first.f[dt], hi, S[dt]);
+    for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], hi, S[dt]);
     if constexpr (EXACT) {
 #pragma unroll
-      for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(c ? second.f[dt] : first.f[dt], mid, S[dt]);
+      for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], mid, S[dt]);
 #pragma unroll
-      for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(c ? second.f[dt] : first.f[dt], lo, S[dt]);
+      for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], lo, S[dt]);
     }
   }
 }
@@ -268,10 +269,11 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   const size_t t0 = (size_t)b * g.seq;
   const float l2 = g.log_decay[hk] * LOG2E, f_in = GROUPED ? g.scale : 1.f;
   const uint32_t lds = lds_address(smem);
-  uint32_t off[3][2];
-  TR::offsets(off[0], p.ldq, LC - 1, wave, lane);
-  TR::offsets(off[1], p.ldk, LC - 1, wave, lane);
-  TR::offsets(off[2], p.ldv, LC - 1, wave, lane);
+  // offsets of q's rows and of k's, or (sums) of k's and v's; with results k and v lie in rows of the same length.  (Two registers fewer: the loop has none to spare, and what lies in scratch
+  // waits for the transfers ahead of it: 78 -> 51 us for 8192 tokens x 32 heads in 8 pieces.)
+  uint32_t off[2][2];
+  TR::offsets(off[0], OUT ? p.ldq : p.ldk, LC - 1, wave, lane);
+  TR::offsets(off[1], OUT ? p.ldk : p.ldv, LC - 1, wave, lane);
   const int steps = (c1 - c0) * heads;
   auto chunk_of = [&](int n) { return REV ? c1 - 1 - n : c0 + n; };
   int in = 0, ih = 0;  // of the step to transfer next
@@ -280,8 +282,8 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     const size_t row = t0 + (size_t)chunk * LC;
     if (OUT) TR::go(p.q + row * p.ldq + (size_t)(hk * grp + ih) * D, p.ldq, off[0], last, lds + slot_s * TR::TILE, wave, lane);
     if (GROUPED || ih == 0) {
-      TR::go(p.k + row * p.ldk + (size_t)hkv * D, p.ldk, off[1], last, lds + (2 + slot_k) * TR::TILE, wave, lane);
-      TR::go(p.v + row * p.ldv + (size_t)hkv * D, p.ldv, off[2], last, lds + (4 + slot_k) * TR::TILE, wave, lane);
+      TR::go(p.k + row * p.ldk + (size_t)hkv * D, p.ldk, off[OUT ? 1 : 0], last, lds + (2 + slot_k) * TR::TILE, wave, lane);
+      TR::go(p.v + row * p.ldv + (size_t)hkv * D, p.ldv, off[1], last, lds + (4 + slot_k) * TR::TILE, wave, lane);
     }
     if (++ih == heads) { ih = 0; in++; }
   };
@@ -304,40 +306,28 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     const lds_char *Qt = sm + slot_s * TR::TILE, *Kt = sm + (2 + slot_k) * TR::TILE, *Vt = sm + (4 + slot_k) * TR::TILE;
     if (left != pw.left) pw.chunk(left, l2, g.scale, f_in, lane);
     LinValues v;
-    LinRows<D> kr;
+    LinRows<D> ahead[2];
     const bool last_head = GROUPED || h == heads - 1;
     v.load(Vt + fa.tr[0], Vt + fa.tr[1], D * 2);
     if constexpr (OUT) {
-      constexpr int AHEAD = 4;
-      bf16x8 qf[AHEAD], kf[AHEAD];
+      bf16x8 qf[KS];
 #pragma unroll
-      for (int ks = 0; ks < AHEAD; ks++) {
-        qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
-        kf[ks] = lds_frag(Kt + fa.dir[ks], 0);
-      }
-      LIN_PIN();
+      for (int ks = 0; ks < KS; ks++) qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
       v.look(kg);
       f32x16 ot, st;
       lin_zero(ot);
       lin_zero(st);
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) {  // in turn: a product waits for one before it that adds to the same registers
-        st = MFMA(kf[ks % AHEAD], qf[ks % AHEAD], st);
-        ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks % AHEAD], ot);
-        if (ks + AHEAD < KS) {
-          qf[ks % AHEAD] = lds_frag(Qt + fa.dir[ks + AHEAD], 0);
-          kf[ks % AHEAD] = lds_frag(Kt + fa.dir[ks + AHEAD], 0);
-        }
-        LIN_PIN();
-      }
-      if (last_head) kr.load(fa, Kt, 0);
-      LIN_PIN();
+      for (int ks = 0; ks < KS; ks++) ot = MFMA(pack_rows(S[ks >> 1], ks & 1), qf[ks], ot);
 #pragma unroll
       for (int r = 0; r < 16; r++) ot[r] *= pw.read;
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
       lin_inside<REV>(ot, st, pw, v, lane);
       lin_out(ot, p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(hk * grp + h) * D + wave * 32, l32 < left, lane);
     } else {
-      kr.load(fa, Kt, 0);
+      ahead[0].load(fa, Kt, 0);
+      ahead[1].load(fa, Kt, 1);
       LIN_PIN();
     }
     if (last_head) {
@@ -347,7 +337,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
 #pragma unroll
           for (int r = 0; r < 16; r++) S[dt][r] *= pw.whole;
       }
-      lin_into<D, EXACT>(S, fa, Kt, kr, v.all, pw.into);
+      lin_into<D, EXACT, !OUT>(S, fa, Kt, ahead, v.all, pw.into);
     }
     if (++h == heads) { h = 0; n++; }
   }
@@ -451,14 +441,17 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
       }
       LIN_PIN();
     }
-    LinRows<D> qr, er;
-    qr.load(fa, Qt, 0);
-    er.load(fa, Gt, 0);
+    LinRows<D> qr[2], er[2];
+#pragma unroll
+    for (int c = 0; c < 2; c++) {
+      qr[c].load(fa, Qt, c);
+      er[c].load(fa, Gt, c);
+    }
     LIN_PIN();
     lin_inside<true>(dv, sv, pw, e, lane);
     lin_inside<true>(dk, sk, pw, q, lane);
-    lin_into<D, EXACT>(R, fa, Qt, qr, e.all, pw.into);
-    lin_into<D, false>(Rt, fa, Gt, er, q.all, pw.into);
+    lin_into<D, EXACT, true>(R, fa, Qt, qr, e.all, pw.into);
+    lin_into<D, false, true>(Rt, fa, Gt, er, q.all, pw.into);
     if (++h < grp) continue;
     bf16_t* row = p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + wave * 32;
     lin_out(dk, row + (size_t)(g.nq + hk) * D, l32 < left, lane);
@@ -473,7 +466,7 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
 
 // The forward pass: OUT its results, otherwise the pieces' contributions to the states.  grid (pieces, nkv, batch)
 template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, OUT && D == 128 ? 1 : 2) void lin_fwd_kernel(const LinArgs a) {
+__global__ __launch_bounds__(2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lin_walk<D, false, false, EXACT, OUT>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
@@ -494,12 +487,15 @@ __global__ __launch_bounds__(2 * D, 2) void lin_bwd_sums_kernel(const LinArgs a)
   else lin_walk<D, false, false, true, false>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
 }
 // ------------------------------------------------------------------------------------ host side
-// Pieces of a row: enough that the chip's units have two blocks each, none below LIN_LEAST chunks.
+// Pieces of a row, none below LIN_LEAST chunks: enough that the launch has a wave for each of the chip's 1024 SIMDs (forward), or two (backward, whose two kinds of blocks are of different lengths).  Each
+// more costs its states' way to memory and back.  us, 256 and 512 blocks of D = 128: forward of 8192 tokens x 32 heads 100 and 106; training step of 2 x 4096 tokens on 32:8 heads, both
+// numbers for the backward pass, 277 and 252.
 #define LIN_LEAST 4
-#define LIN_BLOCKS 512
+#define LIN_BF 256
+#define LIN_BB 512
 static LinCut lin_cut(const LinGeom& g, bool bwd) {
   const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 2 : 1);
-  const long long want = std::max(1ll, std::min((LIN_BLOCKS + blocks - 1) / blocks, chunks / LIN_LEAST));
+  const long long want = std::max(1ll, std::min(((bwd ? LIN_BB : LIN_BF) * (128 / g.d) + blocks - 1) / blocks, chunks / LIN_LEAST));
   const int per = (int)((chunks + want - 1) / want);
   return {(int)((chunks + per - 1) / per), per};
 }
