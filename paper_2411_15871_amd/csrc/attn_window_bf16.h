@@ -50,25 +50,15 @@ struct WindowSeen {
   // f(mt, r, seen) for every element of the lane's column
   template <class F>
   __device__ __forceinline__ void each(int kb, int kg, F f) const {
-    const int at = kb + 4 * kg - (iq - window + 1), ahead = min(sinks, iq + 1) - kb - 4 * kg;
-    if (kb >= sinks) {
+    const int at = kb + 4 * kg - (iq - window + 1), ahead = min(sinks, iq + 1) - kb - 4 * kg;  // (a copy of its own for tiles behind the sinks costs dQ the 25 registers it has not)
 #pragma unroll
-      for (int mt = 0; mt < 2; mt++)
+    for (int mt = 0; mt < 2; mt++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-          f(mt, r, (uint32_t)(at + mt * 32 + 8 * (r >> 2) + (r & 3)) < (uint32_t)window);
-          if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // (32 comparisons ahead of their use take more scalar registers than there are)
-        }
-    } else {
-#pragma unroll
-      for (int mt = 0; mt < 2; mt++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-          const int e = mt * 32 + 8 * (r >> 2) + (r & 3);
-          f(mt, r, (uint32_t)(at + e) < (uint32_t)window || e < ahead);
-          if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);
-        }
-    }
+      for (int r = 0; r < 16; r++) {
+        const int e = mt * 32 + 8 * (r >> 2) + (r & 3);
+        f(mt, r, (uint32_t)(at + e) < (uint32_t)window || e < ahead);
+        if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // (32 comparisons ahead of their use take more scalar registers than there are)
+      }
   }
 };
 
