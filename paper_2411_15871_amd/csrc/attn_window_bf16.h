@@ -368,7 +368,7 @@ struct WindowWalk {
   __device__ __forceinline__ uint32_t rows() const { return (uint32_t)n; }
   __device__ __forceinline__ bool ragged(int ti) const { return ti >= whole; }
 };
-// grid: window_grid(nkv, sink_blocks * sink_units + blocks - sink_blocks, batch)
+// grid: window_grid(nkv, blocks - sink_blocks + sink_blocks * sink_units, batch): the blocks without sinks, which are of one length, then the short units of the others, which fill up the last round
 template <int D>
 __global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
                                                                           const float* __restrict__ lse, const float* __restrict__ lse2, const float* __restrict__ delta,
@@ -381,16 +381,16 @@ __global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
   const int nq = g.nq, nkv = g.nkv, hk = window_head(blockIdx.x, nkv), grp = nq / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, seq = g.seq;
   const WindowUnit u = window_unit(g.batch);
-  const int cut = p.sink_blocks * p.sink_units;
-  if (u.id >= cut + p.blocks - p.sink_blocks) return;
-  const bool sink = u.id < cut;
-  const int jb = sink ? u.id / p.sink_units : p.sink_blocks + u.id - cut, chunk = sink ? u.id % p.sink_units : 0;
+  const int cut = p.sink_blocks * p.sink_units, whole_blocks = p.blocks - p.sink_blocks, id = u.id - whole_blocks;
+  if (id >= cut) return;
+  const bool sink = id >= 0;
+  const int jb = sink ? id / p.sink_units : p.sink_blocks + u.id, chunk = sink ? id % p.sink_units : 0;
   const size_t t0 = (size_t)u.b * seq, T = (size_t)g.batch * seq;
   const int j0 = jb * WB_BLOCK, jw = j0 + wave * 32, jk = jw + l32, row = min(jk, seq - 1);
   const int q0 = j0 / AB_KT * AB_KT, last = sink ? seq : (int)min((long long)seq, (long long)j0 + WB_BLOCK - 1 + g.window), nt = (last - q0 + AB_KT - 1) / AB_KT;
   const int f0 = sink ? chunk * p.sink_chunk : 0, f1 = sink ? min(grp * nt, f0 + p.sink_chunk) : grp * nt;
   const bool partial = p.sink_units > 1 && sink;
-  float* prow = part + ((((size_t)u.b * nkv + hk) * cut + u.id) * WB_BLOCK + wave * 32) * (2 * D);
+  float* prow = part + ((((size_t)u.b * nkv + hk) * cut + id) * WB_BLOCK + wave * 32) * (2 * D);
   const int live = seq - jw;
   if (f0 >= f1) return;  // a later sink block has fewer tiles than units; the merge knows
   const bf16_t* rows = qkv + t0 * ld;
@@ -562,11 +562,12 @@ static WindowTiled window_tiled(const WindowGeom& g0) {
   const long long have = (long long)g0.batch * g0.nq * p.blocks;
   const WindowTiles longest(p.g, p.blocks - 1);
   p.parts = (int)std::max(1ll, std::min(2ll * attn_num_cus() / std::max(1ll, have), (long long)longest.count() / 4));
-  // key blocks that hold sinks: units as long as another block's walk, at most 64; where there are more than eight such blocks they fill the chip uncut
+  // Key blocks that hold sinks walk on to the row's end.  Where they are few they are cut into units, about as many as the chip has units, of four tiles at least; more than eight blocks fill the
+  // chip uncut.
   const int grp = g0.nq / g0.nkv, whole = grp * ((g0.seq + AB_KT - 1) / AB_KT);
-  const int plain = grp * ((std::min((long long)p.g.window + WB_BLOCK - 1, (long long)g0.seq) + AB_KT - 1) / AB_KT + 1);
   p.sink_blocks = (p.g.sinks + WB_BLOCK - 1) / WB_BLOCK;
-  p.sink_chunk = std::max({plain, 8, (whole + 63) / 64});
+  const long long sink_tiles = (long long)g0.batch * g0.nkv * p.sink_blocks * whole;
+  p.sink_chunk = (int)std::max({4ll, (sink_tiles + attn_num_cus() - 1) / attn_num_cus(), (whole + 63ll) / 64});
   p.sink_units = p.sink_blocks > 0 && p.sink_blocks <= 8 ? (whole + p.sink_chunk - 1) / p.sink_chunk : 1;
   if (p.sink_units == 1) p.sink_chunk = whole;
   return p;
@@ -617,7 +618,7 @@ static int window_bwd(const WindowTiled& p, const bf16_t* qkv, const bf16_t* o, 
   float *lse2 = (float*)ws, *part = (float*)(ws + dh_align_up((size_t)g.nq * g.batch * g.seq * sizeof(float), 256));
   attn_window_dq_bf16_kernel<D><<<window_grid(g.nq, p.blocks, g.batch), AB_THREADS, lds_dq, s>>>(p, qkv, o, dout, lse, lse2, delta, dqkv);
   DH_LAUNCH_CHECK();
-  attn_window_dkv_bf16_kernel<D><<<window_grid(g.nkv, p.sink_blocks * p.sink_units + p.blocks - p.sink_blocks, g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, dout, lse, lse2, delta, dqkv, part);
+  attn_window_dkv_bf16_kernel<D><<<window_grid(g.nkv, p.blocks - p.sink_blocks + p.sink_blocks * p.sink_units, g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, dout, lse, lse2, delta, dqkv, part);
   DH_LAUNCH_CHECK();
   if (p.sink_units > 1) {
     attn_window_sinks_kernel<D><<<dim3(g.nkv, p.sink_blocks * (WB_BLOCK / 4), g.batch), 256, 0, s>>>(p, qkv, dout, lse, delta, part, dqkv);
