@@ -2,8 +2,8 @@
 //
 // A block of 128 queries walks the 64-key tiles of the sinks that lie before its window, then those of its window up to the diagonal: about (window + 128 + sinks) / 64 tiles whatever the
 // row's length.  Which keys of a tile a row sees is two comparisons an element (one behind the sinks), made only where some row of the wave does not see the whole tile.  A block of 128 keys
-// walks, head after head of its group, the query tiles from its own position to the window's end; blocks that hold sinks walk on to the row's end, cut into units whose partial results a
-// launch behind adds in order.
+// walks, head after head of its group, the query tiles from its own position to the window's end; blocks that hold sinks walk on to the row's end.  Where blocks are few, or rounds of them would leave
+// the chip idle, their walks are cut into units whose partial results a launch behind adds in order (4096 rows of 4:1 heads, window 1024, backward pass 121 -> 75 us).
 //
 // Probabilities and their gradients round to bf16 before the products that take them, as the causal kernels' do: matrix instructions of the full rate take nothing else.
 //
@@ -20,9 +20,35 @@ struct WindowTiled {
   WindowGeom g;   // window and sinks at most seq
   int blocks;     // of 128 rows, a sequence
   int parts;      // forward: units that share a block's tiles
-  int sink_blocks, sink_units, sink_chunk;  // key blocks that hold sinks, the units of each and their tiles
+  // dK/dV: a key block's walk is cut into units of `chunk` tiles, blocks that hold sinks (they walk on to the row's end) into others.  One unit: the block writes its results itself.
+  int plain_units, plain_chunk, sink_blocks, sink_units, sink_chunk;
   float exp_scale;  // score -> exponent of 2
 };
+__host__ __device__ static inline int window_units(const WindowTiled& p) { return (p.blocks - p.sink_blocks) * p.plain_units + p.sink_blocks * p.sink_units; }  // of dK/dV, a head
+// Partial results of a head's dK/dV: [units of the blocks without sinks, if these are cut][units of the others, if these are].
+__host__ __device__ static inline int window_parts(const WindowTiled& p) {
+  return (p.plain_units > 1 ? (p.blocks - p.sink_blocks) * p.plain_units : 0) + (p.sink_units > 1 ? p.sink_blocks * p.sink_units : 0);
+}
+struct WindowKeys128 { int jb, chunk, f0, f1, q0, nt, part; };  // a unit: key block, its run of tiles [f0, f1), counted through the heads of the group, nt of each head from row q0 on; partial result or -1
+__host__ __device__ static inline int window_key_tiles(const WindowTiled& p, int jb) {  // of one head
+  const int j0 = jb * WB_BLOCK, q0 = j0 / AB_KT * AB_KT;
+  const long long end = jb < p.sink_blocks ? p.g.seq : (long long)j0 + WB_BLOCK - 1 + p.g.window;
+  return (int)(((end < p.g.seq ? end : p.g.seq) - q0 + AB_KT - 1) / AB_KT);
+}
+__device__ __forceinline__ WindowKeys128 window_keys128(const WindowTiled& p, int unit, int grp) {
+  const int plain = (p.blocks - p.sink_blocks) * p.plain_units;
+  const bool sink = unit >= plain;
+  const int id = sink ? unit - plain : unit, units = sink ? p.sink_units : p.plain_units, ch = sink ? p.sink_chunk : p.plain_chunk;
+  WindowKeys128 k;
+  k.jb = id / units + (sink ? 0 : p.sink_blocks);
+  k.chunk = id % units;
+  k.q0 = k.jb * WB_BLOCK / AB_KT * AB_KT;
+  k.nt = window_key_tiles(p, k.jb);
+  k.f0 = min(k.chunk * ch, grp * k.nt);
+  k.f1 = min(k.f0 + ch, grp * k.nt);
+  k.part = units == 1 ? -1 : id + (sink && p.plain_units > 1 ? plain : 0);
+  return k;
+}
 // Heads of a group next to one another on the same XCD (workgroups go to the eight in turn), whose L2 then holds their keys and values once.
 __device__ __forceinline__ int window_head(int x, int n) { return n % 8 == 0 ? (x & 7) * (n >> 3) + (x >> 3) : x; }
 struct WindowUnit { int id, b; };
@@ -246,23 +272,20 @@ __global__ __launch_bounds__(256) void attn_window_combine_kernel(const WindowTi
 }
 
 // ================================================================================ backward: dQ
-// As docs_dq_block; stores the rows' delta and lse2 for the dK/dV launch behind it.  grid: window_grid(nq, blocks, batch)
-template <int D>
-__global__ __launch_bounds__(AB_THREADS, 2) void attn_window_dq_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
-                                                                        const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv) {
+// As docs_dq_block: block ib of head h, sequence b.  STORE: leaves the rows' delta and lse2 for the dK/dV launch behind it; otherwise attn_window_prep_kernel has.
+template <int D, bool STORE>
+__device__ __forceinline__ void window_dq_block(const WindowTiled& p, int ib, int h, int b, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                                const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv) {
   using TL = ATile<D>;
   constexpr int RING = 2;
   extern __shared__ __attribute__((aligned(1024))) char smem[];  // K ring, then V ring
   const lds_char* sm = (const lds_char*)smem;
   const WindowGeom& g = p.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
-  const int nq = g.nq, nkv = g.nkv, h = window_head(blockIdx.x, nq), hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, seq = g.seq;
-  const WindowUnit u = window_unit(g.batch);
-  if (u.id >= p.blocks) return;
-  const int ib = p.blocks - 1 - u.id;
+  const int nq = g.nq, nkv = g.nkv, hk = h / (nq / nkv), ld = (nq + 2 * nkv) * D, seq = g.seq;
   const WindowTiles tiles(g, ib);
   const int f1 = tiles.count();
-  const size_t t0 = (size_t)u.b * seq, head = (size_t)h * g.batch * seq + t0;
+  const size_t t0 = (size_t)b * seq, head = (size_t)h * g.batch * seq + t0;
   const int iw = ib * WB_BLOCK + wave * 32, iq = iw + l32, row = min(iq, seq - 1);
   const bf16_t* rows = qkv + t0 * ld;
   const char* kbase = reinterpret_cast<const char*>(rows + (size_t)(nq + hk) * D);
@@ -298,7 +321,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_dq_bf16_kernel(cons
       for (int e = 0; e < 8; e++) dl = fmaf((float)dof[ks][e], (float)of[ks][e], dl);
     dl += __shfl_xor(dl, 32, 64);
   }
-  if (kg == 0 && iq < seq) {
+  if (STORE && kg == 0 && iq < seq) {
     delta[head + iq] = dl;
     lse2[head + iq] = l2;
   }
@@ -368,31 +391,24 @@ struct WindowWalk {
   __device__ __forceinline__ uint32_t rows() const { return (uint32_t)n; }
   __device__ __forceinline__ bool ragged(int ti) const { return ti >= whole; }
 };
-// grid: window_grid(nkv, blocks - sink_blocks + sink_blocks * sink_units, batch): the blocks without sinks, which are of one length, then the short units of the others, which fill up the last round
+// Unit `unit` of key/value head hk, sequence b: the blocks without sinks, which are of one length, then the short units of the others, which fill up the last round.
 template <int D>
-__global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
-                                                                          const float* __restrict__ lse, const float* __restrict__ lse2, const float* __restrict__ delta,
-                                                                          bf16_t* __restrict__ dqkv, float* __restrict__ part) {
+__device__ __forceinline__ void window_dkv_block(const WindowTiled& p, int unit, int hk, int b, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+                                                 const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   using TL = ATile<D>;
   constexpr bool PINNED = D == 128;
   extern __shared__ __attribute__((aligned(1024))) char smem[];  // Q ring, dO ring, lse2 ring, delta ring
   const lds_char* sm = (const lds_char*)smem;
   const WindowGeom& g = p.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
-  const int nq = g.nq, nkv = g.nkv, hk = window_head(blockIdx.x, nkv), grp = nq / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, seq = g.seq;
-  const WindowUnit u = window_unit(g.batch);
-  const int cut = p.sink_blocks * p.sink_units, whole_blocks = p.blocks - p.sink_blocks, id = u.id - whole_blocks;
-  if (id >= cut) return;
-  const bool sink = id >= 0;
-  const int jb = sink ? id / p.sink_units : p.sink_blocks + u.id, chunk = sink ? id % p.sink_units : 0;
-  const size_t t0 = (size_t)u.b * seq, T = (size_t)g.batch * seq;
-  const int j0 = jb * WB_BLOCK, jw = j0 + wave * 32, jk = jw + l32, row = min(jk, seq - 1);
-  const int q0 = j0 / AB_KT * AB_KT, last = sink ? seq : (int)min((long long)seq, (long long)j0 + WB_BLOCK - 1 + g.window), nt = (last - q0 + AB_KT - 1) / AB_KT;
-  const int f0 = sink ? chunk * p.sink_chunk : 0, f1 = sink ? min(grp * nt, f0 + p.sink_chunk) : grp * nt;
-  const bool partial = p.sink_units > 1 && sink;
-  float* prow = part + ((((size_t)u.b * nkv + hk) * cut + id) * WB_BLOCK + wave * 32) * (2 * D);
-  const int live = seq - jw;
-  if (f0 >= f1) return;  // a later sink block has fewer tiles than units; the merge knows
+  const int nq = g.nq, nkv = g.nkv, grp = nq / nkv, hq = hk * grp, ld = (nq + 2 * nkv) * D, ldo = nq * D, seq = g.seq;
+  if (unit >= window_units(p)) return;
+  const WindowKeys128 k = window_keys128(p, unit, grp);
+  const int q0 = k.q0, nt = k.nt, f0 = k.f0, f1 = k.f1;
+  if (f0 >= f1) return;  // a shorter block has fewer tiles than units; the merge knows
+  const size_t t0 = (size_t)b * seq, T = (size_t)g.batch * seq;
+  const int jw = k.jb * WB_BLOCK + wave * 32, jk = jw + l32, row = min(jk, seq - 1), live = seq - jw;
+  float* prow = part + ((((size_t)b * nkv + hk) * window_parts(p) + k.part) * WB_BLOCK + wave * 32) * (2 * D);
   const bf16_t* rows = qkv + t0 * ld;
   const bf16_t* kcol = rows + (size_t)(nq + hk) * D;
   const char* qbase = reinterpret_cast<const char*>(rows + (size_t)q0 * ld + (size_t)hq * D);
@@ -498,7 +514,7 @@ __global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const 
   const float scale = g.scale;
   auto dk_quad = [&](int dt, int q4) { return f32x4{dkt[dt][4 * q4] * scale, dkt[dt][4 * q4 + 1] * scale, dkt[dt][4 * q4 + 2] * scale, dkt[dt][4 * q4 + 3] * scale}; };
   auto dv_quad = [&](int dt, int q4) { return f32x4{dvt[dt][4 * q4], dvt[dt][4 * q4 + 1], dvt[dt][4 * q4 + 2], dvt[dt][4 * q4 + 3]}; };
-  if (partial) {
+  if (k.part >= 0) {
     float* reg = reinterpret_cast<float*>(smem) + wave * (32 * D);
     wave_rows_out_f32<D>(reg, lane, dk_quad, [&](int r) { return r < live ? prow + (size_t)r * (2 * D) : nullptr; });
     __builtin_amdgcn_wave_barrier();
@@ -521,17 +537,72 @@ __global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const 
     window_row_dkv(g, rows, dout + t0 * ldo, lse + t0, delta + t0, T, hk, j, to, to + (size_t)nkv * D);
   }
 }
-// Adds the units of the key blocks that hold sinks, in order.  grid (nkv, sink_blocks * 32, batch): 4 keys a block, a wave each
+// Delta and lse2 of every row, as attn_bwd_prep_kernel: the numbers the dQ blocks use.  Two lanes a row of a head.
 template <int D>
-__global__ __launch_bounds__(256) void attn_window_sinks_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+__global__ __launch_bounds__(64) void attn_window_prep_kernel(const WindowGeom g, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout, const float* __restrict__ lse, float* __restrict__ lse2,
+                                                              float* __restrict__ delta) {
+  const size_t T = (size_t)g.batch * g.seq, i = (size_t)blockIdx.x * 32 + (threadIdx.x >> 1);
+  if (i >= T * g.nq) return;
+  const int kg = threadIdx.x & 1, h = (int)(i % g.nq);
+  const size_t t = i / g.nq, at = (size_t)h * T + t;
+  const bf16_t *orow = o + i * D + kg * 8, *drow = dout + i * D + kg * 8;
+  bf16x8 a[D / 16], b[D / 16];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) {
+    a[ks] = *reinterpret_cast<const bf16x8*>(drow + ks * 16);
+    b[ks] = *reinterpret_cast<const bf16x8*>(orow + ks * 16);
+  }
+  float half = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) half = fmaf((float)a[ks][e], (float)b[ks][e], half);
+  const float other = __shfl_xor(half, 1, 64);
+  if (kg == 0) {
+    delta[at] = half + other;
+    lse2[at] = lse[at] * LOG2E;
+  }
+}
+// The two as launches of their own (dQ first: it stores what the dK/dV blocks read), grids window_grid(nq, blocks, batch) and window_grid(nkv, units, batch) ...
+template <int D>
+__global__ __launch_bounds__(AB_THREADS, 2) void attn_window_dq_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                                                        const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv) {
+  const WindowUnit u = window_unit(p.g.batch);
+  if (u.id < p.blocks) window_dq_block<D, true>(p, p.blocks - 1 - u.id, window_head(blockIdx.x, p.g.nq), u.b, qkv, o, dout, lse, lse2, delta, dqkv);
+}
+template <int D>
+__global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+                                                                          const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
+  const WindowUnit u = window_unit(p.g.batch);
+  window_dkv_block<D>(p, u.id, window_head(blockIdx.x, p.g.nkv), u.b, qkv, dout, lse, lse2, delta, dqkv, part);
+}
+// ... and as one, behind attn_window_prep_kernel, for grids that leave units of the chip idle: dK/dV units (the longer ones) first.  grid (units * nkv + blocks * nq, batch)
+template <int D>
+__global__ __launch_bounds__(AB_THREADS) void attn_window_bwd_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
+                                                                          const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ delta, bf16_t* __restrict__ dqkv,
+                                                                          float* __restrict__ part) {
+  const int nq = p.g.nq, nkv = p.g.nkv, n_k = window_units(p) * nkv, id = blockIdx.x;
+  if (id < n_k) {
+    const int unit = __builtin_amdgcn_readfirstlane(id / nkv);
+    window_dkv_block<D>(p, unit, id - unit * nkv, blockIdx.y, qkv, dout, lse, lse2, delta, dqkv, part);
+  } else {
+    const int x = id - n_k, block = __builtin_amdgcn_readfirstlane(x / nq);
+    window_dq_block<D, false>(p, p.blocks - 1 - block, x - block * nq, blockIdx.y, qkv, o, dout, lse, lse2, delta, dqkv);
+  }
+}
+// Adds the units of key blocks [first, first + y / 32) in order.  grid (nkv, blocks * 32, batch): 4 keys a block, a wave each
+template <int D>
+__global__ __launch_bounds__(256) void attn_window_merge_kernel(const WindowTiled p, int first, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
                                                                 const float* __restrict__ delta, const float* __restrict__ part, bf16_t* __restrict__ dqkv) {
   const WindowGeom& g = p.g;
-  const int hk = blockIdx.x, b = blockIdx.z, j = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, nkv = g.nkv, jb = j / WB_BLOCK;
+  const int hk = blockIdx.x, b = blockIdx.z, j = first * WB_BLOCK + blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, nkv = g.nkv, jb = j / WB_BLOCK;
   if (j >= g.seq) return;
   constexpr int CPL = 2 * D / 64;
-  const int ld = (g.nq + 2 * nkv) * D, cut = p.sink_blocks * p.sink_units;
-  const int tiles = (g.nq / nkv) * ((g.seq - jb * WB_BLOCK + AB_KT - 1) / AB_KT), units = (tiles + p.sink_chunk - 1) / p.sink_chunk;
-  const float* from = part + ((((size_t)b * nkv + hk) * cut + (size_t)jb * p.sink_units) * WB_BLOCK + j % WB_BLOCK) * (2 * D) + lane * CPL;
+  const int ld = (g.nq + 2 * nkv) * D, tiles = (g.nq / nkv) * window_key_tiles(p, jb);
+  const bool sink = jb < p.sink_blocks;
+  const int ch = sink ? p.sink_chunk : p.plain_chunk, units = (tiles + ch - 1) / ch, plain = (p.blocks - p.sink_blocks) * p.plain_units;
+  const int at = sink ? jb * p.sink_units + (p.plain_units > 1 ? plain : 0) : (jb - p.sink_blocks) * p.plain_units;
+  const float* from = part + ((((size_t)b * nkv + hk) * window_parts(p) + at) * WB_BLOCK + j % WB_BLOCK) * (2 * D) + lane * CPL;
   float s[CPL] = {}, top = 0.f;
 #pragma unroll 8
   for (int c = 0; c < units; c++)
@@ -551,6 +622,14 @@ __global__ __launch_bounds__(256) void attn_window_sinks_kernel(const WindowTile
 }
 
 // ------------------------------------------------------------------------------------ host side
+// Whether both halves of the backward pass go out as one launch: up to so many 128-row blocks of all heads.  us, two launches and one, by blocks: D = 128: 128 (1000 rows of 8 heads, window 300) 41.8 and
+// 26.9, 160 (4096 rows of 4:1, window 1024) 83.9 and 74.7, 512 (2 x 2048 of 8, window 512) 69.1 and 69.5, 640 (4096 of 16:4, window 1024) 161 and 175; D = 64: 128 23.6 and 16.0, 512 38.7 and
+// 37.7, 1280 (4 x 2048 of 16:4, window 256) 94.7 and 91.7, 2560 (8192 of 32:8, window 512) 191 and 205.
+#define WB_ONE_128 512
+#define WB_ONE_64 1280
+// Tiles that a part of a forward block holds at least.  us, 4 and 8: 2 x 2048 rows of 8 heads, window 512, 32.4 and 21.8; 2 x 2001 of 8 heads of 64, window 300, 17.7 and 13.6; 1000 of 8,
+// window 300, 15.5 and 17.2.
+#define WB_PART 8
 static WindowTiled window_tiled(const WindowGeom& g0) {
   WindowTiled p = {};
   p.g = g0;
@@ -558,15 +637,33 @@ static WindowTiled window_tiled(const WindowGeom& g0) {
   p.g.sinks = std::min(g0.sinks, g0.seq);
   p.blocks = (g0.seq + WB_BLOCK - 1) / WB_BLOCK;
   p.exp_scale = (float)(1.4426950408889634 / sqrt((double)g0.d));
-  // forward: parts until the chip's units have two blocks each, none of fewer than four tiles
+  // forward: parts until the chip's units have two blocks each
   const long long have = (long long)g0.batch * g0.nq * p.blocks;
   const WindowTiles longest(p.g, p.blocks - 1);
-  p.parts = (int)std::max(1ll, std::min(2ll * attn_num_cus() / std::max(1ll, have), (long long)longest.count() / 4));
-  // Key blocks that hold sinks walk on to the row's end.  Where they are few they are cut into units, about as many as the chip has units, of four tiles at least; more than eight blocks fill the
-  // chip uncut.
-  const int grp = g0.nq / g0.nkv, whole = grp * ((g0.seq + AB_KT - 1) / AB_KT);
+  p.parts = (int)std::max(1ll, std::min(2ll * attn_num_cus() / std::max(1ll, have), (long long)longest.count() / WB_PART));
+  // dK/dV: the number of units a block without sinks is cut into whose launch is expected to be through first, in tiles of one unit: rounds of resident units (two a unit of the chip at D = 64), each
+  // with three tiles for its beginning and end, and for a cut the merge's launch and its way through memory.
+  const int grp = g0.nq / g0.nkv, slots = attn_num_cus() * (g0.d == 64 ? 2 : 1);
   p.sink_blocks = (p.g.sinks + WB_BLOCK - 1) / WB_BLOCK;
-  const long long sink_tiles = (long long)g0.batch * g0.nkv * p.sink_blocks * whole;
+  const long long pairs = (long long)g0.batch * g0.nkv, plain_blocks = pairs * (p.blocks - p.sink_blocks);
+  p.plain_units = 1;
+  p.plain_chunk = p.blocks > p.sink_blocks ? grp * window_key_tiles(p, p.sink_blocks) : 1;  // the first is as long as any
+  if (plain_blocks > 0 && plain_blocks < 2 * slots) {
+    const int tiles = p.plain_chunk;
+    double best = 1e30;
+    for (int u = 1; u <= 16 && (u == 1 || tiles / u >= 4); u++) {
+      const long long n = plain_blocks * u;
+      const double cost = (double)((n + slots - 1) / slots) * ((tiles + u - 1) / u + 3) + (u > 1 ? 2.5 + n * (g0.d / 128.0) * 0.03 : 0.0);
+      if (cost < best) {
+        best = cost;
+        p.plain_units = u;
+        p.plain_chunk = (tiles + u - 1) / u;
+      }
+    }
+  }
+  // Blocks that hold sinks walk on to the row's end.  Where they are few they are cut into units, about as many as the chip has units, of four tiles at least; more than eight fill the chip uncut.
+  const int whole = grp * ((g0.seq + AB_KT - 1) / AB_KT);
+  const long long sink_tiles = pairs * p.sink_blocks * whole;
   p.sink_chunk = (int)std::max({4ll, (sink_tiles + attn_num_cus() - 1) / attn_num_cus(), (whole + 63ll) / 64});
   p.sink_units = p.sink_blocks > 0 && p.sink_blocks <= 8 ? (whole + p.sink_chunk - 1) / p.sink_chunk : 1;
   if (p.sink_units == 1) p.sink_chunk = whole;
@@ -602,7 +699,7 @@ int dh_launch_window_fwd_bf16(const WindowGeom& g, const bf16_t* qkv, bf16_t* o,
 size_t dh_window_bwd_bf16_ws_bytes(const WindowGeom& g) {
   const WindowTiled p = window_tiled(g);
   return dh_align_up((size_t)g.nq * g.batch * g.seq * sizeof(float), 256) +
-         (p.sink_units > 1 ? (size_t)g.batch * g.nkv * p.sink_blocks * p.sink_units * WB_BLOCK * 2 * g.d * sizeof(float) : 0);
+         (size_t)g.batch * g.nkv * window_parts(p) * WB_BLOCK * 2 * g.d * sizeof(float);
 }
 template <int D>
 static int window_bwd(const WindowTiled& p, const bf16_t* qkv, const bf16_t* o, const bf16_t* dout, const float* lse, bf16_t* dqkv, float* delta, char* ws, hipStream_t s) {
@@ -613,15 +710,24 @@ static int window_bwd(const WindowTiled& p, const bf16_t* qkv, const bf16_t* o, 
   if (!set) {
     if (int rc = set_lds(attn_window_dq_bf16_kernel<D>, lds_dq)) return rc;
     if (int rc = set_lds(attn_window_dkv_bf16_kernel<D>, lds_dkv)) return rc;
+    if (int rc = set_lds(attn_window_bwd_bf16_kernel<D>, lds_dkv)) return rc;
     set = true;
   }
   float *lse2 = (float*)ws, *part = (float*)(ws + dh_align_up((size_t)g.nq * g.batch * g.seq * sizeof(float), 256));
-  attn_window_dq_bf16_kernel<D><<<window_grid(g.nq, p.blocks, g.batch), AB_THREADS, lds_dq, s>>>(p, qkv, o, dout, lse, lse2, delta, dqkv);
-  DH_LAUNCH_CHECK();
-  attn_window_dkv_bf16_kernel<D><<<window_grid(g.nkv, p.blocks - p.sink_blocks + p.sink_blocks * p.sink_units, g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, dout, lse, lse2, delta, dqkv, part);
-  DH_LAUNCH_CHECK();
-  if (p.sink_units > 1) {
-    attn_window_sinks_kernel<D><<<dim3(g.nkv, p.sink_blocks * (WB_BLOCK / 4), g.batch), 256, 0, s>>>(p, qkv, dout, lse, delta, part, dqkv);
+  if ((long long)p.blocks * (g.nq + g.nkv) * g.batch <= (D == 128 ? WB_ONE_128 : WB_ONE_64)) {
+    attn_window_prep_kernel<D><<<(unsigned)(((size_t)g.batch * g.seq * g.nq + 31) / 32), 64, 0, s>>>(g, o, dout, lse, lse2, delta);
+    DH_LAUNCH_CHECK();
+    attn_window_bwd_bf16_kernel<D><<<dim3(window_units(p) * g.nkv + p.blocks * g.nq, g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, o, dout, lse, lse2, delta, dqkv, part);
+    DH_LAUNCH_CHECK();
+  } else {
+    attn_window_dq_bf16_kernel<D><<<window_grid(g.nq, p.blocks, g.batch), AB_THREADS, lds_dq, s>>>(p, qkv, o, dout, lse, lse2, delta, dqkv);
+    DH_LAUNCH_CHECK();
+    attn_window_dkv_bf16_kernel<D><<<window_grid(g.nkv, window_units(p), g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, dout, lse, lse2, delta, dqkv, part);
+    DH_LAUNCH_CHECK();
+  }
+  const int first = p.sink_units > 1 ? 0 : p.sink_blocks, cut = (p.plain_units > 1 ? p.blocks : p.sink_blocks) - first;  // blocks that were cut: few enough for the launch's y
+  if (cut > 0 && (p.plain_units > 1 || p.sink_units > 1)) {
+    attn_window_merge_kernel<D><<<dim3(g.nkv, cut * (WB_BLOCK / 4), g.batch), 256, 0, s>>>(p, first, qkv, dout, lse, delta, part, dqkv);
     DH_LAUNCH_CHECK();
   }
   return DH_OK;

@@ -11,7 +11,8 @@
 //
 // Long rows are cut into pieces that run side by side: a first launch sums each piece's own contribution to the state, a second one carries the states along the pieces, a third makes
 // the results.  States that leave the call come from products whose weighted rows are split into three bf16 terms (24 bits: float32's own): EXACT.  Within a piece the state only feeds
-// bf16 products, and its weighted rows are rounded once.
+// products that take it rounded to bf16, as they take the weighted scores, and its weighted rows go in two terms: with one, errors against 64 bits (relative norms, where the result's own
+// rounding makes 1.7e-3) were 2.7e-3 and are 2.3e-3, for 103 and 109 us at 8192 tokens x 32 heads.
 //
 // Bound by memory: q, k, v, o once, k and v again for the pieces' states.
 #include <algorithm>
@@ -170,8 +171,8 @@ struct LinRows {  // a tile's transposed fragments of 16 tokens
     for (int dt = 0; dt < D / 32; dt++) f[dt] = lds_frag_tr(rows + fa.tp[dt][0], rows + fa.tp[dt][1], c * 16 * D * 2);
   }
 };
-// S += rows^T * (values on their way into the state).  PIN: the fragments are in `ahead` already.  EXACT: the weighted values in three terms.
-template <int D, bool EXACT, bool PIN>
+// S += rows^T * (values on their way into the state), these weighted and taken in TERMS bf16 terms.  PIN: the fragments are in `ahead` already.
+template <int D, int TERMS, bool PIN>
 __device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& fa, const lds_char* rows, const LinRows<D> (&ahead)[2], const bf16x8 (&v)[2], const float (&into)[2][8]) {
 #pragma unroll
   for (int c = 0; c < 2; c++) {
@@ -180,10 +181,10 @@ __device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& 
     for (int e = 0; e < 8; e++) {
       const float x = (float)v[c][e] * into[c][e];
       hi[e] = (bf16_t)x;
-      if constexpr (EXACT) {
+      if constexpr (TERMS > 1) {
         const float y = x - (float)hi[e];
         mid[e] = (bf16_t)y;
-        lo[e] = (bf16_t)(y - (float)mid[e]);
+        if constexpr (TERMS > 2) lo[e] = (bf16_t)(y - (float)mid[e]);
       }
     }
     LinRows<D> k;
@@ -191,9 +192,11 @@ __device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& 
     else k.load(fa, rows, c);
 #pragma unroll
     for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], hi, S[dt]);
-    if constexpr (EXACT) {
+    if constexpr (TERMS > 1) {
 #pragma unroll
       for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], mid, S[dt]);
+    }
+    if constexpr (TERMS > 2) {
 #pragma unroll
       for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], lo, S[dt]);
     }
@@ -337,7 +340,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
 #pragma unroll
           for (int r = 0; r < 16; r++) S[dt][r] *= pw.whole;
       }
-      lin_into<D, EXACT, !OUT>(S, fa, Kt, ahead, v.all, pw.into);
+      lin_into<D, EXACT ? 3 : 2, !OUT>(S, fa, Kt, ahead, v.all, pw.into);
     }
     if (++h == heads) { h = 0; n++; }
   }
@@ -450,8 +453,8 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
     LIN_PIN();
     lin_inside<true>(dv, sv, pw, e, lane);
     lin_inside<true>(dk, sk, pw, q, lane);
-    lin_into<D, EXACT, true>(R, fa, Qt, qr, e.all, pw.into);
-    lin_into<D, false, true>(Rt, fa, Gt, er, q.all, pw.into);
+    lin_into<D, EXACT ? 3 : 2, true>(R, fa, Qt, qr, e.all, pw.into);
+    lin_into<D, 2, true>(Rt, fa, Gt, er, q.all, pw.into);
     if (++h < grp) continue;
     bf16_t* row = p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + wave * 32;
     lin_out(dk, row + (size_t)(g.nq + hk) * D, l32 < left, lane);
