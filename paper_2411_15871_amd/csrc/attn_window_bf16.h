@@ -7,8 +7,9 @@
 //
 // Probabilities and their gradients round to bf16 before the products that take them, as the causal kernels' do: matrix instructions of the full rate take nothing else.
 //
-// Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN: a row whose result is not finite is made again by the wave from what it sees
-// alone (window_rows.h).
+// Masked probabilities are zeros, and a zero times an infinity or a NaN of a row that is not seen is a NaN: a wave whose result is not finite looks, as the kernels of packed documents do, whether
+// its masked tiles hold such values that a row does not see, and only then walks its tiles again (window_again_*).  8192 rows of 32:8 heads, window
+// 1024, us: forward 170 -> 260 with one token of NaNs, 150 with nothing else; backward 600 -> 1930 (one token), 1860 (a gradient's row), 1940 (nothing else).
 //
 // Bound by matrix products (4 D flops a visible pair forward, 14 with the backward pass) from windows of some hundred on, below that by what a block begins and ends with.
 #pragma once
@@ -88,7 +89,72 @@ struct WindowSeen {
   }
 };
 
+// ---- Results that are not finite: attn_docs_bf16.h's steps, where what a row sees is two intervals, the sinks before its window and the window.
+// The lane's interval and the wave's, as docs_seen; rows behind the sequence's end are copies of its last one.
+__device__ __forceinline__ DocsSeen window_interval(const WindowGeom& g, int iw, bool window) {
+  const int last = min(iw + 31, g.seq - 1), i = min(iw + (docs_lane() & 31), last);
+  auto lo = [&](int row) { return max(0, row - g.window + 1); };
+  if (window) return {lo(i), i + 1 - lo(i), lo(iw), last + 1, lo(last), iw + 1};
+  return {0, min(g.sinks, lo(i)), 0, min(g.sinks, lo(last)), 0, min(g.sinks, lo(iw))};
+}
+// f(first row, interval) for tiles [f0, f1) of a query block, for each of the two intervals that some row of the wave has there.
+template <class F>
+__device__ __forceinline__ void window_again_tiles(const WindowGeom& g, const WindowTiles& tiles, int iw, int f0, int f1, F f) {
+#pragma unroll 1
+  for (int x = 2 * f0; x < 2 * f1; x++) {
+    const int kb = tiles.tile(x >> 1) * AB_KT;
+    const DocsSeen see = window_interval(g, iw, x & 1);
+    if (kb < see.any1 && kb + AB_KT > see.any0) f(kb, see);
+  }
+}
+// f(first row, the lane's seen rows) for those of them that some row of the wave does not see whole.
+template <class F>
+__device__ __forceinline__ void window_masked_tiles(const WindowGeom& g, const WindowTiles& tiles, int iw, int f0, int f1, F f) {
+  const WindowSeen see = {iw, 0, g.window, g.sinks};
+#pragma unroll 1
+  for (int x = f0; x < f1; x++) {
+    const int kb = tiles.tile(x) * AB_KT;
+    if (!see.none(kb) && see.part(kb)) f(kb, docs_bits(window_interval(g, iw, false), kb) | docs_bits(window_interval(g, iw, true), kb));
+  }
+}
+
 // ================================================================================ forward
+// The rows `bad` of a wave again, as docs_again_fwd.  q, o, lse: of the wave's first row; part_o, part_ml: likewise, of a part, or nullptr.
+template <int D>
+__device__ __forceinline__ void window_again_fwd(const WindowTiled& p, const WindowTiles& tiles, int iw, int f0, int f1, bool bad, const DocsRows& k, const DocsRows& v, const bf16_t* q, bf16_t* o,
+                                                 float* lse, float* part_o, float* part_ml, char* tile) {
+  const WindowGeom& g = p.g;
+  bool arrives = false, none = false;
+  window_masked_tiles(g, tiles, iw, f0, f1, [&](int kb, uint64_t seen) {
+    const DocsOdd odd = docs_odd<D>(v, kb, DOCS_ODD);
+    arrives |= (odd.some & ~seen) != 0;
+    none |= (odd.all & seen) != 0;
+  });
+  const uint64_t rows = __ballot(bad && arrives && !none);
+  if (rows == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first results of these rows, which other lanes have stored, are in place
+  const int lane = docs_lane(), r = lane & 31;
+  DocsTiled softmax = {};
+  softmax.exp_scale = p.exp_scale;
+  float m = -3.0e38f, l = 0.f;
+  f32x16 ot[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(ot[dt]);
+  window_again_tiles(g, tiles, iw, f0, f1, [&](int kb, const DocsSeen& see) {
+    f32x16 st[2];
+    docs_again_scores<D>(st, tile, k, kb, q + (size_t)min(r, g.seq - 1 - iw) * k.ld, true);
+    docs_softmax<D, false, true>(softmax, see, kb, lane >> 5, st, ot, m, l);
+    docs_again_add<D>(ot, st, tile, v, kb, see);
+  });
+  const bool on = ((rows | rows >> 32) >> r) & 1;
+  if (part_o) {
+    docs_again_out<D>(ot, 1.f, part_o + (size_t)r * D, on);
+    if (on) { part_ml[r * 2] = m; part_ml[r * 2 + 1] = l; }
+  } else {
+    docs_again_out<D>(ot, 1.f / l, o + (size_t)r * g.nq * D, on);
+    if (on) lse[r] = (m + log2f(l)) * 0.6931471805599453f;
+  }
+}
 // grid: window_grid(nq, blocks * parts, batch)
 template <int D>
 __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_fwd_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o, float* __restrict__ lse,
@@ -188,42 +254,39 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_fwd_bf16_kernel(con
   __syncthreads();  // every wave is done with the K/V rings: their LDS serves the output turn
   const int live = seq - iw;  // rows of the wave that there are
   const size_t head = (size_t)h * g.batch * seq + t0;
+  const bool bad = l32 < live && docs_not_finite<D / 32>(ot) && l == l;
+  bf16_t* orow = o + ((t0 + iw) * nq + h) * D;
+  float *prow = nullptr, *pml = nullptr;
   if (p.parts > 1) {
     const size_t unit = (((size_t)u.b * nq + h) * p.blocks + ib) * p.parts + part;
-    float* prow = part_o + (unit * WB_BLOCK + wave * 32) * D;
+    prow = part_o + (unit * WB_BLOCK + wave * 32) * D;
+    pml = part_ml + (unit * WB_BLOCK + wave * 32) * 2;
     wave_rows_out_f32<D>(
         reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
         [&](int dt, int q4) { return f32x4{ot[dt][4 * q4], ot[dt][4 * q4 + 1], ot[dt][4 * q4 + 2], ot[dt][4 * q4 + 3]}; },
         [&](int r) { return r < live ? prow + (size_t)r * D : nullptr; });
     if (lane < 32 && lane < live) {
-      float* pml = part_ml + (unit * WB_BLOCK + wave * 32 + l32) * 2;
-      pml[0] = m;
-      pml[1] = l;
+      pml[l32 * 2] = m;
+      pml[l32 * 2 + 1] = l;
     }
-    return;
+  } else {
+    const float inv = 1.0f / l;
+    wave_rows_out_bf16<D>(
+        reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+        [&](int dt, int q4) { return f32x4{ot[dt][4 * q4] * inv, ot[dt][4 * q4 + 1] * inv, ot[dt][4 * q4 + 2] * inv, ot[dt][4 * q4 + 3] * inv}; },
+        [&](int r) { return r < live ? orow + (size_t)r * nq * D : nullptr; });
+    if (lane < 32 && lane < live) lse[head + iq] = (m + log2f(l)) * 0.6931471805599453f;
   }
-  bf16_t* orow = o + ((t0 + iw) * nq + h) * D;
-  const bool bad = l32 < live && (docs_not_finite<D / 32>(ot) || !(l < INFINITY));
-  const float inv = 1.0f / l;
-  wave_rows_out_bf16<D>(
-      reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
-      [&](int dt, int q4) { return f32x4{ot[dt][4 * q4] * inv, ot[dt][4 * q4 + 1] * inv, ot[dt][4 * q4 + 2] * inv, ot[dt][4 * q4 + 3] * inv}; },
-      [&](int r) { return r < live ? orow + (size_t)r * nq * D : nullptr; });
-  if (lane < 32 && lane < live) lse[head + iq] = (m + log2f(l)) * 0.6931471805599453f;
-  uint64_t again = __ballot(bad);
-  if (again == 0) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first results of these rows, which other lanes have stored, are in place
-#pragma unroll 1
-  for (uint32_t w = (uint32_t)(again | again >> 32); w != 0; w &= w - 1) {
-    const int i = iw + __builtin_ctz(w);
-    window_row_fwd(g, rows, h, i, o + ((t0 + i) * nq + h) * D, lse + head + i);
-  }
+  if (!__any(bad)) return;
+  const DocsRows k = {rows + (size_t)(nq + hk) * D, (size_t)ld, 0, docs_scalar(seq) - 1}, v = {k.base + (size_t)nkv * D, (size_t)ld, 0, k.last};
+  window_again_fwd<D>(p, tiles, docs_scalar(iw), docs_scalar(f0), docs_scalar(f1), bad, k, v, rows + (size_t)iw * ld + (size_t)h * D, orow, lse + head + iw, prow, pml,
+                      smem + wave * (32 * D) * sizeof(float));
 }
 
 // Merges the parts of every block.  grid (nq, ceil(seq / 16), batch): 16 rows a block, 16 lanes a row
 template <int D>
-__global__ __launch_bounds__(256) void attn_window_combine_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                                                                  bf16_t* __restrict__ o, float* __restrict__ lse) {
+__global__ __launch_bounds__(256) void attn_window_combine_kernel(const WindowTiled p, const float* __restrict__ part_o, const float* __restrict__ part_ml, bf16_t* __restrict__ o,
+                                                                  float* __restrict__ lse) {
   const WindowGeom& g = p.g;
   const int h = blockIdx.x, b = blockIdx.z, nq = g.nq, i = blockIdx.y * 16 + (threadIdx.x >> 4), row = min(i, g.seq - 1);
   constexpr int CPT = D / 16;
@@ -246,32 +309,49 @@ __global__ __launch_bounds__(256) void attn_window_combine_kernel(const WindowTi
       acc[e] += w * v[0]; acc[e + 1] += w * v[1]; acc[e + 2] += w * v[2]; acc[e + 3] += w * v[3];
     }
   }
+  if (i >= g.seq) return;
   const float inv = 1.0f / L;
-  float top = 0.f;
-#pragma unroll
-  for (int e = 0; e < CPT; e++) top = max_of(top, __builtin_fabsf(acc[e]));
-  const bool live = i < g.seq;
   bf16_t* orow = o + ((t0 + row) * nq + h) * D;
-  if (live) {
 #pragma unroll
-    for (int e = 0; e < CPT; e += 4) {
-      const bf16x4 x = {(bf16_t)(acc[e] * inv), (bf16_t)(acc[e + 1] * inv), (bf16_t)(acc[e + 2] * inv), (bf16_t)(acc[e + 3] * inv)};
-      *reinterpret_cast<bf16x4*>(orow + c0 + e) = x;
-    }
-    if (c0 == 0) lse[(size_t)h * g.batch * g.seq + t0 + row] = (M + log2f(L)) * 0.6931471805599453f;
+  for (int e = 0; e < CPT; e += 4) {
+    const bf16x4 x = {(bf16_t)(acc[e] * inv), (bf16_t)(acc[e + 1] * inv), (bf16_t)(acc[e + 2] * inv), (bf16_t)(acc[e + 3] * inv)};
+    *reinterpret_cast<bf16x4*>(orow + c0 + e) = x;
   }
-  const uint64_t again = __ballot(live && (!(top < INFINITY) || !(L < INFINITY)));
-  if (again == 0) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll 1
-  for (int r = 0; r < 4; r++) {
-    if (((again >> (16 * r)) & 0xffff) == 0) continue;
-    const int k = blockIdx.y * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 4 + r;
-    window_row_fwd(g, qkv + t0 * (size_t)(nq + 2 * g.nkv) * D, h, k, o + ((t0 + k) * nq + h) * D, lse + (size_t)h * g.batch * g.seq + t0 + k);
-  }
+  if (c0 == 0) lse[(size_t)h * g.batch * g.seq + t0 + row] = (M + log2f(L)) * 0.6931471805599453f;
 }
 
 // ================================================================================ backward: dQ
+// The rows `bad` of a wave again, as docs_again_dq.  q, dout, dq: of the wave's first row.
+template <int D>
+__device__ __forceinline__ void window_again_dq(const WindowTiled& p, const WindowTiles& tiles, int iw, bool bad, float l2, float dl, const DocsRows& k, const DocsRows& v, const bf16_t* q,
+                                                const bf16_t* dout, bf16_t* dq, char* tile) {
+  const WindowGeom& g = p.g;
+  const int lane = docs_lane(), r = lane & 31, at = min(r, g.seq - 1 - iw), n = tiles.count();
+  const size_t ldo = (size_t)g.nq * D;
+  bool arrives = (docs_odd<D>({dout + at * ldo, 0, 0, 0}, 0, DOCS_LARGE).some >> lane) & 1;
+  window_masked_tiles(g, tiles, iw, 0, n, [&](int kb, uint64_t seen) {
+    arrives |= ((docs_odd<D>(k, kb, DOCS_ODD).some | docs_odd<D>(v, kb, DOCS_LARGE).some) & ~seen) != 0;
+  });
+  const uint64_t rows = __ballot(bad && arrives);
+  if (rows == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first results of these rows, which other lanes have stored, are in place
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++) acc_zero<false>(acc[dt]);
+  window_again_tiles(g, tiles, iw, 0, n, [&](int kb, const DocsSeen& see) {
+    f32x16 st[2], dp[2];
+    docs_again_scores<D>(st, tile, k, kb, q + at * k.ld, true);
+    docs_again_scores<D>(dp, tile, v, kb, dout + at * ldo, true);
+    const uint64_t seen = docs_bits(see, kb);
+#pragma unroll
+    for (int mt = 0; mt < 2; mt++)
+#pragma unroll
+      for (int i = 0; i < 16; i++)
+        st[mt][i] = docs_where((uint32_t)(seen >> (32 * mt)) >> (4 * (lane >> 5)), 8 * (i >> 2) + (i & 3), fast_exp2(fmaf(st[mt][i], p.exp_scale, -l2)) * (dp[mt][i] - dl));
+    docs_again_add<D>(acc, st, tile, k, kb, see);
+  });
+  docs_again_out<D>(acc, g.scale, dq + r * k.ld, ((rows | rows >> 32) >> r) & 1);
+}
 // As docs_dq_block: block ib of head h, sequence b.  STORE: leaves the rows' delta and lse2 for the dK/dV launch behind it; otherwise attn_window_prep_kernel has.
 template <int D, bool STORE>
 __device__ __forceinline__ void window_dq_block(const WindowTiled& p, int ib, int h, int b, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o, const bf16_t* __restrict__ dout,
@@ -366,20 +446,15 @@ __device__ __forceinline__ void window_dq_block(const WindowTiled& p, int ib, in
   __syncthreads();
   const int live = seq - iw;
   bf16_t* out = dqkv + (t0 + iw) * ld + (size_t)h * D;
-  const bool bad = l32 < live && docs_not_finite<D / 32>(dqt);
+  const bool bad = l32 < live && docs_not_finite<D / 32>(dqt) && l2 == l2 && __builtin_isfinite(dl);
   const float scale = g.scale;
   wave_rows_out_bf16<D>(
       reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
       [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4] * scale, dqt[dt][4 * q4 + 1] * scale, dqt[dt][4 * q4 + 2] * scale, dqt[dt][4 * q4 + 3] * scale}; },
       [&](int r) { return r < live ? out + (size_t)r * ld : nullptr; });
-  const uint64_t again = __ballot(bad);
-  if (again == 0) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll 1
-  for (uint32_t w = (uint32_t)(again | again >> 32); w != 0; w &= w - 1) {
-    const int i = iw + __builtin_ctz(w);
-    window_row_dq(g, rows, dout + ((t0 + i) * nq + h) * D, lse[head + i], delta[head + i], h, i, dqkv + (t0 + i) * ld + (size_t)h * D);
-  }
+  if (!__any(bad)) return;
+  const DocsRows k = {rows + (size_t)(nq + hk) * D, (size_t)ld, 0, docs_scalar(seq) - 1}, v = {k.base + (size_t)nkv * D, (size_t)ld, 0, k.last};
+  window_again_dq<D>(p, tiles, docs_scalar(iw), bad, l2, dl, k, v, rows + (size_t)iw * ld + (size_t)h * D, dout + ((t0 + iw) * nq + h) * D, out, smem + wave * (32 * D) * sizeof(float));
 }
 
 // ================================================================================ backward: dK, dV
@@ -393,7 +468,7 @@ struct WindowWalk {
 };
 // Unit `unit` of key/value head hk, sequence b: the blocks without sinks, which are of one length, then the short units of the others, which fill up the last round.
 template <int D>
-__device__ __forceinline__ void window_dkv_block(const WindowTiled& p, int unit, int hk, int b, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+__device__ __forceinline__ void window_dkv_block(const WindowTiled& p, int unit, int hk, int b, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
                                                  const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   using TL = ATile<D>;
   constexpr bool PINNED = D == 128;
@@ -514,28 +589,30 @@ __device__ __forceinline__ void window_dkv_block(const WindowTiled& p, int unit,
   const float scale = g.scale;
   auto dk_quad = [&](int dt, int q4) { return f32x4{dkt[dt][4 * q4] * scale, dkt[dt][4 * q4 + 1] * scale, dkt[dt][4 * q4 + 2] * scale, dkt[dt][4 * q4 + 3] * scale}; };
   auto dv_quad = [&](int dt, int q4) { return f32x4{dvt[dt][4 * q4], dvt[dt][4 * q4 + 1], dvt[dt][4 * q4 + 2], dvt[dt][4 * q4 + 3]}; };
+  const bool bad = l32 < live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt));
+  bf16_t* out = dqkv + (t0 + jw) * ld + (size_t)(nq + hk) * D;
   if (k.part >= 0) {
     float* reg = reinterpret_cast<float*>(smem) + wave * (32 * D);
     wave_rows_out_f32<D>(reg, lane, dk_quad, [&](int r) { return r < live ? prow + (size_t)r * (2 * D) : nullptr; });
     __builtin_amdgcn_wave_barrier();
     wave_rows_out_f32<D>(reg, lane, dv_quad, [&](int r) { return r < live ? prow + (size_t)r * (2 * D) + D : nullptr; });
-    return;
+  } else {
+    bf16_t* reg = reinterpret_cast<bf16_t*>(smem) + wave * (32 * D);
+    wave_rows_out_bf16<D>(reg, lane, dk_quad, [&](int r) { return r < live ? out + (size_t)r * ld : nullptr; });
+    __builtin_amdgcn_wave_barrier();
+    wave_rows_out_bf16<D>(reg, lane, dv_quad, [&](int r) { return r < live ? out + (size_t)r * ld + (size_t)nkv * D : nullptr; });
   }
-  const bool bad = l32 < live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt));
-  bf16_t* out = dqkv + (t0 + jw) * ld + (size_t)(nq + hk) * D;
-  bf16_t* reg = reinterpret_cast<bf16_t*>(smem) + wave * (32 * D);
-  wave_rows_out_bf16<D>(reg, lane, dk_quad, [&](int r) { return r < live ? out + (size_t)r * ld : nullptr; });
-  __builtin_amdgcn_wave_barrier();
-  wave_rows_out_bf16<D>(reg, lane, dv_quad, [&](int r) { return r < live ? out + (size_t)r * ld + (size_t)nkv * D : nullptr; });
-  const uint64_t again = __ballot(bad);
-  if (again == 0) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll 1
-  for (uint32_t w = (uint32_t)(again | again >> 32); w != 0; w &= w - 1) {
-    const int j = jw + __builtin_ctz(w);
-    bf16_t* to = dqkv + (t0 + j) * ld + (size_t)(nq + hk) * D;
-    window_row_dkv(g, rows, dout + t0 * ldo, lse + t0, delta + t0, T, hk, j, to, to + (size_t)nkv * D);
-  }
+  if (!__any(bad)) return;
+  const int keys = docs_scalar(jw), last = docs_scalar(seq) - 1, h0 = docs_scalar(hq), mine = min(keys + (docs_lane() & 31), last), from = docs_scalar(q0);
+  const DocsSeen see = {mine, window_queries_end(g, mine) - mine, keys, docs_scalar(walk.any1), min(keys + 31, last), docs_scalar(walk.all1)};
+  const DocsUnit run = {0, docs_scalar(f0), docs_scalar(f1), k.part};
+  const DocsSpan span = {from / AB_KT, docs_scalar(nt), 0, 0};
+  const DocsRows q = {rows + (size_t)h0 * D, (size_t)ld, 0, last}, e = {dout + t0 * ldo + (size_t)h0 * D, (size_t)ldo, 0, last};
+  DocsTiled docs = {};
+  docs.a.v.T = (int)T;
+  docs.exp_scale = p.exp_scale;
+  docs_again_dkv<D, false>(docs, see, bad, run, span, q, e, lse2 + (size_t)h0 * T + t0, delta + (size_t)h0 * T + t0, kcol + (size_t)keys * ld, ld, (size_t)nkv * D, out, prow, scale,
+                           smem + wave * (32 * D) * sizeof(float));
 }
 // Delta and lse2 of every row, as attn_bwd_prep_kernel: the numbers the dQ blocks use.  Two lanes a row of a head.
 template <int D>
@@ -571,10 +648,10 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_dq_bf16_kernel(cons
   if (u.id < p.blocks) window_dq_block<D, true>(p, p.blocks - 1 - u.id, window_head(blockIdx.x, p.g.nq), u.b, qkv, o, dout, lse, lse2, delta, dqkv);
 }
 template <int D>
-__global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
+__global__ __launch_bounds__(AB_THREADS) void attn_window_dkv_bf16_kernel(const WindowTiled p, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
                                                                           const float* __restrict__ lse2, const float* __restrict__ delta, bf16_t* __restrict__ dqkv, float* __restrict__ part) {
   const WindowUnit u = window_unit(p.g.batch);
-  window_dkv_block<D>(p, u.id, window_head(blockIdx.x, p.g.nkv), u.b, qkv, dout, lse, lse2, delta, dqkv, part);
+  window_dkv_block<D>(p, u.id, window_head(blockIdx.x, p.g.nkv), u.b, qkv, dout, lse2, delta, dqkv, part);
 }
 // ... and as one, behind attn_window_prep_kernel, for grids that leave units of the chip idle: dK/dV units (the longer ones) first.  grid (units * nkv + blocks * nq, batch)
 template <int D>
@@ -584,7 +661,7 @@ __global__ __launch_bounds__(AB_THREADS) void attn_window_bwd_bf16_kernel(const 
   const int nq = p.g.nq, nkv = p.g.nkv, n_k = window_units(p) * nkv, id = blockIdx.x;
   if (id < n_k) {
     const int unit = __builtin_amdgcn_readfirstlane(id / nkv);
-    window_dkv_block<D>(p, unit, id - unit * nkv, blockIdx.y, qkv, dout, lse, lse2, delta, dqkv, part);
+    window_dkv_block<D>(p, unit, id - unit * nkv, blockIdx.y, qkv, dout, lse2, delta, dqkv, part);
   } else {
     const int x = id - n_k, block = __builtin_amdgcn_readfirstlane(x / nq);
     window_dq_block<D, false>(p, p.blocks - 1 - block, x - block * nq, blockIdx.y, qkv, o, dout, lse, lse2, delta, dqkv);
@@ -592,8 +669,7 @@ __global__ __launch_bounds__(AB_THREADS) void attn_window_bwd_bf16_kernel(const 
 }
 // Adds the units of key blocks [first, first + y / 32) in order.  grid (nkv, blocks * 32, batch): 4 keys a block, a wave each
 template <int D>
-__global__ __launch_bounds__(256) void attn_window_merge_kernel(const WindowTiled p, int first, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse,
-                                                                const float* __restrict__ delta, const float* __restrict__ part, bf16_t* __restrict__ dqkv) {
+__global__ __launch_bounds__(256) void attn_window_merge_kernel(const WindowTiled p, int first, const float* __restrict__ part, bf16_t* __restrict__ dqkv) {
   const WindowGeom& g = p.g;
   const int hk = blockIdx.x, b = blockIdx.z, j = first * WB_BLOCK + blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, nkv = g.nkv, jb = j / WB_BLOCK;
   if (j >= g.seq) return;
@@ -603,22 +679,15 @@ __global__ __launch_bounds__(256) void attn_window_merge_kernel(const WindowTile
   const int ch = sink ? p.sink_chunk : p.plain_chunk, units = (tiles + ch - 1) / ch, plain = (p.blocks - p.sink_blocks) * p.plain_units;
   const int at = sink ? jb * p.sink_units + (p.plain_units > 1 ? plain : 0) : (jb - p.sink_blocks) * p.plain_units;
   const float* from = part + ((((size_t)b * nkv + hk) * window_parts(p) + at) * WB_BLOCK + j % WB_BLOCK) * (2 * D) + lane * CPL;
-  float s[CPL] = {}, top = 0.f;
+  float s[CPL] = {};
 #pragma unroll 8
   for (int c = 0; c < units; c++)
 #pragma unroll
     for (int e = 0; e < CPL; e++) s[e] += from[(size_t)c * WB_BLOCK * 2 * D + e];
-  const size_t t0 = (size_t)b * g.seq, T = (size_t)g.batch * g.seq;
-  bf16_t* dk = dqkv + (t0 + j) * ld + (size_t)(g.nq + hk) * D;
+  bf16_t* dk = dqkv + ((size_t)b * g.seq + j) * ld + (size_t)(g.nq + hk) * D;
   const int c0 = lane * CPL;
 #pragma unroll
-  for (int e = 0; e < CPL; e++) {
-    top = max_of(top, __builtin_fabsf(s[e]));
-    (c0 < D ? dk + c0 : dk + (size_t)nkv * D + c0 - D)[e] = (bf16_t)s[e];
-  }
-  if (!__any(!(top < INFINITY))) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  window_row_dkv(g, qkv + t0 * ld, dout + t0 * g.nq * D, lse + t0, delta + t0, T, hk, j, dk, dk + (size_t)nkv * D);
+  for (int e = 0; e < CPL; e++) (c0 < D ? dk + c0 : dk + (size_t)nkv * D + c0 - D)[e] = (bf16_t)s[e];
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -687,7 +756,7 @@ static int window_fwd(const WindowTiled& p, const bf16_t* qkv, bf16_t* o, float*
   attn_window_fwd_bf16_kernel<D><<<window_grid(g.nq, p.blocks * p.parts, g.batch), AB_THREADS, lds, s>>>(p, qkv, o, lse, ws, part_ml);
   DH_LAUNCH_CHECK();
   if (p.parts > 1) {  // few blocks: ceil(seq / 16) fits the launch's y
-    attn_window_combine_kernel<D><<<dim3(g.nq, (g.seq + 15) / 16, g.batch), 256, 0, s>>>(p, qkv, ws, part_ml, o, lse);
+    attn_window_combine_kernel<D><<<dim3(g.nq, (g.seq + 15) / 16, g.batch), 256, 0, s>>>(p, ws, part_ml, o, lse);
     DH_LAUNCH_CHECK();
   }
   return DH_OK;
@@ -722,12 +791,12 @@ static int window_bwd(const WindowTiled& p, const bf16_t* qkv, const bf16_t* o, 
   } else {
     attn_window_dq_bf16_kernel<D><<<window_grid(g.nq, p.blocks, g.batch), AB_THREADS, lds_dq, s>>>(p, qkv, o, dout, lse, lse2, delta, dqkv);
     DH_LAUNCH_CHECK();
-    attn_window_dkv_bf16_kernel<D><<<window_grid(g.nkv, window_units(p), g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, dout, lse, lse2, delta, dqkv, part);
+    attn_window_dkv_bf16_kernel<D><<<window_grid(g.nkv, window_units(p), g.batch), AB_THREADS, lds_dkv, s>>>(p, qkv, dout, lse2, delta, dqkv, part);
     DH_LAUNCH_CHECK();
   }
   const int first = p.sink_units > 1 ? 0 : p.sink_blocks, cut = (p.plain_units > 1 ? p.blocks : p.sink_blocks) - first;  // blocks that were cut: few enough for the launch's y
   if (cut > 0 && (p.plain_units > 1 || p.sink_units > 1)) {
-    attn_window_merge_kernel<D><<<dim3(g.nkv, cut * (WB_BLOCK / 4), g.batch), 256, 0, s>>>(p, first, qkv, dout, lse, delta, part, dqkv);
+    attn_window_merge_kernel<D><<<dim3(g.nkv, cut * (WB_BLOCK / 4), g.batch), 256, 0, s>>>(p, first, part, dqkv);
     DH_LAUNCH_CHECK();
   }
   return DH_OK;

@@ -1,6 +1,9 @@
 // Attention with a sliding window and sinks: what its sources share.
 #pragma once
-#include "window_rows.h"
+#include "mixers.h"
+
+// The queries that see key j are rows j .. end - 1.
+__device__ __forceinline__ int window_queries_end(const WindowGeom& g, int j) { return j < g.sinks ? g.seq : (int)min((long long)g.seq, (long long)j + g.window); }
 
 int dh_launch_window_fwd_bf16(const WindowGeom& g, const bf16_t* qkv, bf16_t* o, float* lse, void* ws, hipStream_t stream);
 size_t dh_window_fwd_bf16_ws_bytes(const WindowGeom& g);

@@ -102,15 +102,18 @@ def test_a_whole_window_is_causal_attention(dh, tt, d):
 
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("tt,nq,nkv,d", [(BF, 4, 2, 128), (BF, 2, 2, 64), (F, 2, 1, 64)])
-def test_what_a_row_does_not_see_does_not_reach_it(dh, tt, nq, nkv, d, bad):
-    seq, window, sinks, at = 420, 70, 6, [3, 100, 101, 260, 419]
+@pytest.mark.parametrize("tt,nq,nkv,d,seq,window,sinks", [(BF, 4, 2, 128, 420, 70, 6), (BF, 2, 2, 64, 420, 70, 6), (F, 2, 1, 64, 420, 70, 6),
+                                                          (BF, 2, 1, 128, 1500, 1300, 70),  # parts of a walk over keys
+                                                          (BF, 40, 8, 128, 1300, 200, 4),   # as many blocks as take two launches
+                                                          (BF, 4, 4, 64, 700, 400, 130)])
+def test_what_a_row_does_not_see_does_not_reach_it(dh, tt, nq, nkv, d, seq, window, sinks, bad):
+    at, last = [3, 100, 101, 260, seq - 1], seq - 1
     c = Case(dh, tt, 1, seq, window, sinks, nq, nkv, d)
     a, b = nq * d, (nq + nkv) * d
     c.qkv[100, b:] = bad                     # a value
     c.qkv[101, a + 3] = bad                  # a key's element
     c.qkv[260, b + 5] = bad
-    c.qkv[419, :a] = bad                     # the last row's query: it sees the sinks
+    c.qkv[last, :a] = bad                    # the last row's query: it sees the sinks
     c.qkv[3, b + 1::7] = bad                 # a sink, which every later row sees
     if d == 64:
         c.qkv[3, b + 1::7] = 0.5
@@ -119,7 +122,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(dh, tt, nq, nkv, d, bad):
     c.upload()
     c.forward()
     c.backward()
-    hurt = c.seen[:, at].any(1) | torch.tensor([i == 419 for i in range(seq)])       # rows with such a key or query
+    hurt = c.seen[:, at].any(1) | torch.tensor([i == last for i in range(seq)])       # rows with such a key or query
     grad = hurt | torch.tensor([i == 300 for i in range(seq)])
     keys = c.seen[grad].any(0)                                                       # keys that a hurt row sees
     fwd = R.attention(c.seen, nq, nkv, d, c.qkv)
@@ -130,6 +133,30 @@ def test_what_a_row_does_not_see_does_not_reach_it(dh, tt, nq, nkv, d, bad):
     R.check(c.dqkv[:, a:b], bwd["dk"], "dk", ~keys[:, None])
     R.check(c.dqkv[:, b:], bwd["dv"], "dv", ~keys[:, None])
     assert not torch.isfinite(c.o[100].float()).all() and not torch.isfinite(c.dqkv[300].float()).all()
+
+
+@pytest.mark.parametrize("nq,nkv,d,seq,window,sinks", [(4, 2, 128, 420, 70, 6), (2, 2, 64, 420, 70, 0), (2, 1, 128, 1500, 1300, 70), (40, 8, 128, 1300, 200, 4)])
+@pytest.mark.parametrize("which", ["qkv", "dout"])
+def test_nothing_but_nans_from_a_row_on(dh, nq, nkv, d, seq, window, sinks, which):
+    """A step that has diverged: what sees such a row is a NaN, what sees none is as without them."""
+    c, first = Case(dh, BF, 1, seq, window, sinks, nq, nkv, d), seq // 2
+    (c.qkv if which == "qkv" else c.dout)[first:] = math.nan
+    c.upload()
+    c.forward()
+    c.backward()
+    a = nq * d
+    if which == "qkv":
+        assert torch.isnan(c.o[first:].float()).all() and torch.isnan(c.lse[:, first:]).all()
+    assert torch.isnan(c.dqkv[first:].float()).all()
+    fine, keys = torch.arange(seq) < first, ~c.seen[first:].any(0)
+    fwd = R.attention(c.seen, nq, nkv, d, c.qkv)
+    R.check(c.o, fwd["o"], "o", fine[:, None])
+    bwd = R.attention(c.seen, nq, nkv, d, c.qkv, c.dout, c.o.cpu(), c.lse.cpu())
+    R.check(c.dqkv[:, :a], bwd["dq"], "dq", fine[:, None])
+    b = a + nkv * d
+    R.check(c.dqkv[:, a:b], bwd["dk"], "dk", keys[:, None])
+    R.check(c.dqkv[:, b:], bwd["dv"], "dv", keys[:, None])
+    assert torch.isnan(c.dqkv[~keys.cuda(), a:].float()).all()
 
 
 def test_scores_of_minus_infinity(dh):
