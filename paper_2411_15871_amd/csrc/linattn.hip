@@ -3,7 +3,7 @@
 #include "linattn.h"
 
 // ------------------------------------------------------------------------------------ states along the pieces of a row
-// grid (ceil(d * d / 1024), nkv * passes, batch), four elements a thread, LIN_BATCH pieces of them in flight (4 and 16, 32 pieces of 16 states of 128: 14.6 and LIN_US us)
+// grid (ceil(d * d / 1024), nkv * passes, batch), four elements a thread, LIN_BATCH pieces of them in flight (4 and 16, two passes of 16 pieces of 16 states of 128: 14.6 and 12.0 us)
 #define LIN_BATCH 16
 __global__ __launch_bounds__(256) void lin_carry_kernel(const LinGeom g, int pieces, int tokens, const LinCarry c0, const LinCarry c1) {
   const int b = blockIdx.z, hk = blockIdx.y % g.nkv, e = (blockIdx.x * 256 + threadIdx.x) * 4, dd = g.d * g.d;

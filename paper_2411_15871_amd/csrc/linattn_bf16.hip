@@ -99,16 +99,14 @@ struct LinPowers {
 };
 // The values of 32 tokens in a wave's columns, as the matrix instruction takes them.
 struct LinValues {
-  bf16x8 all[2], kept[2];  // kept: zeros in the place of tokens that hold an infinity or a NaN, which a zero's product would carry to tokens that do not see them
-  uint32_t odd;            // those tokens
+  bf16x8 all[2];
+  uint32_t odd;  // tokens that hold an infinity or a NaN, which a zero's product would carry to tokens that do not see them
   __device__ __forceinline__ void load(const lds_char* t0, const lds_char* t1, int row_bytes) {
 #pragma unroll
     for (int c = 0; c < 2; c++) all[c] = lds_frag_tr(t0, t1, c * 16 * row_bytes);
   }
-  __device__ __forceinline__ void look(int kg) {
+  __device__ __forceinline__ void look() {
     typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
-    kept[0] = all[0];
-    kept[1] = all[1];
     odd = 0;
     const u16x8 m0 = __builtin_bit_cast(u16x8, all[0]) & (unsigned short)0x7fff, m1 = __builtin_bit_cast(u16x8, all[1]) & (unsigned short)0x7fff;
     const u16x8 m = __builtin_elementwise_max(m0, m1);
@@ -120,11 +118,6 @@ struct LinValues {
       const uint64_t x = __ballot(m0[e] >= 0x7f80), y = __ballot(m1[e] >= 0x7f80);
       odd |= ((uint32_t)x ? 1u << lin_token(0, e, 0) : 0) | ((uint32_t)(x >> 32) ? 1u << lin_token(0, e, 1) : 0);
       odd |= ((uint32_t)y ? 1u << lin_token(1, e, 0) : 0) | ((uint32_t)(y >> 32) ? 1u << lin_token(1, e, 1) : 0);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-      kept[0][e] = (odd >> lin_token(0, e, kg)) & 1 ? (bf16_t)0.f : all[0][e];
-      kept[1][e] = (odd >> lin_token(1, e, kg)) & 1 ? (bf16_t)0.f : all[1][e];
     }
   }
 };
@@ -140,8 +133,18 @@ __device__ __forceinline__ void lin_inside(f32x16& ot, f32x16& st, const LinPowe
   for (int r = 0; r < 16; r++)
     st[r] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, st[r] * p.weight[r]) & (uint32_t)__builtin_amdgcn_sbfe((int)p.seen, r, 1));
   const bf16x8 pf[2] = {pack_rows(st, 0), pack_rows(st, 1)};
-  ot = MFMA(v.kept[0], pf[0], ot);
-  ot = MFMA(v.kept[1], pf[1], ot);
+  if (v.odd == 0) {
+    ot = MFMA(v.all[0], pf[0], ot);
+    ot = MFMA(v.all[1], pf[1], ot);
+    return;
+  }
+  bf16x8 kept[2];  // the others
+#pragma unroll
+  for (int c = 0; c < 2; c++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) kept[c][e] = (v.odd >> lin_token(c, e, kg)) & 1 ? (bf16_t)0.f : v.all[c][e];
+  ot = MFMA(kept[0], pf[0], ot);
+  ot = MFMA(kept[1], pf[1], ot);
 #pragma unroll 1
   for (uint32_t odd = v.odd; odd != 0; odd &= odd - 1) {  // token by token, to those that see it
     const int j = __builtin_ctz(odd);
@@ -160,8 +163,8 @@ __device__ __forceinline__ void lin_inside(f32x16& ot, f32x16& st, const LinPowe
     for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
   }
 }
-// Where a wave has a SIMD to itself fragments are asked for ahead, and what is asked for stays in its place: left to the compiler each is read right before the product that takes it, which
-// then waits for LDS.  With two waves a SIMD these cover such waits, and registers count for more.
+// Where a wave does little else (sums of states) fragments are asked for ahead, and what is asked for stays in its place: left to the compiler each is read right before the product that takes it,
+// which then waits for LDS.  Elsewhere the waves of a SIMD cover such waits, and registers count for more.
 #define LIN_PIN() __builtin_amdgcn_sched_barrier(0)
 template <int D>
 struct LinRows {  // a tile's transposed fragments of 16 tokens
@@ -273,7 +276,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   const float l2 = g.log_decay[hk] * LOG2E, f_in = GROUPED ? g.scale : 1.f;
   const uint32_t lds = lds_address(smem);
   // offsets of q's rows and of k's, or (sums) of k's and v's; with results k and v lie in rows of the same length.  (Two registers fewer: the loop has none to spare, and what lies in scratch
-  // waits for the transfers ahead of it: 78 -> 51 us for 8192 tokens x 32 heads in 8 pieces.)
+  // waits for the transfers ahead of it: 78 -> 60 us for the results of 8192 tokens x 32 heads in 8 pieces.)
   uint32_t off[2][2];
   TR::offsets(off[0], OUT ? p.ldq : p.ldk, LC - 1, wave, lane);
   TR::offsets(off[1], OUT ? p.ldk : p.ldv, LC - 1, wave, lane);
@@ -316,7 +319,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
       bf16x8 qf[KS];
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) qf[ks] = lds_frag(Qt + fa.dir[ks], 0);
-      v.look(kg);
+      v.look();
       f32x16 ot, st;
       lin_zero(ot);
       lin_zero(st);
@@ -349,121 +352,79 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   }
 }
 
-// dk and dv, from the row's end, over the group's heads: a wave holds its columns of R (for dv) and of its transpose (for dk), so that q and dout are read once.  LDS: two slots each of K, V, Q, dO tiles.
+// dk and dv, from the row's end, over the group's heads.  Both are the same form: dv has the state R, rows of Q against keys, values of dO; dk has R's transpose, rows of dO against values, values
+// of Q.  Half of a block's waves takes one of them each, off the same tiles, so that a SIMD has two waves: one that holds both states has it to itself and moves half of its registers to and from the
+// accumulators' (2 x 4096 tokens on 32:8 heads, a training step: 285 -> 264 us).  Bound by the products' chains and the vector arithmetic between them; scores in two chains, or the state's products between
+// the scores' and theirs, take registers that there are not (283 and 280 us).  LDS: two slots each of K, V, Q, dO tiles.
 template <int D, bool EXACT>
 __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p, int piece, int hk, int b, char* smem) {
   using TR = LinTransfer<D>;
   constexpr int W = D / 32, KS = D / 16;
   const lds_char* sm = (const lds_char*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
+  const int lane = threadIdx.x & 63, both = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), is_dk = both >= W, wave = both - is_dk * W, l32 = lane & 31, kg = lane >> 5;
   const LinGeom& g = a.g;
-  const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), ld = (g.nq + 2 * g.nkv) * D, ldo = g.nq * D;
+  const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), ld = (g.nq + 2 * g.nkv) * D, ldo = g.nq * D, ldx = is_dk ? ldo : ld;
   const size_t t0 = (size_t)b * g.seq;
   const float l2 = g.log_decay[hk] * LOG2E;
   const uint32_t lds = lds_address(smem);
   uint32_t off[2][2];
   TR::offsets(off[0], ld, LC - 1, wave, lane);
-  TR::offsets(off[1], ldo, LC - 1, wave, lane);
-  const int steps = (c1 - c0) * grp;
+  TR::offsets(off[1], ldx, LC - 1, wave, lane);
+  const int steps = (c1 - c0) * grp, column = (g.nq + is_dk * g.nkv + hk) * D, to = (g.nq + (1 - is_dk) * g.nkv + hk) * D;
   int in = 0, ih = 0;
-  auto issue = [&]() {
+  auto issue = [&]() {  // each half the tiles that its products begin with
     const int chunk = c1 - 1 - in, slot_s = (in * grp + ih) & 1, slot_c = in & 1, last = min(LC, g.seq - chunk * LC) - 1;
-    const bf16_t* row = p.qkv + (t0 + (size_t)chunk * LC) * ld;
-    if (ih == 0) {
-      TR::go(row + (size_t)(g.nq + hk) * D, ld, off[0], last, lds + slot_c * TR::TILE, wave, lane);
-      TR::go(row + (size_t)(g.nq + g.nkv + hk) * D, ld, off[0], last, lds + (2 + slot_c) * TR::TILE, wave, lane);
-    }
-    TR::go(row + (size_t)(hk * grp + ih) * D, ld, off[0], last, lds + (4 + slot_s) * TR::TILE, wave, lane);
-    TR::go(p.dout + (t0 + (size_t)chunk * LC) * ldo + (size_t)(hk * grp + ih) * D, ldo, off[1], last, lds + (6 + slot_s) * TR::TILE, wave, lane);
+    const size_t row = t0 + (size_t)chunk * LC;
+    if (ih == 0) TR::go(p.qkv + row * ld + column, ld, off[0], last, lds + (2 * is_dk + slot_c) * TR::TILE, wave, lane);
+    const bf16_t* x = is_dk ? p.dout + row * ldo : p.qkv + row * ld;
+    TR::go(x + (size_t)(hk * grp + ih) * D, ldx, off[1], last, lds + (4 + 2 * is_dk + slot_s) * TR::TILE, wave, lane);
     if (++ih == grp) { ih = 0; in++; }
   };
   issue();
   LinFrag<D> fa;
   fa.init(lane, wave);
-  f32x16 R[W], Rt[W];
-  const float* state = p.state ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr;
-  lin_state_load<D>(R, state, false, wave, lane);
-  lin_state_load<D>(Rt, state, true, wave, lane);
+  f32x16 R[W];
+  lin_state_load<D>(R, p.state ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr, is_dk, wave, lane);
   LinPowers<true> pw;
   pw.scores(l2, g.scale, lane);
   pw.chunk(LC, l2, 1.f, g.scale, lane);
-  f32x16 dk, dv;
-  bf16x8 kf[KS], vf[KS];
+  f32x16 out;
   int n = 0, h = 0;
   for (int s = 0; s < steps; s++) {
-    dma_wait<0>();
+    if (h == 0 && s > 0) dma_wait<2>(); else dma_wait<0>();  // the tiles stand before a chunk's two stores
     __syncthreads();
     if (s + 1 < steps) issue();
     const int chunk = c1 - 1 - n, left = min(LC, g.seq - chunk * LC);
-    const lds_char *Kt = sm + (n & 1) * TR::TILE, *Vt = sm + (2 + (n & 1)) * TR::TILE, *Qt = sm + (4 + (s & 1)) * TR::TILE, *Gt = sm + (6 + (s & 1)) * TR::TILE;
+    const lds_char *At = sm + (2 * is_dk + (n & 1)) * TR::TILE, *Xt = sm + (4 + 2 * is_dk + (s & 1)) * TR::TILE, *Yt = sm + (6 - 2 * is_dk + (s & 1)) * TR::TILE;
     if (left != pw.left) pw.chunk(left, l2, 1.f, g.scale, lane);
-    LinValues q, e;
-    q.load(Qt + fa.tr[0], Qt + fa.tr[1], D * 2);
-    e.load(Gt + fa.tr[0], Gt + fa.tr[1], D * 2);
-    constexpr int AHEAD = 4;
-    bf16x8 qd[AHEAD], ed[AHEAD];
-#pragma unroll
-    for (int ks = 0; ks < AHEAD; ks++) {
-      qd[ks] = lds_frag(Qt + fa.dir[ks], 0);
-      ed[ks] = lds_frag(Gt + fa.dir[ks], 0);
-    }
+    LinValues y;
+    y.load(Yt + fa.tr[0], Yt + fa.tr[1], D * 2);
     if (h == 0) {
+      lin_zero(out);
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) {
-        kf[ks] = lds_frag(Kt + fa.dir[ks], 0);
-        vf[ks] = lds_frag(Vt + fa.dir[ks], 0);
-      }
-      LIN_PIN();
-      lin_zero(dk);
-      lin_zero(dv);
+      for (int ks = 0; ks < KS; ks++) out = MFMA(pack_rows(R[ks >> 1], ks & 1), lds_frag(At + fa.dir[ks], 0), out);
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) {
-        dv = MFMA(pack_rows(R[ks >> 1], ks & 1), kf[ks], dv);
-        dk = MFMA(pack_rows(Rt[ks >> 1], ks & 1), vf[ks], dk);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; r++) { dk[r] *= pw.read; dv[r] *= pw.read; }
+      for (int r = 0; r < 16; r++) out[r] *= pw.read;
 #pragma unroll
       for (int dt = 0; dt < W; dt++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) { R[dt][r] *= pw.whole; Rt[dt][r] *= pw.whole; }
+        for (int r = 0; r < 16; r++) R[dt][r] *= pw.whole;
     }
-    LIN_PIN();
-    q.look(kg);
-    e.look(kg);
-    f32x16 sv, sk;
-    lin_zero(sv);
-    lin_zero(sk);
+    y.look();
+    f32x16 st;
+    lin_zero(st);
 #pragma unroll
-    for (int ks = 0; ks < KS; ks++) {
-      sv = MFMA(qd[ks % AHEAD], kf[ks], sv);
-      sk = MFMA(ed[ks % AHEAD], vf[ks], sk);
-      if (ks + AHEAD < KS) {
-        qd[ks % AHEAD] = lds_frag(Qt + fa.dir[ks + AHEAD], 0);
-        ed[ks % AHEAD] = lds_frag(Gt + fa.dir[ks + AHEAD], 0);
-      }
-      LIN_PIN();
-    }
-    LinRows<D> qr[2], er[2];
-#pragma unroll
-    for (int c = 0; c < 2; c++) {
-      qr[c].load(fa, Qt, c);
-      er[c].load(fa, Gt, c);
-    }
-    LIN_PIN();
-    lin_inside<true>(dv, sv, pw, e, lane);
-    lin_inside<true>(dk, sk, pw, q, lane);
-    lin_into<D, EXACT ? 3 : 2, true>(R, fa, Qt, qr, e.all, pw.into);
-    lin_into<D, 2, true>(Rt, fa, Gt, er, q.all, pw.into);
+    for (int ks = 0; ks < KS; ks++) st = MFMA(lds_frag(Xt + fa.dir[ks], 0), lds_frag(At + fa.dir[ks], 0), st);
+    lin_inside<true>(out, st, pw, y, lane);
+    LinRows<D> ahead[2];
+    lin_into<D, EXACT ? 3 : 2, false>(R, fa, Xt, ahead, y.all, pw.into);
     if (++h < grp) continue;
-    bf16_t* row = p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + wave * 32;
-    lin_out(dk, row + (size_t)(g.nq + hk) * D, l32 < left, lane);
-    lin_out(dv, row + (size_t)(g.nq + g.nkv + hk) * D, l32 < left, lane);
+    lin_out(out, p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + to + wave * 32, l32 < left, lane);
     h = 0;
     n++;
   }
   if constexpr (EXACT) {
-    if (p.sum) lin_state_store<D>(R, p.sum + ((size_t)b * g.nkv + hk) * D * D, wave, lane);
+    if (p.sum && !is_dk) lin_state_store<D>(R, p.sum + ((size_t)b * g.nkv + hk) * D * D, wave, lane);
   }
 }
 
@@ -473,13 +434,11 @@ __global__ __launch_bounds__(2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lin_walk<D, false, false, EXACT, OUT>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
-// The backward pass: dk and dv (grid rows y < nkv, the longer ones), then dq.  grid (pieces, 2 * nkv, batch)
+// The backward pass's dk and dv.  grid (pieces, nkv, batch)
 template <int D, bool EXACT>
-__global__ __launch_bounds__(2 * D, 1) void lin_bwd_kernel(const LinArgs a, const LinGrads k) {
+__global__ __launch_bounds__(4 * D, 2) void lin_bwd_kernel(const LinArgs a, const LinGrads k) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int nkv = a.g.nkv, y = blockIdx.y;
-  if (y < nkv) lin_walk_kv<D, EXACT>(a, k, blockIdx.x, y, blockIdx.z, smem);
-  else lin_walk<D, false, false, false, true>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
+  lin_walk_kv<D, EXACT>(a, k, blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
 // The pieces' contributions to R (y < nkv) and to S.  grid (pieces, 2 * nkv, batch)
 template <int D>
@@ -490,9 +449,9 @@ __global__ __launch_bounds__(2 * D, 2) void lin_bwd_sums_kernel(const LinArgs a)
   else lin_walk<D, false, false, true, false>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
 }
 // ------------------------------------------------------------------------------------ host side
-// Pieces of a row, none below LIN_LEAST chunks: enough that the launch has a wave for each of the chip's 1024 SIMDs (forward), or two (backward, whose two kinds of blocks are of different lengths).  Each
-// more costs its states' way to memory and back.  us, 256 and 512 blocks of D = 128: forward of 8192 tokens x 32 heads 100 and 106; training step of 2 x 4096 tokens on 32:8 heads, both
-// numbers for the backward pass, 277 and 252.
+// Pieces of a row, none below LIN_LEAST chunks: enough that the forward pass has a wave for each of the chip's 1024 SIMDs, and that dk and dv, whose blocks have twice the waves of which a unit of the chip
+// holds one block, have a block for each unit (half of LIN_BB; the other half is for dq).  More pieces cost more states' way to memory and back.  us, 256 and 512: forward of 8192 tokens x 32
+// heads 100 and 106; training step of 2 x 4096 tokens on 32:8 heads, blocks of the backward pass, 256, 384, 512, 768 and 1024: 357, 300, 264, 315 and 286.
 #define LIN_LEAST 4
 #define LIN_BF 256
 #define LIN_BB 512
@@ -558,8 +517,11 @@ static int lin_bwd(const LinGeom& g, const bf16_t* qkv, const float* state_in, c
     kv.sum = nullptr;
   }
   const size_t lds = 8 * LC * D * 2;
-  if (kv.sum) lin_bwd_kernel<D, true><<<grid, 2 * D, lds, s>>>(a, kv);
-  else lin_bwd_kernel<D, false><<<grid, 2 * D, lds, s>>>(a, kv);
+  const dim3 one(c.pieces, g.nkv, g.batch);
+  if (kv.sum) lin_bwd_kernel<D, true><<<one, 4 * D, lds, s>>>(a, kv);
+  else lin_bwd_kernel<D, false><<<one, 4 * D, lds, s>>>(a, kv);
+  DH_LAUNCH_CHECK();
+  lin_fwd_kernel<D, false, true><<<one, 2 * D, 6 * LC * D * 2, s>>>(a);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }
