@@ -722,9 +722,9 @@ size_t dh_attn_window_fwd_workspace_bytes(int dtype, int batch, int seq, int win
 int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d, const void* qkv, const void* o, const void* dout, const float* lse,
                        void* dqkv, float* delta, void* ws, size_t ws_bytes, void* stream);
 size_t dh_attn_window_bwd_workspace_bytes(int dtype, int batch, int seq, int window, int sinks, int nq, int nkv, int d);
-/* One token of each sequence: qkv[batch,(nq+2nkv)d] (rotated), at position pos[b] (DEVICE int32, 4-byte aligned; negative: the slot is not in use, its row of o and its cache are
+/* One token of each sequence: qkv[batch,(nq+2nkv)d] (rotated), at position pos[b] (DEVICE int32, 4-byte aligned, below 2^31 - 1 - sinks; negative: the slot is not in use, its row of o and its cache are
  * left as they are).  kv: device [batch, cache_rows, 2*nkv*d], rows [k heads | v heads]: the cache, which holds position p in row p while p < cache_rows, and from there on in row
- * sinks + (p - sinks) mod (cache_rows - sinks), so that cache_rows >= window + sinks rows serve rows of any length.  The call puts the token's key and value into its row and
+ * sinks + (p - sinks) mod (cache_rows - sinks), so that cache_rows >= window + sinks rows (up to 2^30) serve rows of any length.  The call puts the token's key and value into its row and
  * writes o[batch, nq*d]. */
 int dh_attn_window_step(int dtype, int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d, const int32_t* pos, const void* qkv, void* kv, void* o, void* ws,
                         size_t ws_bytes, void* stream);

@@ -39,7 +39,7 @@ int dh_launch_lin_carry(const LinGeom& g, int pieces, int tokens, const LinCarry
 
 // ------------------------------------------------------------------------------------ single tokens
 // Bound by memory: each element of a state is read and written once, 16 bytes a lane.  A block has a state (nkv, batch): d / 4 lanes side by side cover its rows, the row
-// groups take every GROUPS-th row each, and their shares of o meet in LDS, in order.
+// groups take every GROUPS-th row each, and their shares of o meet in LDS, in order.  128 sequences on 32:32 heads of 128, bf16: 99 us, 5.5 TB/s.
 #define LS_THREADS 256
 template <typename T>
 __global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, const int32_t* __restrict__ pos, const T* __restrict__ qkv, const float* state_in, float* state_out,

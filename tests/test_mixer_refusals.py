@@ -62,6 +62,7 @@ def test_window_step():
     refused(INVALID, dh.dh_attn_window_step, *s, *[A] * 4, A + 8, BIG)
     for rows, window, sinks in ((11, 10, 2), (0, 1, 0), (-4, 1, 0), (2 ** 31 - 1, 2 ** 31 - 1, 1)):
         refused(SHAPE, dh.dh_attn_window_step, dh.DH_BF16, 2, rows, window, sinks, 4, 2, 128, A, A, A, A, A, BIG)
+    refused(SHAPE, dh.dh_attn_window_step, dh.DH_BF16, 2, 2 ** 30 + 1, 1024, 4, 4, 2, 128, A, A, A, A, A, BIG)
     need = dh.dh_attn_window_step_workspace_bytes(dh.DH_BF16, 1, 8192, 4096, 4, 4, 1, 128)
     assert need > 0
     refused(SMALL, dh.dh_attn_window_step, dh.DH_BF16, 1, 8192, 4096, 4, 4, 1, 128, A, A, A, A, A, need - 1)
