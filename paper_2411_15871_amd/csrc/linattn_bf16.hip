@@ -262,7 +262,8 @@ struct LinTransfer {
 };
 
 // The pass in its first form, a state for the group and a query row for each of its heads (o, dq); or, with !OUT, sums for the states alone: GROUPED and REV: of R, over the group's heads, from
-// the row's end.  LDS: two slots each of Q, K, V tiles.  (A third, with transfers two steps ahead, brings nothing: 131 -> 133 us for 8192 tokens x 32 heads.)
+// the row's end.  LDS: two slots each of Q, K, V tiles.  (More of them, with transfers further ahead, bring
+// nothing: results of 8192 tokens x 32 heads 131 -> 133 us, sums with three steps ahead 1 %.)
 template <int D, bool GROUPED, bool REV, bool EXACT, bool OUT>
 __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int piece, int hk, int b, char* smem) {
   static_assert(!(GROUPED && OUT), "lin_walk_kv");
