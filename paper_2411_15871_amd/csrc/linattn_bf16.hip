@@ -450,15 +450,19 @@ __global__ __launch_bounds__(2 * D, 2) void lin_bwd_sums_kernel(const LinArgs a)
   else lin_walk<D, false, false, true, false>(a, a.pass[0], blockIdx.x, y - nkv, blockIdx.z, smem);
 }
 // ------------------------------------------------------------------------------------ host side
-// Pieces of a row, none below LIN_LEAST chunks: enough that the forward pass has a wave for each of the chip's 1024 SIMDs, and that dk and dv, whose blocks have twice the waves of which a unit of the chip
-// holds one block, have a block for each unit (half of LIN_BB; the other half is for dq).  More pieces cost more states' way to memory and back.  us, 256 and 512: forward of 8192 tokens x 32
-// heads 100 and 106; training step of 2 x 4096 tokens on 32:8 heads, blocks of the backward pass, 256, 384, 512, 768 and 1024: 357, 300, 264, 315 and 286.
-#define LIN_LEAST 4
+// Pieces of a row: enough that the forward pass has a wave for each of the chip's 1024 SIMDs, and that dk and dv, whose blocks have twice the waves of which a unit of the chip holds one block, have a
+// block for each unit (half of LIN_BB; the other half is for dq).  More pieces cost more states' way to memory and back.  us, 256 and 512: forward of 8192 tokens x 32 heads 100 and 106;
+// training step of 2 x 4096 tokens on 32:8 heads, blocks of the backward pass, 256, 384, 512, 768 and 1024: 357, 300, 264, 315 and 286.
+// Where rows are short for that, a piece holds two steps (a chunk of one head) at least: us, forward and backward, pieces from 1, 2 and 4 chunks on: 3092 tokens of 2:1 heads 26 and 48, 25 and 56, 31 and 70;
+// 256 tokens of 8:2 17 and 41, 23 and 56, 33 and 86; 3 x 1999 of 8:8 heads of 64 26 and 43, 25 and 43, 27 and 48.  Rows of up to eight steps stay whole, without the launches of sums and carry:
+// 192 tokens of 8:8 heads 13.4 and 31.8 whole, 15.5 and 34.5 cut; 256 17.1 and 40.3, and 17.1 and 37.5; 64 of 8:2 13.1 and 31.7, and 16.3 and 39.3; 96 18.3 and 44.2, and 16.4 and 39.6.
+#define LIN_WHOLE 8
 #define LIN_BF 256
 #define LIN_BB 512
 static LinCut lin_cut(const LinGeom& g, bool bwd) {
-  const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 2 : 1);
-  const long long want = std::max(1ll, std::min(((bwd ? LIN_BB : LIN_BF) * (128 / g.d) + blocks - 1) / blocks, chunks / LIN_LEAST));
+  const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 2 : 1), grp = g.nq / g.nkv;
+  if (chunks * grp <= LIN_WHOLE) return {1, (int)chunks};
+  const long long want = std::max(1ll, std::min(((bwd ? LIN_BB : LIN_BF) * (128 / g.d) + blocks - 1) / blocks, grp > 1 ? chunks : chunks / 2));
   const int per = (int)((chunks + want - 1) / want);
   return {(int)((chunks + per - 1) / per), per};
 }

@@ -199,10 +199,13 @@ __global__ __launch_bounds__(2 * D) void lin32_bwd_kernel(const Lin32Args a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
-// Pieces: where the blocks leave units of the chip idle, none below 4 chunks.
+// Pieces: two blocks of the forward pass for each unit of the chip, or one of each of the backward pass's three kinds, down to single chunks.  us, forward and backward, at this and at half of it: 2 x 2048
+// tokens of 8:8 heads of 128 82 and 180, 73 and 202; 4 x 512 of 8:8 heads of 64 27 and 57, 29 and 50; 8192 of 4:4 42 and 82, 47 and 82.  Rows of up to three steps (a chunk of one head) stay whole, without the
+// launches of sums and carry: 64 tokens of 4:4 14 and 14 whole, 17 and 21 cut; 96 19 and 20, 17 and 21; 128 25 and 25, 18 and 21.
 static LinCut lin32_cut(const LinGeom& g, bool bwd) {
   const long long chunks = (g.seq + LC - 1) / LC, blocks = (long long)g.batch * g.nkv * (bwd ? 3 : 1);
-  const long long want = std::max(1ll, std::min((512 + blocks - 1) / blocks, chunks / 4));
+  if (chunks * (g.nq / g.nkv) <= 3) return {1, (int)chunks};
+  const long long want = std::max(1ll, std::min(((bwd ? 768 : 512) + blocks - 1) / blocks, chunks));
   const int per = (int)((chunks + want - 1) / want);
   return {(int)((chunks + per - 1) / per), per};
 }
