@@ -77,6 +77,15 @@ def test_head_layouts(dh, tt, nq, nkv, d):
     c.check()
 
 
+@pytest.mark.parametrize("tt,batch,nq,nkv,d", [(BF, 1, 128, 128, 64), (BF, 1, 128, 64, 128), (BF, 2, 96, 96, 128), (BF, 5, 128, 128, 64), (F, 1, 96, 96, 32), (F, 2, 64, 32, 64)])
+def test_many_heads(dh, tt, batch, nq, nkv, d):
+    """Enough heads to fill the chip: pieces of many chunks, rows that stay whole."""
+    c = Case(dh, tt, batch, 427, nq, nkv, d).upload()
+    c.forward()
+    c.backward()
+    c.check()
+
+
 @pytest.mark.parametrize("tt", [BF, F])
 @pytest.mark.parametrize("decay", [0.0, -1e-6, -0.01, -1.0, -30.0, -200.0, -math.inf])
 def test_decays(dh, tt, decay):
