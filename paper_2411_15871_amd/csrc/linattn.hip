@@ -38,54 +38,74 @@ int dh_launch_lin_carry(const LinGeom& g, int pieces, int tokens, const LinCarry
 }
 
 // ------------------------------------------------------------------------------------ single tokens
-// Bound by memory: each element of a state is read and written once, 16 bytes a lane.  A block has a state (nkv, batch): d / 4 lanes side by side cover its rows, the row
-// groups take every GROUPS-th row each, and their shares of o meet in LDS, in order.  128 sequences on 32:32 heads of 128, bf16: 99 us, 5.5 TB/s.
+// Bound by memory: each element of a state is read and written once, 16 bytes a lane, LS_ROWS of them in flight, for up to GH query heads of its group (further ones read what the thread has stored).  A
+// block has `cols` columns of a state: cols / 4 lanes side by side cover its rows, the row groups take every groups-th row each, and their shares of o meet in LDS, in order.
+// Where blocks are few a state's columns are shared out over several (LS_BLOCKS).  bf16, heads of 128, us, whole states a block and shared: one sequence on 32:8 7.3 and 5.3, 16 9.4 and 7.6; 128 on
+// 32:32 106 (97 on another card, 5.5 TB/s) either way.  (With a head of the group after the other over the state 16.7 for one sequence, 37 instead of 19 for 64 on 32:8.)
 #define LS_THREADS 256
-template <typename T>
-__global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, const int32_t* __restrict__ pos, const T* __restrict__ qkv, const float* state_in, float* state_out,
+#define LS_ROWS 4
+#define LS_BLOCKS 1024
+template <typename T, int GH>
+__global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, int cols, const int32_t* __restrict__ pos, const T* __restrict__ qkv, const float* state_in, float* state_out,
                                                               T* __restrict__ o) {
-  extern __shared__ float sm[];  // [groups][d]
-  const int hk = blockIdx.x, b = blockIdx.y, d = g.d, grp = g.nq / g.nkv, per = d / 4, groups = LS_THREADS / per, r = threadIdx.x / per, c = threadIdx.x % per * 4;
+  extern __shared__ float sm[];  // k[d], q[GH][d], shares of o [groups][GH][cols]
+  const int hk = blockIdx.y, b = blockIdx.z, d = g.d, grp = g.nq / g.nkv, per = cols / 4, groups = LS_THREADS / per, r = threadIdx.x / per, cl = threadIdx.x % per * 4, c = blockIdx.x * cols + cl;
   const int p = pos ? pos[b] : 1;
   if (p < 0) return;
+  float *ks = sm, *qs = ks + d, *red = qs + GH * d;
   const float lam = expf(g.log_decay[hk]);
   const T* token = qkv + (size_t)b * (g.nq + 2 * g.nkv) * d;
   const T *k = token + (size_t)(g.nq + hk) * d, *v = k + (size_t)g.nkv * d;
-  const size_t st = ((size_t)b * g.nkv + hk) * d * d;
+  const size_t st = ((size_t)b * g.nkv + hk) * d * d + c;
   const bool on = r < groups;
   f32x4 v4 = {0.f, 0.f, 0.f, 0.f};
   if (on)
 #pragma unroll
     for (int e = 0; e < 4; e++) v4[e] = to_f32(v[c + e]);
-  for (int h = hk * grp; h < (hk + 1) * grp; h++) {
-    const T* q = token + (size_t)h * d;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int e = threadIdx.x; e < d; e += LS_THREADS) ks[e] = to_f32(k[e]);
+  for (int h0 = 0; h0 < grp; h0 += GH) {
+    const T* q = token + (size_t)(hk * grp + h0) * d;
+    const int heads = min(GH, grp - h0);
+    for (int e = threadIdx.x; e < GH * d; e += LS_THREADS) qs[e] = e < heads * d ? to_f32(q[e]) : 0.f;
+    __syncthreads();
+    f32x4 acc[GH];
+#pragma unroll
+    for (int h = 0; h < GH; h++) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (on) {
-      for (int x = r; x < d; x += groups) {
-        f32x4* out = reinterpret_cast<f32x4*>(state_out + st + (size_t)x * d + c);
-        f32x4 S;
-        if (h == hk * grp) {
-          S = p == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4*>(state_in + st + (size_t)x * d + c);
-          const float kx = to_f32(k[x]);
+      const float* from = h0 == 0 ? state_in : state_out;
+      for (int x0 = r; x0 < d; x0 += groups * LS_ROWS) {
+        f32x4 S[LS_ROWS];
 #pragma unroll
-          for (int e = 0; e < 4; e++) S[e] = fmaf(kx, v4[e], lam * S[e]);
-          *out = S;
-        } else {
-          S = *out;  // what this thread has stored
+        for (int u = 0; u < LS_ROWS; u++) {
+          const int x = x0 + u * groups;
+          S[u] = x < d && (h0 > 0 || p != 0) ? *reinterpret_cast<const f32x4*>(from + st + (size_t)x * d) : f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const float qx = to_f32(q[x]);
 #pragma unroll
-        for (int e = 0; e < 4; e++) acc[e] = fmaf(qx, S[e], acc[e]);
+        for (int u = 0; u < LS_ROWS; u++) {
+          const int x = x0 + u * groups;
+          if (x >= d) break;
+          if (h0 == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) S[u][e] = fmaf(ks[x], v4[e], lam * S[u][e]);
+            *reinterpret_cast<f32x4*>(state_out + st + (size_t)x * d) = S[u];
+          }
+#pragma unroll
+          for (int h = 0; h < GH; h++) {
+            const float qx = qs[h * d + x];
+#pragma unroll
+            for (int e = 0; e < 4; e++) acc[h][e] = fmaf(qx, S[u][e], acc[h][e]);
+          }
+        }
       }
-      *reinterpret_cast<f32x4*>(sm + r * d + c) = acc;
+#pragma unroll
+      for (int h = 0; h < GH; h++) *reinterpret_cast<f32x4*>(red + (r * GH + h) * cols + cl) = acc[h];
     }
     __syncthreads();
-    if ((int)threadIdx.x < d) {
+    for (int e = threadIdx.x; e < heads * cols; e += LS_THREADS) {
       float s = 0.f;
-      for (int w = 0; w < groups; w++) s += sm[w * d + threadIdx.x];
-      o[((size_t)b * g.nq + h) * d + threadIdx.x] = from_f32<T>(s * g.scale);
+      for (int w = 0; w < groups; w++) s += red[w * GH * cols + e];
+      o[((size_t)b * g.nq + hk * grp + h0 + e / cols) * d + blockIdx.x * cols + e % cols] = from_f32<T>(s * g.scale);
     }
-    __syncthreads();
   }
 }
 
@@ -136,6 +156,21 @@ extern "C" int dh_linattn_bwd(int dtype, int batch, int seq, int nq, int nkv, in
   if (dtype == DH_BF16) return dh_launch_linattn_bwd_bf16(g, (const bf16_t*)qkv, state_in, (const bf16_t*)dout, dstate_out, (bf16_t*)dqkv, dstate_in, ws, s);
   return dh_launch_linattn_bwd_f32(g, (const float*)qkv, state_in, (const float*)dout, dstate_out, (float*)dqkv, dstate_in, ws, s);
 }
+template <typename T, int GH>
+static void lin_step_launch(const LinGeom& g, const int32_t* pos, const T* qkv, const float* state_in, float* state_out, T* o, hipStream_t s) {
+  int cols = g.d;
+  while ((long long)g.batch * g.nkv * (g.d / cols) < LS_BLOCKS && cols % 8 == 0 && cols >= 64) cols /= 2;
+  const size_t lds = (size_t)((1 + GH) * g.d + LS_THREADS / (cols / 4) * GH * cols) * sizeof(float);
+  lin_step_kernel<T, GH><<<dim3(g.d / cols, g.nkv, g.batch), LS_THREADS, lds, s>>>(g, cols, pos, qkv, state_in, state_out, o);
+}
+template <typename T>
+static void lin_step(const LinGeom& g, const int32_t* pos, const T* qkv, const float* state_in, float* state_out, T* o, hipStream_t s) {
+  const int grp = g.nq / g.nkv;
+  if (grp > 4) lin_step_launch<T, 8>(g, pos, qkv, state_in, state_out, o, s);
+  else if (grp > 2) lin_step_launch<T, 4>(g, pos, qkv, state_in, state_out, o, s);
+  else if (grp > 1) lin_step_launch<T, 2>(g, pos, qkv, state_in, state_out, o, s);
+  else lin_step_launch<T, 1>(g, pos, qkv, state_in, state_out, o, s);
+}
 extern "C" int dh_linattn_step(int dtype, int batch, int nq, int nkv, int d, float scale, const float* log_decay, const int32_t* pos, const void* qkv, const float* state_in,
                                float* state_out, void* o, void* stream) {
   if (int rc = mix_check("linattn_step", dtype, batch, 1, nq, nkv, d)) return rc;
@@ -147,9 +182,8 @@ extern "C" int dh_linattn_step(int dtype, int batch, int nq, int nkv, int d, flo
     DH_FAIL(DH_ERR_INVALID_ARG, "linattn_step: state_out overlaps state_in other than as a whole");
   const LinGeom g = {batch, 1, nq, nkv, d, scale, log_decay};
   hipStream_t s = (hipStream_t)stream;
-  const size_t lds = (size_t)(LS_THREADS / (d / 4)) * d * sizeof(float);
-  if (dtype == DH_BF16) lin_step_kernel<bf16_t><<<dim3(nkv, batch), LS_THREADS, lds, s>>>(g, pos, (const bf16_t*)qkv, state_in, state_out, (bf16_t*)o);
-  else lin_step_kernel<float><<<dim3(nkv, batch), LS_THREADS, lds, s>>>(g, pos, (const float*)qkv, state_in, state_out, (float*)o);
+  if (dtype == DH_BF16) lin_step<bf16_t>(g, pos, (const bf16_t*)qkv, state_in, state_out, (bf16_t*)o, s);
+  else lin_step<float>(g, pos, (const float*)qkv, state_in, state_out, (float*)o, s);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }

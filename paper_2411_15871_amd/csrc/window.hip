@@ -163,17 +163,22 @@ __global__ __launch_bounds__(WS_THREADS) void window_step_kernel(const WindowSte
 // grid (nq, batch), d threads
 template <typename T>
 __global__ void window_step_merge_kernel(const WindowStep a, const int32_t* __restrict__ pos, const float* __restrict__ part, T* __restrict__ o) {
-  const int b = blockIdx.y, h = blockIdx.x, d = a.g.d, c = threadIdx.x;
+  extern __shared__ float sm[];  // reference maximum of each block's share, then their sums
+  const int b = blockIdx.y, h = blockIdx.x, d = a.g.d, c = threadIdx.x, n = a.splits;
   if (pos[b] < 0) return;
-  const float* of = part + ((size_t)b * a.g.nq + h) * a.splits * (d + 2);
+  const float* of = part + ((size_t)b * a.g.nq + h) * n * (d + 2);
+  for (int s = c; s < n; s += d) {
+    sm[s] = of[(size_t)s * (d + 2)];
+    sm[n + s] = of[(size_t)s * (d + 2) + 1];
+  }
+  __syncthreads();
   float M = -3.0e38f, L = 0.f, A = 0.f;
-  for (int s = 0; s < a.splits; s++) M = __builtin_elementwise_maximum(M, of[(size_t)s * (d + 2)]);
-  for (int s = 0; s < a.splits; s++) {
-    const float* at = of + (size_t)s * (d + 2);
-    if (at[1] == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(at[0] - M);
-    L = fmaf(f, at[1], L);
-    A = fmaf(f, at[2 + c], A);
+  for (int s = 0; s < n; s++) M = __builtin_elementwise_maximum(M, sm[s]);
+#pragma unroll 8
+  for (int s = 0; s < n; s++) {
+    const float l = sm[n + s], x = of[(size_t)s * (d + 2) + 2 + c], f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(sm[s] - M);
+    L = fmaf(f, l, L);
+    A = l == 0.f ? A : fmaf(f, x, A);
   }
   o[((size_t)b * a.g.nq + h) * d + c] = from_f32<T>(A / L);
 }
@@ -251,7 +256,7 @@ static int window_step_launch(const WindowStep& a, const int32_t* pos, const T* 
   window_step_kernel<T, LANES, GH><<<dim3((unsigned)a.splits * ((grp + GH - 1) / GH), a.g.nkv, a.g.batch), WS_THREADS, lds, s>>>(a, pos, qkv, kv, o, part);
   DH_LAUNCH_CHECK();
   if (a.splits > 1) {
-    window_step_merge_kernel<T><<<dim3(a.g.nq, a.g.batch), a.g.d, 0, s>>>(a, pos, part, o);
+    window_step_merge_kernel<T><<<dim3(a.g.nq, a.g.batch), a.g.d, 2 * a.splits * sizeof(float), s>>>(a, pos, part, o);
     DH_LAUNCH_CHECK();
   }
   return DH_OK;
