@@ -228,11 +228,13 @@ extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int
 
 // Query heads that a block takes at once: up to 8; a group of more is shared out evenly over blocks, which read the cache again.
 static int step_heads(int grp) { return grp > 4 ? 8 : grp > 2 ? 4 : grp; }
-// Blocks that share a sequence's keys: none holds fewer than 128, and there are no more blocks than the chip takes at a time by far.
+// Blocks that share a sequence's keys: none holds fewer than 128, and there are no more than give each unit of the chip one.  us, 256, 512 and 1024 blocks, bf16, heads of 128: one sequence on 32:8, window
+// 4096, 15.9, 17.8 and 17.7; 4 23.9, 25.1 and 32.1; 32 107, 117 and 132; 64 200, 201 and 226; 16 with window 1024 23.1, 24.2 and 29.7; 48 on 16:2 39, 44 and 44.
+#define WS_BLOCKS 256
 static WindowStep window_step_of(int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d) {
   WindowStep a = {window_geom(batch, cache_rows, window, sinks, nq, nkv, d), 0, 1};
   const long long most = std::min((long long)window + sinks, (long long)cache_rows), grp = nq / nkv, blocks = (long long)batch * nkv * ((grp + step_heads(grp) - 1) / step_heads(grp));
-  a.splits = (int)std::max(1ll, std::min({(most + 127) / 128, (1024 + blocks - 1) / blocks, 256ll}));
+  a.splits = (int)std::max(1ll, std::min({(most + 127) / 128, (WS_BLOCKS + blocks - 1) / blocks, 256ll}));
   a.chunk = (int)((most + a.splits - 1) / a.splits);
   return a;
 }
