@@ -4,8 +4,8 @@
 
 // ------------------------------------------------------------------------------------ single tokens
 // Bound by memory: each visible row of the cache is read once.  LANES lanes read a row of a head, 8 elements each, so that a wave has 64 / LANES rows in flight a load; each such
-// group keeps a reference maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.  64 sequences on 32:8 heads of 128, window 4096, of mixed lengths, bf16: 145 to 160 us, 5.6 to 6.1 TB/s (264 with
-// sums across lanes through LDS, a maximum that follows every row and no rows fetched ahead).
+// group keeps a reference maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.  64 sequences of mixed lengths on 32:8 heads of 128,
+// window 4096, bf16: 145 to 160 us, 5.6 to 6.1 TB/s (264 with sums across lanes through LDS, a maximum that follows every row and no rows fetched ahead).
 struct WindowStep {
   WindowGeom g;  // seq: rows of the cache
   int chunk;     // keys of a block

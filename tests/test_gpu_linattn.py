@@ -214,7 +214,7 @@ def test_no_tokens(dh):
 
 
 # ------------------------------------------------------------------------------------ single tokens
-@pytest.mark.parametrize("tt,nq,nkv,d", [(BF, 4, 1, 128), (BF, 8, 8, 64), (F, 4, 2, 64), (F, 3, 1, 40), (F, 2, 2, 8), (BF, 16, 2, 64), (F, 2, 2, 128)])
+@pytest.mark.parametrize("tt,nq,nkv,d", [(BF, 4, 1, 128), (BF, 8, 8, 64), (F, 4, 2, 64), (F, 3, 1, 40), (F, 2, 2, 8), (BF, 16, 2, 64), (F, 2, 2, 128), (F, 3, 3, 72), (F, 10, 1, 104), (BF, 20, 1, 128)])
 @pytest.mark.parametrize("in_place", [True, False])
 def test_single_tokens(dh, tt, nq, nkv, d, in_place):
     pos = [5, -1, 0, 17]
