@@ -16,7 +16,6 @@
 //
 // Bound by memory: q, k, v, o once, k and v again for the pieces' states.
 #include <algorithm>
-#include <type_traits>
 #include "attn_tiles.h"
 #include "dma.h"
 #include "linattn.h"
@@ -261,18 +260,18 @@ struct LinTransfer {
   }
 };
 
-// The pass in its first form, a state for the group and a query row for each of its heads (o, dq); or, with !OUT, sums for the states alone: GROUPED and REV: of R, over the group's heads, from
-// the row's end.  LDS: two slots each of Q, K, V tiles.  (More of them, with transfers further ahead, bring
+// The pass in its first form, a state for the group and a query row for each of its heads (o, dq), which TEAMS of D / 32 waves share out; or, with !OUT, sums for the states alone: GROUPED and REV: of R, over the group's heads, from
+// the row's end.  LDS: two slots each of each team's Q tiles and of K and V tiles.  (More of them, with transfers further ahead, bring
 // nothing: results of 8192 tokens x 32 heads 131 -> 133 us, sums with three steps ahead 1 %.)
-template <int D, bool GROUPED, bool REV, bool EXACT, bool OUT>
+template <int D, bool GROUPED, bool REV, bool EXACT, bool OUT, int TEAMS = 1>
 __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int piece, int hk, int b, char* smem) {
-  static_assert(!(GROUPED && OUT), "lin_walk_kv");
+  static_assert(!(GROUPED && OUT) && (OUT || TEAMS == 1), "lin_walk_kv; a team a head");
   using TR = LinTransfer<D>;
   constexpr int W = D / 32, KS = D / 16;
   const lds_char* sm = (const lds_char*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, kg = lane >> 5;
+  const int lane = threadIdx.x & 63, both = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = TEAMS > 1 ? both / W : 0, wave = both - team * W, l32 = lane & 31;
   const LinGeom& g = a.g;
-  const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), heads = GROUPED || OUT ? grp : 1;
+  const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), heads = GROUPED ? grp : OUT ? (grp + TEAMS - 1) / TEAMS : 1;
   const size_t t0 = (size_t)b * g.seq;
   const float l2 = g.log_decay[hk] * LOG2E, f_in = GROUPED ? g.scale : 1.f;
   const uint32_t lds = lds_address(smem);
@@ -283,14 +282,15 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   TR::offsets(off[1], OUT ? p.ldk : p.ldv, LC - 1, wave, lane);
   const int steps = (c1 - c0) * heads;
   auto chunk_of = [&](int n) { return REV ? c1 - 1 - n : c0 + n; };
+  constexpr int KT = 2 * TEAMS;  // tiles of LDS before K's
   int in = 0, ih = 0;  // of the step to transfer next
   auto issue = [&]() {
     const int chunk = chunk_of(in), slot_s = (in * heads + ih) & 1, slot_k = GROUPED ? slot_s : in & 1, last = min(LC, g.seq - chunk * LC) - 1, hkv = GROUPED ? hk * grp + ih : hk;
     const size_t row = t0 + (size_t)chunk * LC;
-    if (OUT) TR::go(p.q + row * p.ldq + (size_t)(hk * grp + ih) * D, p.ldq, off[0], last, lds + slot_s * TR::TILE, wave, lane);
+    if (OUT) TR::go(p.q + row * p.ldq + (size_t)(hk * grp + min(team * heads + ih, grp - 1)) * D, p.ldq, off[0], last, lds + (team * 2 + slot_s) * TR::TILE, wave, lane);
     if (GROUPED || ih == 0) {
-      TR::go(p.k + row * p.ldk + (size_t)hkv * D, p.ldk, off[OUT ? 1 : 0], last, lds + (2 + slot_k) * TR::TILE, wave, lane);
-      TR::go(p.v + row * p.ldv + (size_t)hkv * D, p.ldv, off[1], last, lds + (4 + slot_k) * TR::TILE, wave, lane);
+      if (TEAMS == 1 || team == 0) TR::go(p.k + row * p.ldk + (size_t)hkv * D, p.ldk, off[OUT ? 1 : 0], last, lds + (KT + slot_k) * TR::TILE, wave, lane);
+      if (TEAMS == 1 || team == 1) TR::go(p.v + row * p.ldv + (size_t)hkv * D, p.ldv, off[1], last, lds + (KT + 2 + slot_k) * TR::TILE, wave, lane);
     }
     if (++ih == heads) { ih = 0; in++; }
   };
@@ -310,7 +310,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     __syncthreads();  // and every wave is done with the step before, whose slots the next one takes
     if (s + 1 < steps) issue();
     const int chunk = chunk_of(n), left = min(LC, g.seq - chunk * LC), slot_s = s & 1, slot_k = GROUPED ? slot_s : n & 1;
-    const lds_char *Qt = sm + slot_s * TR::TILE, *Kt = sm + (2 + slot_k) * TR::TILE, *Vt = sm + (4 + slot_k) * TR::TILE;
+    const lds_char *Qt = sm + (team * 2 + slot_s) * TR::TILE, *Kt = sm + (KT + slot_k) * TR::TILE, *Vt = sm + (KT + 2 + slot_k) * TR::TILE;
     if (left != pw.left) pw.chunk(left, l2, g.scale, f_in, lane);
     LinValues v;
     LinRows<D> ahead[2];
@@ -331,7 +331,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) st = MFMA(lds_frag(Kt + fa.dir[ks], 0), qf[ks], st);
       lin_inside<REV>(ot, st, pw, v, lane);
-      lin_out(ot, p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(hk * grp + h) * D + wave * 32, l32 < left, lane);
+      lin_out(ot, p.out + (t0 + (size_t)chunk * LC + l32) * p.ldo + (size_t)(hk * grp + min(team * heads + h, grp - 1)) * D + wave * 32, l32 < left, lane);
     } else {
       ahead[0].load(fa, Kt, 0);
       ahead[1].load(fa, Kt, 1);
@@ -349,7 +349,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
     if (++h == heads) { h = 0; n++; }
   }
   if constexpr (EXACT) {
-    if (p.sum) lin_state_store<D>(S, p.sum + (OUT ? (size_t)b * g.nkv + hk : ((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D, wave, lane);
+    if (p.sum && team == 0) lin_state_store<D>(S, p.sum + (OUT ? (size_t)b * g.nkv + hk : ((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D, wave, lane);
   }
 }
 
@@ -362,7 +362,7 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
   using TR = LinTransfer<D>;
   constexpr int W = D / 32, KS = D / 16;
   const lds_char* sm = (const lds_char*)smem;
-  const int lane = threadIdx.x & 63, both = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), is_dk = both >= W, wave = both - is_dk * W, l32 = lane & 31, kg = lane >> 5;
+  const int lane = threadIdx.x & 63, both = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), is_dk = both >= W, wave = both - is_dk * W, l32 = lane & 31;
   const LinGeom& g = a.g;
   const int grp = g.nq / g.nkv, chunks = (g.seq + LC - 1) / LC, c0 = piece * a.per, c1 = min(chunks, c0 + a.per), ld = (g.nq + 2 * g.nkv) * D, ldo = g.nq * D, ldx = is_dk ? ldo : ld;
   const size_t t0 = (size_t)b * g.seq;
@@ -430,10 +430,10 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
 }
 
 // The forward pass: OUT its results, otherwise the pieces' contributions to the states.  grid (pieces, nkv, batch)
-template <int D, bool EXACT, bool OUT>
-__global__ __launch_bounds__(2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
+template <int D, bool EXACT, bool OUT, int TEAMS>
+__global__ __launch_bounds__(TEAMS * 2 * D, 2) void lin_fwd_kernel(const LinArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  lin_walk<D, false, false, EXACT, OUT>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
+  lin_walk<D, false, false, EXACT, OUT, TEAMS>(a, a.pass[0], blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
 // The backward pass's dk and dv.  grid (pieces, nkv, batch)
 template <int D, bool EXACT>
@@ -471,29 +471,32 @@ size_t dh_linattn_bf16_ws_bytes(const LinGeom& g, bool bwd) {
   const LinCut c = lin_cut(g, bwd);
   return c.pieces == 1 ? 0 : (bwd ? 2 : 1) * lin_states(g, c.pieces) * sizeof(float);
 }
+// The forward pass's results.  From four heads of a group on two teams of waves share them and the tiles of keys and values, each with the state: us, one team and two, 2 x 4096 tokens of 32:8 heads 74.5 and
+// 67.5, 64 of 8:2 13.2 and 10.9, 4 x 2048 of 32:8 heads of 64 38.7 and 32.4; but 8192 of 24:8 62.7 and 67.2, 3092 of 2:1 26.2 and 27.1, and dq, whose rows come from further away, gains nothing.
+template <int D, bool EXACT>
+static int lin_results(const LinArgs& a, hipStream_t s) {
+  const dim3 grid(a.pieces, a.g.nkv, a.g.batch);
+  if (a.g.nq / a.g.nkv >= 4) lin_fwd_kernel<D, EXACT, true, 2><<<grid, 4 * D, 8 * LC * D * 2, s>>>(a);
+  else lin_fwd_kernel<D, EXACT, true, 1><<<grid, 2 * D, 6 * LC * D * 2, s>>>(a);
+  DH_LAUNCH_CHECK();
+  return DH_OK;
+}
 template <int D>
 static int lin_fwd(const LinGeom& g, const bf16_t* qkv, const float* state_in, bf16_t* o, float* state_out, float* ws, hipStream_t s) {
   const int ld = (g.nq + 2 * g.nkv) * D;
   const LinCut c = lin_cut(g, false);
   LinArgs a = {g, c.pieces, c.per, {}};
   a.pass[0] = {qkv, qkv + (size_t)g.nq * D, qkv + (size_t)(g.nq + g.nkv) * D, o, ld, ld, ld, g.nq * D, state_in, state_out, 0};
-  const dim3 grid(c.pieces, g.nkv, g.batch);
-  const size_t lds = 6 * LC * D * 2;
   if (c.pieces > 1) {
     a.pass[0].state = nullptr;
     a.pass[0].sum = ws;
-    lin_fwd_kernel<D, true, false><<<grid, 2 * D, lds, s>>>(a);
+    lin_fwd_kernel<D, true, false, 1><<<dim3(c.pieces, g.nkv, g.batch), 2 * D, 6 * LC * D * 2, s>>>(a);
     DH_LAUNCH_CHECK();
     if (int rc = dh_launch_lin_carry(g, c.pieces, c.per * LC, {ws, state_in, state_out, 0}, nullptr, s)) return rc;
     a.pass[0].state = ws;
-  } else if (state_out) {
-    lin_fwd_kernel<D, true, true><<<grid, 2 * D, lds, s>>>(a);
-    DH_LAUNCH_CHECK();
-    return DH_OK;
+    return lin_results<D, false>(a, s);
   }
-  lin_fwd_kernel<D, false, true><<<grid, 2 * D, lds, s>>>(a);
-  DH_LAUNCH_CHECK();
-  return DH_OK;
+  return state_out ? lin_results<D, true>(a, s) : lin_results<D, false>(a, s);
 }
 int dh_launch_linattn_fwd_bf16(const LinGeom& g, const bf16_t* qkv, const float* state_in, bf16_t* o, float* state_out, void* ws, hipStream_t s) {
   return g.d == 128 ? lin_fwd<128>(g, qkv, state_in, o, state_out, (float*)ws, s) : lin_fwd<64>(g, qkv, state_in, o, state_out, (float*)ws, s);
@@ -526,7 +529,7 @@ static int lin_bwd(const LinGeom& g, const bf16_t* qkv, const float* state_in, c
   if (kv.sum) lin_bwd_kernel<D, true><<<one, 4 * D, lds, s>>>(a, kv);
   else lin_bwd_kernel<D, false><<<one, 4 * D, lds, s>>>(a, kv);
   DH_LAUNCH_CHECK();
-  lin_fwd_kernel<D, false, true><<<one, 2 * D, 6 * LC * D * 2, s>>>(a);
+  lin_fwd_kernel<D, false, true, 1><<<one, 2 * D, 6 * LC * D * 2, s>>>(a);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }

@@ -69,7 +69,7 @@ def test_both_passes(dh, tt, nq, nkv, d, batch, seq, state):
     c.check()
 
 
-@pytest.mark.parametrize("tt,nq,nkv,d", [(F, 1, 1, 8), (F, 4, 2, 128), (F, 5, 5, 24), (F, 2, 1, 32), (BF, 16, 1, 64), (BF, 8, 8, 128), (BF, 12, 4, 128)])
+@pytest.mark.parametrize("tt,nq,nkv,d", [(F, 1, 1, 8), (F, 4, 2, 128), (F, 5, 5, 24), (F, 2, 1, 32), (BF, 16, 1, 64), (BF, 8, 8, 128), (BF, 12, 4, 128), (BF, 10, 2, 128), (BF, 7, 1, 64)])
 def test_head_layouts(dh, tt, nq, nkv, d):
     c = Case(dh, tt, 2, 150, nq, nkv, d).upload()
     c.forward()
