@@ -455,6 +455,10 @@ __device__ __forceinline__ void wave_rows_out_bf16(bf16_t* reg, int lane, Quad q
     if (dst != nullptr) *reinterpret_cast<bf16x8*>(dst + ch * 8) = v;
   }
 }
+// Wave `wave`'s part of the block's LDS once the tile loop is through, 32 x D x 4 bytes: the rows it gives out pass through it, of whichever type, and behind them what it loads to make some of these
+// again.  The waves do not wait for one another between the two, so that both must begin at the same byte.
+template <typename T, int D>
+__device__ __forceinline__ T* wave_region(char* smem, int wave) { return reinterpret_cast<T*>(smem + wave * (32 * D) * sizeof(float)); }
 #define AF_TAU 8.0f  // log2 of the headroom a row's probabilities may take over its reference maximum
 #define AB_PIN() __builtin_amdgcn_sched_barrier(0)
 

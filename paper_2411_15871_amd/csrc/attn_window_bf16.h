@@ -262,7 +262,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_fwd_bf16_kernel(con
     prow = part_o + (unit * WB_BLOCK + wave * 32) * D;
     pml = part_ml + (unit * WB_BLOCK + wave * 32) * 2;
     wave_rows_out_f32<D>(
-        reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
+        wave_region<float, D>(smem, wave), lane,
         [&](int dt, int q4) { return f32x4{ot[dt][4 * q4], ot[dt][4 * q4 + 1], ot[dt][4 * q4 + 2], ot[dt][4 * q4 + 3]}; },
         [&](int r) { return r < live ? prow + (size_t)r * D : nullptr; });
     if (lane < 32 && lane < live) {
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_fwd_bf16_kernel(con
   } else {
     const float inv = 1.0f / l;
     wave_rows_out_bf16<D>(
-        reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+        wave_region<bf16_t, D>(smem, wave), lane,
         [&](int dt, int q4) { return f32x4{ot[dt][4 * q4] * inv, ot[dt][4 * q4 + 1] * inv, ot[dt][4 * q4 + 2] * inv, ot[dt][4 * q4 + 3] * inv}; },
         [&](int r) { return r < live ? orow + (size_t)r * nq * D : nullptr; });
     if (lane < 32 && lane < live) lse[head + iq] = (m + log2f(l)) * 0.6931471805599453f;
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_window_fwd_bf16_kernel(con
   if (!__any(bad)) return;
   const DocsRows k = {rows + (size_t)(nq + hk) * D, (size_t)ld, 0, docs_scalar(seq) - 1}, v = {k.base + (size_t)nkv * D, (size_t)ld, 0, k.last};
   window_again_fwd<D>(p, tiles, docs_scalar(iw), docs_scalar(f0), docs_scalar(f1), bad, k, v, rows + (size_t)iw * ld + (size_t)h * D, orow, lse + head + iw, prow, pml,
-                      smem + wave * (32 * D) * sizeof(float));
+                      wave_region<char, D>(smem, wave));
 }
 
 // Merges the parts of every block.  grid (nq, ceil(seq / 16), batch): 16 rows a block, 16 lanes a row
@@ -449,12 +449,12 @@ __device__ __forceinline__ void window_dq_block(const WindowTiled& p, int ib, in
   const bool bad = l32 < live && docs_not_finite<D / 32>(dqt) && l2 == l2 && __builtin_isfinite(dl);
   const float scale = g.scale;
   wave_rows_out_bf16<D>(
-      reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+      wave_region<bf16_t, D>(smem, wave), lane,
       [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4] * scale, dqt[dt][4 * q4 + 1] * scale, dqt[dt][4 * q4 + 2] * scale, dqt[dt][4 * q4 + 3] * scale}; },
       [&](int r) { return r < live ? out + (size_t)r * ld : nullptr; });
   if (!__any(bad)) return;
   const DocsRows k = {rows + (size_t)(nq + hk) * D, (size_t)ld, 0, docs_scalar(seq) - 1}, v = {k.base + (size_t)nkv * D, (size_t)ld, 0, k.last};
-  window_again_dq<D>(p, tiles, docs_scalar(iw), bad, l2, dl, k, v, rows + (size_t)iw * ld + (size_t)h * D, dout + ((t0 + iw) * nq + h) * D, out, smem + wave * (32 * D) * sizeof(float));
+  window_again_dq<D>(p, tiles, docs_scalar(iw), bad, l2, dl, k, v, rows + (size_t)iw * ld + (size_t)h * D, dout + ((t0 + iw) * nq + h) * D, out, wave_region<char, D>(smem, wave));
 }
 
 // ================================================================================ backward: dK, dV
@@ -592,12 +592,12 @@ __device__ __forceinline__ void window_dkv_block(const WindowTiled& p, int unit,
   const bool bad = l32 < live && (docs_not_finite<D / 32>(dkt) || docs_not_finite<D / 32>(dvt));
   bf16_t* out = dqkv + (t0 + jw) * ld + (size_t)(nq + hk) * D;
   if (k.part >= 0) {
-    float* reg = reinterpret_cast<float*>(smem) + wave * (32 * D);
+    float* reg = wave_region<float, D>(smem, wave);
     wave_rows_out_f32<D>(reg, lane, dk_quad, [&](int r) { return r < live ? prow + (size_t)r * (2 * D) : nullptr; });
     __builtin_amdgcn_wave_barrier();
     wave_rows_out_f32<D>(reg, lane, dv_quad, [&](int r) { return r < live ? prow + (size_t)r * (2 * D) + D : nullptr; });
   } else {
-    bf16_t* reg = reinterpret_cast<bf16_t*>(smem) + wave * (32 * D);
+    bf16_t* reg = wave_region<bf16_t, D>(smem, wave);
     wave_rows_out_bf16<D>(reg, lane, dk_quad, [&](int r) { return r < live ? out + (size_t)r * ld : nullptr; });
     __builtin_amdgcn_wave_barrier();
     wave_rows_out_bf16<D>(reg, lane, dv_quad, [&](int r) { return r < live ? out + (size_t)r * ld + (size_t)nkv * D : nullptr; });
@@ -612,7 +612,7 @@ __device__ __forceinline__ void window_dkv_block(const WindowTiled& p, int unit,
   docs.a.v.T = (int)T;
   docs.exp_scale = p.exp_scale;
   docs_again_dkv<D, false>(docs, see, bad, run, span, q, e, lse2 + (size_t)h0 * T + t0, delta + (size_t)h0 * T + t0, kcol + (size_t)keys * ld, ld, (size_t)nkv * D, out, prow, scale,
-                           smem + wave * (32 * D) * sizeof(float));
+                           wave_region<char, D>(smem, wave));
 }
 // Delta and lse2 of every row, as attn_bwd_prep_kernel: the numbers the dQ blocks use.  Two lanes a row of a head.
 template <int D>
