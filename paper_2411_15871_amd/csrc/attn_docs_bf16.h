@@ -386,7 +386,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
   float* lrow = lse + (size_t)h * T + iw;
   if (u.slot >= 0) {  // partial result of this unit
     wave_rows_out_f32<D>(
-        reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
+        wave_region<float, D>(smem, wave), lane,
         [&](int dt, int q4) { return f32x4{ot[dt][4 * q4], ot[dt][4 * q4 + 1], ot[dt][4 * q4 + 2], ot[dt][4 * q4 + 3]}; },
         [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * D : nullptr; });
     if (lane < 32 && (store >> lane) & 1) {
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
   } else {
     const float inv = 1.0f / l;
     wave_rows_out_bf16<D>(
-        reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+        wave_region<bf16_t, D>(smem, wave), lane,
         [&](int dt, int q4) { return f32x4{ot[dt][4 * q4] * inv, ot[dt][4 * q4 + 1] * inv, ot[dt][4 * q4 + 2] * inv, ot[dt][4 * q4 + 3] * inv}; },
         [&](int r) { return (store >> r) & 1 ? orow + (size_t)r * nq * D : nullptr; });
     if (lane < 32 && (store >> lane) & 1) lrow[l32] = (m + log2f(l)) * 0.6931471805599453f;
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(AB_THREADS, 2) void attn_docs_fwd_bf16_kernel(const
     const int first = docs_scalar(live0), last = docs_scalar(live1) - 1;
     const DocsUnit unit = {0, docs_scalar(u.f0), docs_scalar(u.f1), docs_scalar(u.slot)};
     const DocsRows k = {kcol, (size_t)ld, first, last}, v = {kcol + (size_t)nkv * D, (size_t)ld, first, last};
-    docs_again_fwd<D, CAP>(p, see, bad, unit, k, v, qkv + (size_t)iw * ld + (size_t)h * D, ld, orow, (size_t)nq * D, lrow, prow, pml, smem + wave * (32 * D) * sizeof(float));
+    docs_again_fwd<D, CAP>(p, see, bad, unit, k, v, qkv + (size_t)iw * ld + (size_t)h * D, ld, orow, (size_t)nq * D, lrow, prow, pml, wave_region<char, D>(smem, wave));
   }
 }
 
@@ -608,12 +608,12 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
   const float scale = CAP ? 4.f * p.a.scale : p.a.scale;
   if (u.slot >= 0) {
     wave_rows_out_f32<D>(
-        reinterpret_cast<float*>(smem) + wave * (32 * D), lane,
+        wave_region<float, D>(smem, wave), lane,
         [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4], dqt[dt][4 * q4 + 1], dqt[dt][4 * q4 + 2], dqt[dt][4 * q4 + 3]}; },
         [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * D : nullptr; });
   } else {
     wave_rows_out_bf16<D>(
-        reinterpret_cast<bf16_t*>(smem) + wave * (32 * D), lane,
+        wave_region<bf16_t, D>(smem, wave), lane,
         [&](int dt, int q4) { return f32x4{dqt[dt][4 * q4] * scale, dqt[dt][4 * q4 + 1] * scale, dqt[dt][4 * q4 + 2] * scale, dqt[dt][4 * q4 + 3] * scale}; },
         [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld : nullptr; });
   }
@@ -622,7 +622,7 @@ __device__ __forceinline__ void docs_dq_block(const DocsTiled& p, int id, int h,
     const DocsUnit unit = {0, docs_scalar(u.f0), docs_scalar(u.f1), docs_scalar(u.slot)};
     const DocsRows k = {kcol, (size_t)ld, first, last}, v = {kcol + (size_t)nkv * D, (size_t)ld, first, last};
     docs_again_dq<D, CAP>(p, see, bad, l2, dl, unit, k, v, qkv + (size_t)iw * ld + (size_t)h * D, ld, dout + ((size_t)iw * nq + h) * D, (size_t)nq * D, out, prow, scale,
-                          smem + wave * (32 * D) * sizeof(float));
+                          wave_region<char, D>(smem, wave));
   }
 }
 
@@ -861,12 +861,12 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
   float* prow = part + (((size_t)u.slot * nkv + hk) * DOCS_BLOCK + wave * 32) * (2 * D);
   bf16_t* out = dqkv + (size_t)jw * ld + (size_t)(nq + hk) * D;
   if (u.slot >= 0) {
-    float* reg = reinterpret_cast<float*>(smem) + wave * (32 * D);
+    float* reg = wave_region<float, D>(smem, wave);
     wave_rows_out_f32<D>(reg, lane, dk_quad, [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * (2 * D) : nullptr; });
     __builtin_amdgcn_wave_barrier();
     wave_rows_out_f32<D>(reg, lane, dv_quad, [&](int r) { return (store >> r) & 1 ? prow + (size_t)r * (2 * D) + D : nullptr; });
   } else {
-    bf16_t* reg = reinterpret_cast<bf16_t*>(smem) + wave * (32 * D);
+    bf16_t* reg = wave_region<bf16_t, D>(smem, wave);
     wave_rows_out_bf16<D>(reg, lane, dk_quad, [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld : nullptr; });
     __builtin_amdgcn_wave_barrier();
     wave_rows_out_bf16<D>(reg, lane, dv_quad, [&](int r) { return (store >> r) & 1 ? out + (size_t)r * ld + (size_t)nkv * D : nullptr; });
@@ -877,7 +877,7 @@ __device__ __forceinline__ void docs_dkv_block(const DocsTiled& p, int id, int h
     const DocsSpan run = {docs_scalar(span.first), docs_scalar(span.n), 0, 0};
     const DocsRows q = {qkv + (size_t)h0 * D, (size_t)ld, first, last}, g = {dout + (size_t)h0 * D, (size_t)ldo, first, last};
     docs_again_dkv<D, CAP>(p, see, bad, unit, run, q, g, lse2 + (size_t)h0 * T, delta + (size_t)h0 * T, qkv + (size_t)key * ld + (size_t)(nq + docs_scalar(hk)) * D, ld, (size_t)nkv * D, out, prow,
-                           scale, smem + wave * (32 * D) * sizeof(float));
+                           scale, wave_region<char, D>(smem, wave));
   }
 }
 

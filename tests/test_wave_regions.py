@@ -9,7 +9,7 @@ import pytest
 from paper_2411_15871_amd import build as B
 
 
-@pytest.mark.parametrize("name", ["attn_window_bf16.h"])
+@pytest.mark.parametrize("name", ["attn_window_bf16.h", "attn_docs_bf16.h"])
 def test_each_wave_keeps_to_its_part(name):
     source = open(os.path.join(B.CSRC, name)).read()
     assert len(re.findall(r"wave_region<\w+, D>\(smem, wave\)", source)) >= 8  # forward, dQ, dK/dV: rows in either type (forward, dK/dV) or one, and what is made again
