@@ -731,7 +731,7 @@ int dh_attn_window_step(int dtype, int batch, int cache_rows, int window, int si
 size_t dh_attn_window_step_workspace_bytes(int dtype, int batch, int cache_rows, int window, int sinks, int nq, int nkv, int d);
 
 /* Linear attention with a decay: each key/value head has a state S of d x d (key index first), S_t = lambda S_(t-1) + k_t v_t^T with lambda = exp(log_decay[head]), and each query
- * head reads its group's, o_t = scale S_t^T q_t.  log_decay: DEVICE float32 [nkv], constants, at most 0 (minus infinity: no memory).  state_in: device float32 [batch,nkv,d,d], what the
+ * head reads its group's, o_t = scale S_t^T q_t.  log_decay: DEVICE float32 [nkv], constants, at most 0 (minus infinity: no memory, each token sees itself alone).  state_in: device float32 [batch,nkv,d,d], what the
  * sequences begin with (NULL: zeros); state_out: likewise, S behind the last token (NULL: not wanted; seq = 0: state_in); the two may not overlap.  States are float32 and are summed in float32, also
  * for DH_BF16, whose products with a state take it rounded to bf16.
  * Backward: dqkv (dk, dv summed over the query heads of a group in a fixed order) from dout[T,nq*d] and dstate_out, the gradient of state_out (NULL: none); dstate_in: that of

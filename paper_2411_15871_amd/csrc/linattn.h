@@ -8,7 +8,9 @@ struct LinGeom {
   const float* log_decay;
 };
 #define LC 32  // tokens of a chunk
-// lambda^m; log2 of lambda may be minus infinity
+// log2 of lambda may be minus infinity: then each token sees itself alone, and what others leave is not multiplied by zero (an infinity or a NaN would pass) but left out.
+__device__ __forceinline__ bool lin_alone(float l2) { return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, l2)) == (int)0xff800000; }
+// lambda^m
 __device__ __forceinline__ float lin_pow(float l2, int m) { return m == 0 ? 1.f : __builtin_amdgcn_exp2f(l2 * (float)m); }
 
 // Pieces of a row, `per` chunks each, that run side by side.

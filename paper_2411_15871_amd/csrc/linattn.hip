@@ -11,6 +11,7 @@ __global__ __launch_bounds__(256) void lin_carry_kernel(const LinGeom g, int pie
   const LinCarry& c = (int)blockIdx.y >= g.nkv ? c1 : c0;
   const size_t head = (size_t)b * g.nkv + hk;
   const float l2 = g.log_decay[hk] * 1.4426950408889634f, f = lin_pow(l2, tokens), f_last = lin_pow(l2, g.seq - (pieces - 1) * tokens);
+  const bool alone = lin_alone(l2);
   f32x4 run = {0.f, 0.f, 0.f, 0.f};
   if (c.first) run = *reinterpret_cast<const f32x4*>(c.first + head * dd + e);
   float* at = c.sums + head * pieces * dd + e;
@@ -26,7 +27,7 @@ __global__ __launch_bounds__(256) void lin_carry_kernel(const LinGeom g, int pie
       if (i0 + u >= pieces) break;
       const int s = c.rev ? pieces - 1 - i0 - u : i0 + u;
       *reinterpret_cast<f32x4*>(at + (size_t)s * dd) = run;
-      run = run * (s == pieces - 1 ? f_last : f) + sum[u];
+      run = alone ? sum[u] : run * (s == pieces - 1 ? f_last : f) + sum[u];
     }
   }
   if (c.last) *reinterpret_cast<f32x4*>(c.last + head * dd + e) = run;
@@ -53,7 +54,8 @@ __global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, i
   const int p = pos ? pos[b] : 1;
   if (p < 0) return;
   float *ks = sm, *qs = ks + d, *red = qs + GH * d;
-  const float lam = expf(g.log_decay[hk]);
+  const float log_decay = g.log_decay[hk], lam = expf(log_decay);
+  const bool begins = p == 0 || lin_alone(log_decay * 1.4426950408889634f);  // what state_in holds does not count
   const T* token = qkv + (size_t)b * (g.nq + 2 * g.nkv) * d;
   const T *k = token + (size_t)(g.nq + hk) * d, *v = k + (size_t)g.nkv * d;
   const size_t st = ((size_t)b * g.nkv + hk) * d * d + c;
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(LS_THREADS) void lin_step_kernel(const LinGeom g, i
 #pragma unroll
         for (int u = 0; u < LS_ROWS; u++) {
           const int x = x0 + u * groups;
-          S[u] = x < d && (h0 > 0 || p != 0) ? *reinterpret_cast<const f32x4*>(from + st + (size_t)x * d) : f32x4{0.f, 0.f, 0.f, 0.f};
+          S[u] = x < d && (h0 > 0 || !begins) ? *reinterpret_cast<const f32x4*>(from + st + (size_t)x * d) : f32x4{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
         for (int u = 0; u < LS_ROWS; u++) {

@@ -65,10 +65,20 @@ __device__ __forceinline__ int lin_row(int dt, int r, int kg) { return 32 * dt +
 __device__ __forceinline__ int lin_token(int c, int e, int kg) { return 16 * c + 8 * (e >> 2) + 4 * kg + (e & 3); }    // token of element e of fragment c
 
 
+// The lane's number taken anew: what only heads of no memory need is made in their branches and takes no registers of the loops around these.
+__device__ __forceinline__ int lin_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+// The register of a score tile that holds the score of the lane's token (its column) with itself, or -1: the other half of the wave has it.
+__device__ __forceinline__ int lin_own(int lane) { return ((lane >> 2) & 1) == lane >> 5 ? 4 * ((lane & 31) >> 3) + (lane & 3) : -1; }
+
 // What a chunk's arithmetic multiplies by.  Powers of lambda: of a score, of the state that a token reads, of a row on its way into the state.  REV: the row is walked from its end.
 template <bool REV>
 struct LinPowers {
   float weight[16], into[2][8], whole, read;
+  bool alone;     // each token sees itself alone
   uint32_t seen;  // bit r: the lane's token sees that of score register r
   int left;       // tokens of the chunk
   __device__ __forceinline__ void scores(float l2, float f, int lane) {
@@ -79,11 +89,16 @@ struct LinPowers {
   __device__ __forceinline__ void chunk(int n, float l2, float f_read, float f_in, int lane) {  // rows behind the chunk's n are copies of its last one, which count for nothing
     const int l32 = lane & 31, kg = lane >> 5;
     left = n;
+    alone = lin_alone(l2);
     seen = 0;
 #pragma unroll
     for (int r = 0; r < 16; r++) {
       const int j = lin_token(r >> 3, r & 7, kg);
       seen |= (REV ? j >= l32 && j < n : j <= l32) ? 1u << r : 0u;
+    }
+    if (alone) {
+      const int own = lin_own(lin_lane());
+      seen &= own >= 0 ? 1u << own : 0u;
     }
 #pragma unroll
     for (int c = 0; c < 2; c++)
@@ -157,7 +172,7 @@ __device__ __forceinline__ void lin_inside(f32x16& ot, f32x16& st, const LinPowe
     lin_zero(add);
     add = MFMA(v0, pf[0], add);
     add = MFMA(v1, pf[1], add);
-    const bool here = REV ? j >= l32 : j <= l32;
+    const bool here = p.alone ? j == l32 : REV ? j >= l32 : j <= l32;
 #pragma unroll
     for (int r = 0; r < 16; r++) ot[r] = here ? ot[r] + add[r] : ot[r];
   }
@@ -203,6 +218,21 @@ __device__ __forceinline__ void lin_into(f32x16 (&S)[D / 32], const LinFrag<D>& 
       for (int dt = 0; dt < D / 32; dt++) S[dt] = MFMA(k.f[dt], lo, S[dt]);
     }
   }
+}
+// The state behind tokens that see themselves alone: the last one's k v^T.  (Within the row it stays zero.)
+template <int D>
+__device__ __forceinline__ void lin_state_alone(f32x16 (&S)[D / 32], const lds_char* Kt, const lds_char* Vt, int last, int wave) {
+  using TL = ATile<D>;
+  const int lane = lin_lane(), l32 = lane & 31, kg = lane >> 5;
+  const float v = (float)*reinterpret_cast<const __attribute__((address_space(3))) bf16_t*>(Vt + (TL::off(last, wave * 32 + (l32 & ~3)) + (l32 & 3)) * 2);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int c = 0; c < 2; c++) {
+      const bf16x8 k = lds_frag(Kt + TL::off(last, 32 * dt + 16 * c + 8 * kg) * 2, 0);
+#pragma unroll
+      for (int e = 0; e < 8; e++) S[dt][8 * c + e] = (float)k[e] * v;
+    }
 }
 // The state a wave begins with (its 32 columns; transposed: of the transposed one), and the one it leaves.
 template <int D>
@@ -298,7 +328,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
   LinFrag<D> fa;
   fa.init(lane, wave);
   f32x16 S[W];
-  lin_state_load<D>(S, OUT && p.state ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr, p.transposed, wave, lane);
+  lin_state_load<D>(S, OUT && p.state && !lin_alone(l2) ? p.state + (((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D : nullptr, p.transposed, wave, lane);
   LinPowers<REV> pw;
   if constexpr (OUT) pw.scores(l2, g.scale, lane);
   pw.chunk(LC, l2, g.scale, f_in, lane);
@@ -337,7 +367,7 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
       ahead[1].load(fa, Kt, 1);
       LIN_PIN();
     }
-    if (last_head) {
+    if (last_head && !pw.alone) {
       if (!GROUPED || h == 0) {
 #pragma unroll
         for (int dt = 0; dt < W; dt++)
@@ -347,6 +377,9 @@ __device__ __forceinline__ void lin_walk(const LinArgs& a, const LinPass& p, int
       lin_into<D, EXACT ? 3 : 2, !OUT>(S, fa, Kt, ahead, v.all, pw.into);
     }
     if (++h == heads) { h = 0; n++; }
+  }
+  if constexpr (EXACT && !GROUPED) {  // (of R nothing is left)
+    if (pw.alone) lin_state_alone<D>(S, sm + (KT + ((c1 - c0 - 1) & 1)) * TR::TILE, sm + (KT + 2 + ((c1 - c0 - 1) & 1)) * TR::TILE, pw.left - 1, wave);
   }
   if constexpr (EXACT) {
     if (p.sum && team == 0) lin_state_store<D>(S, p.sum + (OUT ? (size_t)b * g.nkv + hk : ((size_t)b * g.nkv + hk) * a.pieces + piece) * D * D, wave, lane);
@@ -404,8 +437,9 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
       lin_zero(out);
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) out = MFMA(pack_rows(R[ks >> 1], ks & 1), lds_frag(At + fa.dir[ks], 0), out);
+      const bool none = pw.alone && pw.read == 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; r++) out[r] *= pw.read;
+      for (int r = 0; r < 16; r++) out[r] = none ? 0.f : out[r] * pw.read;
 #pragma unroll
       for (int dt = 0; dt < W; dt++)
 #pragma unroll
@@ -421,6 +455,10 @@ __device__ __forceinline__ void lin_walk_kv(const LinArgs& a, const LinGrads& p,
     lin_into<D, EXACT ? 3 : 2, false>(R, fa, Xt, ahead, y.all, pw.into);
     if (++h < grp) continue;
     lin_out(out, p.dqkv + (t0 + (size_t)chunk * LC + l32) * ld + to + wave * 32, l32 < left, lane);
+    if (pw.alone) {
+#pragma unroll
+      for (int dt = 0; dt < W; dt++) lin_zero(R[dt]);
+    }
     h = 0;
     n++;
   }

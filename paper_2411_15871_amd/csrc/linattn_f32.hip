@@ -34,7 +34,9 @@ __device__ __forceinline__ void lin32_walk(const Lin32Args& a, const Lin32Pass& 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, kg = lane >> 5, d = g.d, grp = g.nq / g.nkv, col = wave * 32 + l32;
   const int chunks = (g.seq + LC - 1) / LC, c0 = piece * a.cut.per, c1 = min(chunks, c0 + a.cut.per), heads = GROUPED || OUT ? grp : 1, steps = (c1 - c0) * heads;
   const size_t t0 = (size_t)b * g.seq;
-  const float l2 = g.log_decay[hk] * 1.4426950408889634f, f_read = GROUPED ? 1.f : g.scale, f_in = GROUPED ? g.scale : 1.f;
+  const float l2 = g.log_decay[hk] * 1.4426950408889634f;
+  const bool alone = lin_alone(l2);
+  const float f_read = GROUPED ? 1.f : g.scale, f_in = GROUPED ? g.scale : 1.f;
   float *Qs = sm, *Ks = sm + TILE, *Vs = sm + 2 * TILE;
   auto chunk_of = [&](int n) { return REV ? c1 - 1 - n : c0 + n; };
   float4 nq[VECS], nk[VECS], nv[VECS];  // the next step's rows
@@ -69,16 +71,18 @@ __device__ __forceinline__ void lin32_walk(const Lin32Args& a, const Lin32Pass& 
 #pragma unroll
     for (int r = 0; r < 16; r++) {
       const int x = 32 * dt + lin32_row(r, kg);
-      S[dt][r] = OUT && p.state && x < d && col < d ? p.state[st + (p.transposed ? (size_t)col * d + x : (size_t)x * d + col)] : 0.f;
+      S[dt][r] = OUT && p.state && x < d && col < d && (GROUPED || !alone) ? p.state[st + (p.transposed ? (size_t)col * d + x : (size_t)x * d + col)] : 0.f;
     }
   float weight[OUT ? 16 : 1];
   if constexpr (OUT) {
 #pragma unroll
     for (int r = 0; r < 16; r++) weight[r] = g.scale * lin_pow(l2, max(0, REV ? lin32_row(r, kg) - l32 : l32 - lin32_row(r, kg)));
   }
-  int n = 0, h = 0;
+  const int lo = REV || alone ? l32 : 0, hi = !REV || alone ? l32 + 1 : LC;  // the tokens of a chunk that the lane's sees
+  int n = 0, h = 0, left = 0;
   for (int s = 0; s < steps; s++) {
-    const int chunk = chunk_of(n), left = min(LC, g.seq - chunk * LC);
+    const int chunk = chunk_of(n);
+    left = min(LC, g.seq - chunk * LC);
     __syncthreads();  // every wave is done with the step before
     if (OUT && (!GROUPED || h == 0)) put(Qs, nq);
     if (GROUPED || h == 0) { put(Ks, nk); put(Vs, nv); }
@@ -108,14 +112,15 @@ __device__ __forceinline__ void lin32_walk(const Lin32Args& a, const Lin32Pass& 
         }
       if (!GROUPED || h == 0) {
         const float read = f_read * (REV ? l32 < left ? lin_pow(l2, left - 1 - l32) : 0.f : lin_pow(l2, l32 + 1));
+        const bool none = GROUPED && alone && read == 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r++) ot[r] *= read;
+        for (int r = 0; r < 16; r++) ot[r] = none ? 0.f : ot[r] * read;
       }
       uint32_t odd = 0;  // bit r: register r's token of the lane's half holds an infinity or a NaN in some column of the wave: a zero times it would reach tokens that do not see it
 #pragma unroll
       for (int r = 0; r < 16; r++) {
         const int j = lin32_row(r, kg);
-        const bool seen = REV ? j >= l32 && j < left : j <= l32;
+        const bool seen = j >= lo && j < (REV ? min(hi, left) : hi);
         sc[r] = seen ? sc[r] * weight[r] : 0.f;
         odd |= __builtin_isfinite(v[r]) ? 0u : 1u << r;
       }
@@ -136,7 +141,7 @@ __device__ __forceinline__ void lin32_walk(const Lin32Args& a, const Lin32Pass& 
             for (int x = 0; x < 16; x++) add[x] = 0.f;
             add = MFMA32(kg == half ? v[r] : 0.f, kg == half ? sc[r] : 0.f, add);
             const int j = lin32_row(r, half);
-            const bool here = REV ? j >= l32 : j <= l32;
+            const bool here = j >= lo && j < hi;
 #pragma unroll
             for (int x = 0; x < 16; x++) ot[x] = here ? ot[x] + add[x] : ot[x];
           }
@@ -151,7 +156,7 @@ __device__ __forceinline__ void lin32_walk(const Lin32Args& a, const Lin32Pass& 
         }
       }
     }
-    if (GROUPED || h == heads - 1) {
+    if ((GROUPED || h == heads - 1) && !(OUT && alone)) {  // (alone: it stays zero within the row)
       if (!GROUPED || h == 0) {
         const float f = lin_pow(l2, left);
 #pragma unroll
@@ -169,9 +174,23 @@ __device__ __forceinline__ void lin32_walk(const Lin32Args& a, const Lin32Pass& 
 #pragma unroll
         for (int dt = 0; dt < W; dt++) S[dt] = MFMA32(Ks[lin32_row(r, kg) * LD + 32 * dt + l32], v[r], S[dt]);
     }
-    if (++h == heads) { h = 0; n++; }
+    if (++h == heads) {
+      h = 0;
+      n++;
+      if (OUT && GROUPED && alone) {
+#pragma unroll
+        for (int dt = 0; dt < W; dt++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) S[dt][r] = 0.f;
+      }
+    }
   }
-  if (p.sum) {
+  if (p.sum && alone) {  // the last token's k v^T, of R nothing
+    float* to = p.sum + (OUT ? ((size_t)b * g.nkv + hk) * d * d : st);
+    const float *k = Ks + (left - 1) * LD, *own = Vs + (left - 1) * LD;
+#pragma unroll 1
+    for (int e = threadIdx.x; e < d * d; e += 2 * D) to[e] = GROUPED ? 0.f : k[e / d] * own[e % d];
+  } else if (p.sum) {
     float* to = p.sum + (OUT ? ((size_t)b * g.nkv + hk) * d * d : st);
 #pragma unroll
     for (int dt = 0; dt < W; dt++)
