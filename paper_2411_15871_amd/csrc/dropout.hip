@@ -174,9 +174,9 @@ static unsigned drop_blocks(size_t vecs) { return (unsigned)std::min((vecs + DRO
 static bool drop_direct(int T, int H) { return T > 0 && T <= 2048 && (long long)T * H <= 8 << 20; }
 static int drop_groups(int T, int H) {
   const int cols = (H / 8 + DB_COLS - 1) / DB_COLS;
-  return std::max(1, std::min((T + 15) / 16, (2048 + cols - 1) / cols));
+  return (int)std::max(1ll, std::min((T + 15ll) / 16, (2048ll + cols - 1) / cols));
 }
-static int drop_per(int T, int H) { return (T + drop_groups(T, H) - 1) / drop_groups(T, H); }
+static int drop_per(int T, int H) { return (int)(((long long)T + drop_groups(T, H) - 1) / drop_groups(T, H)); }
 
 extern "C" int dh_dropout_add_fwd(int dtype, int T, int H, const void* a, const void* b, const void* bias, float p, const uint64_t* rng, uint32_t site, void* out, void* stream) {
   if (int rc = check_drop("dropout_add_fwd", dtype, T, H, p, rng)) return rc;
