@@ -141,16 +141,19 @@ __global__ __launch_bounds__(1024) void dropout_bwd_direct_kernel(const DropArgs
     *to = accumulate ? *to + t : t;
   }
 }
-// dbias from n partial rows, in their order by threads and then in the threads' order.  A block has 32 columns, 8 threads each.
+// dbias from n partial rows, in their order by threads and then in the threads' order.  A block has 32 columns, 8 threads each.  Blocks stand along x and y, up to DROP_X along x: a launch counts its
+// threads along an axis in 32 bits, which 2^29 columns with 8 threads each would pass.
+#define DROP_X 65536
 __global__ __launch_bounds__(256) void dropout_bias_finish_kernel(const float* __restrict__ partial, int n, int H, int accumulate, float* __restrict__ dbias) {
   __shared__ float red[8][33];
-  const int c = threadIdx.x & 31, l = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  const uint32_t c = threadIdx.x & 31, col = (blockIdx.y * gridDim.x + blockIdx.x) * 32 + c;
+  const int l = threadIdx.x >> 5;
   float s = 0.f;
-  if (col < H)
+  if (col < (uint32_t)H)
     for (int r = l; r < n; r += 8) s += partial[(size_t)r * H + col];
   red[l][c] = s;
   __syncthreads();
-  if (l == 0 && col < H) {
+  if (l == 0 && col < (uint32_t)H) {
     for (int x = 1; x < 8; x++) s += red[x][c];
     dbias[col] = accumulate ? dbias[col] + s : s;
   }
@@ -227,7 +230,8 @@ extern "C" int dh_dropout_add_bwd(int dtype, int T, int H, const void* dout, flo
     else dropout_bwd_bias_kernel<float><<<grid, DB_COLS * DB_LANES, 0, s>>>(d, T, per, (const float*)dout, (float*)dx, (float*)ws);
     DH_LAUNCH_CHECK();
   }
-  dropout_bias_finish_kernel<<<(H + 31) / 32, 256, 0, s>>>((const float*)ws, groups, H, accumulate, dbias);
+  const unsigned columns = (unsigned)((H + 31ll) / 32), along = std::min(columns, (unsigned)DROP_X);
+  dropout_bias_finish_kernel<<<dim3(along, (columns + along - 1) / along), 256, 0, s>>>((const float*)ws, groups, H, accumulate, dbias);
   DH_LAUNCH_CHECK();
   return DH_OK;
 }

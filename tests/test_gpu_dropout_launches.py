@@ -51,3 +51,21 @@ def test_the_last_number_of_rows(dh):
         total += x[r:r + 2 ** 26].sum(0, dtype=torch.float64)
     # each block's sums are whole numbers below 2^24: exact; then 2048 of them, 256 in a row by eight threads, and these
     assert ((dbias.double() - total).abs() <= 264 * R.W * total).all()
+
+
+def test_the_last_number_of_columns(dh):
+    """2^29 columns have more threads than a launch counts along an axis; 2^31 - 8 are the last that there are."""
+    H = 2 ** 29
+    x = torch.ones((1, H), dtype=BF, device="cuda")
+    rng = torch.tensor([5, 6], dtype=torch.int64, device="cuda")
+    n = dh.dh_dropout_add_bwd_ws_bytes(1, H)
+    ws, dbias = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda"), torch.full((H,), 3.0, device="cuda")
+    dh.dh_dropout_add_bwd(dh.DH_BF16, 1, H, x, 0.5, rng, 1, x, dbias, True, ws, n)
+    v = H // 8 - 1
+    assert x[0, -8:].tolist() == [0.0 if b < 32768 else 2.0 for w in R.philox([v, 0, 6, 1], [5, 0]) for b in (w & 0xFFFF, w >> 16)]
+    assert torch.equal(dbias, 3.0 + x[0].float())
+    del x, ws, dbias
+    H = 2 ** 31 - 8
+    dbias = torch.full((H,), 3.0, device="cuda")
+    dh.dh_dropout_add_bwd(dh.DH_BF16, 0, H, None, 0.5, None, 1, None, dbias, False, None, 0)
+    assert not dbias.any()
