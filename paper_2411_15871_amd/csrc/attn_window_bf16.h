@@ -11,7 +11,8 @@
 // its masked tiles hold such values that a row does not see, and only then walks its tiles again (window_again_*).  8192 rows of 32:8 heads, window
 // 1024, us: forward 170 -> 260 with one token of NaNs, 150 with nothing else; backward 600 -> 1930 (one token), 1860 (a gradient's row), 1940 (nothing else).
 //
-// Bound by matrix products (4 D flops a visible pair forward, 14 with the backward pass) from windows of some hundred on, below that by what a block begins and ends with.
+// Bound by matrix products (4 D flops a visible pair forward, 10 of the backward pass, which do 14 here: dQ and dK/dV each form S and dP for themselves) from windows of some hundred on, below that
+// by what a block begins and ends with.
 #pragma once
 #include "window.h"
 

@@ -42,7 +42,7 @@ int dh_launch_lin_carry(const LinGeom& g, int pieces, int tokens, const LinCarry
 // Bound by memory: each element of a state is read and written once, 16 bytes a lane, LS_ROWS of them in flight, for up to GH query heads of its group (further ones read what the thread has stored).  A
 // block has `cols` columns of a state: cols / 4 lanes side by side cover its rows, the row groups take every groups-th row each, and their shares of o meet in LDS, in order.
 // Where blocks are few a state's columns are shared out over several (LS_BLOCKS).  bf16, heads of 128, us, whole states a block and shared: one sequence on 32:8 7.3 and 5.3, 16 9.4 and 7.6; 128 on
-// 32:32 106 (90 on another card, 6.0 TB/s) either way.  (With a head of the group after the other over the state 16.7 for one sequence, 37 instead of 19 for 64 on 32:8.)
+// 32:32 106, 5.1 TB/s, either way (88 where the same states come again and the chip still holds some of their 268 MB).  (With a head of the group after the other over the state 16.7 for one sequence, 37 instead of 19 for 64 on 32:8.)
 #define LS_THREADS 256
 #define LS_ROWS 4
 #define LS_BLOCKS 1024

@@ -4,8 +4,9 @@
 
 // ------------------------------------------------------------------------------------ single tokens
 // Bound by memory: each visible row of the cache is read once.  LANES lanes read a row of a head, 8 elements each, so that a wave has 64 / LANES rows in flight a load; each such
-// group keeps a reference maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.  64 sequences of mixed lengths on 32:8 heads of 128,
-// window 4096, bf16: 145 to 160 us, 5.6 to 6.1 TB/s (264 with sums across lanes through LDS, a maximum that follows every row and no rows fetched ahead).
+// group keeps a reference maximum, sum and accumulators of its own for up to GH query heads, and all groups meet in LDS, in order.  64 sequences on 32:8 heads of 128, window 4096, bf16: all windows
+// full 200 us, 5.4 TB/s; of mixed lengths, an eighth of them unused and an eighth at their first token, 147 to 162 us for 660 to 720 MB of visible rows, 4.3 to 4.5 TB/s: the longest end last (264 with
+// sums across lanes through LDS, a maximum that follows every row and no rows fetched ahead).
 struct WindowStep {
   WindowGeom g;  // seq: rows of the cache
   int chunk;     // keys of a block
@@ -226,7 +227,7 @@ extern "C" int dh_attn_window_bwd(int dtype, int batch, int seq, int window, int
   return dh_launch_window_bwd_f32(g, (const float*)qkv, (const float*)o, (const float*)dout, lse, (float*)dqkv, delta, (hipStream_t)stream);
 }
 
-// Query heads that a block takes at once: up to 8; a group of more is shared out evenly over blocks, which read the cache again.
+// Query heads that a block takes at once: up to 8; a group of more goes over several blocks, 8 each and the rest in the last (9 are 8 and 1), each of which reads the cache again.
 static int step_heads(int grp) { return grp > 4 ? 8 : grp > 2 ? 4 : grp; }
 // Blocks that share a sequence's keys: none holds fewer than 128, and there are no more than give each unit of the chip one.  us, 256, 512 and 1024 blocks, bf16, heads of 128: one sequence on 32:8, window
 // 4096, 15.9, 17.8 and 17.7; 4 23.9, 25.1 and 32.1; 32 107, 117 and 132; 64 200, 201 and 226; 16 with window 1024 23.1, 24.2 and 29.7; 48 on 16:2 39, 44 and 44.
